@@ -318,6 +318,109 @@ int warp_set_scoring(warp_index* index, int32_t mode);
 int warp_set_timing(warp_index* idx, int32_t enable);
 int warp_stage_timings(const warp_index* idx, double* total_ms, int64_t* launches, int32_t n);
 
+/*
+ * The token encoder's head: the operators that train it and serve it, beside the search over the tokens that it
+ * makes. All pointers are device memory unless said otherwise; every call enqueues its work on `hip_stream` (a
+ * hipStream_t, NULL for the default stream) of the current device, allocates nothing and returns once the work is
+ * enqueued. Rows are `*_stride` elements apart (at least the row's width where there is more than one row) and
+ * start at any address that suits one element. Zero rows are valid and enqueue nothing, except that gradient sums
+ * over no rows are written as zeros.
+ *
+ * Element types. Everything is computed in 32 bits and rounded once, to nearest, when it is stored.
+ */
+enum { WARP_F32 = 0, WARP_F16 = 1, WARP_BF16 = 2 };
+
+/*
+ * Layer norm of rows x [rows][cols]:
+ *   mean = sum(x) / cols, rstd = 1 / sqrt(sum((x - mean)^2) / cols + eps)
+ *   y = (x - mean) * rstd * weight + bias
+ *   cols         1..16384 (above: WARP_ENOTSUP)
+ *   dtype        of x and y
+ *   weight, bias [cols] of param_dtype (WARP_F32 or dtype); NULL for ones and zeros
+ *   y            may be x itself (same stride)
+ *   mean, rstd   [rows] fp32 for the backward pass, both or neither
+ */
+int warp_layer_norm(const void* x, int64_t x_stride, int64_t rows, int32_t cols, int32_t dtype, const void* weight,
+                    const void* bias, int32_t param_dtype, float eps, void* y, int64_t y_stride, float* mean,
+                    float* rstd, void* hip_stream);
+
+/*
+ * Layer norm's backward pass for the gradient dy of y, with h = (x - mean) * rstd and c = dy * weight:
+ *   dx = rstd * (c - sum(c) / cols - h * sum(c * h) / cols)
+ *   dweight = sum over rows of dy * h, dbias = sum over rows of dy
+ *   mean, rstd       [rows] as warp_layer_norm gave them
+ *   dweight, dbias   [cols] of param_dtype; either may be NULL. Summed in an order that depends on the sizes alone
+ *   dx               may be dy or x itself (same stride)
+ *   scratch          warp_layer_norm_backward_scratch bytes; may be NULL without dweight and dbias
+ */
+int warp_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, int64_t rows,
+                             int32_t cols, int32_t dtype, const void* weight, int32_t param_dtype, const float* mean,
+                             const float* rstd, void* dx, int64_t dx_stride, void* dweight, void* dbias,
+                             void* scratch, int64_t scratch_bytes, void* hip_stream);
+/* Host-only: bytes of scratch that the call above needs for these sizes (WARP_EINVAL for bad ones). */
+int warp_layer_norm_backward_scratch(int64_t rows, int32_t cols, int64_t* bytes);
+
+/*
+ * Rows in 8-bit integers, with a scale for each: x is about q * scale. With a = max |x| of the row,
+ *   q = round-half-even(x * f), f = 127 / a rounded to fp32; scale = a * (1 / 127)
+ * A row whose a is below 2^-120 has q = 0; one with an infinity or a NaN has q = 0 and a NaN for its scale.
+ *   q       [rows] rows of int8, 16-byte aligned, q_stride a multiple of 16 and at least cols rounded up to a
+ *           multiple of 128; the columns up to there are set to zero
+ *   scale   [rows] fp32
+ * warp_layer_norm_int8 quantises the rows that warp_layer_norm would give, before any rounding to 16 bits.
+ */
+int warp_quantize_rows(const void* x, int64_t x_stride, int64_t rows, int32_t cols, int32_t dtype, int8_t* q,
+                       int64_t q_stride, float* scale, void* hip_stream);
+int warp_layer_norm_int8(const void* x, int64_t x_stride, int64_t rows, int32_t cols, int32_t dtype,
+                         const void* weight, const void* bias, int32_t param_dtype, float eps, int8_t* q,
+                         int64_t q_stride, float* scale, void* hip_stream);
+
+/*
+ * Product of 8-bit rows (token activations) with the 8-bit rows of a weight, one for each output channel:
+ *   out[m][c] = (sum_j a[m][j] * w[c][j]) * w_scale[c] * a_scale[m] + bias[c]
+ * The sum is exact (int32); it is rounded to fp32 once.
+ *   a [rows], w [n]  rows of k int8 in the layout of warp_quantize_rows: 16-byte aligned, strides multiples of 16
+ *                    and at least k rounded up to a multiple of 128, zeros from column k up to there
+ *   n                1 and more output channels
+ *   k                1..131071 (above: WARP_ENOTSUP, a sum could pass 32 bits)
+ *   bias             [n] fp32 or NULL
+ *   out              [rows][n] of out_dtype, rows out_stride elements apart
+ */
+int warp_linear_int8(const int8_t* a, int64_t a_stride, const float* a_scale, int64_t rows, const int8_t* w,
+                     int64_t w_stride, const float* w_scale, int32_t n, int32_t k, const float* bias, void* out,
+                     int64_t out_stride, int32_t out_dtype, void* hip_stream);
+
+/*
+ * One AdamW step (decoupled weight decay) over many tensors, with t = step (1 and more):
+ *   m = beta1 * m + (1 - beta1) * g,  v = beta2 * v + (1 - beta2) * g^2
+ *   p = p * (1 - lr * weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ *   tensors      host array of n_tensors. `param` and `grad` hold n elements of dtype and grad_dtype; a tensor with
+ *                n = 0 or a NULL grad is left as it is. `moment` is where its moments start in m and v, a multiple
+ *                of 256; they take n rounded up to a multiple of 256, and those of two tensors must not overlap
+ *   bits         32: m and v are fp32; m_scale and v_scale are not used.
+ *                8: m is int8, v uint8, and each block of 256 elements has a scale S in m_scale and v_scale (fp32,
+ *                one for each 256 of m and v): m = S * sign(c) * (c / 127)^2, v = S * (c / 255)^4. S is the block's
+ *                largest magnitude (at least 2^-126); a code counts the cutoffs ((j - 1/2) / 127)^2 or
+ *                ((j - 1/2) / 255)^4, j = 1, 2, ..., that the magnitude over S reaches, and is at least 1 for a
+ *                v above zero, so that a step is never divided by a v that was lost. p takes the new m and v before
+ *                they are coded. A NaN or infinite gradient makes its block's moments NaN
+ *   m, v         16-byte aligned. Zeros (codes and scales) are the start of a training
+ *   grad_scale   device fp32 that every gradient is multiplied by, or NULL (a clipping factor, for instance)
+ */
+typedef struct warp_adamw_tensor {
+    void* param;
+    const void* grad;
+    int64_t n;
+    int64_t moment;
+} warp_adamw_tensor;
+int warp_adamw_step(const warp_adamw_tensor* tensors, int32_t n_tensors, int32_t dtype, int32_t grad_dtype,
+                    int32_t bits, void* m, float* m_scale, void* v, float* v_scale, double lr, double beta1,
+                    double beta2, double eps, double weight_decay, int64_t step, const float* grad_scale,
+                    void* hip_stream);
+/* The values that n 8-bit moments stand for (n a multiple of 256): out_m and out_v [n] fp32. */
+int warp_adamw_moments(const int8_t* m, const float* m_scale, const uint8_t* v, const float* v_scale, int64_t n,
+                       float* out_m, float* out_v, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

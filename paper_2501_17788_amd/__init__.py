@@ -2,9 +2,19 @@
 
 The search path (WARP_SELECT, implicit decompression, two-stage reduction,
 top-k) runs in hand-written HIP kernels behind the C ABI of include/warp.h;
-`warp` is its Python binding.
+`warp` is its Python binding. `encoder` binds the operators of the token encoder's head
+from the same library: layer norm, int8 products and the AdamW step.
 """
 from .warp import (  # noqa: F401
     EINVAL, EDEVICE, ENOMEM, ENOTSUP, EXPORTS, FRAC_BITS, SCORING_EQ1_LITERAL, SCORING_PAPER, STAGES, T_PRIME_C,
     T_PRIME_MAX, Index, WarpError, build_index, initial_centroids, last_error, lib, sample_passages, t_prime_policy,
 )
+
+try:
+    import torch  # noqa: F401
+except ImportError:  # the blocking search of host arrays needs no torch
+    pass
+else:
+    from .encoder import (  # noqa: F401
+        AdamW, QuantizedRows, layer_norm, layer_norm_backward, layer_norm_int8, linear_int8, quantize_rows,
+    )

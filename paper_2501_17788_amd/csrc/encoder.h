@@ -1,0 +1,83 @@
+// Shared by the kernels of the token encoder's head (norm.hip, linear_int8.hip, adamw.hip): element
+// types, vectors of any element alignment, wave reductions, and the checks of their C entry points.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "warp.h"
+
+namespace warp {
+
+// engine.hip: records the message that warp_last_error() returns and gives back `code`
+int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+// the current device is a gfx950 (looked up once per device)
+int require_device();
+
+constexpr int kWave = 64;
+constexpr int kInt8Pad = 128;  // int8 rows are padded with zeros to a multiple of this many columns
+
+inline int dtype_bytes(int32_t dtype) { return dtype == WARP_F32 ? 4 : 2; }
+inline bool dtype_ok(int32_t dtype) { return dtype == WARP_F32 || dtype == WARP_F16 || dtype == WARP_BF16; }
+
+// A launch's own error, without taking one that an earlier call of the process left behind.
+#define WARP_LAUNCH(...)                                                                             \
+    do {                                                                                             \
+        (void)hipGetLastError();                                                                     \
+        __VA_ARGS__;                                                                                 \
+        const hipError_t e_ = hipGetLastError();                                                     \
+        if (e_ != hipSuccess) return fail(WARP_EDEVICE, "kernel launch failed: %s", hipGetErrorString(e_)); \
+    } while (0)
+
+// V elements at any address that suits one element: gfx950 loads and stores 16 bytes at once from
+// any 4-byte (and, more slowly, any) address, so rows of odd width take the same instructions.
+template <typename T, int V>
+struct __attribute__((packed, aligned(sizeof(T)))) Vec {
+    T e[V];
+};
+
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> load_vec(const T* p) {
+    return *reinterpret_cast<const Vec<T, V>*>(p);
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void store_vec(T* p, const Vec<T, V>& v) {
+    *reinterpret_cast<Vec<T, V>*>(p) = v;
+}
+
+// Sum over the wave's 64 lanes, returned to every lane: four steps inside rows of 16 lanes, then
+// the rows' sums carried up to lane 63.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppHalfMirror = 0x141, kDppMirror = 0x140;
+constexpr int kDppBcast15 = 0x142, kDppBcast31 = 0x143;
+
+__device__ __forceinline__ float as_f(uint32_t u) { return __uint_as_float(u); }
+__device__ __forceinline__ uint32_t as_u(float f) { return __float_as_uint(f); }
+
+__device__ __forceinline__ float wave_sum(float x) {
+    x += as_f(dpp<kDppXor1, 0xf>(as_u(x)));
+    x += as_f(dpp<kDppXor2, 0xf>(as_u(x)));
+    x += as_f(dpp<kDppHalfMirror, 0xf>(as_u(x)));
+    x += as_f(dpp<kDppMirror, 0xf>(as_u(x)));
+    x += as_f(dpp<kDppBcast15, 0xa>(as_u(x)));
+    x += as_f(dpp<kDppBcast31, 0xc>(as_u(x)));
+    return as_f((uint32_t)__builtin_amdgcn_readlane((int)as_u(x), 63));
+}
+
+// The same for the largest of unsigned numbers (magnitudes of floats by their bits: a NaN is above
+// infinity, which is above every number).
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+    x = max(x, dpp<kDppXor1, 0xf>(x));
+    x = max(x, dpp<kDppXor2, 0xf>(x));
+    x = max(x, dpp<kDppHalfMirror, 0xf>(x));
+    x = max(x, dpp<kDppMirror, 0xf>(x));
+    x = max(x, dpp<kDppBcast15, 0xa>(x));
+    x = max(x, dpp<kDppBcast31, 0xc>(x));
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+
+}  // namespace warp

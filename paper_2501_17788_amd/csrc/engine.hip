@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -17,6 +18,7 @@
 #include <utility>
 #include <vector>
 
+#include "encoder.h"
 #include "engine.h"
 #include "warp.h"
 
@@ -29,10 +31,10 @@ constexpr size_t kNoAllocBytes = (size_t)256 << 20;
 static __device__ __align__(256) unsigned char scratch[kNoAllocBytes];
 
 namespace {
-
 thread_local std::string g_err;
+}  // namespace
 
-int fail(int code, const char* fmt, ...) {
+int warp::fail(int code, const char* fmt, ...) {
     char buf[512];
     va_list ap;
     va_start(ap, fmt);
@@ -41,6 +43,8 @@ int fail(int code, const char* fmt, ...) {
     g_err = buf;
     return code;
 }
+
+namespace {
 
 #define HIP_TRY(expr)                                                                         \
     do {                                                                                      \
@@ -185,8 +189,10 @@ int check_device() {
     return WARP_OK;
 }
 
-// Per-device address of `scratch`, set by bind_noalloc_scratch.
 constexpr int kMaxDevices = 64;
+std::atomic<bool> g_device_ok[kMaxDevices];  // check_device() has passed on the device
+
+// Per-device address of `scratch`, set by bind_noalloc_scratch.
 std::mutex g_scratch_lock;
 unsigned char* g_scratch_ptr[kMaxDevices] = {};
 
@@ -211,6 +217,19 @@ unsigned char* noalloc_scratch(int dev) {
     std::lock_guard<std::mutex> g(g_scratch_lock);
     return g_scratch_ptr[dev];
 }
+
+}  // namespace
+
+int warp::require_device() {
+    int dev = -1;
+    if (hipGetDevice(&dev) == hipSuccess && dev >= 0 && dev < kMaxDevices && g_device_ok[dev]) return WARP_OK;
+    (void)hipGetLastError();
+    const int rc = check_device();
+    if (!rc && dev >= 0 && dev < kMaxDevices) g_device_ok[dev] = true;
+    return rc;
+}
+
+namespace {
 
 bool is_index(const warp_index* idx) {
     if (!idx) return false;

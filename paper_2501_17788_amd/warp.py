@@ -26,7 +26,8 @@ EXPORTS = (
     "warp_index_free", "warp_index_info", "warp_search", "warp_search_async", "warp_index_sync",
     "warp_search_debug", "warp_centroid_filter_scores", "warp_set_timing", "warp_stage_timings",
     "warp_t_prime_policy", "warp_set_scoring", "warp_build_index", "warp_search_noalloc",
-    "warp_kmeans_sample_size",
+    "warp_kmeans_sample_size", "warp_layer_norm", "warp_layer_norm_backward", "warp_layer_norm_backward_scratch",
+    "warp_layer_norm_int8", "warp_quantize_rows", "warp_linear_int8", "warp_adamw_step", "warp_adamw_moments",
 )
 
 
@@ -49,6 +50,7 @@ def _load() -> ctypes.CDLL:
         raise ImportError(f"{LIB_PATH} is not built; run __graft_entry__.build() (hipcc, gfx950)")
     lib = ctypes.CDLL(LIB_PATH)
     P, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+    f32, f64 = ctypes.c_float, ctypes.c_double
     sig = {
         "warp_fixed_point_bits": ([], ctypes.c_int),
         "warp_last_error": ([], ctypes.c_char_p),
@@ -68,6 +70,15 @@ def _load() -> ctypes.CDLL:
         "warp_kmeans_sample_size": ([i64, ctypes.c_double, P], ctypes.c_int),
         "warp_set_scoring": ([P, i32], ctypes.c_int),
         "warp_build_index": ([P, P, i64, i32, P, i32, P, i64, i32, i32, i64, P, P, P, P, P, P, P], ctypes.c_int),
+        "warp_layer_norm": ([P, i64, i64, i32, i32, P, P, i32, f32, P, i64, P, P, P], ctypes.c_int),
+        "warp_layer_norm_backward": ([P, i64, P, i64, i64, i32, i32, P, i32, P, P, P, i64, P, P, P, i64, P],
+                                     ctypes.c_int),
+        "warp_layer_norm_backward_scratch": ([i64, i32, P], ctypes.c_int),
+        "warp_layer_norm_int8": ([P, i64, i64, i32, i32, P, P, i32, f32, P, i64, P, P], ctypes.c_int),
+        "warp_quantize_rows": ([P, i64, i64, i32, i32, P, i64, P, P], ctypes.c_int),
+        "warp_linear_int8": ([P, i64, P, i64, P, i64, P, i32, i32, P, P, i64, i32, P], ctypes.c_int),
+        "warp_adamw_step": ([P, i32, i32, i32, i32, P, P, P, P, f64, f64, f64, f64, f64, i64, P, P], ctypes.c_int),
+        "warp_adamw_moments": ([P, P, P, P, i64, P, P, P], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         f = getattr(lib, name)

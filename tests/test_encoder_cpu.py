@@ -1,0 +1,161 @@
+"""Refusals of the token encoder's operators: bad arguments are rejected before a device is touched."""
+import ctypes
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+w = pytest.importorskip("paper_2501_17788_amd")
+
+lib = w.lib
+P = 1 << 20  # an aligned address that no call below reads
+
+
+def refused(rc, code, needle):
+    assert rc == code, (rc, w.last_error())
+    assert needle in w.last_error(), w.last_error()
+
+
+def norm(**over):
+    a = dict(x=P, x_stride=64, rows=4, cols=64, dtype=0, weight=None, bias=None, param_dtype=0, eps=1e-5, y=P,
+             y_stride=64, mean=None, rstd=None, stream=None)
+    a.update(over)
+    return lib.warp_layer_norm(*a.values())
+
+
+@pytest.mark.parametrize("over,code,needle", [
+    (dict(rows=-1), w.EINVAL, "rows"),
+    (dict(rows=1 << 31), w.ENOTSUP, "rows"),
+    (dict(cols=0), w.EINVAL, "cols"),
+    (dict(cols=16385, x_stride=16385, y_stride=16385), w.ENOTSUP, "columns"),
+    (dict(dtype=3), w.EINVAL, "dtype"),
+    (dict(dtype=-1), w.EINVAL, "dtype"),
+    (dict(param_dtype=2), w.EINVAL, "weight and bias"),
+    (dict(dtype=1, param_dtype=2), w.EINVAL, "weight and bias"),
+    (dict(x=None), w.EINVAL, "null"),
+    (dict(y=None), w.EINVAL, "null"),
+    (dict(x_stride=63), w.EINVAL, "stride"),
+    (dict(y_stride=-64), w.EINVAL, "stride"),
+    (dict(x=P + 2), w.EINVAL, "misaligned"),
+    (dict(weight=P + 1), w.EINVAL, "misaligned"),
+    (dict(eps=-1.0), w.EINVAL, "eps"),
+    (dict(eps=float("nan")), w.EINVAL, "eps"),
+    (dict(mean=P), w.EINVAL, "together"),
+])
+def test_layer_norm_refusals(over, code, needle):
+    refused(norm(**over), code, needle)
+
+
+def back(**over):
+    a = dict(dy=P, dy_stride=64, x=P, x_stride=64, rows=4, cols=64, dtype=0, weight=None, param_dtype=0, mean=P,
+             rstd=P, dx=P, dx_stride=64, dw=P, db=P, scratch=P, bytes=1 << 30, stream=None)
+    a.update(over)
+    return lib.warp_layer_norm_backward(*a.values())
+
+
+@pytest.mark.parametrize("over,needle", [
+    (dict(rows=-1), "rows"), (dict(dy=None), "null"), (dict(dx=None), "null"), (dict(mean=None), "null"),
+    (dict(rstd=None), "null"), (dict(dy_stride=3), "stride"), (dict(dx_stride=3), "stride"),
+    (dict(scratch=None), "scratch"), (dict(bytes=511), "scratch"), (dict(dw=P + 1), "misaligned"),
+    (dict(param_dtype=1), "weight and bias"),
+])
+def test_layer_norm_backward_refusals(over, needle):
+    refused(back(**over), w.EINVAL, needle)
+
+
+def test_layer_norm_backward_scratch():
+    out = ctypes.c_int64()
+    for rows, cols in ((0, 1), (1, 1), (4, 64), (10 ** 6, 1024), (10 ** 6, 16384)):
+        assert lib.warp_layer_norm_backward_scratch(rows, cols, ctypes.byref(out)) == 0
+        assert out.value % (8 * cols) == 0 and out.value <= 8 * cols * min(rows, 4096)
+    refused(lib.warp_layer_norm_backward_scratch(-1, 4, ctypes.byref(out)), w.EINVAL, "sizes")
+    refused(lib.warp_layer_norm_backward_scratch(1, 0, ctypes.byref(out)), w.EINVAL, "sizes")
+    refused(lib.warp_layer_norm_backward_scratch(1, 4, None), w.EINVAL, "sizes")
+
+
+@pytest.mark.parametrize("over", [
+    dict(q=None), dict(scale=None), dict(q=P + 8), dict(q_stride=100), dict(q_stride=136), dict(scale=P + 2),
+])
+def test_int8_rows_refusals(over):
+    a = dict(x=P, x_stride=100, rows=4, cols=100, dtype=2, q=P, q_stride=128, scale=P, stream=None)
+    a.update(over)
+    assert lib.warp_quantize_rows(*a.values()) == w.EINVAL
+    b = dict(x=P, x_stride=100, rows=4, cols=100, dtype=2, weight=None, bias=None, pt=0, eps=1e-5, q=a["q"],
+             q_stride=a["q_stride"], scale=a["scale"], stream=None)
+    assert lib.warp_layer_norm_int8(*b.values()) == w.EINVAL
+
+
+@pytest.mark.parametrize("over,code,needle", [
+    (dict(rows=-1), w.EINVAL, "rows"), (dict(n=0), w.EINVAL, "n and k"), (dict(k=0), w.EINVAL, "n and k"),
+    (dict(k=131_072, a_stride=1 << 18, w_stride=1 << 18), w.ENOTSUP, "131071"),
+    (dict(rows=(1 << 24) + 1), w.ENOTSUP, "rows"), (dict(n=(1 << 21) + 1, out_stride=1 << 22), w.ENOTSUP, "channels"),
+    (dict(a=None), w.EINVAL, "null"), (dict(w=None), w.EINVAL, "null"), (dict(a_scale=None), w.EINVAL, "null"),
+    (dict(w_scale=None), w.EINVAL, "null"), (dict(out=None), w.EINVAL, "null"),
+    (dict(a=P + 4), w.EINVAL, "alignment"), (dict(w=P + 4), w.EINVAL, "alignment"),
+    (dict(a_stride=112), w.EINVAL, "alignment"), (dict(w_stride=136), w.EINVAL, "alignment"),
+    (dict(out=P + 1), w.EINVAL, "misaligned"), (dict(bias=P + 2), w.EINVAL, "misaligned"),
+    (dict(out_stride=6), w.EINVAL, "stride"), (dict(dtype=9), w.EINVAL, "dtype"),
+])
+def test_linear_int8_refusals(over, code, needle):
+    a = dict(a=P, a_stride=128, a_scale=P, rows=5, w=P, w_stride=128, w_scale=P, n=7, k=100, bias=None, out=P,
+             out_stride=7, dtype=2, stream=None)
+    a.update(over)
+    refused(lib.warp_linear_int8(*a.values()), code, needle)
+
+
+@pytest.mark.parametrize("over,needle", [
+    (dict(n_tensors=-1), "list"), (dict(tensors=None), "list"), (dict(dtype=4), "dtype"), (dict(grad_dtype=-2), "dtype"),
+    (dict(bits=16), "bits"), (dict(beta1=1.0), "betas"), (dict(beta2=-0.1), "betas"), (dict(beta1=float("nan")), "betas"),
+    (dict(lr=-1.0), "lr"), (dict(eps=float("inf")), "lr"), (dict(decay=float("nan")), "lr"), (dict(step=0), "step"),
+    (dict(m=None), "moments"), (dict(v=None), "moments"), (dict(bits=8, m_scale=None), "moments"),
+    (dict(m=P + 4), "misaligned"), (dict(grad_scale=P + 1), "misaligned"),
+    (dict(row=(P, P, -1, 0)), "elements"), (dict(row=(P, P, 1 << 33, 0)), "elements"),
+    (dict(row=(P, P, 9, 128)), "256"), (dict(row=(P, P, 9, -256)), "256"), (dict(row=(0, P, 9, 0)), "null"),
+    (dict(row=(P + 2, P, 9, 0)), "misaligned"),
+])
+def test_adamw_refusals(over, needle):
+    table = np.array([over.pop("row", (P, P, 9, 256))], np.int64)
+    a = dict(tensors=table.ctypes.data, n_tensors=1, dtype=0, grad_dtype=0, bits=32, m=P, m_scale=P, v=P, v_scale=P,
+             lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, decay=0.0, step=1, grad_scale=None, stream=None)
+    a.update(over)
+    refused(lib.warp_adamw_step(*a.values()), w.EINVAL, needle)
+
+
+def test_adamw_moments_refusals():
+    for over in (dict(n=-256), dict(n=100), dict(m=None), dict(out_v=None), dict(v=P + 1)):
+        a = dict(m=P, m_scale=P, v=P, v_scale=P, n=256, out_m=P, out_v=P, stream=None)
+        a.update(over)
+        assert lib.warp_adamw_moments(*a.values()) == w.EINVAL
+
+
+def test_binding_refuses_host_and_odd_tensors():
+    x = torch.zeros(4, 8)
+    one = torch.ones(8)
+    with pytest.raises(ValueError, match="device"):
+        w.layer_norm(x)
+    with pytest.raises(ValueError, match="device"):
+        w.quantize_rows(x)
+    with pytest.raises(ValueError, match="dy"):
+        w.layer_norm_backward(x[:3], x, one, torch.zeros(4), torch.zeros(4))
+    with pytest.raises(ValueError, match="mean"):
+        w.layer_norm_backward(x, x, one, torch.zeros(3), torch.zeros(4))
+    with pytest.raises(ValueError, match="contiguous tensors"):
+        w.AdamW([x])
+    with pytest.raises(ValueError, match="no parameters"):
+        w.AdamW([])
+    with pytest.raises(ValueError, match="bits"):
+        w.AdamW([x], bits=4)
+    q = w.QuantizedRows.from_int8(torch.ones(2, 5, dtype=torch.int8), torch.ones(2))
+    assert q.values.shape == (2, 128) and q.cols == 5 and int(q.values.sum()) == 10
+    with pytest.raises(ValueError, match="columns"):
+        w.linear_int8(q, w.QuantizedRows(q.values, q.scale, 6))
+    with pytest.raises(ValueError, match="padded"):
+        w.linear_int8(w.QuantizedRows(q.values[:, :64], q.scale, 5), q)
+    with pytest.raises(ValueError, match="scale"):
+        w.linear_int8(w.QuantizedRows(q.values, q.scale[:1], 5), q)
+    with pytest.raises(ValueError, match="dtype"):
+        w.linear_int8(q, q, dtype=torch.float64)
+    with pytest.raises(ValueError, match="bias"):
+        w.linear_int8(q, q, bias=torch.ones(3))
+    with pytest.raises(ValueError, match="int8"):
+        w.QuantizedRows.from_int8(torch.ones(2, 5), torch.ones(2))
