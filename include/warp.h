@@ -379,8 +379,9 @@ int warp_layer_norm_int8(const void* x, int64_t x_stride, int64_t rows, int32_t 
  * Product of 8-bit rows (token activations) with the 8-bit rows of a weight, one for each output channel:
  *   out[m][c] = (sum_j a[m][j] * w[c][j]) * w_scale[c] * a_scale[m] + bias[c]
  * The sum is exact (int32); it is rounded to fp32 once.
- *   a [rows], w [n]  rows of k int8 in the layout of warp_quantize_rows: 16-byte aligned, strides multiples of 16
- *                    and at least k rounded up to a multiple of 128, zeros from column k up to there
+ *   a [rows], w [n]  rows of k int8 in the layout of warp_quantize_rows: 16-byte aligned, strides multiples of 16,
+ *                    at least k rounded up to a multiple of 128 and at most 2^23 (above: WARP_ENOTSUP), zeros from
+ *                    column k up to that multiple
  *   n                1 and more output channels
  *   k                1..131071 (above: WARP_ENOTSUP, a sum could pass 32 bits)
  *   bias             [n] fp32 or NULL
