@@ -8,7 +8,6 @@ any row stride (a dimension's elements one after the other); leading dimensions 
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 from typing import NamedTuple
 
@@ -40,28 +39,35 @@ class QuantizedRows(NamedTuple):
         return cls(padded, scale.to(torch.float32).contiguous(), cols)
 
 
-@contextlib.contextmanager
-def _on(stream, tensors):
-    """Makes `stream` current while a call allocates and enqueues, and keeps its inputs alive for it."""
+_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _here(first, *others):
+    """The current stream's handle, if that is where a call on these tensors works; None if their device is not
+    the current one. What torch.cuda.current_stream() gives, without making a Python object of it."""
+    index = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"expected tensors on {first.device}, got {t.device}")
+    if index < 0:
+        raise ValueError(f"expected device tensors, got {first.device}")
+    return _raw_stream(index) if index == _device() else None
+
+
+def _there(stream, tensors, call, *args):
+    """call(*args) with `stream` (or the current one of the tensors' device) current, so that outputs and copies
+    are allocated and enqueued there; the tensors are kept for its work."""
     dev = tensors[0].device
+    if not tensors[0].is_cuda:
+        raise ValueError(f"expected device tensors, got {dev}")
+    stream = torch.cuda.current_stream(dev) if stream is None else stream
     with torch.cuda.device(dev), torch.cuda.stream(stream):
         for t in tensors:
             if t is not None:
                 t.record_stream(stream)
-        yield
-
-
-def _run(stream, tensors, call):
-    """call() with the current stream of the tensors' device, or with `stream`."""
-    dev = tensors[0].device
-    for t in tensors:
-        if t is not None and (t.device != dev or not t.is_cuda):
-            raise ValueError(f"expected device tensors on {dev}, got {t.device}")
-    if stream is None and dev.index == torch.cuda.current_device():
-        return call(torch.cuda.current_stream(dev).cuda_stream)
-    stream = torch.cuda.current_stream(dev) if stream is None else stream
-    with _on(stream, tensors):
-        return call(stream.cuda_stream)
+        return call(*args)
 
 
 def _rows(x, name):
@@ -106,17 +112,18 @@ def _ptr(t):
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, stream=None):
     """Layer norm over the last dimension of x [..., cols]: (y like x, mean, rstd), the row statistics in
     float32 [...] for `layer_norm_backward`. weight and bias [cols] are float32 or of x's type."""
-    def call(s):
-        w, b, pt = _params(x, weight, bias)
-        r, rows, stride = _rows(x, "x")
-        cols = r.shape[-1]
-        y = torch.empty(r.shape, dtype=r.dtype, device=r.device)
-        mean, rstd = torch.empty((2, *r.shape[:-1]), dtype=torch.float32, device=r.device).unbind(0)
-        _check(lib.warp_layer_norm(r.data_ptr(), stride, rows, cols, _DTYPES[r.dtype], _ptr(w), _ptr(b), _DTYPES[pt],
-                                   eps, y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(), s))
-        return y, mean, rstd
-
-    return _run(stream, (x, weight, bias), call)
+    s = _here(x, weight, bias) if stream is None else None
+    if s is None:
+        return _there(stream, (x, weight, bias), layer_norm, x, weight, bias, eps)
+    weight, bias, pt = _params(x, weight, bias)
+    x, rows, stride = _rows(x, "x")
+    shape = x.shape
+    cols = shape[-1]
+    y = torch.empty(shape, dtype=x.dtype, device=x.device)
+    mean, rstd = torch.empty((2, *shape[:-1]), dtype=torch.float32, device=x.device).unbind(0)
+    _check(lib.warp_layer_norm(x.data_ptr(), stride, rows, cols, _DTYPES[x.dtype], _ptr(weight), _ptr(bias),
+                               _DTYPES[pt], eps, y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(), s))
+    return y, mean, rstd
 
 
 def layer_norm_backward(dy, x, weight, mean, rstd, stream=None):
@@ -127,24 +134,22 @@ def layer_norm_backward(dy, x, weight, mean, rstd, stream=None):
     for name, t in (("mean", mean), ("rstd", rstd)):
         if t.shape != x.shape[:-1] or t.dtype != torch.float32 or not t.is_contiguous():
             raise ValueError(f"{name} must be what layer_norm gave: contiguous float32 {tuple(x.shape[:-1])}")
-
-    def call(s):
-        w, _, pt = _params(x, weight, None)
-        r, rows, stride = _rows(x, "x")
-        d, _, d_stride = _rows(dy, "dy")
-        cols = r.shape[-1]
-        need = ctypes.c_int64()
-        _check(lib.warp_layer_norm_backward_scratch(rows, cols, ctypes.byref(need)))
-        dx = torch.empty(r.shape, dtype=r.dtype, device=r.device)
-        dw, db = torch.empty((2, cols), dtype=pt, device=r.device).unbind(0)
-        scratch = torch.empty(need.value, dtype=torch.uint8, device=r.device)
-        _check(lib.warp_layer_norm_backward(d.data_ptr(), d_stride, r.data_ptr(), stride, rows, cols,
-                                            _DTYPES[r.dtype], _ptr(w), _DTYPES[pt], mean.data_ptr(), rstd.data_ptr(),
-                                            dx.data_ptr(), cols, dw.data_ptr(), db.data_ptr(), scratch.data_ptr(),
-                                            need.value, s))
-        return dx, dw, db
-
-    return _run(stream, (x, dy, weight, mean, rstd), call)
+    s = _here(x, dy, weight, mean, rstd) if stream is None else None
+    if s is None:
+        return _there(stream, (x, dy, weight, mean, rstd), layer_norm_backward, dy, x, weight, mean, rstd)
+    weight, _, pt = _params(x, weight, None)
+    x, rows, stride = _rows(x, "x")
+    dy, _, dy_stride = _rows(dy, "dy")
+    cols = x.shape[-1]
+    need = ctypes.c_int64()
+    _check(lib.warp_layer_norm_backward_scratch(rows, cols, ctypes.byref(need)))
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dw, db = torch.empty((2, cols), dtype=pt, device=x.device).unbind(0)
+    scratch = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+    _check(lib.warp_layer_norm_backward(dy.data_ptr(), dy_stride, x.data_ptr(), stride, rows, cols, _DTYPES[x.dtype],
+                                        _ptr(weight), _DTYPES[pt], mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(),
+                                        cols, dw.data_ptr(), db.data_ptr(), scratch.data_ptr(), need.value, s))
+    return dx, dw, db
 
 
 def _int8_out(x, rows):
@@ -155,29 +160,29 @@ def _int8_out(x, rows):
 def quantize_rows(x, stream=None) -> QuantizedRows:
     """Rows of x [..., cols] in 8 bits with a scale each: token activations, or a weight [n, cols] with a
     scale for each output channel."""
-    def call(s):
-        r, rows, stride = _rows(x, "x")
-        cols = r.shape[-1]
-        q, scale = _int8_out(r, rows)
-        _check(lib.warp_quantize_rows(r.data_ptr(), stride, rows, cols, _DTYPES[r.dtype], q.data_ptr(), q.shape[1],
-                                      scale.data_ptr(), s))
-        return QuantizedRows(q, scale, cols)
-
-    return _run(stream, (x,), call)
+    s = _here(x) if stream is None else None
+    if s is None:
+        return _there(stream, (x,), quantize_rows, x)
+    x, rows, stride = _rows(x, "x")
+    cols = x.shape[-1]
+    q, scale = _int8_out(x, rows)
+    _check(lib.warp_quantize_rows(x.data_ptr(), stride, rows, cols, _DTYPES[x.dtype], q.data_ptr(), q.shape[1],
+                                  scale.data_ptr(), s))
+    return QuantizedRows(q, scale, cols)
 
 
 def layer_norm_int8(x, weight=None, bias=None, eps: float = 1e-5, stream=None) -> QuantizedRows:
     """`quantize_rows` of `layer_norm`'s rows in one pass, without rounding them to x's type in between."""
-    def call(s):
-        w, b, pt = _params(x, weight, bias)
-        r, rows, stride = _rows(x, "x")
-        cols = r.shape[-1]
-        q, scale = _int8_out(r, rows)
-        _check(lib.warp_layer_norm_int8(r.data_ptr(), stride, rows, cols, _DTYPES[r.dtype], _ptr(w), _ptr(b),
-                                        _DTYPES[pt], eps, q.data_ptr(), q.shape[1], scale.data_ptr(), s))
-        return QuantizedRows(q, scale, cols)
-
-    return _run(stream, (x, weight, bias), call)
+    s = _here(x, weight, bias) if stream is None else None
+    if s is None:
+        return _there(stream, (x, weight, bias), layer_norm_int8, x, weight, bias, eps)
+    weight, bias, pt = _params(x, weight, bias)
+    x, rows, stride = _rows(x, "x")
+    cols = x.shape[-1]
+    q, scale = _int8_out(x, rows)
+    _check(lib.warp_layer_norm_int8(x.data_ptr(), stride, rows, cols, _DTYPES[x.dtype], _ptr(weight), _ptr(bias),
+                                    _DTYPES[pt], eps, q.data_ptr(), q.shape[1], scale.data_ptr(), s))
+    return QuantizedRows(q, scale, cols)
 
 
 def linear_int8(a: QuantizedRows, w: QuantizedRows, bias=None, dtype=torch.bfloat16, stream=None):
@@ -185,30 +190,29 @@ def linear_int8(a: QuantizedRows, w: QuantizedRows, bias=None, dtype=torch.bfloa
     float32, in `dtype`. The integer sums are exact."""
     if dtype not in _DTYPES:
         raise ValueError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
-    if a.cols != w.cols:
-        raise ValueError(f"tokens of {a.cols} columns against a weight of {w.cols}")
-    for name, r in (("a", a), ("w", w)):
-        v, s = r.values, r.scale
-        if v.dtype != torch.int8 or v.dim() != 2 or (v.stride(1) != 1 and v.shape[1] > 1) or v.shape[1] < r.cols:
-            raise ValueError(f"{name}: int8 rows of at least {r.cols} columns are needed")
+    (av, sa, cols), (wv, sw, w_cols) = a, w
+    if cols != w_cols:
+        raise ValueError(f"tokens of {cols} columns against a weight of {w_cols}")
+    padded = -(-cols // PAD) * PAD
+    for name, v, s in (("a", av, sa), ("w", wv, sw)):
+        if v.dtype != torch.int8 or v.dim() != 2 or v.stride(1) != 1:
+            raise ValueError(f"{name}: int8 rows of contiguous elements are needed")
         if s.dtype != torch.float32 or s.shape != v.shape[:1] or not s.is_contiguous():
             raise ValueError(f"{name}: a contiguous float32 scale for each row is needed")
-        # what the kernels read of a row must lie inside the tensor
-        if v.shape[1] < -(-r.cols // PAD) * PAD:
+        if v.shape[1] < padded:  # what the kernels read of a row must lie inside the tensor
             raise ValueError(f"{name}: rows of {v.shape[1]} columns are not padded to a multiple of {PAD}; "
                              "see QuantizedRows.from_int8")
-    rows, n = a.values.shape[0], w.values.shape[0]
+    rows, n = av.shape[0], wv.shape[0]
     if bias is not None and (bias.shape != (n,) or bias.dtype != torch.float32):
         raise ValueError(f"bias must be float32 ({n},), got {bias.dtype} {tuple(bias.shape)}")
-    def call(s):
-        b = None if bias is None else bias.contiguous()
-        out = torch.empty((rows, n), dtype=dtype, device=a.values.device)
-        _check(lib.warp_linear_int8(a.values.data_ptr(), a.values.stride(0), a.scale.data_ptr(), rows,
-                                    w.values.data_ptr(), w.values.stride(0), w.scale.data_ptr(), n, a.cols,
-                                    _ptr(b), out.data_ptr(), n, _DTYPES[dtype], s))
-        return out
-
-    return _run(stream, (a.values, a.scale, w.values, w.scale, bias), call)
+    s = _here(av, sa, wv, sw, bias) if stream is None else None
+    if s is None:
+        return _there(stream, (av, sa, wv, sw, bias), linear_int8, a, w, bias, dtype)
+    bias = None if bias is None else bias.contiguous()
+    out = torch.empty((rows, n), dtype=dtype, device=av.device)
+    _check(lib.warp_linear_int8(av.data_ptr(), av.stride(0), sa.data_ptr(), rows, wv.data_ptr(), wv.stride(0),
+                                sw.data_ptr(), n, cols, _ptr(bias), out.data_ptr(), n, _DTYPES[dtype], s))
+    return out
 
 
 class AdamW:
@@ -233,6 +237,7 @@ class AdamW:
             raise ValueError(f"parameters must be float32, float16 or bfloat16, got {first.dtype}")
         self.lr, self.betas, self.eps, self.weight_decay, self.bits = lr, tuple(betas), eps, weight_decay, bits
         self.steps = 0
+        self._dtype = first.dtype
         self._sizes = [p.numel() for p in self.params]
         room = -(-np.asarray(self._sizes, np.int64) // BLOCK) * BLOCK
         ends = np.cumsum(room)
@@ -253,57 +258,56 @@ class AdamW:
         """One step. grads: a contiguous tensor like each parameter, all of one floating type, or None for a
         parameter that this step leaves as it is. grad_scale: a float32 device tensor of one element that
         every gradient is multiplied by."""
-        params, sizes, table = self.params, self._sizes, self._table
+        params, index = self.params, self.m.get_device()
         if len(grads) != len(params):
             raise ValueError(f"{len(grads)} gradients for {len(params)} parameters")
-        dev, dtype, grad_dtype = self.m.device, params[0].dtype, None
-        pointers = []
-        for p, g, n in zip(params, grads, sizes):
-            if g is None:
-                pointers.append(0)
-                continue
-            if grad_dtype is None:
-                grad_dtype = g.dtype
-                if grad_dtype not in _DTYPES:
-                    raise ValueError(f"gradients must be float32, float16 or bfloat16, got {grad_dtype}")
-            if (g.dtype is not grad_dtype or g.numel() != n or g.device != dev or not g.is_contiguous()
-                    or p.numel() != n or p.device != dev or p.dtype is not dtype or not p.is_contiguous()):
-                raise ValueError("gradients must be contiguous tensors of one type and of their parameters' sizes, "
-                                 "and parameters as they were given")
-            pointers.append(g.data_ptr())
+        given, sizes = grads, self._sizes
+        if any(g is None for g in grads):
+            given = [g for g in grads if g is not None]
+            sizes = [n for g, n in zip(grads, sizes) if g is not None]
+        dtype = given[0].dtype if given else torch.float32
+        if dtype not in _DTYPES:
+            raise ValueError(f"gradients must be float32, float16 or bfloat16, got {dtype}")
+        if not self._fit(given, sizes, dtype):
+            raise ValueError("gradients must be contiguous tensors of one type and of their parameters' sizes, on "
+                             f"{self.m.device}")
+        if not self._fit(params, self._sizes, self._dtype):
+            raise ValueError("parameters must stay contiguous tensors of their type, size and device")
         if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1
-                                       or grad_scale.device != dev):
+                                       or grad_scale.get_device() != index):
             raise ValueError("grad_scale must be a float32 device tensor of one element")
-        table[:, 0] = [p.data_ptr() for p in params]
-        table[:, 1] = pointers
-        if grad_dtype is None:
-            grad_dtype = torch.float32
-
-        def call(s):
-            _check(lib.warp_adamw_step(table.ctypes.data, len(params), _DTYPES[dtype], _DTYPES[grad_dtype], self.bits,
-                                       self.m.data_ptr(), _ptr(self.m_scale), self.v.data_ptr(), _ptr(self.v_scale),
-                                       self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay,
-                                       self.steps + 1, _ptr(grad_scale), s))
-
-        if stream is None:
-            _run(None, (self.m,), call)
-        else:
-            _run(stream, (self.m, self.v, self.m_scale, self.v_scale, grad_scale, *params, *grads), call)
+        s = _here(self.m) if stream is None else None
+        if s is None:
+            return _there(stream, (self.m, self.v, self.m_scale, self.v_scale, grad_scale, *params, *grads),
+                          self.step, grads, grad_scale)
+        table = self._table
+        table[:, 0] = [*map(torch.Tensor.data_ptr, params)]
+        table[:, 1] = ([*map(torch.Tensor.data_ptr, grads)] if given is grads
+                       else [0 if g is None else g.data_ptr() for g in grads])
+        _check(lib.warp_adamw_step(table.ctypes.data, len(params), _DTYPES[self._dtype], _DTYPES[dtype], self.bits,
+                                   self.m.data_ptr(), _ptr(self.m_scale), self.v.data_ptr(), _ptr(self.v_scale),
+                                   self.lr, *self.betas, self.eps, self.weight_decay, self.steps + 1,
+                                   _ptr(grad_scale), s))
         self.steps += 1
+
+    def _fit(self, tensors, sizes, dtype) -> bool:
+        """Whether these are contiguous tensors of these sizes, of one type, on the moments' device."""
+        index = self.m.get_device()
+        return ([*map(torch.Tensor.numel, tensors)] == sizes and all(map(torch.Tensor.is_contiguous, tensors))
+                and all(t.dtype is dtype for t in tensors)
+                and all(i == index for i in map(torch.Tensor.get_device, tensors)))
 
     def moments(self, stream=None):
         """The flat float32 moments (m, v): with 32 bits the optimizer's own, with 8 the values of its codes."""
         if self.bits == 32:
             return self.m, self.v
-
-        def call(s):
-            out = torch.empty((2, self.size), dtype=torch.float32, device=self.m.device).unbind(0)
-            _check(lib.warp_adamw_moments(self.m.data_ptr(), self.m_scale.data_ptr(), self.v.data_ptr(),
-                                          self.v_scale.data_ptr(), self.size, out[0].data_ptr(), out[1].data_ptr(),
-                                          s))
-            return out
-
-        return _run(stream, (self.m, self.v, self.m_scale, self.v_scale), call)
+        s = _here(self.m) if stream is None else None
+        if s is None:
+            return _there(stream, (self.m, self.v, self.m_scale, self.v_scale), self.moments)
+        m, v = torch.empty((2, self.size), dtype=torch.float32, device=self.m.device).unbind(0)
+        _check(lib.warp_adamw_moments(self.m.data_ptr(), self.m_scale.data_ptr(), self.v.data_ptr(),
+                                      self.v_scale.data_ptr(), self.size, m.data_ptr(), v.data_ptr(), s))
+        return m, v
 
     def state_dict(self) -> dict:
         """What a checkpoint holds: the number of steps, the bits and the moments (the tensors themselves)."""
