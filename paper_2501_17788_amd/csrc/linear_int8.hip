@@ -31,6 +31,14 @@ constexpr int kBand = 4;
 typedef const __attribute__((address_space(1))) void global_void;
 typedef __attribute__((address_space(3))) void lds_void;
 
+// All but this wave's newest N loads have landed and its LDS reads too; then the same for every wave.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // A row's eight 16-byte pieces lie in LDS in an order of their own, piece ^ key, so that the rows that eight
 // neighbouring lanes read one piece of lie in different banks. Token blocks read rows 0 .. 15 in order. A
 // channel block j reads rows 4 j + i % 4 + 16 (i / 4), which gives a lane 16 neighbouring channels of a token.
@@ -39,20 +47,25 @@ template <int BN>
 __device__ __forceinline__ int channel_key(int row) { return (row & 3) | (row / (4 * BN) & 1) << 2; }
 
 // A workgroup makes a tile of TM tokens by TN channels with WM x WN waves. Each K step's rows are copied to LDS
-// by loads that pass no registers, into one of two buffers, while the matrix cores work on the other. The two
-// buffers are arrays of their own, so that the compiler sees that a read of one needs no wait for loads into the
-// other. Bound by the matrix cores and, at their rate, by power: a product of 8192 x 8192 by 8192 runs at 2.5e15
+// by loads that pass no registers, into one of STAGES buffers, while the matrix cores work on another. The
+// buffers are arrays of their own, so that the compiler sees that a read of one needs no wait for loads into
+// another. Bound by the matrix cores and, at their rate, by power: a product of 8192 x 8192 by 8192 runs at 2.5e15
 // operations a second with random values, 3.0e15 with zeros; counters show the matrix cores busy 61% of cycles.
-template <typename T, int TM, int TN, int WM, int WN>
+template <typename T, int TM, int TN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs g) {
     constexpr int kWaves = WM * WN;
     constexpr int kBM = TM / WM / 16, kBN = TN / WN / 16;  // 16 x 16 blocks of a wave
     constexpr int kLoadM = TM / 8 / kWaves, kLoadN = TN / 8 / kWaves;  // loads of 8 rows by a wave
+    static_assert(STAGES == 2 || STAGES == 4, "two or four buffers");
     static_assert(kLoadM * 8 * kWaves == TM && kLoadN * 8 * kWaves == TN, "whole loads");
     __shared__ __attribute__((aligned(16))) int8_t a0[TM * kStep];
     __shared__ __attribute__((aligned(16))) int8_t a1[TM * kStep];
+    __shared__ __attribute__((aligned(16))) int8_t a2[STAGES > 2 ? TM * kStep : 16];
+    __shared__ __attribute__((aligned(16))) int8_t a3[STAGES > 2 ? TM * kStep : 16];
     __shared__ __attribute__((aligned(16))) int8_t w0[TN * kStep];
     __shared__ __attribute__((aligned(16))) int8_t w1[TN * kStep];
+    __shared__ __attribute__((aligned(16))) int8_t w2[STAGES > 2 ? TN * kStep : 16];
+    __shared__ __attribute__((aligned(16))) int8_t w3[STAGES > 2 ? TN * kStep : 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, q = lane >> 4;
     const int wm = (wave / WN) * (TM / WM), wn = (wave % WN) * (TN / WN);
     // tiles of one XCD (every eighth workgroup) are neighbours: its L2 then serves their common rows
@@ -113,23 +126,39 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs g) {
     };
     // The operands of each half step are read while the matrix cores work on the half step before it, so the first
     // half of a step overlaps the second half of the last one, across the barrier.
-    auto step = [&](int k, int steps, const int8_t* la, const int8_t* lw, int8_t* na, int8_t* nw) {
-        __syncthreads();  // this step's rows have landed, and the other buffer's have all been read
-        if (k + 1 < steps) load(na, nw);
+    constexpr int kLoads = kLoadM + kLoadN;
+    const int steps = g.k / kStep;
+    auto step = [&](int k, const int8_t* la, const int8_t* lw, int8_t* na, int8_t* nw) {
+        // this step's rows have landed (the loads of STAGES - 2 later steps may be under way), and the buffer that
+        // is loaded next has been read by all
+        if (STAGES == 2 || k + 1 >= steps) wait_loads<0>();
+        else if (k + 2 >= steps) wait_loads<kLoads>();
+        else wait_loads<2 * kLoads>();
+        if (k + STAGES - 1 < steps) load(na, nw);
         read(part[0], la, lw, 0);
         if (k) multiply(part[1]);
         read(part[1], la, lw, 1);
         multiply(part[0]);
     };
     load(a0, w0);
-    const int steps = g.k / kStep;
-    step(0, steps, a0, w0, a1, w1);
-    int k = 1;
-    for (; k + 1 < steps; k += 2) {
-        step(k, steps, a1, w1, a0, w0);
-        step(k + 1, steps, a0, w0, a1, w1);
+    if (STAGES == 2) {
+        step(0, a0, w0, a1, w1);
+        int k = 1;
+        for (; k + 1 < steps; k += 2) {
+            step(k, a1, w1, a0, w0);
+            step(k + 1, a0, w0, a1, w1);
+        }
+        if (k < steps) step(k, a1, w1, a0, w0);
+    } else {
+        if (1 < steps) load(a1, w1);
+        if (2 < steps) load(a2, w2);
+        for (int k = 0; k < steps; k += 4) {
+            step(k, a0, w0, a3, w3);
+            if (k + 1 < steps) step(k + 1, a1, w1, a0, w0);
+            if (k + 2 < steps) step(k + 2, a2, w2, a1, w1);
+            if (k + 3 < steps) step(k + 3, a3, w3, a2, w2);
+        }
     }
-    if (k < steps) step(k, steps, a1, w1, a0, w0);
     multiply(part[1]);
     // D[row][col] of a block lies in lane col + 16 (row / 4), element row % 4: lane (li, q) holds channels
     // 16 q + 4 j + r, r = 0 .. 3, of token li of block i
@@ -160,64 +189,119 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs g) {
     }
 }
 
-// Each wave multiplies 32 tokens by 32 channels straight from memory: v_mfma_i32_16x16x64_i8 takes 16 bytes of
-// row lane % 16 from each lane, and lane / 16 picks the quarter of 64 columns.
-template <typename T>
-__global__ __launch_bounds__(256) void k_linear_direct(LinearArgs g) {
+// Few tiles: a workgroup's eight waves share the columns of one tile of 16 BM tokens by 16 BN channels. Wave w takes
+// the steps w, w + 8, ..., straight from memory, and the waves' sums meet in LDS (integer additions: their order does
+// not matter).
+constexpr int kSplit = 8;
+template <typename T, int BM, int BN>
+__global__ __launch_bounds__(64 * kSplit) void k_linear_split(LinearArgs g) {
+    constexpr int TM = 16 * BM, TN = 16 * BN, kRow = TN + 4;  // a row's padding spreads rows over the banks
+    __shared__ int sums[TM * kRow];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, q = lane >> 4;
-    const int64_t m0 = (int64_t)blockIdx.x * 64 + (wave & 1) * 32;
-    const int64_t c0 = (int64_t)blockIdx.y * 64 + (wave >> 1) * 32;
-    const int8_t *pa[2], *pw[2];
+    const int64_t m0 = (int64_t)blockIdx.x * TM, c0 = (int64_t)blockIdx.y * TN;
+    for (int i = threadIdx.x; i < TM * kRow; i += 64 * kSplit) sums[i] = 0;
+    const int8_t *pa[BM], *pw[BN];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int64_t m = m0 + 16 * i + li, c = c0 + 16 * i + li;
-        pa[i] = g.a + (m < g.rows ? m : g.rows - 1) * g.a_stride + 16 * q;
-        pw[i] = g.w + (c < g.n ? c : g.n - 1) * g.w_stride + 16 * q;
-    }
-    int4v acc[2][2] = {};
-    for (int k = 0; k < g.k; k += 64) {
-        int4v va[2], vw[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) va[i] = *(const int4v*)(pa[i] + k), vw[i] = *(const int4v*)(pw[i] + k);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vw[j], va[i], acc[i][j], 0, 0, 0);
-    }
-    // lane (li, q) holds channels 4 q .. 4 q + 3 of block j for token li of block i
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < BM; ++i) {
         const int64_t m = m0 + 16 * i + li;
-        if (m >= g.rows) continue;
-        const float sa = g.a_scale[m];
+        pa[i] = g.a + (m < g.rows ? m : g.rows - 1) * g.a_stride + 16 * q + wave * kStep;
+    }
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < BN; ++j) {
+        const int64_t c = c0 + 16 * j + li;
+        pw[j] = g.w + (c < g.n ? c : g.n - 1) * g.w_stride + 16 * q + wave * kStep;
+    }
+    // a step's pieces are under way while the one before is multiplied
+    struct Pieces {
+        int4v a[2][BM], w[2][BN];
+    } p0, p1;
+    auto load = [&](Pieces& p) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int64_t c = c0 + 16 * j + 4 * q + r;
-                if (c < g.n) {
-                    const float b = g.bias ? g.bias[c] : 0.f;
-                    ((T*)g.out)[m * g.out_stride + c] = (T)((float)acc[i][j][r] * g.w_scale[c] * sa + b);
-                }
-            }
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int j = 0; j < BN; ++j) p.w[h][j] = *(const int4v*)(pw[j] + 64 * h);
+#pragma unroll
+            for (int i = 0; i < BM; ++i) p.a[h][i] = *(const int4v*)(pa[i] + 64 * h);
+        }
+#pragma unroll
+        for (int i = 0; i < BM; ++i) pa[i] += kSplit * kStep;
+#pragma unroll
+        for (int j = 0; j < BN; ++j) pw[j] += kSplit * kStep;
+    };
+    int4v acc[BM][BN] = {};
+    auto multiply = [&](const Pieces& p) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < BM; ++i)
+#pragma unroll
+                for (int j = 0; j < BN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(p.w[h][j], p.a[h][i], acc[i][j], 0, 0, 0);
+    };
+    int left = (g.k / kStep - wave + kSplit - 1) / kSplit;  // this wave's steps
+    if (left > 0) load(p0);
+    for (; left > 0; left -= 2) {
+        if (left > 1) load(p1);
+        multiply(p0);
+        if (left > 2) load(p0);
+        if (left > 1) multiply(p1);
+    }
+    __syncthreads();
+    if (wave * kStep < g.k) {
+#pragma unroll
+        for (int i = 0; i < BM; ++i)
+#pragma unroll
+            for (int j = 0; j < BN; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) atomicAdd(&sums[(16 * i + li) * kRow + 16 * j + 4 * q + r], acc[i][j][r]);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < TM * TN; i += 64 * kSplit) {
+        const int row = i / TN, col = i % TN;
+        const int64_t m = m0 + row, c = c0 + col;
+        if (m < g.rows && c < g.n)
+            ((T*)g.out)[m * g.out_stride + c] =
+                (T)((float)sums[row * kRow + col] * g.w_scale[c] * g.a_scale[m] + (g.bias ? g.bias[c] : 0.f));
     }
 }
 
+template <typename T, int BM, int BN>
+void split(const LinearArgs& g, hipStream_t s) {
+    const dim3 grid((uint32_t)((g.rows + 16 * BM - 1) / (16 * BM)), (g.n + 16 * BN - 1) / (16 * BN));
+    hipLaunchKernelGGL((k_linear_split<T, BM, BN>), grid, dim3(64 * kSplit), 0, s, g);
+}
+
+template <typename T, int TM, int TN, int WM, int WN, int STAGES>
+void tiles(const LinearArgs& g, hipStream_t s) {
+    const int64_t n = ((g.rows + TM - 1) / TM) * ((g.n + TN - 1) / TN);
+    hipLaunchKernelGGL((k_linear_tile<T, TM, TN, WM, WN, STAGES>), dim3((uint32_t)n), dim3(64 * WM * WN), 0, s, g);
+}
+
+inline int64_t cover(int64_t n, int64_t of) { return (n + of - 1) / of; }
+
+// Which kernel, by measured times (us, in a graph, operands in the caches; tokens x channels x columns):
+// * up to six 16 x 16 tiles a compute unit, a tile's columns are split among waves, 16 x 16, 32 x 16 or 32 x 32 tiles so
+//   that there are about as many tiles as compute units: 1 x 1024 x 1024 2.8 (64 x 128 tiles 5.9), 64 x 1024 x 1024 3.3
+//   (7.0), 128 x 1024 x 1024 3.9 (16 x 16 4.1, 32 x 32 4.7), 300 x 800 x 800 4.5 (6.5), 256 x 1024 x 4096 10.6 (15.5)
+// * tiles of 64 x 128, three workgroups on a compute unit; with no more tiles than compute units one of four stages:
+//   512 x 4096 x 4096 19.4 (two stages 24.3), 1771 x 1003 x 771 7.9 (128 x 128 10.5), 10,000 x 800 x 800 17.8
+//   (128 x 128 21.9, 256 x 256 21.4)
+// * tiles of 128 x 128, two workgroups on a compute unit, where all of them run at once and those of 64 x 128 would not:
+//   2000 x 4000 x 4000 41.7 (51.4), 65,536 x 128 x 1024 19.9 (21.3)
+// * tiles of 256 x 256 where their rounds, each as long as 2.3 of 64 x 128, are fewer: 16,384 x 1024 x 1024 27.3 (31.7),
+//   20,000 x 1500 x 2000 80.5 (95.6), 20,000 x 800 x 800 38.2 (30.2, not taken)
 template <typename T>
 void linear(const LinearArgs& g, hipStream_t s) {
-    if (g.rows > 64) {
-        const int64_t big = ((g.rows + 255) / 256) * ((g.n + 255) / 256);
-        if (big >= 256) {
-            hipLaunchKernelGGL((k_linear_tile<T, 256, 256, 2, 4>), dim3((uint32_t)big), dim3(512), 0, s, g);
-            return;
-        }
-        const int64_t mid = ((g.rows + 127) / 128) * ((g.n + 127) / 128);
-        hipLaunchKernelGGL((k_linear_tile<T, 128, 128, 2, 2>), dim3((uint32_t)mid), dim3(256), 0, s, g);
-        return;
-    }
-    const dim3 grid((uint32_t)((g.rows + 63) / 64), (g.n + 63) / 64);
-    hipLaunchKernelGGL(k_linear_direct<T>, grid, dim3(256), 0, s, g);
+    constexpr int64_t kUnits = 256;
+    const int64_t m = g.rows, n = g.n, t16 = cover(m, 16) * cover(n, 16), t64 = cover(m, 64) * cover(n, 128);
+    if (t16 <= kUnits) return split<T, 1, 1>(g, s);
+    if (t16 <= 2 * kUnits) return split<T, 2, 1>(g, s);
+    if (t16 <= 6 * kUnits) return split<T, 2, 2>(g, s);
+    if (t64 <= kUnits) return tiles<T, 64, 128, 2, 2, 4>(g, s);
+    if (t64 > 3 * kUnits && cover(m, 128) * cover(n, 128) <= 2 * kUnits) return tiles<T, 128, 128, 2, 2, 2>(g, s);
+    if (23 * cover(cover(m, 256) * cover(n, 256), kUnits) * 3 * kUnits < 10 * t64)
+        return tiles<T, 256, 256, 2, 4, 2>(g, s);
+    tiles<T, 64, 128, 2, 2, 2>(g, s);
 }
 
 }  // namespace
@@ -250,6 +334,9 @@ extern "C" int warp_linear_int8(const int8_t* a, int64_t a_stride, const float* 
         return fail(WARP_EINVAL, "%s: misaligned pointer", what);
     if (rows > 1 && out_stride < n)
         return fail(WARP_EINVAL, "%s: a row stride of %lld is below %d columns", what, (long long)out_stride, n);
+    if (cover(rows, 64) * cover(n, 128) >= 1 << 24)
+        return fail(WARP_ENOTSUP, "%s: %lld rows by %d channels are more than 2^24 tiles of 64 x 128", what,
+                    (long long)rows, n);
     const int rc = require_device();
     if (rc || !rows) return rc;
     const LinearArgs g{a, a_stride, a_scale, rows, w, w_stride, w_scale, n, padded, bias, out, out_stride};

@@ -95,6 +95,7 @@ def test_int8_rows_refusals(over):
     (dict(a_stride=112), w.EINVAL, "alignment"), (dict(w_stride=136), w.EINVAL, "alignment"),
     (dict(out=P + 1), w.EINVAL, "misaligned"), (dict(bias=P + 2), w.EINVAL, "misaligned"),
     (dict(a_stride=(1 << 23) + 16), w.ENOTSUP, "2^23"), (dict(w_stride=1 << 24), w.ENOTSUP, "2^23"),
+    (dict(rows=1 << 24, n=1 << 21, out_stride=1 << 21), w.ENOTSUP, "tiles"),
     (dict(out_stride=6), w.EINVAL, "stride"), (dict(dtype=9), w.EINVAL, "dtype"),
 ])
 def test_linear_int8_refusals(over, code, needle):
