@@ -358,7 +358,7 @@ int warp_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, i
                              const float* rstd, void* dx, int64_t dx_stride, void* dweight, void* dbias,
                              void* scratch, int64_t scratch_bytes, void* hip_stream);
 /* Host-only: bytes of scratch that the call above needs for these sizes (WARP_EINVAL for bad ones). */
-int warp_layer_norm_backward_scratch(int64_t rows, int32_t cols, int64_t* bytes);
+int warp_layer_norm_backward_scratch(int64_t rows, int32_t cols, int32_t dtype, int64_t* bytes);
 
 /*
  * Rows in 8-bit integers, with a scale for each: x is about q * scale. With a = max |x| of the row,

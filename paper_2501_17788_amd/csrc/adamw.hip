@@ -99,10 +99,7 @@ __device__ __forceinline__ float v_code(float x) {
 
 // Largest over the 32 lanes of a half wave.
 __device__ __forceinline__ uint32_t half_max(uint32_t x) {
-    x = max(x, dpp<kDppXor1, 0xf>(x));
-    x = max(x, dpp<kDppXor2, 0xf>(x));
-    x = max(x, dpp<kDppHalfMirror, 0xf>(x));
-    x = max(x, dpp<kDppMirror, 0xf>(x));
+    x = quarter_max(x);
     return max(x, (uint32_t)__shfl_xor((int)x, 16));
 }
 

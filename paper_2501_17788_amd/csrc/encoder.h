@@ -46,8 +46,8 @@ __device__ __forceinline__ void store_vec(T* p, const Vec<T, V>& v) {
     *reinterpret_cast<Vec<T, V>*>(p) = v;
 }
 
-// Sum over the wave's 64 lanes, returned to every lane: four steps inside rows of 16 lanes, then
-// the rows' sums carried up to lane 63.
+// Sums over 16 lanes of a wave or all 64, returned to every lane: four steps inside 16 lanes, then
+// those sums carried up to lane 63.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ uint32_t dpp(uint32_t x) {
     return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
@@ -58,11 +58,14 @@ constexpr int kDppBcast15 = 0x142, kDppBcast31 = 0x143;
 __device__ __forceinline__ float as_f(uint32_t u) { return __uint_as_float(u); }
 __device__ __forceinline__ uint32_t as_u(float f) { return __float_as_uint(f); }
 
-__device__ __forceinline__ float wave_sum(float x) {
+__device__ __forceinline__ float quarter_sum(float x) {  // over 16 lanes
     x += as_f(dpp<kDppXor1, 0xf>(as_u(x)));
     x += as_f(dpp<kDppXor2, 0xf>(as_u(x)));
     x += as_f(dpp<kDppHalfMirror, 0xf>(as_u(x)));
-    x += as_f(dpp<kDppMirror, 0xf>(as_u(x)));
+    return x + as_f(dpp<kDppMirror, 0xf>(as_u(x)));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+    x = quarter_sum(x);
     x += as_f(dpp<kDppBcast15, 0xa>(as_u(x)));
     x += as_f(dpp<kDppBcast31, 0xc>(as_u(x)));
     return as_f((uint32_t)__builtin_amdgcn_readlane((int)as_u(x), 63));
@@ -70,11 +73,14 @@ __device__ __forceinline__ float wave_sum(float x) {
 
 // The same for the largest of unsigned numbers (magnitudes of floats by their bits: a NaN is above
 // infinity, which is above every number).
-__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+__device__ __forceinline__ uint32_t quarter_max(uint32_t x) {
     x = max(x, dpp<kDppXor1, 0xf>(x));
     x = max(x, dpp<kDppXor2, 0xf>(x));
     x = max(x, dpp<kDppHalfMirror, 0xf>(x));
-    x = max(x, dpp<kDppMirror, 0xf>(x));
+    return max(x, dpp<kDppMirror, 0xf>(x));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+    x = quarter_max(x);
     x = max(x, dpp<kDppBcast15, 0xa>(x));
     x = max(x, dpp<kDppBcast31, 0xc>(x));
     return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);

@@ -6,7 +6,9 @@
 //
 // Everything is computed in 32 bits; y, dx, dw and db are rounded once, to their own type. A row stays
 // in registers between its loads and its stores, so each element is read once and written once, and
-// the variance sums squared distances from the finished mean.
+// the variance sums squared distances from the finished mean. Bound by memory; a large copy moves 5.1 to 5.6 TB/s.
+// 131,072 rows of 1,024 bfloat16: forward 103 us (5.2 TB/s), backward with its sums 162 us (5.0 TB/s); 100,000 of 128:
+// 10 and 20 us; 65,536 of 1,024 to int8 38 us (5.3 TB/s); 32 of 768: 3.3 and 6.9 us, two launches in the backward pass.
 #include "encoder.h"
 
 namespace warp {
@@ -14,6 +16,16 @@ namespace warp {
 namespace {
 
 constexpr int kNormal = 0, kNormInt8 = 1, kInt8 = 2;  // what k_rows makes of a row
+
+// N words at any address
+template <int N>
+struct __attribute__((packed, aligned(1))) Words {
+    uint32_t e[N];
+};
+template <>
+struct Words<0> {
+    uint32_t e[1];
+};
 
 struct RowArgs {
     const void* x;
@@ -32,7 +44,7 @@ struct RowArgs {
     float* scale;
 };
 
-// Where a lane's vector j of a row lies. WAVES waves share a row of COLS columns; the row's last
+// Where a lane's vector j of a row lies, of the `threads` lanes that share the row. The row's last
 // vector is moved back so that it ends with the row, and its first `skip` elements are left to its
 // neighbour: it reads and writes them too (the same values) and leaves them out of sums.
 struct Place {
@@ -63,70 +75,104 @@ __device__ __forceinline__ void load_params(const void* p, bool f32, int at, flo
     }
 }
 
-// Sum (or largest) over the WAVES waves of a row's workgroup; `part` has a slot for each wave.
-template <int WAVES>
+// Sum (or largest) over the LANES lanes of a row: a quarter of a wave, a wave, or a workgroup of several, whose `part`
+// has a slot for each.
+template <int LANES>
 __device__ __forceinline__ float row_sum(float x, float* part) {
+    if (LANES == 16) return quarter_sum(x);
     x = wave_sum(x);
-    if (WAVES == 1) return x;
+    if (LANES == kWave) return x;
     __syncthreads();  // the last reduction's slots have been read
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
     float s = 0.f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) s += part[w];
+    for (int w = 0; w < LANES / kWave; ++w) s += part[w];
     return s;
 }
-template <int WAVES>
+template <int LANES>
 __device__ __forceinline__ uint32_t row_max(uint32_t x, float* part) {
+    if (LANES == 16) return quarter_max(x);
     x = wave_max(x);
-    if (WAVES == 1) return x;
+    if (LANES == kWave) return x;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = as_f(x);
     __syncthreads();
     uint32_t s = 0;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) s = max(s, as_u(part[w]));
+    for (int w = 0; w < LANES / kWave; ++w) s = max(s, as_u(part[w]));
     return s;
 }
 
-// One row by WAVES waves, NC vectors of V elements in each lane; a workgroup of max(4, WAVES) waves.
-template <typename T, int V, int NC, int WAVES, bool RAGGED, int MODE>
-__global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void k_rows(RowArgs a) {
-    __shared__ float part[WAVES];
-    constexpr int kRows = WAVES < 4 ? 4 / WAVES : 1;  // rows of a workgroup
-    constexpr int kThreads = WAVES * kWave;           // of a row
-    const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+// q = rint(v * inv) of four elements as the bytes of a word: adding 1.5 * 2^23 to the rounded product rounds it to
+// the nearest even integer, whose two's complement is then in the sum's low bits.
+__device__ __forceinline__ uint32_t four_bytes(const float* v, float inv) {
+#pragma clang fp contract(off)
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = as_u(v[i] * inv + 12582912.0f);
+    const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u);
+    return __builtin_amdgcn_perm(u[3], u[2], 0x04000c0cu) | lo;
+}
+
+// Rows by LANES lanes, NC vectors of V elements in each; a workgroup of 256 lanes or LANES, if more. A workgroup goes
+// through several rows where there are many: the next row is loaded while one is worked on, and up to 32 columns a
+// lane their weights and biases stay in registers (65,536 rows of 1,024 to int8: 71 us without both, 38 us with). Rows
+// of at most 32 vectors take 16 lanes each (100,000 of 128 bfloat16: 23 us by whole waves, 10 us).
+template <typename T, int V, int NC, int LANES, bool RAGGED, int MODE>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rows(RowArgs a) {
+    __shared__ float part[16];
+    constexpr int kRows = LANES < 256 ? 256 / LANES : 1;  // rows of a workgroup
+    constexpr bool kKeep = NC * V <= 32 && MODE != kInt8;
+    const int t = threadIdx.x % LANES;
     const int cols = a.cols;
     const float inv_n = 1.0f / (float)cols;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? threadIdx.x >> 6 : 0); row < a.rows;
-         row += (int64_t)gridDim.x * kRows) {
-        const T* x = (const T*)a.x + row * a.x_stride;
-        float v[NC][V];
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
+    Vec<T, V> next[NC];
+    auto load = [&](int64_t r) {
+        const T* x = (const T*)a.x + r * a.x_stride;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-            const Place p = place<V, RAGGED>(j, kThreads, t, cols);
-            if (p.in) {
-                const auto r = load_vec<T, V>(x + p.at);
-#pragma unroll
-                for (int i = 0; i < V; ++i) v[j][i] = (float)r.e[i];
-            }
+            const Place p = place<V, RAGGED>(j, LANES, t, cols);
+            if (p.in) next[j] = load_vec<T, V>(x + p.at);
         }
+    };
+    if (row < a.rows) load(row);
+    float w[kKeep ? NC : 1][V], b[kKeep ? NC : 1][V];
+    auto params = [&](int j, int k, const Place& p) {  // of vector j, into w[k] and b[k]
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[k][i] = 1.f, b[k][i] = 0.f;
+        if (p.in && a.weight) load_params<T, V>(a.weight, a.params_f32, p.at, w[k]);
+        if (p.in && a.bias) load_params<T, V>(a.bias, a.params_f32, p.at, b[k]);
+    };
+    if (kKeep) {
+#pragma unroll
+        for (int j = 0; j < NC; ++j) params(j, j, place<V, RAGGED>(j, LANES, t, cols));
+    }
+    for (; row < a.rows; row += step) {
+        float v[NC][V];
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[j][i] = (float)next[j].e[i];
+        if (row + step < a.rows) load(row + step);
         if (MODE != kInt8) {
             float s = 0.f;
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-                const Place p = place<V, RAGGED>(j, kThreads, t, cols);
+                const Place p = place<V, RAGGED>(j, LANES, t, cols);
                 if (p.in) {
 #pragma unroll
                     for (int i = 0; i < V; ++i)
                         if (!RAGGED || i >= p.skip) s += v[j][i];
                 }
             }
-            const float mean = row_sum<WAVES>(s, part) * inv_n;
+            const float mean = row_sum<LANES>(s, part) * inv_n;
             s = 0.f;
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-                const Place p = place<V, RAGGED>(j, kThreads, t, cols);
+                const Place p = place<V, RAGGED>(j, LANES, t, cols);
                 if (p.in) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
@@ -135,36 +181,24 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void k_rows(RowArgs a
                     }
                 }
             }
-            const float rstd = 1.0f / sqrtf(row_sum<WAVES>(s, part) * inv_n + a.eps);
+            const float rstd = 1.0f / sqrtf(row_sum<LANES>(s, part) * inv_n + a.eps);
             if (t == 0 && a.mean) {
                 a.mean[row] = mean;
                 a.rstd[row] = rstd;
             }
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-                const Place p = place<V, RAGGED>(j, kThreads, t, cols);
-                if (p.in) {
+                const int k = kKeep ? j : 0;
+                if (!kKeep) params(j, k, place<V, RAGGED>(j, LANES, t, cols));
 #pragma unroll
-                    for (int i = 0; i < V; ++i) v[j][i] *= rstd;
-                    float w[V];
-                    if (a.weight) {
-                        load_params<T, V>(a.weight, a.params_f32, p.at, w);
-#pragma unroll
-                        for (int i = 0; i < V; ++i) v[j][i] *= w[i];
-                    }
-                    if (a.bias) {
-                        load_params<T, V>(a.bias, a.params_f32, p.at, w);
-#pragma unroll
-                        for (int i = 0; i < V; ++i) v[j][i] += w[i];
-                    }
-                }
+                for (int i = 0; i < V; ++i) v[j][i] = v[j][i] * rstd * w[k][i] + b[k][i];
             }
         }
         if (MODE == kNormal) {
             T* y = (T*)a.y + row * a.y_stride;
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-                const Place p = place<V, RAGGED>(j, kThreads, t, cols);
+                const Place p = place<V, RAGGED>(j, LANES, t, cols);
                 if (p.in) {
                     Vec<T, V> r;
 #pragma unroll
@@ -176,28 +210,33 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void k_rows(RowArgs a
             uint32_t m = 0;
 #pragma unroll
             for (int j = 0; j < NC; ++j)
-                if (place<V, RAGGED>(j, kThreads, t, cols).in) {
+                if (place<V, RAGGED>(j, LANES, t, cols).in) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) m = max(m, as_u(v[j][i]) & 0x7fffffffu);
                 }
-            const float top = as_f(row_max<WAVES>(m, part));
+            const float top = as_f(row_max<LANES>(m, part));
             // 127 / top is finite for a top of at least 2^-120; a row of smaller numbers is a row of zeros, and one
             // with an infinity or a NaN has zeros too and a scale that is no number, which its products then are
             const bool some = top >= 0x1p-120f && top < INFINITY;
             const float inv = some ? 127.0f / top : 0.f;
+            const uint32_t keep = some ? ~0u : 0u;
             int8_t* q = a.q + row * a.q_stride;
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-                const Place p = place<V, RAGGED>(j, kThreads, t, cols);
+                const Place p = place<V, RAGGED>(j, LANES, t, cols);
                 if (p.in) {
-                    Vec<int8_t, V> r;
+                    if (V == 1) {
+                        q[p.at] = some ? (int8_t)(int)rintf(v[j][0] * inv) : (int8_t)0;
+                    } else {
+                        Words<V / 4> r;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) r.e[i] = some ? (int8_t)(int)rintf(v[j][i] * inv) : (int8_t)0;
-                    store_vec<int8_t, V>(q + p.at, r);
+                        for (int i = 0; i < V / 4; ++i) r.e[i] = four_bytes(v[j] + 4 * i, inv) & keep;
+                        *reinterpret_cast<Words<V / 4>*>(q + p.at) = r;
+                    }
                 }
             }
             const int padded = (cols + kInt8Pad - 1) / kInt8Pad * kInt8Pad;
-            for (int c = cols + t; c < padded; c += kThreads) q[c] = 0;
+            for (int c = cols + t; c < padded; c += LANES) q[c] = 0;
             if (t == 0) a.scale[row] = top < INFINITY ? top * (1.0f / 127.0f) : NAN;
         }
     }
@@ -219,44 +258,52 @@ struct BackArgs {
 };
 
 // dx, and each workgroup's share of dw and db. The weight and both sums of a lane's columns stay in registers
-// over all rows of the workgroup; no atomics, so the sums' order is fixed by the sizes alone.
-template <typename T, int V, int NC, int WAVES, bool RAGGED>
-__global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void k_rows_back(BackArgs a) {
-    extern __shared__ float lds[];  // [2][cols] where waves have rows of their own; else [2 * WAVES]
-    constexpr int kRows = WAVES < 4 ? 4 / WAVES : 1;
-    constexpr int kThreads = WAVES * kWave;
-    const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+// over all rows of the workgroup; no atomics, so the sums' order is fixed by the sizes alone. With the next row's loads
+// under way and four waves on each SIMD instead of two, 131,072 rows of 1,024 went from 240 to 150 us.
+template <typename T, int V, int NC, int LANES, bool RAGGED>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rows_back(BackArgs a) {
+    // two waves' sums of their columns where waves have rows of their own; else two sums of each wave
+    __shared__ float lds[LANES <= kWave ? 2 * 2 * NC * V * kWave : 2 * 16];
+    constexpr int kRows = LANES < 256 ? 256 / LANES : 1;
+    const int t = threadIdx.x % LANES;
     const int wave = threadIdx.x >> 6;
     const int cols = a.cols;
     const float inv_n = 1.0f / (float)cols;
     float w[NC][V], dw[NC][V], db[NC][V];
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-        const Place p = place<V, RAGGED>(j, kThreads, t, cols);
+        const Place p = place<V, RAGGED>(j, LANES, t, cols);
 #pragma unroll
         for (int i = 0; i < V; ++i) w[j][i] = 1.f, dw[j][i] = 0.f, db[j][i] = 0.f;
         if (p.in && a.weight) load_params<T, V>(a.weight, a.params_f32, p.at, w[j]);
     }
-    for (int64_t row = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave : 0); row < a.rows;
-         row += (int64_t)gridDim.x * kRows) {
-        const T* x = (const T*)a.x + row * a.x_stride;
-        const T* dy = (const T*)a.dy + row * a.dy_stride;
-        float h[NC][V], c[NC][V];
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
+    Vec<T, V> next_x[NC], next_dy[NC];
+    float next_mean = 0.f, next_rstd = 0.f;
+    auto load = [&](int64_t r) {
+        const T* x = (const T*)a.x + r * a.x_stride;
+        const T* dy = (const T*)a.dy + r * a.dy_stride;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-            const Place p = place<V, RAGGED>(j, kThreads, t, cols);
-            if (p.in) {
-                const auto rx = load_vec<T, V>(x + p.at);
-                const auto rd = load_vec<T, V>(dy + p.at);
-#pragma unroll
-                for (int i = 0; i < V; ++i) h[j][i] = (float)rx.e[i], c[j][i] = (float)rd.e[i];
-            }
+            const Place p = place<V, RAGGED>(j, LANES, t, cols);
+            if (p.in) next_x[j] = load_vec<T, V>(x + p.at), next_dy[j] = load_vec<T, V>(dy + p.at);
         }
-        const float mean = a.mean[row], rstd = a.rstd[row];
+        next_mean = a.mean[r], next_rstd = a.rstd[r];
+    };
+    if (row < a.rows) load(row);
+    for (; row < a.rows; row += step) {
+        float h[NC][V], c[NC][V];
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) h[j][i] = (float)next_x[j].e[i], c[j][i] = (float)next_dy[j].e[i];
+        const float mean = next_mean, rstd = next_rstd;
+        if (row + step < a.rows) load(row + step);
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-            const Place p = place<V, RAGGED>(j, kThreads, t, cols);
+            const Place p = place<V, RAGGED>(j, LANES, t, cols);
             if (p.in) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
@@ -268,20 +315,21 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void k_rows_back(Back
                 }
             }
         }
-        s1 = wave_sum(s1), s2 = wave_sum(s2);
-        if (WAVES > 1) {
+        if (LANES == 16) s1 = quarter_sum(s1), s2 = quarter_sum(s2);
+        else s1 = wave_sum(s1), s2 = wave_sum(s2);
+        if (LANES > kWave) {
             __syncthreads();
             if ((threadIdx.x & 63) == 0) lds[2 * wave] = s1, lds[2 * wave + 1] = s2;
             __syncthreads();
             s1 = s2 = 0.f;
 #pragma unroll
-            for (int k = 0; k < WAVES; ++k) s1 += lds[2 * k], s2 += lds[2 * k + 1];
+            for (int k = 0; k < LANES / kWave; ++k) s1 += lds[2 * k], s2 += lds[2 * k + 1];
         }
         s1 *= inv_n, s2 *= inv_n;
         T* dx = (T*)a.dx + row * a.dx_stride;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-            const Place p = place<V, RAGGED>(j, kThreads, t, cols);
+            const Place p = place<V, RAGGED>(j, LANES, t, cols);
             if (p.in) {
                 Vec<T, V> r;
 #pragma unroll
@@ -291,89 +339,114 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void k_rows_back(Back
         }
     }
     if (!a.parts) return;
-    float* out = a.parts + (int64_t)blockIdx.x * 2 * cols;
-    if (WAVES == 1) {
-        // the four waves' sums one after the other; a moved-back vector leaves its first elements out
-        for (int k = 0; k < 4; ++k) {
-            if (wave == k) {
+    if (LANES == 16) {  // the sums of a wave's four rows meet in each of them
 #pragma unroll
-                for (int j = 0; j < NC; ++j) {
-                    const Place p = place<V, RAGGED>(j, kThreads, t, cols);
-                    if (p.in) {
+        for (int j = 0; j < NC; ++j)
 #pragma unroll
-                        for (int i = 0; i < V; ++i)
-                            if (!RAGGED || i >= p.skip) {
-                                float& sw = lds[p.at + i];
-                                float& sb = lds[cols + p.at + i];
-                                sw = k == 0 ? dw[j][i] : sw + dw[j][i];
-                                sb = k == 0 ? db[j][i] : sb + db[j][i];
-                            }
+            for (int i = 0; i < V; ++i)
+#pragma unroll
+                for (int k = 16; k < kWave; k <<= 1) dw[j][i] += __shfl_xor(dw[j][i], k), db[j][i] += __shfl_xor(db[j][i], k);
+    }
+    if (LANES <= kWave) {
+        // the four waves' sums meet in the first: two and two, then one and one
+        constexpr int kHeld = 2 * NC * V;
+#pragma unroll
+        for (int half = 2; half; half >>= 1) {
+            float* slot = lds + (wave & (half - 1)) * kHeld * kWave + (threadIdx.x & 63);
+            __syncthreads();
+            if (wave >= half && wave < 2 * half) {
+#pragma unroll
+                for (int j = 0; j < NC; ++j)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        slot[(2 * (j * V + i)) * kWave] = dw[j][i];
+                        slot[(2 * (j * V + i) + 1) * kWave] = db[j][i];
                     }
-                }
             }
             __syncthreads();
-        }
-        for (int c = threadIdx.x; c < 2 * cols; c += 256) out[c] = lds[c];
-    } else {
+            if (wave < half) {
 #pragma unroll
-        for (int j = 0; j < NC; ++j) {
-            const Place p = place<V, RAGGED>(j, kThreads, t, cols);
-            if (p.in) {
+                for (int j = 0; j < NC; ++j)
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    out[p.at + i] = dw[j][i];
-                    out[cols + p.at + i] = db[j][i];
-                }
+                    for (int i = 0; i < V; ++i) {
+                        dw[j][i] += slot[(2 * (j * V + i)) * kWave];
+                        db[j][i] += slot[(2 * (j * V + i) + 1) * kWave];
+                    }
             }
+        }
+        if (threadIdx.x >= LANES) return;
+    }
+    float* out = a.parts + (int64_t)blockIdx.x * 2 * cols;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+        const Place p = place<V, RAGGED>(j, LANES, t, cols);
+        if (p.in) {
+            Vec<float, V> rw, rb;
+#pragma unroll
+            for (int i = 0; i < V; ++i) rw.e[i] = dw[j][i], rb.e[i] = db[j][i];
+            store_vec<float, V>(out + p.at, rw);
+            store_vec<float, V>(out + cols + p.at, rb);
         }
     }
 }
 
-// dw and db: the workgroups' shares added up. A workgroup takes 64 of the 2 cols sums, 16 threads each.
+// dw and db: the workgroups' shares added up. A workgroup takes 32 of the 2 cols sums, 32 threads each.
 __global__ __launch_bounds__(1024) void k_join_params(const float* parts, int32_t n_parts, int32_t cols, void* dw,
                                                       void* db, int32_t dtype) {
-    __shared__ float lds[16][64];
+    __shared__ float lds[32][33];
     const int64_t n = 2 * (int64_t)cols;
-    const int64_t c = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
-    const int slice = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     float s = 0.f;
-    if (c < n)
-        for (int g = slice; g < n_parts; g += 16) s += parts[g * n + c];
-    lds[slice][threadIdx.x & 63] = s;
+    if (c < n) {
+        float v[32];  // all loads at once: the shares come from other XCDs' memory
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] = slice + 32 * k < n_parts ? parts[(slice + 32 * k) * n + c] : 0.f;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) s += v[k];
+    }
+    lds[slice][lane] = s;
     __syncthreads();
-    if (slice || c >= n) return;
-    for (int k = 1; k < 16; ++k) s += lds[k][threadIdx.x];
-    void* out = c < cols ? dw : db;
-    const int64_t at = c < cols ? c : c - cols;
+    // 32 neighbouring lanes take one column's slices
+    s = lds[lane][slice];
+#pragma unroll
+    for (int k = 16; k; k >>= 1) s += __shfl_xor(s, k);
+    const int64_t out_c = (int64_t)blockIdx.x * 32 + slice;
+    if (lane || out_c >= n) return;
+    void* out = out_c < cols ? dw : db;
+    const int64_t at = out_c < cols ? out_c : out_c - cols;
     if (!out) return;
     if (dtype == WARP_F32) ((float*)out)[at] = s;
     else if (dtype == WARP_F16) ((_Float16*)out)[at] = (_Float16)s;
     else ((__bf16*)out)[at] = (__bf16)s;
 }
 
+constexpr int kMaxParts = 1024;  // workgroups of the backward kernel
 constexpr int kMaxGrid = 2048;  // workgroups of the forward kernels: eight on each of 256 compute units
 
-template <typename T, int V, int NC, int WAVES, int MODE>
+template <typename T, int V, int NC, int LANES, int MODE>
 void rows_launch(const RowArgs& a, hipStream_t s) {
-    constexpr int kRows = WAVES < 4 ? 4 / WAVES : 1;
+    constexpr int kRows = LANES < 256 ? 256 / LANES : 1;
     const int64_t need = (a.rows + kRows - 1) / kRows;
-    const dim3 grid((uint32_t)(need < kMaxGrid ? need : kMaxGrid)), block(WAVES < 4 ? 256 : WAVES * 64);
-    if (a.cols % V) hipLaunchKernelGGL((k_rows<T, V, NC, WAVES, true, MODE>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_rows<T, V, NC, WAVES, false, MODE>), grid, block, 0, s, a);
+    const dim3 grid((uint32_t)(need < kMaxGrid ? need : kMaxGrid)), block(LANES < 256 ? 256 : LANES);
+    if (a.cols % V) hipLaunchKernelGGL((k_rows<T, V, NC, LANES, true, MODE>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_rows<T, V, NC, LANES, false, MODE>), grid, block, 0, s, a);
 }
 
 template <typename T, int MODE>
 void rows_of(const RowArgs& a, hipStream_t s) {
     constexpr int V = 16 / sizeof(T);
-    const int lane = (a.cols + kWave * V - 1) / (kWave * V);  // vectors a lane of one wave would hold
-    if (a.cols < V) rows_launch<T, 1, 1, 1, MODE>(a, s);
-    else if (lane <= 1) rows_launch<T, V, 1, 1, MODE>(a, s);
-    else if (lane <= 2) rows_launch<T, V, 2, 1, MODE>(a, s);
-    else if (lane <= 4) rows_launch<T, V, 4, 1, MODE>(a, s);
-    else if (lane <= 8) rows_launch<T, V, 2, 4, MODE>(a, s);
-    else if (lane <= 16) rows_launch<T, V, 4, 4, MODE>(a, s);
-    else if (lane <= 32) rows_launch<T, V, 8, 4, MODE>(a, s);
-    else rows_launch<float, 4, 4, 16, MODE>(a, s);  // only fp32 rows: kMaxCols is 32 vectors of 16-bit elements
+    const int vectors = (a.cols + V - 1) / V;  // of a row
+    if (a.cols < V) rows_launch<T, 1, 1, 16, MODE>(a, s);
+    else if (vectors <= 16) rows_launch<T, V, 1, 16, MODE>(a, s);
+    else if (vectors <= 32) rows_launch<T, V, 2, 16, MODE>(a, s);
+    else if (vectors <= 64) rows_launch<T, V, 1, 64, MODE>(a, s);
+    else if (vectors <= 128) rows_launch<T, V, 2, 64, MODE>(a, s);
+    else if (vectors <= 256) rows_launch<T, V, 4, 64, MODE>(a, s);
+    else if (vectors <= 512) rows_launch<T, V, 2, 256, MODE>(a, s);
+    else if (vectors <= 1024) rows_launch<T, V, 4, 256, MODE>(a, s);
+    else if (vectors <= 2048) rows_launch<T, V, 4, 512, MODE>(a, s);
+    else rows_launch<float, 4, 8, 512, MODE>(a, s);  // only fp32 rows: kMaxCols is 2048 vectors of 16-bit elements
 }
 
 template <int MODE>
@@ -383,38 +456,41 @@ void rows_any(int32_t dtype, const RowArgs& a, hipStream_t s) {
     else rows_of<__bf16, MODE>(a, s);
 }
 
-constexpr int kMaxCols = 16384;  // 16 waves of 64 lanes of 16 elements
+constexpr int kMaxCols = 16384;  // 512 lanes of 32 columns
 
-int back_waves(int32_t cols) {
-    const int per = kWave * 32;  // columns of a wave: 32 of each of five arrays in a lane's registers; 16 of 16 waves'
-    return cols <= per ? 1 : cols <= 4 * per ? 4 : 16;
+// Lanes of a row in the backward kernel, which holds five arrays of a lane's columns: at most 32 columns a lane.
+int back_lanes(int32_t cols, int32_t dtype) {
+    if (cols <= 32 * (16 / dtype_bytes(dtype))) return 16;
+    return cols <= 32 * kWave ? kWave : cols <= 32 * 256 ? 256 : 512;
 }
 
-int back_grid(int64_t rows, int32_t cols) {
-    const int waves = back_waves(cols);
-    const int64_t need = waves == 1 ? (rows + 3) / 4 : rows;
-    const int64_t most = waves == 16 ? 256 : 512;
-    return (int)(need < most ? need : most);
+int back_grid(int64_t rows, int32_t cols, int32_t dtype) {
+    const int lanes = back_lanes(cols, dtype), at_once = lanes < 256 ? 256 / lanes : 1;
+    const int64_t need = (rows + at_once - 1) / at_once;
+    const int64_t most = cols <= kWave * 16 ? kMaxParts : lanes == 512 ? 256 : 512;  // as many as fit the registers
+    const int64_t some = need < 256 ? need : need / 4 < 256 ? 256 : need / 4;
+    return (int)(some < most ? some : most);
 }
 
-template <typename T, int V, int NC, int WAVES>
+template <typename T, int V, int NC, int LANES>
 void back_launch(const BackArgs& a, int grid, hipStream_t s) {
-    const size_t lds = WAVES == 1 ? 2 * sizeof(float) * a.cols : 2 * sizeof(float) * WAVES;
-    const dim3 block(WAVES < 4 ? 256 : WAVES * 64);
-    if (a.cols % V) hipLaunchKernelGGL((k_rows_back<T, V, NC, WAVES, true>), dim3(grid), block, lds, s, a);
-    else hipLaunchKernelGGL((k_rows_back<T, V, NC, WAVES, false>), dim3(grid), block, lds, s, a);
+    const dim3 block(LANES < 256 ? 256 : LANES);
+    if (a.cols % V) hipLaunchKernelGGL((k_rows_back<T, V, NC, LANES, true>), dim3(grid), block, 0, s, a);
+    else hipLaunchKernelGGL((k_rows_back<T, V, NC, LANES, false>), dim3(grid), block, 0, s, a);
 }
 
 template <typename T>
-void back_of(const BackArgs& a, int grid, int waves, hipStream_t s) {
+void back_of(const BackArgs& a, int grid, int lanes, hipStream_t s) {
     constexpr int V = 16 / sizeof(T), N = 32 / V;
-    const int lane = (a.cols + kWave * V - 1) / (kWave * V);
-    if (a.cols < V) back_launch<T, 1, 1, 1>(a, grid, s);
-    else if (lane <= N / 4) back_launch<T, V, N / 4, 1>(a, grid, s);
-    else if (lane <= N / 2) back_launch<T, V, N / 2, 1>(a, grid, s);
-    else if (waves == 1) back_launch<T, V, N, 1>(a, grid, s);
-    else if (waves == 4) back_launch<T, V, N, 4>(a, grid, s);
-    else back_launch<T, V, N / 2, 16>(a, grid, s);
+    const int vectors = (a.cols + V - 1) / V;
+    if (a.cols < V) back_launch<T, 1, 1, 16>(a, grid, s);
+    else if (vectors <= 16) back_launch<T, V, 1, 16>(a, grid, s);
+    else if (lanes == 16) back_launch<T, V, 2, 16>(a, grid, s);
+    else if (lanes == kWave && vectors <= N / 4 * kWave) back_launch<T, V, N / 4, kWave>(a, grid, s);
+    else if (lanes == kWave && vectors <= N / 2 * kWave) back_launch<T, V, N / 2, kWave>(a, grid, s);
+    else if (lanes == kWave) back_launch<T, V, N, kWave>(a, grid, s);
+    else if (lanes == 256) back_launch<T, V, N, 256>(a, grid, s);
+    else back_launch<T, V, N, 512>(a, grid, s);
 }
 
 int check_rows(const char* what, const void* x, int64_t stride, int64_t rows, int32_t cols, int32_t dtype) {
@@ -504,10 +580,10 @@ int warp_quantize_rows(const void* x, int64_t x_stride, int64_t rows, int32_t co
     return WARP_OK;
 }
 
-int warp_layer_norm_backward_scratch(int64_t rows, int32_t cols, int64_t* bytes) {
-    if (!bytes || rows < 0 || cols < 1)
+int warp_layer_norm_backward_scratch(int64_t rows, int32_t cols, int32_t dtype, int64_t* bytes) {
+    if (!bytes || rows < 0 || cols < 1 || !dtype_ok(dtype))
         return fail(WARP_EINVAL, "layer norm backward: bad sizes");
-    *bytes = (int64_t)back_grid(rows, cols) * 2 * cols * (int64_t)sizeof(float);
+    *bytes = (int64_t)back_grid(rows, cols, dtype) * 2 * cols * (int64_t)sizeof(float);
     return WARP_OK;
 }
 
@@ -524,7 +600,7 @@ int warp_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, i
     if (rc) return rc;
     if (rows && (!mean || !rstd)) return fail(WARP_EINVAL, "%s: null pointer", what);
     const bool sums = dweight || dbias;
-    const int grid = back_grid(rows, cols);
+    const int grid = back_grid(rows, cols, dtype);
     const int64_t need = (int64_t)grid * 2 * cols * (int64_t)sizeof(float);
     if (sums && need && (!scratch || scratch_bytes < need || (uintptr_t)scratch % 4))
         return fail(WARP_EINVAL, "%s: needs %lld bytes of scratch (got %lld)", what, (long long)need,
@@ -534,14 +610,14 @@ int warp_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, i
     hipStream_t s = (hipStream_t)hip_stream;
     BackArgs a{dy, dy_stride, x, x_stride, rows, cols, weight, param_dtype == WARP_F32, mean, rstd, dx, dx_stride,
                sums ? (float*)scratch : nullptr};
-    const int waves = back_waves(cols);
+    const int lanes = back_lanes(cols, dtype);
     if (rows) {
-        if (dtype == WARP_F32) WARP_LAUNCH(back_of<float>(a, grid, waves, s));
-        else if (dtype == WARP_F16) WARP_LAUNCH(back_of<_Float16>(a, grid, waves, s));
-        else WARP_LAUNCH(back_of<__bf16>(a, grid, waves, s));
+        if (dtype == WARP_F32) WARP_LAUNCH(back_of<float>(a, grid, lanes, s));
+        else if (dtype == WARP_F16) WARP_LAUNCH(back_of<_Float16>(a, grid, lanes, s));
+        else WARP_LAUNCH(back_of<__bf16>(a, grid, lanes, s));
     }
     if (sums)  // without rows: zeros
-        WARP_LAUNCH(hipLaunchKernelGGL(k_join_params, dim3((2 * cols + 63) / 64), dim3(1024), 0, s,
+        WARP_LAUNCH(hipLaunchKernelGGL(k_join_params, dim3((2 * cols + 31) / 32), dim3(1024), 0, s,
                                        (const float*)scratch, rows ? grid : 0, cols, dweight, dbias, param_dtype));
     return WARP_OK;
 }

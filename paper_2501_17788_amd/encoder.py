@@ -142,7 +142,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, stream=None):
     dy, _, dy_stride = _rows(dy, "dy")
     cols = x.shape[-1]
     need = ctypes.c_int64()
-    _check(lib.warp_layer_norm_backward_scratch(rows, cols, ctypes.byref(need)))
+    _check(lib.warp_layer_norm_backward_scratch(rows, cols, _DTYPES[x.dtype], ctypes.byref(need)))
     dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     dw, db = torch.empty((2, cols), dtype=pt, device=x.device).unbind(0)
     scratch = torch.empty(need.value, dtype=torch.uint8, device=x.device)

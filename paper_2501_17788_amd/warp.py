@@ -73,7 +73,7 @@ def _load() -> ctypes.CDLL:
         "warp_layer_norm": ([P, i64, i64, i32, i32, P, P, i32, f32, P, i64, P, P, P], ctypes.c_int),
         "warp_layer_norm_backward": ([P, i64, P, i64, i64, i32, i32, P, i32, P, P, P, i64, P, P, P, i64, P],
                                      ctypes.c_int),
-        "warp_layer_norm_backward_scratch": ([i64, i32, P], ctypes.c_int),
+        "warp_layer_norm_backward_scratch": ([i64, i32, i32, P], ctypes.c_int),
         "warp_layer_norm_int8": ([P, i64, i64, i32, i32, P, P, i32, f32, P, i64, P, P], ctypes.c_int),
         "warp_quantize_rows": ([P, i64, i64, i32, i32, P, i64, P, P], ctypes.c_int),
         "warp_linear_int8": ([P, i64, P, i64, P, i64, P, i32, i32, P, P, i64, i32, P], ctypes.c_int),

@@ -66,11 +66,11 @@ def test_layer_norm_backward_refusals(over, needle):
 def test_layer_norm_backward_scratch():
     out = ctypes.c_int64()
     for rows, cols in ((0, 1), (1, 1), (4, 64), (10 ** 6, 1024), (10 ** 6, 16384)):
-        assert lib.warp_layer_norm_backward_scratch(rows, cols, ctypes.byref(out)) == 0
+        assert lib.warp_layer_norm_backward_scratch(rows, cols, 0, ctypes.byref(out)) == 0
         assert out.value % (8 * cols) == 0 and out.value <= 8 * cols * min(rows, 4096)
-    refused(lib.warp_layer_norm_backward_scratch(-1, 4, ctypes.byref(out)), w.EINVAL, "sizes")
-    refused(lib.warp_layer_norm_backward_scratch(1, 0, ctypes.byref(out)), w.EINVAL, "sizes")
-    refused(lib.warp_layer_norm_backward_scratch(1, 4, None), w.EINVAL, "sizes")
+    refused(lib.warp_layer_norm_backward_scratch(-1, 4, 0, ctypes.byref(out)), w.EINVAL, "sizes")
+    refused(lib.warp_layer_norm_backward_scratch(1, 0, 0, ctypes.byref(out)), w.EINVAL, "sizes")
+    refused(lib.warp_layer_norm_backward_scratch(1, 4, 0, None), w.EINVAL, "sizes")
 
 
 @pytest.mark.parametrize("over", [
