@@ -7,6 +7,10 @@
 // relative to their value, so values near the block's largest are kept to 1%, and v reaches down to 2e-10 of it.
 // A code counts the cutoffs that the magnitude over S reaches. The new m and v are computed without fused
 // multiply-adds, so that every step's codes follow from the formulas' 32-bit operations alone.
+//
+// Bound by memory: 96M parameters, moments in 32 bits 467 us in fp32 (5.7 TB/s), moments in 8 bits 297 us in fp32 and
+// 168 us in bfloat16 (5.7 TB/s). There the arithmetic, some 70 operations an element, takes nearly as long: with the
+// exact square root and division in the step it was the bound (240 us).
 #include <cmath>
 
 #include "encoder.h"
@@ -15,7 +19,7 @@ namespace warp {
 
 namespace {
 
-constexpr int kMaxTensors = 64;     // of one launch: their records travel in the kernel's arguments
+constexpr int kMaxTensors = 104;    // of one launch: their records travel in the kernel's arguments (at most 4 KB)
 constexpr int kBlock = 256;         // elements that share a scale; the kernel's threads too
 constexpr int kPer = 8;             // elements of a thread
 constexpr int kChunk = 256 * kPer;  // elements of a workgroup
@@ -34,10 +38,14 @@ struct StepArgs {
     float root, eps;        // 1 / sqrt(1 - b2^t)
 };
 
-template <typename T, int V>
+static_assert(sizeof(StepArgs) <= 4096, "the arguments of a launch");
+
+// V elements of which `left` are there. NT: not kept in the caches: gradients are not read again, and moments a step later. The
+// parameters are, by the next forward pass. 96M fp32 parameters and gradients, 32-bit moments: 525 us without, 467 us with.
+template <typename T, int V, bool NT = true>
 __device__ __forceinline__ void load_some(const T* p, int64_t left, float (&out)[V]) {
     if (left >= V) {
-        const auto v = load_vec<T, V>(p);
+        const auto v = NT ? stream_in<T, V>(p) : load_vec<T, V>(p);
 #pragma unroll
         for (int i = 0; i < V; ++i) out[i] = (float)v.e[i];
     } else {
@@ -45,13 +53,14 @@ __device__ __forceinline__ void load_some(const T* p, int64_t left, float (&out)
         for (int i = 0; i < V; ++i) out[i] = i < left ? (float)p[i] : 0.f;
     }
 }
-template <typename T, int V>
+template <typename T, int V, bool NT = true>
 __device__ __forceinline__ void store_some(T* p, int64_t left, const float (&in)[V]) {
     if (left >= V) {
         Vec<T, V> v;
 #pragma unroll
         for (int i = 0; i < V; ++i) v.e[i] = (T)in[i];
-        store_vec<T, V>(p, v);
+        if (NT) stream_out<T, V>(p, v);
+        else store_vec<T, V>(p, v);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
@@ -65,19 +74,23 @@ __device__ __forceinline__ void moments(const StepArgs& a, float g, float& m, fl
     m = m * a.b1 + g * a.c1;
     v = v * a.b2 + (g * g) * a.c2;
 }
+// The parameter after its step. The 8-bit kernel, which is bound by its arithmetic, takes the approximate square root
+// and reciprocal (within 1 ulp each; a v below 2^-126 counts as zero).
+template <bool FAST>
 __device__ __forceinline__ float moved(const StepArgs& a, float p, float m, float v) {
+    if (FAST)
+        return p * a.decay - a.rate * m * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v) * a.root + a.eps);
     return p * a.decay - a.rate * m / (sqrtf(v) * a.root + a.eps);
 }
 
-__device__ __forceinline__ float m_value(int c, float s) {
+__device__ __forceinline__ float m_value(float c, float s) {
 #pragma clang fp contract(off)
-    const float t = (float)c * (1.0f / 127.0f);
-    const float u = t * t;
-    return (c < 0 ? -u : u) * s;
+    const float t = c * (1.0f / 127.0f);
+    return t * fabsf(t) * s;
 }
-__device__ __forceinline__ float v_value(int c, float s) {
+__device__ __forceinline__ float v_value(float c, float s) {
 #pragma clang fp contract(off)
-    const float t = (float)c * (1.0f / 255.0f);
+    const float t = c * (1.0f / 255.0f);
     const float u = t * t;
     return (u * u) * s;
 }
@@ -85,16 +98,23 @@ __device__ __forceinline__ float v_value(int c, float s) {
 // it a little down gives that number or one less, and one comparison with the next cutoff settles which.
 __device__ __forceinline__ float m_code(float x) {
 #pragma clang fp contract(off)
-    const float c = floorf(__builtin_amdgcn_sqrtf(x) * 127.0f + 0.499f);
+    const float c = floorf(__builtin_fmaf(__builtin_amdgcn_sqrtf(x), 127.0f, 0.499f));
     const float t = (c + 0.5f) * (1.0f / 127.0f);
-    return x >= t * t ? c + 1.0f : c;
+    return c + (x >= t * t ? 1.0f : 0.0f);
 }
 __device__ __forceinline__ float v_code(float x) {
 #pragma clang fp contract(off)
-    const float c = floorf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(x)) * 255.0f + 0.499f);
+    const float c = floorf(__builtin_fmaf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(x)), 255.0f, 0.499f));
     const float t = (c + 0.5f) * (1.0f / 255.0f);
     const float u = t * t;
-    return x >= u * u ? c + 1.0f : c;
+    return c + (x >= u * u ? 1.0f : 0.0f);
+}
+// The low bytes of four whole numbers' two's complements: after the addition of 1.5 * 2^23 they are the sum's low bits.
+__device__ __forceinline__ uint32_t four_bytes(const float* c) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = as_u(c[i] + 12582912.0f);
+    return __builtin_amdgcn_perm(u[3], u[2], 0x04000c0cu) | __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u);
 }
 
 // Largest over the 32 lanes of a half wave.
@@ -119,24 +139,30 @@ __global__ __launch_bounds__(256) void k_adamw(StepArgs a) {
     const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
     const int64_t padded = (n + kBlock - 1) / kBlock * kBlock;
     if (BITS == 32) {
-        constexpr int V = 4;
+        constexpr int V = 4, N = kPer / V;
+        float p[N][V], g[N][V], m[N][V], v[N][V];
 #pragma unroll
-        for (int j = 0; j < kPer / V; ++j) {
+        for (int j = 0; j < N; ++j) {
+            const int64_t i = base + (j * 256 + threadIdx.x) * V;
+            if (i < n) {
+                load_some<T, V, false>(param + i, n - i, p[j]);
+                load_some<G, V>(grad + i, n - i, g[j]);
+                load_some<float, V>((const float*)a.m + moment + i, V, m[j]);  // whole: padded to 256
+                load_some<float, V>((const float*)a.v + moment + i, V, v[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
             const int64_t i = base + (j * 256 + threadIdx.x) * V;
             if (i >= n) continue;
-            float p[V], g[V], m[V], v[V];
-            load_some<T, V>(param + i, n - i, p);
-            load_some<G, V>(grad + i, n - i, g);
-            load_some<float, V>((const float*)a.m + moment + i, n - i, m);
-            load_some<float, V>((const float*)a.v + moment + i, n - i, v);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                moments(a, g[e] * gs, m[e], v[e]);
-                p[e] = moved(a, p[e], m[e], v[e]);
+                moments(a, g[j][e] * gs, m[j][e], v[j][e]);
+                p[j][e] = moved<false>(a, p[j][e], m[j][e], v[j][e]);
             }
-            store_some<T, V>(param + i, n - i, p);
-            store_some<float, V>((float*)a.m + moment + i, n - i, m);
-            store_some<float, V>((float*)a.v + moment + i, n - i, v);
+            store_some<T, V, false>(param + i, n - i, p[j]);
+            store_some<float, V>((float*)a.m + moment + i, n - i, m[j]);
+            store_some<float, V>((float*)a.v + moment + i, n - i, v[j]);
         }
     } else {
         constexpr int V = kPer;  // a block is 32 lanes of 8 elements
@@ -144,37 +170,33 @@ __global__ __launch_bounds__(256) void k_adamw(StepArgs a) {
         if (i >= padded) return;  // half waves at a time
         const int64_t s = (moment + i) / kBlock;
         float p[V], g[V], m[V], v[V];
-        load_some<T, V>(param + i, n - i, p);
+        load_some<T, V, false>(param + i, n - i, p);
         load_some<G, V>(grad + i, n - i, g);
-        int8_t* cm = (int8_t*)a.m + moment + i;
-        uint8_t* cv = (uint8_t*)a.v + moment + i;
-        const auto om = load_vec<int8_t, V>(cm);
-        const auto ov = load_vec<uint8_t, V>(cv);
+        uint32_t* cm = (uint32_t*)((int8_t*)a.m + moment + i);
+        uint32_t* cv = (uint32_t*)((uint8_t*)a.v + moment + i);
+        const auto om = stream_in<uint32_t, 2>(cm), ov = stream_in<uint32_t, 2>(cv);
         const float sm = a.m_scale[s], sv = a.v_scale[s];
         uint32_t top_m = 0, top_v = 0;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            m[e] = m_value(om.e[e], sm);
-            v[e] = v_value(ov.e[e], sv);
+            m[e] = m_value((float)(int8_t)(om.e[e / 4] >> 8 * (e & 3)), sm);
+            v[e] = v_value((float)(uint8_t)(ov.e[e / 4] >> 8 * (e & 3)), sv);
             moments(a, g[e] * gs, m[e], v[e]);
-            p[e] = moved(a, p[e], m[e], v[e]);
+            p[e] = moved<true>(a, p[e], m[e], v[e]);
             top_m = max(top_m, as_u(m[e]) & 0x7fffffffu);
-            top_v = max(top_v, as_u(v[e]) & 0x7fffffffu);
+            top_v = max(top_v, as_u(v[e]));  // no number here is negative
         }
-        store_some<T, V>(param + i, n - i, p);
-        const float nm = as_f(max(half_max(top_m), 0x00800000u)), nv = as_f(max(half_max(top_v), 0x00800000u));
+        store_some<T, V, false>(param + i, n - i, p);
+        const float nm = as_f(max(half_max(top_m), 0x00800000u));
+        const float nv = as_f(max(half_max(top_v) & 0x7fffffffu, 0x00800000u));
         const float im = 1.0f / nm, iv = 1.0f / nv;
-        Vec<int8_t, V> wm;
-        Vec<uint8_t, V> wv;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const int c = (int)m_code(fabsf(m[e]) * im);
-            wm.e[e] = (int8_t)(m[e] < 0.f ? -c : c);
-            const int d = (int)v_code(v[e] * iv);
-            wv.e[e] = (uint8_t)(v[e] > 0.f ? max(d, 1) : d);
+            m[e] = copysignf(m_code(fabsf(m[e]) * im), m[e]);
+            v[e] = fmaxf(v_code(v[e] * iv), v[e] > 0.f ? 1.0f : 0.0f);
         }
-        store_vec<int8_t, V>(cm, wm);
-        store_vec<uint8_t, V>(cv, wv);
+        stream_out<uint32_t, 2>(cm, {four_bytes(m), four_bytes(m + 4)});
+        stream_out<uint32_t, 2>(cv, {four_bytes(v), four_bytes(v + 4)});
         if ((threadIdx.x & 31) == 0) a.m_scale[s] = nm, a.v_scale[s] = nv;
     }
 }
@@ -187,7 +209,7 @@ __global__ __launch_bounds__(256) void k_moments(const int8_t* m, const float* m
         const float sm = m_scale[i / kBlock], sv = v_scale[i / kBlock];
         Vec<float, 4> rm, rv;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) rm.e[e] = m_value(cm.e[e], sm), rv.e[e] = v_value(cv.e[e], sv);
+        for (int e = 0; e < 4; ++e) rm.e[e] = m_value((float)cm.e[e], sm), rv.e[e] = v_value((float)cv.e[e], sv);
         store_vec<float, 4>(out_m + i, rm);
         store_vec<float, 4>(out_v + i, rv);
     }

@@ -46,6 +46,24 @@ __device__ __forceinline__ void store_vec(T* p, const Vec<T, V>& v) {
     *reinterpret_cast<Vec<T, V>*>(p) = v;
 }
 
+// The same for data that is not to stay in the caches.
+template <int BYTES>
+struct Raw {
+    typedef uint32_t type __attribute__((ext_vector_type(BYTES / 4), aligned(1)));
+};
+template <>
+struct Raw<2> {
+    typedef uint16_t type __attribute__((aligned(1)));
+};
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> stream_in(const T* p) {
+    return __builtin_bit_cast(Vec<T, V>, __builtin_nontemporal_load((const typename Raw<sizeof(T) * V>::type*)p));
+}
+template <typename T, int V>
+__device__ __forceinline__ void stream_out(T* p, const Vec<T, V>& v) {
+    __builtin_nontemporal_store(__builtin_bit_cast(typename Raw<sizeof(T) * V>::type, v), (typename Raw<sizeof(T) * V>::type*)p);
+}
+
 // Sums over 16 lanes of a wave or all 64, returned to every lane: four steps inside 16 lanes, then
 // those sums carried up to lane 63.
 template <int CTRL, int ROWS>
