@@ -7,7 +7,7 @@
 // Everything is computed in 32 bits; y, dx, dw and db are rounded once, to their own type. A row stays
 // in registers between its loads and its stores, so each element is read once and written once, and
 // the variance sums squared distances from the finished mean. Bound by memory; a large copy moves 5.1 to 5.6 TB/s.
-// 131,072 rows of 1,024 bfloat16: forward 103 us (5.2 TB/s), backward with its sums 162 us (5.0 TB/s); 100,000 of 128:
+// 131,072 rows of 1,024 bfloat16: forward 88 us (6.1 TB/s), backward with its sums 135 us (6.0 TB/s); 100,000 of 128:
 // 10 and 20 us; 65,536 of 1,024 to int8 38 us (5.3 TB/s); 32 of 768: 3.3 and 6.9 us, two launches in the backward pass.
 #include "encoder.h"
 
@@ -27,6 +27,13 @@ struct Words<0> {
     uint32_t e[1];
 };
 
+// Whether a kernel's inputs pass the caches by: where all that it reads and writes exceeds the 256 MB of the last cache,
+// inputs kept there only displace outputs. 131,072 rows of 1,024 bfloat16: forward 104 us without, 88 us with, backward
+// 160 and 135 us; 30,000 of 2,048 backward 76 and 67 us, forward (245 MB) 41.8 and 42.2 us; 20,000 of 1,024: 14.6 and 17.2 us.
+bool passes_by(int64_t rows, int32_t cols, int element_bytes) {
+    return rows * cols * element_bytes > (int64_t)256 << 20;
+}
+
 struct RowArgs {
     const void* x;
     int64_t x_stride, rows;
@@ -35,6 +42,7 @@ struct RowArgs {
     const void* bias;    // null: zeros
     int32_t params_f32;  // weight and bias are fp32; else of x's type
     float eps;
+    int32_t stream;      // x passes the caches by
     void* y;             // kNormal
     int64_t y_stride;
     float* mean;         // null: not wanted
@@ -135,7 +143,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rows(RowArgs a) {
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
             const Place p = place<V, RAGGED>(j, LANES, t, cols);
-            if (p.in) next[j] = load_vec<T, V>(x + p.at);
+            if (p.in) next[j] = a.stream ? stream_in<T, V>(x + p.at) : load_vec<T, V>(x + p.at);
         }
     };
     if (row < a.rows) load(row);
@@ -254,7 +262,8 @@ struct BackArgs {
     const float* rstd;
     void* dx;
     int64_t dx_stride;
-    float* parts;  // [gridDim.x][2][cols] sums of dy h and of dy over a workgroup's rows; null: not wanted
+    int32_t stream;  // x and dy pass the caches by
+    float* parts;    // [gridDim.x][2][cols] sums of dy h and of dy over a workgroup's rows; null: not wanted
 };
 
 // dx, and each workgroup's share of dw and db. The weight and both sums of a lane's columns stay in registers
@@ -287,7 +296,10 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rows_back(BackArg
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
             const Place p = place<V, RAGGED>(j, LANES, t, cols);
-            if (p.in) next_x[j] = load_vec<T, V>(x + p.at), next_dy[j] = load_vec<T, V>(dy + p.at);
+            if (p.in) {
+                next_x[j] = a.stream ? stream_in<T, V>(x + p.at) : load_vec<T, V>(x + p.at);
+                next_dy[j] = a.stream ? stream_in<T, V>(dy + p.at) : load_vec<T, V>(dy + p.at);
+            }
         }
         next_mean = a.mean[r], next_rstd = a.rstd[r];
     };
@@ -545,7 +557,8 @@ int warp_layer_norm(const void* x, int64_t x_stride, int64_t rows, int32_t cols,
     if (!mean != !rstd) return fail(WARP_EINVAL, "%s: mean and rstd come together", what);
     rc = require_device();
     if (rc || !rows) return rc;
-    RowArgs a{x, x_stride, rows, cols, weight, bias, param_dtype == WARP_F32, eps, y, y_stride, mean, rstd, nullptr, 0,
+    RowArgs a{x, x_stride, rows, cols, weight, bias, param_dtype == WARP_F32, eps,
+              passes_by(rows, cols, 2 * dtype_bytes(dtype)), y, y_stride, mean, rstd, nullptr, 0,
               nullptr};
     WARP_LAUNCH(rows_any<kNormal>(dtype, a, (hipStream_t)hip_stream));
     return WARP_OK;
@@ -562,7 +575,8 @@ int warp_layer_norm_int8(const void* x, int64_t x_stride, int64_t rows, int32_t 
     if (!(eps >= 0.f)) return fail(WARP_EINVAL, "%s: eps must be >= 0", what);
     rc = require_device();
     if (rc || !rows) return rc;
-    RowArgs a{x, x_stride, rows, cols, weight, bias, param_dtype == WARP_F32, eps, nullptr, 0, nullptr, nullptr, q,
+    RowArgs a{x, x_stride, rows, cols, weight, bias, param_dtype == WARP_F32, eps,
+              passes_by(rows, cols, dtype_bytes(dtype) + 1), nullptr, 0, nullptr, nullptr, q,
               q_stride, scale};
     WARP_LAUNCH(rows_any<kNormInt8>(dtype, a, (hipStream_t)hip_stream));
     return WARP_OK;
@@ -575,7 +589,8 @@ int warp_quantize_rows(const void* x, int64_t x_stride, int64_t rows, int32_t co
     if (!rc) rc = check_int8_rows(what, rows, cols, q, q_stride, scale);
     if (!rc) rc = require_device();
     if (rc || !rows) return rc;
-    RowArgs a{x, x_stride, rows, cols, nullptr, nullptr, 1, 0.f, nullptr, 0, nullptr, nullptr, q, q_stride, scale};
+    RowArgs a{x, x_stride, rows, cols, nullptr, nullptr, 1, 0.f, passes_by(rows, cols, dtype_bytes(dtype) + 1), nullptr,
+              0, nullptr, nullptr, q, q_stride, scale};
     WARP_LAUNCH(rows_any<kInt8>(dtype, a, (hipStream_t)hip_stream));
     return WARP_OK;
 }
@@ -609,7 +624,7 @@ int warp_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, i
     if (rc) return rc;
     hipStream_t s = (hipStream_t)hip_stream;
     BackArgs a{dy, dy_stride, x, x_stride, rows, cols, weight, param_dtype == WARP_F32, mean, rstd, dx, dx_stride,
-               sums ? (float*)scratch : nullptr};
+               passes_by(rows, cols, 3 * dtype_bytes(dtype)), sums ? (float*)scratch : nullptr};
     const int lanes = back_lanes(cols, dtype);
     if (rows) {
         if (dtype == WARP_F32) WARP_LAUNCH(back_of<float>(a, grid, lanes, s));
