@@ -9,6 +9,7 @@ any row stride (a dimension's elements one after the other); leading dimensions 
 from __future__ import annotations
 
 import ctypes
+import operator
 from typing import NamedTuple
 
 import numpy as np
@@ -16,6 +17,8 @@ import torch
 
 from .warp import _check, lib
 
+_NONE = type(None)
+_dtype_of = operator.attrgetter("dtype")
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}  # WARP_F32, WARP_F16, WARP_BF16
 PAD = 128    # int8 rows are padded with zeros to a multiple of this width
 BLOCK = 256  # elements of a tensor that share a scale of 8-bit moments
@@ -71,37 +74,41 @@ def _there(stream, tensors, call, *args):
 
 
 def _rows(x, name):
-    """(tensor whose rows have contiguous elements, number of rows, row stride) of x [..., cols]."""
+    """(x or a copy whose rows have contiguous elements, number of rows, row stride) of x [..., cols]."""
     if x.dtype not in _DTYPES:
         raise ValueError(f"{name} must be float32, float16 or bfloat16, got {x.dtype}")
-    if x.dim() == 2 and (x.stride(1) == 1 or x.shape[1] == 1):
-        if x.shape[0] <= 1 or x.stride(0) >= x.shape[1]:
-            return x, x.shape[0], x.stride(0)
-    elif x.dim() == 0:
+    shape = x.shape
+    if len(shape) == 2:
+        rows, cols = shape
+        stride, inner = x.stride()
+        if (inner == 1 or cols == 1) and (stride >= cols or rows <= 1):
+            return x, rows, stride
+    elif not shape:
         raise ValueError(f"{name} must have at least one dimension")
     x = x.contiguous()
-    cols = x.shape[-1]
+    cols = shape[-1]
     if cols < 1:
         raise ValueError(f"{name} has rows of no columns")
     return x, x.numel() // cols, cols
 
 
-def _param(p, cols, name):
-    if p is None:
-        return None
-    if p.shape != (cols,):
-        raise ValueError(f"{name} must have shape ({cols},), got {tuple(p.shape)}")
-    return p.contiguous()
-
-
 def _params(x, weight, bias):
     """weight and bias as the kernels take them, and their dtype."""
-    cols = x.shape[-1]
-    weight, bias = _param(weight, cols, "weight"), _param(bias, cols, "bias")
-    known = [p.dtype for p in (weight, bias) if p is not None]
-    dtype = known[0] if known else torch.float32
-    if any(d != dtype for d in known) or dtype not in (torch.float32, x.dtype):
-        raise ValueError(f"weight and bias must both be float32 or both {x.dtype}, got {known}")
+    shape, dtype = x.shape[-1:], None
+    if weight is not None:
+        if weight.shape != shape:
+            raise ValueError(f"weight must have shape {tuple(shape)}, got {tuple(weight.shape)}")
+        weight, dtype = weight.contiguous(), weight.dtype
+    if bias is not None:
+        if bias.shape != shape:
+            raise ValueError(f"bias must have shape {tuple(shape)}, got {tuple(bias.shape)}")
+        if dtype is not None and bias.dtype is not dtype:
+            raise ValueError(f"weight and bias must be of one type, got {dtype} and {bias.dtype}")
+        bias, dtype = bias.contiguous(), bias.dtype
+    if dtype is None:
+        dtype = torch.float32
+    elif dtype is not torch.float32 and dtype is not x.dtype:
+        raise ValueError(f"weight and bias must be float32 or {x.dtype}, got {dtype}")
     return weight, bias, dtype
 
 
@@ -119,7 +126,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, stream=None):
     x, rows, stride = _rows(x, "x")
     shape = x.shape
     cols = shape[-1]
-    y = torch.empty(shape, dtype=x.dtype, device=x.device)
+    y = torch.empty_like(x) if x.is_contiguous() else torch.empty(shape, dtype=x.dtype, device=x.device)
     mean, rstd = torch.empty((2, *shape[:-1]), dtype=torch.float32, device=x.device).unbind(0)
     _check(lib.warp_layer_norm(x.data_ptr(), stride, rows, cols, _DTYPES[x.dtype], _ptr(weight), _ptr(bias),
                                _DTYPES[pt], eps, y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(), s))
@@ -143,7 +150,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, stream=None):
     cols = x.shape[-1]
     need = ctypes.c_int64()
     _check(lib.warp_layer_norm_backward_scratch(rows, cols, _DTYPES[x.dtype], ctypes.byref(need)))
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dx = torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
     dw, db = torch.empty((2, cols), dtype=pt, device=x.device).unbind(0)
     scratch = torch.empty(need.value, dtype=torch.uint8, device=x.device)
     _check(lib.warp_layer_norm_backward(dy.data_ptr(), dy_stride, x.data_ptr(), stride, rows, cols, _DTYPES[x.dtype],
@@ -262,7 +269,7 @@ class AdamW:
         if len(grads) != len(params):
             raise ValueError(f"{len(grads)} gradients for {len(params)} parameters")
         given, sizes = grads, self._sizes
-        if any(g is None for g in grads):
+        if _NONE in map(type, grads):
             given = [g for g in grads if g is not None]
             sizes = [n for g, n in zip(grads, sizes) if g is not None]
         dtype = given[0].dtype if given else torch.float32
@@ -292,10 +299,10 @@ class AdamW:
 
     def _fit(self, tensors, sizes, dtype) -> bool:
         """Whether these are contiguous tensors of these sizes, of one type, on the moments' device."""
-        index = self.m.get_device()
-        return ([*map(torch.Tensor.numel, tensors)] == sizes and all(map(torch.Tensor.is_contiguous, tensors))
-                and all(t.dtype is dtype for t in tensors)
-                and all(i == index for i in map(torch.Tensor.get_device, tensors)))
+        return not tensors or (
+            [*map(torch.Tensor.numel, tensors)] == sizes and all(map(torch.Tensor.is_contiguous, tensors))
+            and {*map(_dtype_of, tensors)} == {dtype}
+            and {*map(torch.Tensor.get_device, tensors)} == {self.m.get_device()})
 
     def moments(self, stream=None):
         """The flat float32 moments (m, v): with 32 bits the optimizer's own, with 8 the values of its codes."""
