@@ -49,8 +49,13 @@ __device__ __forceinline__ int channel_key(int row) { return (row & 3) | (row / 
 // A workgroup makes a tile of TM tokens by TN channels with WM x WN waves. Each K step's rows are copied to LDS
 // by loads that pass no registers, into one of STAGES buffers, while the matrix cores work on another. The
 // buffers are arrays of their own, so that the compiler sees that a read of one needs no wait for loads into
-// another. Bound by the matrix cores and, at their rate, by power: a product of 8192 x 8192 by 8192 runs at 2.5e15
-// operations a second with random values, 3.0e15 with zeros; counters show the matrix cores busy 61% of cycles.
+// another. Bound by power and by the loads behind the matrix cores: 8192 x 8192 by 8192 takes 437 us (2.5e15
+// operations a second) with random values, 376 us with zeros, 370 us with random values but without its loads (matrix
+// cores busy 61% of cycles, at 1.7 GHz under load); 32,768 x 4096 by 4096 takes 502 us, and 426 us without loads. No faster:
+// quarter steps (520), order pinned by scheduling barriers (495 with operands and sums tied to registers by hand, 1450
+// and more where the compiler spills), tokens loaded two steps ahead (511), workgroups that stay for several tiles and
+// load the next one's first rows before they store (495 to 500), waits by counts instead of a full one (537), tiles by
+// four waves of 128 x 128 (710).
 template <typename T, int TM, int TN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs g) {
     constexpr int kWaves = WM * WN;
@@ -131,7 +136,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs g) {
     auto step = [&](int k, const int8_t* la, const int8_t* lw, int8_t* na, int8_t* nw) {
         // this step's rows have landed (the loads of STAGES - 2 later steps may be under way), and the buffer that
         // is loaded next has been read by all
-        if (STAGES == 2 || k + 1 >= steps) wait_loads<0>();
+        if (STAGES == 2) __syncthreads();
+        else if (k + 1 >= steps) wait_loads<0>();
         else if (k + 2 >= steps) wait_loads<kLoads>();
         else wait_loads<2 * kLoads>();
         if (k + STAGES - 1 < steps) load(na, nw);
