@@ -63,8 +63,9 @@ def _there(stream, tensors, call, *args):
     """call(*args) with `stream` (or the current one of the tensors' device) current, so that outputs and copies
     are allocated and enqueued there; the tensors are kept for its work."""
     dev = tensors[0].device
-    if not tensors[0].is_cuda:
-        raise ValueError(f"expected device tensors, got {dev}")
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise ValueError(f"expected device tensors, got {t.device}")
     stream = torch.cuda.current_stream(dev) if stream is None else stream
     with torch.cuda.device(dev), torch.cuda.stream(stream):
         for t in tensors:
@@ -264,7 +265,9 @@ class AdamW:
     def step(self, grads, grad_scale=None, stream=None) -> None:
         """One step. grads: a contiguous tensor like each parameter, all of one floating type, or None for a
         parameter that this step leaves as it is. grad_scale: a float32 device tensor of one element that
-        every gradient is multiplied by."""
+        every gradient is multiplied by. The number of the step is a constant of the launched kernels: a graph
+        that captured a step repeats that number. Parameters change without autograd's notice (it counts no
+        version)."""
         params, index = self.params, self.m.get_device()
         if len(grads) != len(params):
             raise ValueError(f"{len(grads)} gradients for {len(params)} parameters")

@@ -684,3 +684,62 @@ def test_capture_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(out, work()):
             assert torch.equal(a, b), k
+
+
+# ---------------------------------------------------------------------------- sizes past 32 bits
+
+def test_layer_norm_past_32_bits():
+    """More than 2^31 elements: the last rows equal those of a call on them alone."""
+    rows, cols = 2_100_003, 1024
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda").normal_(generator=gen(20))
+    weight = 1 + 0.1 * randn(gen(21), cols)
+    say("layer norm of", x.numel(), "elements")
+    y, mean, rstd = w.layer_norm(x, weight, None)
+    at = [slice(0, 3), slice(2_097_150, 2_097_155), slice(rows - 3, rows)]
+    for s in at:
+        assert torch.equal(y[s], w.layer_norm(x[s], weight, None)[0])
+    dx = w.layer_norm_backward(y, x, weight, mean, rstd)[0]
+    for s in at:
+        alone = w.layer_norm_backward(y[s], x[s], weight, mean[s].contiguous(), rstd[s].contiguous())[0]
+        assert torch.equal(dx[s], alone)
+    del dx, y
+    q = w.quantize_rows(x)
+    for s in at:
+        alone = w.quantize_rows(x[s])
+        assert torch.equal(q.values[s], alone.values) and torch.equal(q.scale[s], alone.scale)
+
+
+def test_linear_int8_past_32_bits():
+    """More than 2^31 results, and operands of more than 2^31 bytes."""
+    g = gen(22)
+    for rows, n, cols in ((70_001, 32_768, 128), (2_200_001, 33, 1000), (33, 2_097_000, 1100)):
+        a, sa = int8_rows(g, rows, cols)
+        b, sb = int8_rows(g, n, cols)
+        qa, qb = w.QuantizedRows.from_int8(a, sa), w.QuantizedRows.from_int8(b, sb)
+        del a, b
+        say("int8 product", rows, n, cols)
+        out = w.linear_int8(qa, qb)
+        last = w.QuantizedRows(qa.values[-20:].contiguous(), sa[-20:].contiguous(), cols)
+        assert torch.equal(out[-20:], w.linear_int8(last, qb))
+        few = w.QuantizedRows(qb.values[-20:].contiguous(), sb[-20:].contiguous(), cols)
+        assert torch.equal(out[:, -20:], w.linear_int8(qa, few))
+        del out, qa, qb, last, few
+
+
+def test_adamw_past_32_bits():
+    """A tensor of more than 2^31 elements: its last ones move as they do alone."""
+    n = (1 << 31) + 5000
+    for bits in (8, 32):
+        p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+        grad = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+        tail = slice(n - n % 256 - 2560, n)  # whole blocks and the last, partial one
+        grad[tail].normal_(generator=gen(23))
+        say("adamw", bits, n)
+        opt = w.AdamW([p], LR, (B1, B2), EPS, DECAY, bits)
+        opt.step([grad])
+        small = torch.zeros(n - tail.start, dtype=torch.bfloat16, device="cuda")
+        alone = w.AdamW([small], LR, (B1, B2), EPS, DECAY, bits)
+        alone.step([grad[tail].clone()])
+        assert torch.equal(p[tail], small) and not p[:5000].any()
+        assert torch.equal(opt.m[tail.start:], alone.m) and torch.equal(opt.v[tail.start:], alone.v)
+        del opt, p, grad
