@@ -386,6 +386,7 @@ int warp_layer_norm_int8(const void* x, int64_t x_stride, int64_t rows, int32_t 
  *   k                1..131071 (above: WARP_ENOTSUP, a sum could pass 32 bits)
  *   bias             [n] fp32 or NULL
  *   out              [rows][n] of out_dtype, rows out_stride elements apart
+ * WARP_ENOTSUP for more than 2^24 rows, 2^21 channels or 2^24 tiles of 64 x 64 of the result.
  */
 int warp_linear_int8(const int8_t* a, int64_t a_stride, const float* a_scale, int64_t rows, const int8_t* w,
                      int64_t w_stride, const float* w_scale, int32_t n, int32_t k, const float* bias, void* out,

@@ -31,14 +31,6 @@ constexpr int kBand = 4;
 typedef const __attribute__((address_space(1))) void global_void;
 typedef __attribute__((address_space(3))) void lds_void;
 
-// All but this wave's newest N loads have landed and its LDS reads too; then the same for every wave.
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
 // A row's eight 16-byte pieces lie in LDS in an order of their own, piece ^ key, so that the rows that eight
 // neighbouring lanes read one piece of lie in different banks. Token blocks read rows 0 .. 15 in order. A
 // channel block j reads rows 4 j + i % 4 + 16 (i / 4), which gives a lane 16 neighbouring channels of a token.
@@ -47,30 +39,25 @@ template <int BN>
 __device__ __forceinline__ int channel_key(int row) { return (row & 3) | (row / (4 * BN) & 1) << 2; }
 
 // A workgroup makes a tile of TM tokens by TN channels with WM x WN waves. Each K step's rows are copied to LDS
-// by loads that pass no registers, into one of STAGES buffers, while the matrix cores work on another. The
+// by loads that pass no registers, into one of two buffers, while the matrix cores work on the other. The two
 // buffers are arrays of their own, so that the compiler sees that a read of one needs no wait for loads into
-// another. Bound by power and by the loads behind the matrix cores: 8192 x 8192 by 8192 takes 437 us (2.5e15
+// the other. Bound by power and by the loads behind the matrix cores: 8192 x 8192 by 8192 takes 437 us (2.5e15
 // operations a second) with random values, 376 us with zeros, 370 us with random values but without its loads (matrix
 // cores busy 61% of cycles, at 1.7 GHz under load); 32,768 x 4096 by 4096 takes 502 us, and 426 us without loads. No faster:
 // quarter steps (520), order pinned by scheduling barriers (495 with operands and sums tied to registers by hand, 1450
 // and more where the compiler spills), tokens loaded two steps ahead (511), workgroups that stay for several tiles and
 // load the next one's first rows before they store (495 to 500), waits by counts instead of a full one (537), tiles by
-// four waves of 128 x 128 (710).
-template <typename T, int TM, int TN, int WM, int WN, int STAGES>
+// four waves of 128 x 128 (710). Smaller tiles gain nothing from four buffers and waits by counts either.
+template <typename T, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs g) {
     constexpr int kWaves = WM * WN;
     constexpr int kBM = TM / WM / 16, kBN = TN / WN / 16;  // 16 x 16 blocks of a wave
     constexpr int kLoadM = TM / 8 / kWaves, kLoadN = TN / 8 / kWaves;  // loads of 8 rows by a wave
-    static_assert(STAGES == 2 || STAGES == 4, "two or four buffers");
     static_assert(kLoadM * 8 * kWaves == TM && kLoadN * 8 * kWaves == TN, "whole loads");
     __shared__ __attribute__((aligned(16))) int8_t a0[TM * kStep];
     __shared__ __attribute__((aligned(16))) int8_t a1[TM * kStep];
-    __shared__ __attribute__((aligned(16))) int8_t a2[STAGES > 2 ? TM * kStep : 16];
-    __shared__ __attribute__((aligned(16))) int8_t a3[STAGES > 2 ? TM * kStep : 16];
     __shared__ __attribute__((aligned(16))) int8_t w0[TN * kStep];
     __shared__ __attribute__((aligned(16))) int8_t w1[TN * kStep];
-    __shared__ __attribute__((aligned(16))) int8_t w2[STAGES > 2 ? TN * kStep : 16];
-    __shared__ __attribute__((aligned(16))) int8_t w3[STAGES > 2 ? TN * kStep : 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, q = lane >> 4;
     const int wm = (wave / WN) * (TM / WM), wn = (wave % WN) * (TN / WN);
     // tiles of one XCD (every eighth workgroup) are neighbours: its L2 then serves their common rows
@@ -131,40 +118,23 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs g) {
     };
     // The operands of each half step are read while the matrix cores work on the half step before it, so the first
     // half of a step overlaps the second half of the last one, across the barrier.
-    constexpr int kLoads = kLoadM + kLoadN;
     const int steps = g.k / kStep;
     auto step = [&](int k, const int8_t* la, const int8_t* lw, int8_t* na, int8_t* nw) {
-        // this step's rows have landed (the loads of STAGES - 2 later steps may be under way), and the buffer that
-        // is loaded next has been read by all
-        if (STAGES == 2) __syncthreads();
-        else if (k + 1 >= steps) wait_loads<0>();
-        else if (k + 2 >= steps) wait_loads<kLoads>();
-        else wait_loads<2 * kLoads>();
-        if (k + STAGES - 1 < steps) load(na, nw);
+        __syncthreads();  // this step's rows have landed, and the other buffer has been read by all
+        if (k + 1 < steps) load(na, nw);
         read(part[0], la, lw, 0);
         if (k) multiply(part[1]);
         read(part[1], la, lw, 1);
         multiply(part[0]);
     };
     load(a0, w0);
-    if (STAGES == 2) {
-        step(0, a0, w0, a1, w1);
-        int k = 1;
-        for (; k + 1 < steps; k += 2) {
-            step(k, a1, w1, a0, w0);
-            step(k + 1, a0, w0, a1, w1);
-        }
-        if (k < steps) step(k, a1, w1, a0, w0);
-    } else {
-        if (1 < steps) load(a1, w1);
-        if (2 < steps) load(a2, w2);
-        for (int k = 0; k < steps; k += 4) {
-            step(k, a0, w0, a3, w3);
-            if (k + 1 < steps) step(k + 1, a1, w1, a0, w0);
-            if (k + 2 < steps) step(k + 2, a2, w2, a1, w1);
-            if (k + 3 < steps) step(k + 3, a3, w3, a2, w2);
-        }
+    step(0, a0, w0, a1, w1);
+    int k = 1;
+    for (; k + 1 < steps; k += 2) {
+        step(k, a1, w1, a0, w0);
+        step(k + 1, a0, w0, a1, w1);
     }
+    if (k < steps) step(k, a1, w1, a0, w0);
     multiply(part[1]);
     // D[row][col] of a block lies in lane col + 16 (row / 4), element row % 4: lane (li, q) holds channels
     // 16 q + 4 j + r, r = 0 .. 3, of token li of block i
@@ -277,37 +247,42 @@ void split(const LinearArgs& g, hipStream_t s) {
     hipLaunchKernelGGL((k_linear_split<T, BM, BN>), grid, dim3(64 * kSplit), 0, s, g);
 }
 
-template <typename T, int TM, int TN, int WM, int WN, int STAGES>
+template <typename T, int TM, int TN, int WM, int WN>
 void tiles(const LinearArgs& g, hipStream_t s) {
     const int64_t n = ((g.rows + TM - 1) / TM) * ((g.n + TN - 1) / TN);
-    hipLaunchKernelGGL((k_linear_tile<T, TM, TN, WM, WN, STAGES>), dim3((uint32_t)n), dim3(64 * WM * WN), 0, s, g);
+    hipLaunchKernelGGL((k_linear_tile<T, TM, TN, WM, WN>), dim3((uint32_t)n), dim3(64 * WM * WN), 0, s, g);
 }
 
 inline int64_t cover(int64_t n, int64_t of) { return (n + of - 1) / of; }
 
-// Which kernel, by measured times (us, in a graph, operands in the caches; tokens x channels x columns):
-// * up to six 16 x 16 tiles a compute unit, a tile's columns are split among waves, 16 x 16, 32 x 16 or 32 x 32 tiles so
-//   that there are about as many tiles as compute units: 1 x 1024 x 1024 2.8 (64 x 128 tiles 5.9), 64 x 1024 x 1024 3.3
-//   (7.0), 128 x 1024 x 1024 3.9 (16 x 16 4.1, 32 x 32 4.7), 300 x 800 x 800 4.5 (6.5), 256 x 1024 x 4096 10.6 (15.5)
-// * tiles of 64 x 128, three workgroups on a compute unit; with no more tiles than compute units one of four stages:
-//   512 x 4096 x 4096 19.4 (two stages 24.3), 1771 x 1003 x 771 7.9 (128 x 128 10.5), 10,000 x 800 x 800 17.8
-//   (128 x 128 21.9, 256 x 256 21.4)
-// * tiles of 128 x 128, two workgroups on a compute unit, where all of them run at once and those of 64 x 128 would not:
-//   2000 x 4000 x 4000 41.7 (51.4), 65,536 x 128 x 1024 19.9 (21.3)
-// * tiles of 256 x 256 where their rounds, each as long as 2.3 of 64 x 128, are fewer: 16,384 x 1024 x 1024 27.3 (31.7),
-//   20,000 x 1500 x 2000 80.5 (95.6), 20,000 x 800 x 800 38.2 (30.2, not taken)
+// Which kernel, by measured times (us, in a graph, operands in the caches; tokens x channels x columns).
+// Up to four 16 x 16 tiles a compute unit, a tile's columns are split among waves, in 16 x 16, 32 x 16 or 32 x 32 so that
+// there are about as many tiles as compute units: 1 x 1024 x 1024 2.8 (32 x 32 3.7, tiles of 64 x 64 4.5), 64 x 1024 x
+// 1024 3.3 (4.6), 128 x 1024 x 1024 3.9 (16 x 16 4.1, 32 x 32 4.7), 300 x 800 x 800 4.5 (64 x 64 5.0).
+// Else by the time of each kind of tile, in hundredths of a round of 128 x 128 tiles (512 at once, two on a compute unit; up to
+// 256, one on each, take 0.8): a round of 256 x 256 (256 at once) takes 1.66, and 2048 tiles of 64 x 64 take 1.46, with little
+// lost in their last round.
+//                         64 x 64  128 x 128  256 x 256
+//   1771 x 1003 x 771         7.1        9.2       22.9
+//   512 x 4096 x 4096        19.0       22.2       48.1
+//   10,000 x 800 x 800       17.8       20.1       20.6
+//   65,536 x 128 x 1024      21.4       19.8       22.6
+//   2000 x 4000 x 4000       51.2       37.1       50.4
+//   16,384 x 1024 x 1024     34.4       28.7       26.0
+//   8192 x 4096 x 4096        205        141        117
 template <typename T>
 void linear(const LinearArgs& g, hipStream_t s) {
     constexpr int64_t kUnits = 256;
-    const int64_t m = g.rows, n = g.n, t16 = cover(m, 16) * cover(n, 16), t64 = cover(m, 64) * cover(n, 128);
+    const int64_t m = g.rows, n = g.n, t16 = cover(m, 16) * cover(n, 16);
     if (t16 <= kUnits) return split<T, 1, 1>(g, s);
     if (t16 <= 2 * kUnits) return split<T, 2, 1>(g, s);
-    if (t16 <= 6 * kUnits) return split<T, 2, 2>(g, s);
-    if (t64 <= kUnits) return tiles<T, 64, 128, 2, 2, 4>(g, s);
-    if (t64 > 3 * kUnits && cover(m, 128) * cover(n, 128) <= 2 * kUnits) return tiles<T, 128, 128, 2, 2, 2>(g, s);
-    if (23 * cover(cover(m, 256) * cover(n, 256), kUnits) * 3 * kUnits < 10 * t64)
-        return tiles<T, 256, 256, 2, 4, 2>(g, s);
-    tiles<T, 64, 128, 2, 2, 2>(g, s);
+    if (t16 <= 4 * kUnits) return split<T, 2, 2>(g, s);
+    const int64_t t64 = cover(m, 64) * cover(n, 64), t128 = cover(m, 128) * cover(n, 128);
+    const int64_t time64 = 146 * t64 / 2048 + 10, time128 = t128 <= kUnits ? 80 : 100 * cover(t128, 2 * kUnits);
+    const int64_t time256 = 166 * cover(cover(m, 256) * cover(n, 256), kUnits);
+    if (time64 <= time128 && time64 <= time256) tiles<T, 64, 64, 2, 2>(g, s);
+    else if (time128 <= time256) tiles<T, 128, 128, 2, 4>(g, s);
+    else tiles<T, 256, 256, 2, 4>(g, s);
 }
 
 }  // namespace
@@ -340,8 +315,8 @@ extern "C" int warp_linear_int8(const int8_t* a, int64_t a_stride, const float* 
         return fail(WARP_EINVAL, "%s: misaligned pointer", what);
     if (rows > 1 && out_stride < n)
         return fail(WARP_EINVAL, "%s: a row stride of %lld is below %d columns", what, (long long)out_stride, n);
-    if (cover(rows, 64) * cover(n, 128) >= 1 << 24)
-        return fail(WARP_ENOTSUP, "%s: %lld rows by %d channels are more than 2^24 tiles of 64 x 128", what,
+    if (cover(rows, 64) * cover(n, 64) >= 1 << 24)  // of 256 threads each: a grid has at most 2^32
+        return fail(WARP_ENOTSUP, "%s: %lld rows by %d channels are more than 2^24 tiles of 64 x 64", what,
                     (long long)rows, n);
     const int rc = require_device();
     if (rc || !rows) return rc;

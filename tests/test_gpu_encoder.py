@@ -349,7 +349,9 @@ def test_linear_int8(rows):
 
 
 @pytest.mark.parametrize("rows,n,cols", [(2000, 1003, 771), (1025, 2049, 1000), (4096, 512, 256), (300, 5000, 640),
-                                         (33_000, 128, 192), (1, 9001, 2500), (64, 4096, 9000)])
+                                         (33_000, 128, 192), (1, 9001, 2500), (64, 4096, 9000),
+                                         (1990, 3999, 530), (2040, 4000, 100), (4090, 4083, 900), (5000, 3900, 1100),
+                                         (4081, 4096, 65)])
 def test_linear_int8_larger(rows, n, cols):
     g = gen(n)
     a, sa = int8_rows(g, rows, cols)
