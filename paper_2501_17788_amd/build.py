@@ -11,7 +11,8 @@ from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-CSRC = os.path.join(PKG, "csrc")
+CSRC = os.path.join(PKG, "csrc")  # the search engine
+CSRC_ENCODER = os.path.join(PKG, "csrc_encoder")  # the token encoder's operators
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libwarp.so")
@@ -22,12 +23,12 @@ FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result",
     # no packed-FP32 instructions anywhere in the device code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    "-I", INCLUDE, "-I", CSRC,
+    "-I", INCLUDE, "-I", CSRC, "-I", CSRC_ENCODER,
 ]
 
 
 def sources() -> list[str]:
-    return sorted(glob.glob(os.path.join(CSRC, "*.hip")))
+    return sorted(f for d in (CSRC, CSRC_ENCODER) for f in glob.glob(os.path.join(d, "*.hip")))
 
 
 def _compile(src: str) -> str:
@@ -53,7 +54,7 @@ def _compile_binding() -> str | None:
            "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
            "-isystem", os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include"),
            "-isystem", sysconfig.get_paths()["include"],
-           "-c", os.path.join(CSRC, "encoder_binding.cpp"), "-o", obj]
+           "-c", os.path.join(CSRC_ENCODER, "encoder_binding.cpp"), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"g++ failed on encoder_binding.cpp:\n{r.stdout}\n{r.stderr}")

@@ -8,6 +8,11 @@
 
 namespace warp {
 
+// engine.hip: records the message that warp_last_error() returns and gives back `code`
+int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+// the current device is a gfx950 (looked up once per device)
+int require_device();
+
 constexpr int kDim = 128;          // token embedding dimension
 constexpr int kFrac = 26;          // fixed-point fraction bits of token and doc scores
 constexpr int kMaxQtok = 32;       // query_maxlen

@@ -18,7 +18,6 @@
 #include <utility>
 #include <vector>
 
-#include "encoder.h"
 #include "engine.h"
 #include "warp.h"
 

@@ -5,14 +5,10 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "engine.h"  // fail, require_device
 #include "warp.h"
 
 namespace warp {
-
-// engine.hip: records the message that warp_last_error() returns and gives back `code`
-int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
-// the current device is a gfx950 (looked up once per device)
-int require_device();
 
 constexpr int kWave = 64;
 constexpr int kInt8Pad = 128;  // int8 rows are padded with zeros to a multiple of this many columns
