@@ -193,15 +193,26 @@ Tensor linear_int8(const Tensor& av, const Tensor& sa, int64_t cols, const Tenso
     return out;
 }
 
-// `table`: the optimizer's records (warp_adamw_tensor) for its parameters, with their sizes and moments filled in
-void adamw_step(const py::list& params, const py::sequence& grads, int64_t table, at::ScalarType dtype, int32_t bits,
-                const Tensor& m, const MaybeTensor& m_scale, const Tensor& v, const MaybeTensor& v_scale, double lr,
-                double beta1, double beta2, double eps, double weight_decay, int64_t step,
+// `table`: the optimizer's `count` records (warp_adamw_tensor) for its parameters, with sizes and moments filled in
+void adamw_step(const py::list& params, const py::sequence& grads, int64_t table, size_t count, at::ScalarType dtype,
+                int32_t bits, const Tensor& m, const MaybeTensor& m_scale, const Tensor& v, const MaybeTensor& v_scale,
+                double lr, double beta1, double beta2, double eps, double weight_decay, int64_t step,
                 const MaybeTensor& grad_scale) {
     const size_t n = params.size();
+    if (n != count) refuse(n, " parameters, and ", count, " when the optimizer was made");
     if (py::len(grads) != n) refuse(py::len(grads), " gradients for ", n, " parameters");
     auto* records = reinterpret_cast<warp_adamw_tensor*>(table);
     const auto device = m.device();
+    const int64_t size = n ? records[n - 1].moment + (records[n - 1].n + kBlock - 1) / kBlock * kBlock : 0;
+    const bool eight = bits == 8;
+    for (const Tensor* t : {&m, &v})
+        if (t->numel() != size || !t->is_contiguous() || !t->is_cuda() || t->device() != device ||
+            t->scalar_type() != (!eight ? at::kFloat : t == &m ? at::kChar : at::kByte))
+            refuse("the moments are no longer the ones that the optimizer made");
+    for (const MaybeTensor* t : {&m_scale, &v_scale})
+        if (eight && (!*t || (*t)->numel() != size / kBlock || !(*t)->is_contiguous() || (*t)->device() != device ||
+                      (*t)->scalar_type() != at::kFloat))
+            refuse("the moments' scales are no longer the ones that the optimizer made");
     at::ScalarType grad_type = at::kFloat;
     bool any = false;
     const py::object fast = py::reinterpret_steal<py::object>(PySequence_Fast(grads.ptr(), "grads must be a sequence"));
@@ -237,6 +248,13 @@ void adamw_step(const py::list& params, const py::sequence& grads, int64_t table
 }
 
 py::tuple adamw_moments(const Tensor& m, const Tensor& m_scale, const Tensor& v, const Tensor& v_scale) {
+    on_device(m);
+    for (const Tensor* t : {&m_scale, &v, &v_scale}) on_device(m, *t);
+    if (m.scalar_type() != at::kChar || v.scalar_type() != at::kByte || m_scale.scalar_type() != at::kFloat ||
+        v_scale.scalar_type() != at::kFloat || v.numel() != m.numel() || m_scale.numel() * kBlock != m.numel() ||
+        v_scale.numel() * kBlock != m.numel() || !m.is_contiguous() || !v.is_contiguous() || !m_scale.is_contiguous() ||
+        !v_scale.is_contiguous())
+        refuse("the moments are no longer the ones that the optimizer made");
     const c10::DeviceGuard guard(m.device());
     const auto f32 = m_scale.options();
     Tensor out_m = at::empty({m.numel()}, f32), out_v = at::empty({m.numel()}, f32);

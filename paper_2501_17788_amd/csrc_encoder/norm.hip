@@ -402,6 +402,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rows_back(BackArg
     }
 }
 
+constexpr int kMaxParts = 1024;  // workgroups of the backward kernel: 32 shares for each of 32 threads below
+
 // dw and db: the workgroups' shares added up. A workgroup takes 32 of the 2 cols sums, 32 threads each.
 __global__ __launch_bounds__(1024) void k_join_params(const float* parts, int32_t n_parts, int32_t cols, void* dw,
                                                       void* db, int32_t dtype) {
@@ -433,7 +435,6 @@ __global__ __launch_bounds__(1024) void k_join_params(const float* parts, int32_
     else ((__bf16*)out)[at] = (__bf16)s;
 }
 
-constexpr int kMaxParts = 1024;  // workgroups of the backward kernel
 constexpr int kMaxGrid = 2048;  // workgroups of the forward kernels: eight on each of 256 compute units
 
 template <typename T, int V, int NC, int LANES, int MODE>

@@ -141,7 +141,7 @@ class AdamW:
         every gradient is multiplied by. The number of the step is a constant of the launched kernels: a graph
         that captured a step repeats that number. Parameters change without autograd's notice (it counts no
         version)."""
-        args = (self.params, grads, self._table_at, self._dtype, self.bits, self.m, self.m_scale, self.v,
+        args = (self.params, grads, self._table_at, len(self._table), self._dtype, self.bits, self.m, self.m_scale, self.v,
                 self.v_scale, self.lr, *self.betas, self.eps, self.weight_decay, self.steps + 1, grad_scale)
         if stream is None:
             _native.adamw_step(*args)

@@ -615,6 +615,66 @@ def test_adamw_gradient_scale_and_checkpoint():
             c.load_state_dict(w.AdamW(p, bits=40 - bits).state_dict())
 
 
+def test_adamw_on_another_stream():
+    g = gen(17)
+    for bits in (32, 8):
+        p = tensors(g, [70_000, 300], torch.float32, 1.0)
+        q = [x.clone() for x in p]
+        grads = [tensors(g, [70_000, 300], torch.float32, 0.1) for _ in range(3)]
+        a, b = w.AdamW(p, bits=bits), w.AdamW(q, bits=bits)
+        for x in grads:
+            a.step(x)
+        torch.cuda.synchronize()
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        for x in grads:
+            b.step(x, stream=s)
+        moments = b.moments(stream=s)
+        torch.cuda.current_stream().wait_stream(s)
+        assert all(torch.equal(x, y) for x, y in zip(p, q))
+        assert all(torch.equal(x, y) for x, y in zip(a.moments(), moments))
+
+
+def test_adamw_refuses_what_changed_underneath():
+    """Parameters, gradients and moments that no longer fit are refused before anything is launched."""
+    p = [torch.ones(300, device="cuda"), torch.ones(5, device="cuda")]
+    grads = [torch.ones_like(x) for x in p]
+    for bits in (32, 8):
+        opt = w.AdamW(p, bits=bits)
+        before = [x.clone() for x in p]
+
+        def refused(match, *args, **kw):
+            with pytest.raises(ValueError, match=match):
+                opt.step(*args, **kw)
+            assert opt.steps == 0 and all(torch.equal(a, b) for a, b in zip(before, p))
+
+        refused("gradients for", grads[:1])
+        refused("gradient 1", [grads[0], grads[1][:4]])
+        refused("gradient 0", [torch.ones(600, device="cuda")[::2], grads[1]])
+        refused("gradient 1", [grads[0], grads[1].half()])
+        refused("gradient 0", [grads[0].cpu(), grads[1]])
+        refused("no tensor", [1.0, grads[1]])
+        refused("float32, float16", [x.double() for x in grads])
+        refused("grad_scale", grads, grad_scale=torch.ones(2, device="cuda"))
+        opt.params.append(torch.ones(7, device="cuda"))
+        refused("when the optimizer was made", grads + [torch.ones(7, device="cuda")])
+        opt.params.pop()
+        kept = opt.params[1]
+        opt.params[1] = torch.ones(6, device="cuda")
+        refused("parameter 1", grads)
+        opt.params[1] = kept
+        m = opt.m
+        opt.m = m[:256]
+        refused("moments", grads)
+        opt.m = m
+        if bits == 8:
+            scale, opt.v_scale = opt.v_scale, None
+            refused("scales", grads)
+            opt.v_scale = scale
+        opt.step(grads)
+        assert opt.steps == 1 and not torch.equal(before[0], p[0])
+
+
 def test_adamw_spoilt_gradients():
     """A NaN or an infinity reaches its element (32 bits) or its block's moments (8 bits), no other."""
     for bits in (32, 8):
