@@ -57,7 +57,8 @@ __device__ __forceinline__ Vec<T, V> stream_in(const T* p) {
 }
 template <typename T, int V>
 __device__ __forceinline__ void stream_out(T* p, const Vec<T, V>& v) {
-    __builtin_nontemporal_store(__builtin_bit_cast(typename Raw<sizeof(T) * V>::type, v), (typename Raw<sizeof(T) * V>::type*)p);
+    typedef typename Raw<sizeof(T) * V>::type R;
+    __builtin_nontemporal_store(__builtin_bit_cast(R, v), (R*)p);
 }
 
 // Sums over 16 lanes of a wave or all 64, returned to every lane: four steps inside 16 lanes, then

@@ -43,8 +43,8 @@ __device__ __forceinline__ int channel_key(int row) { return (row & 3) | (row / 
 // buffers are arrays of their own, so that the compiler sees that a read of one needs no wait for loads into
 // the other. Bound by power and by the loads behind the matrix cores: 8192 x 8192 by 8192 takes 437 us (2.5e15
 // operations a second) with random values, 376 us with zeros, 370 us with random values but without its loads (matrix
-// cores busy 61% of cycles, at 1.7 GHz under load); 32,768 x 4096 by 4096 takes 502 us, and 426 us without loads. No faster:
-// quarter steps (520), order pinned by scheduling barriers (495 with operands and sums tied to registers by hand, 1450
+// cores busy 61% of cycles, at 1.7 GHz under load); 32,768 x 4096 by 4096 takes 502 us, and 426 us without loads. No
+// faster: products of 32 x 32 x 32 (609), quarter steps (520), order pinned by scheduling barriers (495 with operands and sums tied to registers by hand, 1450
 // and more where the compiler spills), tokens loaded two steps ahead (511), workgroups that stay for several tiles and
 // load the next one's first rows before they store (495 to 500), waits by counts instead of a full one (537), tiles by
 // four waves of 128 x 128 (710). Smaller tiles gain nothing from four buffers and waits by counts either.
@@ -58,7 +58,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs g) {
     __shared__ __attribute__((aligned(16))) int8_t a1[TM * kStep];
     __shared__ __attribute__((aligned(16))) int8_t w0[TN * kStep];
     __shared__ __attribute__((aligned(16))) int8_t w1[TN * kStep];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, q = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int li = lane & 15, q = lane >> 4;
     const int wm = (wave / WN) * (TM / WM), wn = (wave % WN) * (TN / WN);
     // tiles of one XCD (every eighth workgroup) are neighbours: its L2 then serves their common rows
     const int tiles_n = (g.n + TN - 1) / TN;
@@ -67,12 +68,14 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs g) {
     const int tile = xcd * per + (xcd < more ? xcd : more) + (blockIdx.x >> 3);
     // and they go through bands of kBand tiles of tokens, channels slower than tokens
     const int tiles_m = tiles / tiles_n, band = tile / (kBand * tiles_n);
-    const int wide = tiles_m - band * kBand < kBand ? tiles_m - band * kBand : kBand, in = tile - band * kBand * tiles_n;
+    const int wide = tiles_m - band * kBand < kBand ? tiles_m - band * kBand : kBand;
+    const int in = tile - band * kBand * tiles_n;
     const int64_t m0 = (int64_t)(band * kBand + in % wide) * TM, c0 = (int64_t)(in / wide) * TN;
 
     // offsets of this lane's pieces from the tile's first rows; rows past the last are the last one again
     uint32_t oa[kLoadM], ow[kLoadN];
-    const int last_m = (int)(g.rows - m0 < TM ? g.rows - m0 : TM) - 1, last_c = (int)(g.n - c0 < TN ? g.n - c0 : TN) - 1;
+    const int last_m = (int)(g.rows - m0 < TM ? g.rows - m0 : TM) - 1;
+    const int last_c = (int)(g.n - c0 < TN ? g.n - c0 : TN) - 1;
 #pragma unroll
     for (int i = 0; i < kLoadM; ++i) {
         const int row = (wave * kLoadM + i) * 8 + (lane >> 3);
@@ -81,17 +84,20 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs g) {
 #pragma unroll
     for (int i = 0; i < kLoadN; ++i) {
         const int row = (wave * kLoadN + i) * 8 + (lane >> 3);
-        ow[i] = (uint32_t)(row < last_c ? row : last_c) * (uint32_t)g.w_stride + 16 * ((lane & 7) ^ channel_key<kBN>(row));
+        ow[i] = (uint32_t)(row < last_c ? row : last_c) * (uint32_t)g.w_stride +
+                16 * ((lane & 7) ^ channel_key<kBN>(row));
     }
     const int8_t* pa = g.a + m0 * g.a_stride;
     const int8_t* pw = g.w + c0 * g.w_stride;
     auto load = [&](int8_t* la, int8_t* lw) {
 #pragma unroll
         for (int i = 0; i < kLoadM; ++i)
-            __builtin_amdgcn_global_load_lds((global_void*)(pa + oa[i]), (lds_void*)(la + (wave * kLoadM + i) * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_void*)(pa + oa[i]), (lds_void*)(la + (wave * kLoadM + i) * 1024),
+                                             16, 0, 0);
 #pragma unroll
         for (int i = 0; i < kLoadN; ++i)
-            __builtin_amdgcn_global_load_lds((global_void*)(pw + ow[i]), (lds_void*)(lw + (wave * kLoadN + i) * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_void*)(pw + ow[i]), (lds_void*)(lw + (wave * kLoadN + i) * 1024),
+                                             16, 0, 0);
         pa += kStep, pw += kStep;
     };
     // where this lane reads its pieces of a block: rows 16 i + li (channels: 4 j + ...) are at fixed distances, and
@@ -256,12 +262,12 @@ void tiles(const LinearArgs& g, hipStream_t s) {
 inline int64_t cover(int64_t n, int64_t of) { return (n + of - 1) / of; }
 
 // Which kernel, by measured times (us, in a graph, operands in the caches; tokens x channels x columns).
-// Up to four 16 x 16 tiles a compute unit, a tile's columns are split among waves, in 16 x 16, 32 x 16 or 32 x 32 so that
-// there are about as many tiles as compute units: 1 x 1024 x 1024 2.8 (32 x 32 3.7, tiles of 64 x 64 4.5), 64 x 1024 x
-// 1024 3.3 (4.6), 128 x 1024 x 1024 3.9 (16 x 16 4.1, 32 x 32 4.7), 300 x 800 x 800 4.5 (64 x 64 5.0).
-// Else by the time of each kind of tile, in hundredths of a round of 128 x 128 tiles (512 at once, two on a compute unit; up to
-// 256, one on each, take 0.8): a round of 256 x 256 (256 at once) takes 1.66, and 2048 tiles of 64 x 64 take 1.46, with little
-// lost in their last round.
+// Up to four 16 x 16 tiles a compute unit, a tile's columns are split among waves, in 16 x 16, 32 x 16 or 32 x 32 so
+// that there are about as many tiles as compute units: 1 x 1024 x 1024 2.8 (32 x 32 3.7, tiles of 64 x 64 4.5), 64 x
+// 1024 x 1024 3.3 (4.6), 128 x 1024 x 1024 3.9 (16 x 16 4.1, 32 x 32 4.7), 300 x 800 x 800 4.5 (64 x 64 5.0).
+// Else by the time of each kind of tile, in hundredths of a round of 128 x 128 tiles (512 at once, two on a compute
+// unit; up to 256, one on each, take 0.8): a round of 256 x 256 (256 at once) takes 1.66, and 2048 tiles of 64 x 64
+// take 1.46, with little lost in their last round.
 //                         64 x 64  128 x 128  256 x 256
 //   1771 x 1003 x 771         7.1        9.2       22.9
 //   512 x 4096 x 4096        19.0       22.2       48.1

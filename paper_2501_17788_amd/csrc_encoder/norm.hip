@@ -27,9 +27,10 @@ struct Words<0> {
     uint32_t e[1];
 };
 
-// Whether a kernel's inputs pass the caches by: where all that it reads and writes exceeds the 256 MB of the last cache,
-// inputs kept there only displace outputs. 131,072 rows of 1,024 bfloat16: forward 104 us without, 88 us with, backward
-// 160 and 135 us; 30,000 of 2,048 backward 76 and 67 us, forward (245 MB) 41.8 and 42.2 us; 20,000 of 1,024: 14.6 and 17.2 us.
+// Whether a kernel's inputs pass the caches by: where all that it reads and writes exceeds the 256 MB of the last
+// cache, inputs kept there only displace outputs. 131,072 rows of 1,024 bfloat16: forward 104 us without, 88 us with,
+// backward 160 and 135 us; 30,000 of 2,048: backward 76 and 67 us, forward (245 MB) 41.8 and 42.2 us; 20,000 of 1,024:
+// forward 14.6 and 17.2 us.
 bool passes_by(int64_t rows, int32_t cols, int element_bytes) {
     return rows * cols * element_bytes > (int64_t)256 << 20;
 }
@@ -357,7 +358,10 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rows_back(BackArg
 #pragma unroll
             for (int i = 0; i < V; ++i)
 #pragma unroll
-                for (int k = 16; k < kWave; k <<= 1) dw[j][i] += __shfl_xor(dw[j][i], k), db[j][i] += __shfl_xor(db[j][i], k);
+                for (int k = 16; k < kWave; k <<= 1) {
+                    dw[j][i] += __shfl_xor(dw[j][i], k);
+                    db[j][i] += __shfl_xor(db[j][i], k);
+                }
     }
     if (LANES <= kWave) {
         // the four waves' sums meet in the first: two and two, then one and one
@@ -471,7 +475,8 @@ void rows_any(int32_t dtype, const RowArgs& a, hipStream_t s) {
 
 constexpr int kMaxCols = 16384;  // 512 lanes of 32 columns
 
-// Lanes of a row in the backward kernel, which holds five arrays of a lane's columns: at most 32 columns a lane.
+// Lanes of a row in the backward kernel, which holds five arrays of a lane's columns: at most 32 columns a lane. (fp32
+// rows above 8,192 columns spill a tenth to a fifth of their registers then, and still move 4.4 TB/s.)
 int back_lanes(int32_t cols, int32_t dtype) {
     if (cols <= 32 * (16 / dtype_bytes(dtype))) return 16;
     return cols <= 32 * kWave ? kWave : cols <= 32 * 256 ? 256 : 512;

@@ -2,10 +2,10 @@
 products of 8-bit rows, and the AdamW step.
 
 As in `warp`, everything runs in the HIP kernels behind the C ABI of include/warp.h. `_encoder.so` (from
-csrc_encoder/encoder_binding.cpp) checks tensors, allocates outputs with torch and passes pointers: a ValueError for tensors
-that do not fit, a WarpError for what the library refuses. A call works on the current stream of its
-tensors' device, or on `stream`; inputs of another stream are the caller's to wait for. Tensors have
-any row stride (a dimension's elements one after the other); leading dimensions are flattened to rows.
+csrc_encoder/encoder_binding.cpp) checks tensors, allocates outputs with torch and passes pointers: a ValueError
+for tensors that do not fit, a WarpError for what the library refuses. A call works on the current stream of its
+tensors' device, or on `stream`; inputs of another stream are the caller's to wait for. Tensors have any row
+stride (a dimension's elements one after the other); leading dimensions are flattened to rows.
 """
 from __future__ import annotations
 
