@@ -5,7 +5,9 @@
 // 8-bit moments. A block of 256 elements shares a scale S, its largest magnitude, and an element keeps a code c
 // of m = S sign(c) (c / 127)^2 or v = S (c / 255)^4: neighbouring codes are 2 / c (m) and 4 / c (v) apart
 // relative to their value, so values near the block's largest are kept to 1%, and v reaches down to 2e-10 of it.
-// A code counts the cutoffs that the magnitude over S reaches. The new m and v are computed without fused
+// A code counts the cutoffs that the magnitude over S reaches. A v rests on its code until one step would move it by
+// half a code: growing gradients are followed, while an element whose gradients fall and not its block's largest keeps
+// its v. The new m and v are computed without fused
 // multiply-adds, so that every step's codes follow from the formulas' 32-bit operations alone.
 //
 // Bound by memory: 96M parameters, moments in 32 bits 467 us in fp32 (5.7 TB/s), moments in 8 bits 297 us in fp32 and
