@@ -396,6 +396,8 @@ int warp_linear_int8(const int8_t* a, int64_t a_stride, const float* a_scale, in
  * One AdamW step (decoupled weight decay) over many tensors, with t = step (1 and more):
  *   m = beta1 * m + (1 - beta1) * g,  v = beta2 * v + (1 - beta2) * g^2
  *   p = p * (1 - lr * weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * The launched kernels hold t and all of `tensors`: the array may be reused once the call returns, and a captured
+ * step repeats its t and its pointers.
  *   tensors      host array of n_tensors. `param` and `grad` hold n elements of dtype and grad_dtype; a tensor with
  *                n = 0 or a NULL grad is left as it is. `moment` is where its moments start in m and v, a multiple
  *                of 256; they take n rounded up to a multiple of 256, and those of two tensors must not overlap
@@ -405,7 +407,8 @@ int warp_linear_int8(const int8_t* a, int64_t a_stride, const float* a_scale, in
  *                largest magnitude (at least 2^-126); a code counts the cutoffs ((j - 1/2) / 127)^2 or
  *                ((j - 1/2) / 255)^4, j = 1, 2, ..., that the magnitude over S reaches, and is at least 1 for a
  *                v above zero, so that a step is never divided by a v that was lost. p takes the new m and v before
- *                they are coded. A NaN or infinite gradient makes its block's moments NaN
+ *                they are coded. A NaN or infinite gradient leaves no finite moments in its block. What fills up
+ *                a tensor's last block has to stay zeros, as a step leaves it
  *   m, v         16-byte aligned. Zeros (codes and scales) are the start of a training
  *   grad_scale   device fp32 that every gradient is multiplied by, or NULL (a clipping factor, for instance)
  */
