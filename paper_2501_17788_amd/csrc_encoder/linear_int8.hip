@@ -41,13 +41,17 @@ __device__ __forceinline__ int channel_key(int row) { return (row & 3) | (row / 
 // A workgroup makes a tile of TM tokens by TN channels with WM x WN waves. Each K step's rows are copied to LDS
 // by loads that pass no registers, into one of two buffers, while the matrix cores work on the other. The two
 // buffers are arrays of their own, so that the compiler sees that a read of one needs no wait for loads into
-// the other. Bound by power and by the loads behind the matrix cores: 8192 x 8192 by 8192 takes 437 us (2.5e15
-// operations a second) with random values, 376 us with zeros, 370 us with random values but without its loads (matrix
-// cores busy 61% of cycles, at 1.7 GHz under load); 32,768 x 4096 by 4096 takes 502 us, and 426 us without loads. No
-// faster: products of 32 x 32 x 32 (609), quarter steps (520), order pinned by scheduling barriers (495 with operands and sums tied to registers by hand, 1450
-// and more where the compiler spills), tokens loaded two steps ahead (511), workgroups that stay for several tiles and
-// load the next one's first rows before they store (495 to 500), waits by counts instead of a full one (537), tiles by
-// four waves of 128 x 128 (710). Smaller tiles gain nothing from four buffers and waits by counts either.
+// the other. Results pass the caches by: 32,768 x 4096 by 4096 went from 502 to 450 us with that, 65,536 x 1024 by 128 from
+// 20 to 16 us, also where the next kernel reads them (26 to 23.5 us with one that does), as the operands stay cached.
+//
+// Bound by power and by the loads behind the matrix cores: 8192 x 8192 by 8192 takes 418 us (2.6e15 operations a second)
+// with random values and 364 us with zeros. With results kept in the caches (437 and 376 us; 32,768 x 4096 by 4096
+// 502 us) it took 370 us without its loads (and 426 us), the matrix cores busy 61% of cycles at 1.7 GHz. No faster, of
+// 502 us: products of 32 x 32 x 32 (609), quarter steps (520), order pinned by scheduling barriers (495 with operands
+// and sums tied to registers by hand, 1450 and more where the compiler spills), tokens loaded two steps ahead (511),
+// workgroups that stay for several tiles and load the next one's first rows before they store (495 to 500), waits by
+// counts instead of a full one (537), tiles by four waves of 128 x 128 (710). Smaller tiles gain nothing from four
+// buffers and waits by counts either, nor from waves that share a tile's columns (a compute unit's loads bound them).
 template <typename T, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs g) {
     constexpr int kWaves = WM * WN;
@@ -162,7 +166,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs g) {
 #pragma unroll
         for (int e = 0; e < kOut; ++e) v.e[e] = (T)((float)acc[i][e >> 2][e & 3] * sw[e] * sa + b[e]);
         if (c + kOut <= g.n) {
-            store_vec<T, kOut>(out, v);
+            stream_out<T, kOut>(out, v);
         } else {
 #pragma unroll
             for (int e = 0; e < kOut; ++e)
@@ -264,28 +268,33 @@ inline int64_t cover(int64_t n, int64_t of) { return (n + of - 1) / of; }
 // Which kernel, by measured times (us, in a graph, operands in the caches; tokens x channels x columns).
 // Up to four 16 x 16 tiles a compute unit, a tile's columns are split among waves, in 16 x 16, 32 x 16 or 32 x 32 so
 // that there are about as many tiles as compute units: 1 x 1024 x 1024 2.8 (32 x 32 3.7, tiles of 64 x 64 4.5), 64 x
-// 1024 x 1024 3.3 (4.6), 128 x 1024 x 1024 3.9 (16 x 16 4.1, 32 x 32 4.7), 300 x 800 x 800 4.5 (64 x 64 5.0).
-// Else by the time of each kind of tile, in hundredths of a round of 128 x 128 tiles (512 at once, two on a compute
-// unit; up to 256, one on each, take 0.8): a round of 256 x 256 (256 at once) takes 1.66, and 2048 tiles of 64 x 64
-// take 1.46, with little lost in their last round.
+// 1024 x 1024 3.3 (4.6), 128 x 1024 x 1024 3.9 (16 x 16 4.1, 32 x 32 4.7), 512 x 512 x 512 3.7 (64 x 64 4.0).
+// Else by a model of the time of each kind of tile, in hundredths of a full round of 128 x 128 tiles, 512 at once: up
+// to 256 of them, one on a compute unit, take 0.7, and a last round costs half of what it does not fill. 64 x 64 tiles
+// have no such steps and lose by long rows; 256 x 256 tiles, 256 at once, gain by them.
 //                         64 x 64  128 x 128  256 x 256
-//   1771 x 1003 x 771         7.1        9.2       22.9
-//   512 x 4096 x 4096        19.0       22.2       48.1
-//   10,000 x 800 x 800       17.8       20.1       20.6
-//   65,536 x 128 x 1024      21.4       19.8       22.6
-//   2000 x 4000 x 4000       51.2       37.1       50.4
-//   16,384 x 1024 x 1024     34.4       28.7       26.0
-//   8192 x 4096 x 4096        205        141        117
+//   1771 x 1003 x 771         7.1        9.4       21.8
+//   512 x 4096 x 4096        18.1       22.0       45.8
+//   2048 x 2048 x 2048       15.8       13.3       26.3
+//   10,000 x 800 x 800       14.2       16.9       17.0
+//   65,536 x 128 x 1024      18.6       16.3       21.2
+//   2000 x 4000 x 4000       54.2       36.6       50.9
+//   16,384 x 1024 x 1024     29.0       23.1       24.4
+//   20,000 x 1500 x 2000      104       82.0       92.1
+//   8192 x 4096 x 4096        208        139        115
 template <typename T>
 void linear(const LinearArgs& g, hipStream_t s) {
     constexpr int64_t kUnits = 256;
-    const int64_t m = g.rows, n = g.n, t16 = cover(m, 16) * cover(n, 16);
+    const int64_t m = g.rows, n = g.n, k = g.k, t16 = cover(m, 16) * cover(n, 16);
     if (t16 <= kUnits) return split<T, 1, 1>(g, s);
     if (t16 <= 2 * kUnits) return split<T, 2, 1>(g, s);
     if (t16 <= 4 * kUnits) return split<T, 2, 2>(g, s);
     const int64_t t64 = cover(m, 64) * cover(n, 64), t128 = cover(m, 128) * cover(n, 128);
-    const int64_t time64 = 146 * t64 / 2048 + 10, time128 = t128 <= kUnits ? 80 : 100 * cover(t128, 2 * kUnits);
-    const int64_t time256 = 166 * cover(cover(m, 256) * cover(n, 256), kUnits);
+    const int64_t t256 = cover(m, 256) * cover(n, 256);
+    const int64_t time64 = 10 + (100 + k / 80) * t64 / 2048;
+    const int64_t time128 =
+        t128 <= kUnits ? 70 : t128 <= 2 * kUnits ? 100 : 50 * cover(t128, 2 * kUnits) + 25 * t128 / kUnits;
+    const int64_t time256 = (150 + 120000 / k) * cover(t256, kUnits);
     if (time64 <= time128 && time64 <= time256) tiles<T, 64, 64, 2, 2>(g, s);
     else if (time128 <= time256) tiles<T, 128, 128, 2, 4>(g, s);
     else tiles<T, 256, 256, 2, 4>(g, s);
