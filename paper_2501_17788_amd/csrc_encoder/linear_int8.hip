@@ -145,26 +145,44 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs g) {
         step(k + 1, a0, w0, a1, w1);
     }
     if (k < steps) step(k, a1, w1, a0, w0);
-    multiply(part[1]);
     // D[row][col] of a block lies in lane col + 16 (row / 4), element row % 4: lane (li, q) holds channels
-    // 16 q + 4 j + r, r = 0 .. 3, of token li of block i
+    // kOut q + 4 j + r, r = 0 .. 3, of token li of block i. The scales are on their way during the last products
+    // (1771 x 771 by 1003 7.2 us without, 6.6 us with).
     constexpr int kOut = 4 * kBN;  // neighbouring channels of a lane
     const int64_t c = c0 + wn + kOut * q;
-    float sw[kOut], b[kOut];
+    constexpr bool kEarly = kBM * kBN <= 16;  // 256 x 256 tiles have no registers for it
+    float sw[kOut], b[kOut], sa[kBM];
+    auto load_scales = [&] {
+        if (kEarly && c + kOut <= g.n) {
+            const auto vw = load_vec<float, kOut>(g.w_scale + c);
+            const auto vb = g.bias ? load_vec<float, kOut>(g.bias + c) : Vec<float, kOut>{};
 #pragma unroll
-    for (int e = 0; e < kOut; ++e) {
-        sw[e] = c + e < g.n ? g.w_scale[c + e] : 0.f;
-        b[e] = c + e < g.n && g.bias ? g.bias[c + e] : 0.f;
-    }
+            for (int e = 0; e < kOut; ++e) sw[e] = vw.e[e], b[e] = vb.e[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < kOut; ++e) {
+                sw[e] = c + e < g.n ? g.w_scale[c + e] : 0.f;
+                b[e] = c + e < g.n && g.bias ? g.bias[c + e] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kBM; ++i) {
+            const int64_t m = m0 + wm + 16 * i + li;
+            if (kEarly) sa[i] = g.a_scale[m < g.rows ? m : g.rows - 1];
+        }
+    };
+    if (kEarly) load_scales();
+    multiply(part[1]);
+    if (!kEarly) load_scales();
 #pragma unroll
     for (int i = 0; i < kBM; ++i) {
         const int64_t m = m0 + wm + 16 * i + li;
         if (m >= g.rows) continue;
-        const float sa = g.a_scale[m];
+        const float s = kEarly ? sa[i] : g.a_scale[m];
         T* out = (T*)g.out + m * g.out_stride + c;
         Vec<T, kOut> v;
 #pragma unroll
-        for (int e = 0; e < kOut; ++e) v.e[e] = (T)((float)acc[i][e >> 2][e & 3] * sw[e] * sa + b[e]);
+        for (int e = 0; e < kOut; ++e) v.e[e] = (T)((float)acc[i][e >> 2][e & 3] * sw[e] * s + b[e]);
         if (c + kOut <= g.n) {
             stream_out<T, kOut>(out, v);
         } else {
