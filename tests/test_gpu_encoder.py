@@ -368,6 +368,21 @@ def test_linear_int8_larger(rows, n, cols):
         assert not bad.any(), (rows, n, cols, t, int(bad.sum()))
 
 
+@pytest.mark.parametrize("rows,n,cols", [(1, 16_384, 300), (1, 16_385, 300), (16, 16_384, 1000), (17, 8192, 129),
+                                         (5, 10_007, 4096), (16_384, 16, 129), (16_001, 1, 2000), (10_001, 15, 1025),
+                                         (500, 512, 1024), (500, 509, 1025), (33, 4999, 2048)])
+def test_linear_int8_one_side_short(rows, n, cols):
+    """Few tokens by many channels and the reverse, and the sizes where one kind of tiles gives way to the next."""
+    g = gen(rows + n)
+    a, sa = int8_rows(g, rows, cols)
+    b, sb = int8_rows(g, n, cols)
+    qa, qb = w.QuantizedRows.from_int8(a, sa), w.QuantizedRows.from_int8(b, sb)
+    for bias in (None, randn(g, n)):
+        want, tol = product(a, sa, b, sb, bias)
+        for t in TYPES.values():
+            close(w.linear_int8(qa, qb, bias, t), want, tol + rounding(want, t), f"{rows} x {cols} by {n} {t}")
+
+
 def test_linear_int8_longest_sum():
     """k at its limit with every product at its largest: the sums need all 32 bits."""
     g = gen(1)
