@@ -193,15 +193,32 @@ Tensor linear_int8(const Tensor& av, const Tensor& sa, int64_t cols, const Tenso
     return out;
 }
 
-// `table`: the optimizer's `count` records (warp_adamw_tensor) for its parameters, with sizes and moments filled in
-void adamw_step(const py::list& params, const py::sequence& grads, int64_t table, size_t count, at::ScalarType dtype,
+// The optimizer's records (warp_adamw_tensor) in a buffer that it owns, held for one call.
+struct Records {
+    Py_buffer view;
+    explicit Records(const py::object& table) {
+        if (PyObject_GetBuffer(table.ptr(), &view, PyBUF_WRITABLE | PyBUF_C_CONTIGUOUS) != 0) {
+            PyErr_Clear();
+            refuse("the optimizer's records must be a writable array in one piece");
+        }
+    }
+    ~Records() { PyBuffer_Release(&view); }
+    Records(const Records&) = delete;
+    Records& operator=(const Records&) = delete;
+};
+
+// `table`: the optimizer's records for its parameters, with sizes and moments filled in
+void adamw_step(const py::list& params, const py::sequence& grads, const py::object& table, at::ScalarType dtype,
                 int32_t bits, const Tensor& m, const MaybeTensor& m_scale, const Tensor& v, const MaybeTensor& v_scale,
                 double lr, double beta1, double beta2, double eps, double weight_decay, int64_t step,
                 const MaybeTensor& grad_scale) {
     const size_t n = params.size();
-    if (n != count) refuse(n, " parameters, and ", count, " when the optimizer was made");
+    const Records held(table);
+    const size_t bytes = (size_t)held.view.len;
+    if (bytes != n * sizeof(warp_adamw_tensor))
+        refuse(n, " parameters, and records of ", bytes / sizeof(warp_adamw_tensor), " when the optimizer was made");
     if (py::len(grads) != n) refuse(py::len(grads), " gradients for ", n, " parameters");
-    auto* records = reinterpret_cast<warp_adamw_tensor*>(table);
+    auto* records = static_cast<warp_adamw_tensor*>(held.view.buf);
     const auto device = m.device();
     const int64_t size = n ? records[n - 1].moment + (records[n - 1].n + kBlock - 1) / kBlock * kBlock : 0;
     const bool eight = bits == 8;

@@ -126,7 +126,6 @@ class AdamW:
         self._table = np.zeros((len(self.params), 4), np.int64)
         self._table[:, 2] = sizes
         self._table[:, 3] = ends - room
-        self._table_at = self._table.ctypes.data
         dev = first.device
         self.m = torch.zeros(self.size, dtype=torch.float32 if bits == 32 else torch.int8, device=dev)
         self.v = torch.zeros(self.size, dtype=torch.float32 if bits == 32 else torch.uint8, device=dev)
@@ -141,8 +140,8 @@ class AdamW:
         every gradient is multiplied by. The number of the step is a constant of the launched kernels: a graph
         that captured a step repeats that number. Parameters change without autograd's notice (it counts no
         version)."""
-        args = (self.params, grads, self._table_at, len(self._table), self._dtype, self.bits, self.m, self.m_scale, self.v,
-                self.v_scale, self.lr, *self.betas, self.eps, self.weight_decay, self.steps + 1, grad_scale)
+        args = (self.params, grads, self._table, self._dtype, self.bits, self.m, self.m_scale, self.v, self.v_scale,
+                self.lr, *self.betas, self.eps, self.weight_decay, self.steps + 1, grad_scale)
         if stream is None:
             _native.adamw_step(*args)
         else:

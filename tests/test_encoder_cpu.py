@@ -161,3 +161,55 @@ def test_binding_refuses_host_and_odd_tensors():
         w.linear_int8(q, q, bias=torch.ones(3))
     with pytest.raises(ValueError, match="int8"):
         w.QuantizedRows.from_int8(torch.ones(2, 5), torch.ones(2))
+
+
+def _bare_optimizer():
+    """An optimizer's host state without a device: what a copy of it takes along."""
+    from paper_2501_17788_amd import encoder
+
+    opt = object.__new__(encoder.AdamW)
+    opt.params, opt.lr, opt.betas, opt.eps, opt.weight_decay, opt.bits = [], 1e-3, (0.9, 0.999), 1e-8, 0.0, 32
+    opt.steps, opt.size, opt._dtype = 0, 256, torch.float32
+    opt._table = np.array([[0, 0, 9, 0]], np.int64)
+    opt.m, opt.v, opt.m_scale, opt.v_scale = torch.zeros(256), torch.zeros(256), None, None
+    return opt
+
+
+@pytest.mark.parametrize("how", ["deepcopy", "pickle"])
+def test_copied_optimizer_has_records_of_its_own(how, monkeypatch):
+    """A step of a copy hands the library the copy's records, not an address inside the original."""
+    import copy
+    import pickle
+
+    from paper_2501_17788_amd import encoder
+
+    seen = []
+
+    class Native:
+        @staticmethod
+        def adamw_step(params, grads, table, *rest):
+            seen.append(table.ctypes.data)
+
+    monkeypatch.setattr(encoder, "_native", Native)
+    opt = _bare_optimizer()
+    twin = copy.deepcopy(opt) if how == "deepcopy" else pickle.loads(pickle.dumps(opt))
+    opt.step([])
+    twin.step([])
+    assert seen == [opt._table.ctypes.data, twin._table.ctypes.data] and seen[0] != seen[1]
+    assert opt.steps == twin.steps == 1
+
+
+def test_binding_refuses_records_that_do_not_fit():
+    """The records are read through their buffer: of the parameters' number, writable, in one piece."""
+    from paper_2501_17788_amd import encoder
+
+    table = np.zeros((2, 4), np.int64)
+    table[:, 2] = 5
+    table[1, 3] = 256
+    fixed = table.copy()
+    fixed.setflags(write=False)
+    x = torch.zeros(512)
+    for bad in (table[:1], np.zeros((2, 8), np.int64)[:, ::2], fixed, table[:, :3].copy(), b"0" * 64, 140_000_000):
+        with pytest.raises(ValueError, match="records"):
+            encoder._native.adamw_step([x[:5], x[5:10]], [None, None], bad, torch.float32, 32, x, None, x, None, 1e-3, 0.9,
+                                       0.999, 1e-8, 0.0, 1, None)

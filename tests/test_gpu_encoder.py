@@ -820,3 +820,25 @@ def test_adamw_past_32_bits():
         assert torch.equal(p[tail], small) and not p[:5000].any()
         assert torch.equal(opt.m[tail.start:], alone.m) and torch.equal(opt.v[tail.start:], alone.v)
         del opt, p, grad
+
+
+def test_adamw_copies_step_on_their_own():
+    """A deep copy and an unpickled optimizer go on as the original does, also after that is gone."""
+    import copy
+    import io
+
+    g = gen(24)
+    grad = tensors(g, [700, 0, 33], torch.float32, 0.1)
+    for bits in (32, 8):
+        opt = w.AdamW(tensors(g, [700, 0, 33], torch.float32, 1.0), bits=bits)
+        opt.step(grad)
+        file = io.BytesIO()
+        torch.save(opt, file)
+        file.seek(0)
+        twins = [copy.deepcopy(opt), torch.load(file, weights_only=False)]
+        opt.step(grad)
+        want = [x.clone() for x in (*opt.params, *opt.moments())]
+        del opt
+        for twin in twins:
+            twin.step(grad)
+            assert all(torch.equal(a, b) for a, b in zip(want, (*twin.params, *twin.moments())))
