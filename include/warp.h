@@ -400,7 +400,8 @@ int warp_linear_int8(const int8_t* a, int64_t a_stride, const float* a_scale, in
  * step repeats its t and its pointers.
  *   tensors      host array of n_tensors. `param` and `grad` hold n elements of dtype and grad_dtype; a tensor with
  *                n = 0 or a NULL grad is left as it is. `moment` is where its moments start in m and v, a multiple
- *                of 256; they take n rounded up to a multiple of 256, and those of two tensors must not overlap
+ *                of 256; they take n rounded up to a multiple of 256. Neither the parameters nor the moments of two
+ *                tensors may overlap
  *   bits         32: m and v are fp32; m_scale and v_scale are not used.
  *                8: m is int8, v uint8, and each block of 256 elements has a scale S in m_scale and v_scale (fp32,
  *                one for each 256 of m and v): m = S * sign(c) * (c / 127)^2, v = S * (c / 255)^4. S is the block's

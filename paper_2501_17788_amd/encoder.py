@@ -95,12 +95,21 @@ def linear_int8(a: QuantizedRows, w: QuantizedRows, bias=None, dtype=torch.bfloa
     return _on(stream, (a.values, a.scale, w.values, w.scale, bias), _native.linear_int8, *a, *w, bias, dtype)
 
 
+def _overlap(tensors):
+    """The places of two of these contiguous tensors that share memory, or None."""
+    spans = sorted((t.data_ptr(), t.numel() * t.element_size(), i) for i, t in enumerate(tensors) if t.numel())
+    for (start, size, i), (after, _, j) in zip(spans, spans[1:]):
+        if after < start + size:
+            return min(i, j), max(i, j)
+    return None
+
+
 class AdamW:
     """AdamW over many tensors, all of one type, one step a call; moments in 32 or in 8 bits.
 
     The moments of all tensors are two flat tensors (with 8 bits also a scale for each block of 256
-    elements), each tensor's part starting at a multiple of 256. `params` are contiguous device tensors and
-    are updated in place."""
+    elements), each tensor's part starting at a multiple of 256. `params` are contiguous device tensors that share
+    no memory (one that a model uses twice is given once) and are updated in place."""
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 0.01, bits: int = 32):
@@ -115,6 +124,8 @@ class AdamW:
                 raise ValueError("parameters must be contiguous tensors of one type on one device")
         if first.dtype not in (torch.float32, torch.float16, torch.bfloat16):
             raise ValueError(f"parameters must be float32, float16 or bfloat16, got {first.dtype}")
+        if shared := _overlap(self.params):  # two workgroups would move the same elements at once
+            raise ValueError("parameters %d and %d share memory" % shared)
         self.lr, self.betas, self.eps, self.weight_decay, self.bits = lr, tuple(betas), eps, weight_decay, bits
         self.steps = 0
         self._dtype = first.dtype

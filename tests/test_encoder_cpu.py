@@ -213,3 +213,15 @@ def test_binding_refuses_records_that_do_not_fit():
         with pytest.raises(ValueError, match="records"):
             encoder._native.adamw_step([x[:5], x[5:10]], [None, None], bad, torch.float32, 32, x, None, x, None, 1e-3, 0.9,
                                        0.999, 1e-8, 0.0, 1, None)
+
+
+def test_overlapping_tensors_are_found():
+    from paper_2501_17788_amd.encoder import _overlap
+
+    flat = torch.zeros(100)
+    apart = [flat[50:100], flat[:0], flat[0:20], flat[20:50], torch.zeros(3), flat[:0]]
+    assert _overlap(apart) is None and _overlap([]) is None
+    assert _overlap([flat, torch.zeros(5), flat]) == (0, 2)
+    assert _overlap([*apart, flat[49:50]]) == (3, 6)
+    assert _overlap([flat[60:70], flat[0:30], flat[10:12]]) == (1, 2)
+    assert _overlap([flat.view(10, 10)[3], flat[39:41]]) == (0, 1)

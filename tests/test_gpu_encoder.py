@@ -842,3 +842,13 @@ def test_adamw_copies_step_on_their_own():
         for twin in twins:
             twin.step(grad)
             assert all(torch.equal(a, b) for a, b in zip(want, (*twin.params, *twin.moments())))
+
+
+def test_adamw_refuses_parameters_that_share_memory():
+    flat = torch.ones(1000, device="cuda")
+    for shared in ([flat, flat], [flat[:600], torch.ones(3, device="cuda"), flat[599:]]):
+        for bits in (32, 8):
+            with pytest.raises(ValueError, match="share memory"):
+                w.AdamW(shared, bits=bits)
+    w.AdamW([flat[600:], flat[:600], flat[:0], flat[:0]]).step([flat[600:].clone(), flat[:600].clone(), None, None])
+    assert (flat < 1).all()
