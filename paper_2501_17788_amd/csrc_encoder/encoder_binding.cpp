@@ -249,8 +249,8 @@ void adamw_step(const py::list& params, const py::sequence& grads, const py::obj
         if (!any) grad_type = g.scalar_type();
         any = true;
         if (!known(grad_type)) refuse("gradients must be float32, float16 or bfloat16, got ", grad_type);
-        if (g.scalar_type() != grad_type || g.device() != device || !g.is_contiguous() || g.numel() != records[i].n)
-            refuse("gradients must be contiguous tensors of one type and of their parameters' sizes, on ", device,
+        if (g.scalar_type() != grad_type || g.device() != device || !g.is_contiguous() || g.sizes() != p.sizes())
+            refuse("gradients must be contiguous tensors of one type and of their parameters' shapes, on ", device,
                    " (gradient ", i, ")");
         records[i].grad = g.const_data_ptr();
     }

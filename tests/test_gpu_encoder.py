@@ -852,3 +852,19 @@ def test_adamw_refuses_parameters_that_share_memory():
                 w.AdamW(shared, bits=bits)
     w.AdamW([flat[600:], flat[:600], flat[:0], flat[:0]]).step([flat[600:].clone(), flat[:600].clone(), None, None])
     assert (flat < 1).all()
+
+
+def test_adamw_refuses_gradients_of_another_shape():
+    """As many elements in another shape (a transposed weight's gradient) would move the wrong ones."""
+    p = [torch.ones(30, 7, device="cuda"), torch.ones(8, device="cuda")]
+    ones = [torch.ones_like(x) for x in p]
+    for bits in (32, 8):
+        opt = w.AdamW(p, bits=bits)
+        for bad in (torch.ones(7, 30, device="cuda"), torch.ones(210, device="cuda"), torch.ones(1, 30, 7, device="cuda")):
+            with pytest.raises(ValueError, match="gradient 0"):
+                opt.step([bad, ones[1]])
+        with pytest.raises(ValueError, match="gradient 1"):
+            opt.step([ones[0], torch.ones(2, 4, device="cuda")])
+        assert opt.steps == 0 and all((x == 1).all() for x in p)
+        opt.step(ones)
+        p = [torch.ones_like(x) for x in p]
