@@ -38,6 +38,10 @@ __device__ __forceinline__ int token_key(int row) { return row & 7; }
 template <int BN>
 __device__ __forceinline__ int channel_key(int row) { return (row & 3) | (row / (4 * BN) & 1) << 2; }
 
+// Waits for this wave's loads into LDS. A barrier alone orders no loads that pass no registers: without this wait it
+// would be the compiler's choice whether other waves find the rows there behind the barrier.
+__device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // A workgroup makes a tile of TM tokens by TN channels with WM x WN waves. Each K step's rows are copied to LDS
 // by loads that pass no registers, into one of two buffers, while the matrix cores work on the other. The two
 // buffers are arrays of their own, so that the compiler sees that a read of one needs no wait for loads into
@@ -130,7 +134,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs g) {
     // half of a step overlaps the second half of the last one, across the barrier.
     const int steps = g.k / kStep;
     auto step = [&](int k, const int8_t* la, const int8_t* lw, int8_t* na, int8_t* nw) {
-        __syncthreads();  // this step's rows have landed, and the other buffer has been read by all
+        landed();
+        __syncthreads();  // this step's rows are there, and the other buffer has been read by all
         if (k + 1 < steps) load(na, nw);
         read(part[0], la, lw, 0);
         if (k) multiply(part[1]);
