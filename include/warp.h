@@ -408,7 +408,7 @@ int warp_linear_int8(const int8_t* a, int64_t a_stride, const float* a_scale, in
  *                largest magnitude (at least 2^-126); a code counts the cutoffs ((j - 1/2) / 127)^2 or
  *                ((j - 1/2) / 255)^4, j = 1, 2, ..., that the magnitude over S reaches, and is at least 1 for a
  *                v above zero, so that a step is never divided by a v that was lost. p takes the new m and v before
- *                they are coded. A NaN or infinite gradient leaves no finite moments in its block. What fills up
+ *                they are coded, with a square root and a reciprocal that are off by up to 1 ulp each. A NaN or infinite gradient leaves no finite moments in its block. What fills up
  *                a tensor's last block has to stay zeros, as a step leaves it
  *   m, v         16-byte aligned. Zeros (codes and scales) are the start of a training
  *   grad_scale   device fp32 that every gradient is multiplied by, or NULL (a clipping factor, for instance)

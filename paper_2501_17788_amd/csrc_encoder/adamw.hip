@@ -77,8 +77,9 @@ __device__ __forceinline__ void moments(const StepArgs& a, float g, float& m, fl
     m = m * a.b1 + g * a.c1;
     v = v * a.b2 + (g * g) * a.c2;
 }
+constexpr int kSubnormal = 0x80;  // a positive one, of the classes of v_cmp_class_f32
 // The parameter after its step. The 8-bit kernel, which is bound by its arithmetic, takes the approximate square root
-// and reciprocal (within 1 ulp each; a v below 2^-126 counts as zero).
+// and reciprocal (within 1 ulp each), except for a v below 2^-126, which that root takes for zero.
 template <bool FAST>
 __device__ __forceinline__ float moved(const StepArgs& a, float p, float m, float v) {
     if (FAST)
@@ -180,6 +181,7 @@ __global__ __launch_bounds__(256) void k_adamw(StepArgs a) {
         const auto om = stream_in<uint32_t, 2>(cm), ov = stream_in<uint32_t, 2>(cv);
         const float sm = a.m_scale[s], sv = a.v_scale[s];
         uint32_t top_m = 0, top_v = 0;
+        bool low = false;  // some v is above zero and below 2^-126
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             m[e] = m_value((float)(int8_t)(om.e[e / 4] >> 8 * (e & 3)), sm);
@@ -188,6 +190,14 @@ __global__ __launch_bounds__(256) void k_adamw(StepArgs a) {
             p[e] = moved<true>(a, p[e], m[e], v[e]);
             top_m = max(top_m, as_u(m[e]) & 0x7fffffffu);
             top_v = max(top_v, as_u(v[e]));  // no number here is negative
+            low |= __builtin_amdgcn_classf(v[e], kSubnormal);
+        }
+        if (low) {  // seldom: the parameters are read again rather than kept
+            float was[V];
+            load_some<T, V, false>(param + i, n - i, was);
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (__builtin_amdgcn_classf(v[e], kSubnormal)) p[e] = moved<false>(a, was[e], m[e], v[e]);
         }
         store_some<T, V, false>(param + i, n - i, p);
         const float nm = as_f(max(half_max(top_m), 0x00800000u));

@@ -868,3 +868,31 @@ def test_adamw_refuses_gradients_of_another_shape():
         assert opt.steps == 0 and all((x == 1).all() for x in p)
         opt.step(ones)
         p = [torch.ones_like(x) for x in p]
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-21, EPS])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_tiny_gradients(bits, eps):
+    """Second moments below the smallest normal number divide as any other: with an eps below their root, the step
+    is the formula's. Alone, and in one block with ordinary gradients. The moments before a step are read back, the new
+    ones follow from them in single fp32 operations; bounds as in reference_step."""
+    f = np.float32
+    tiny = (10.0 ** np.linspace(-20.5, -15, 250) * np.where(np.arange(250) % 3, 1, -1)).astype(f)
+    usual = (10.0 ** np.linspace(-12, 0, 256)).astype(f)
+    mixed = np.where(np.arange(256) % 5, usual, f(2e-20))
+    g = np.concatenate([tiny, np.full(6, 1e-19, f), usual, mixed, tiny[:99]])
+    grad = torch.from_numpy(g).cuda()
+    p = torch.linspace(-1, 1, len(g), device="cuda") * 1e-3
+    opt = w.AdamW([p], LR, (B1, B2), eps, DECAY, bits)
+    for t in (1, 2):
+        m, v = (x.cpu().numpy()[:len(g)].copy() for x in opt.moments())
+        before = f64(p).numpy()
+        opt.step([grad])
+        m = (m * f(B1) + g * f(1 - B1)).astype(np.float64)
+        v = (v * f(B2) + (g * g) * f(1 - B2)).astype(np.float64)
+        assert (v > 0).all() and (v < 2.0 ** -126).any()
+        move = LR / (1 - B1 ** t) * m / (np.sqrt(v) / np.sqrt(1 - B2 ** t) + eps)
+        want = before * (1 - LR * DECAY) - move
+        tol = 3 * U * (abs(before) + abs(want)) + 12 * U * abs(move)
+        off = abs(f64(p).numpy() - want) <= tol
+        assert off.all(), (t, int((~off).sum()), int(np.argmin(off)), p[int(np.argmin(off))].item())
