@@ -24,20 +24,6 @@ DOCS, DOC_TOKENS, QUERY_TOKENS, BATCH = 1024, 24, 8, 64
 SIGNAL = 64  # directions that tell tokens apart
 
 
-class LayerNorm(torch.autograd.Function):
-    """The library's layer norm for torch's autograd."""
-
-    @staticmethod
-    def forward(ctx, x, weight, bias):
-        y, mean, rstd = warp.layer_norm(x, weight, bias)
-        ctx.save_for_backward(x, weight, mean, rstd)
-        return y
-
-    @staticmethod
-    def backward(ctx, dy):
-        return warp.layer_norm_backward(dy, *ctx.saved_tensors)
-
-
 class Data:
     """Hidden states [docs, tokens, WIDTH] bfloat16 of passages and of queries that repeat some of their tokens."""
 
@@ -62,7 +48,7 @@ class Data:
 
 def head(hidden, weight, bias, projection):
     """Unit tokens [..., DIM] of hidden states, for training."""
-    y = LayerNorm.apply(hidden, weight, bias)
+    y = warp.layer_norm(hidden, weight, bias)[0]
     return torch.nn.functional.normalize(y.float() @ projection.t(), dim=-1)
 
 

@@ -84,10 +84,15 @@ Params params_of(const Tensor& x, const MaybeTensor& weight, const MaybeTensor& 
 
 Tensor like(const Tensor& x) { return x.is_contiguous() ? at::empty_like(x) : at::empty(x.sizes(), x.options()); }
 
+bool tracked(const MaybeTensor& t) { return t && t->requires_grad(); }
+
 py::tuple layer_norm(const Tensor& x, const MaybeTensor& weight, const MaybeTensor& bias, double eps) {
     on_device(x);
     on_device(x, weight);
     on_device(x, bias);
+    // autograd's node, which calls this again with gradients off
+    if (at::GradMode::is_enabled() && (x.requires_grad() || tracked(weight) || tracked(bias)))
+        return py::module_::import("paper_2501_17788_amd.encoder").attr("_LayerNorm").attr("apply")(x, weight, bias, eps);
     const c10::DeviceGuard guard(x.device());
     const Rows r = rows_of(x, "x");
     const Params p = params_of(x, weight, bias);

@@ -5,7 +5,8 @@ As in `warp`, everything runs in the HIP kernels behind the C ABI of include/war
 csrc_encoder/encoder_binding.cpp) checks tensors, allocates outputs with torch and passes pointers: a ValueError
 for tensors that do not fit, a WarpError for what the library refuses. A call works on the current stream of its
 tensors' device, or on `stream`; inputs of another stream are the caller's to wait for. Tensors have any row
-stride (a dimension's elements one after the other); leading dimensions are flattened to rows.
+stride (a dimension's elements one after the other); leading dimensions are flattened to rows. autograd follows
+`layer_norm`; 8-bit rows and what is made of them carry no gradient.
 """
 from __future__ import annotations
 
@@ -56,16 +57,36 @@ def _on(stream, tensors, call, *args):
         return call(*args)
 
 
+class _LayerNorm(torch.autograd.Function):
+    """What `layer_norm` is to autograd. The statistics have no gradient, and y no second derivative."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        y, mean, rstd = _native.layer_norm(x, weight, bias, eps)
+        ctx.save_for_backward(x, weight, mean, rstd)
+        ctx.mark_non_differentiable(mean, rstd)
+        ctx.bias_type = None if bias is None else bias.dtype
+        return y, mean, rstd
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, *_):
+        x, weight, mean, rstd = ctx.saved_tensors
+        dx, dw, db = _native.layer_norm_backward(dy, x, weight, mean, rstd)
+        return dx, None if weight is None else dw, None if ctx.bias_type is None else db.to(ctx.bias_type), None
+
+
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, stream=None):
     """Layer norm over the last dimension of x [..., cols]: (y like x, mean, rstd), the row statistics in
-    float32 [...] for `layer_norm_backward`. weight and bias [cols] are float32 or of x's type."""
+    float32 [...] for `layer_norm_backward`. weight and bias [cols] are float32 or of x's type. autograd follows y,
+    not the statistics."""
     if stream is None:
         return _native.layer_norm(x, weight, bias, eps)
     return _on(stream, (x, weight, bias), _native.layer_norm, x, weight, bias, eps)
 
 
 def layer_norm_backward(dy, x, weight, mean, rstd, stream=None):
-    """Gradients (dx, dweight, dbias) of `layer_norm` for the gradient dy of its y. dweight and dbias have
+    """Gradients (dx, dweight, dbias) of `layer_norm` for the gradient dy of its y, unknown to autograd. dweight and dbias have
     weight's type (float32 without a weight)."""
     if stream is None:
         return _native.layer_norm_backward(dy, x, weight, mean, rstd)

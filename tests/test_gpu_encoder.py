@@ -896,3 +896,55 @@ def test_adamw_tiny_gradients(bits, eps):
         tol = 3 * U * (abs(before) + abs(want)) + 12 * U * abs(move)
         off = abs(f64(p).numpy() - want) <= tol
         assert off.all(), (t, int((~off).sum()), int(np.argmin(off)), p[int(np.argmin(off))].item())
+
+
+def test_layer_norm_in_autograd():
+    """Gradients reach x, weight and bias, as the backward call gives them; none under no_grad."""
+    g = gen(25)
+    for t in TYPES.values():
+        for shape, params in (((5, 100), torch.float32), ((2, 3, 777), t), ((64,), t)):
+            cols = shape[-1]
+            x = hidden(g, 6, cols, t).flatten()[:int(np.prod(shape))].view(shape).requires_grad_()
+            weight, bias = ((1 + 0.2 * randn(g, cols)).to(params).requires_grad_() for _ in range(2))
+            dy = randn(g, *shape).to(t)
+            y, mean, rstd = w.layer_norm(x, weight, bias)
+            assert y.requires_grad and not mean.requires_grad and not rstd.requires_grad
+            y.backward(dy)
+            with torch.no_grad():
+                plain, m, r = w.layer_norm(x, weight, bias)
+            assert not plain.requires_grad and torch.equal(plain, y) and torch.equal(m, mean) and torch.equal(r, rstd)
+            want = w.layer_norm_backward(dy, x.detach(), weight.detach(), mean, rstd)
+            for got, ref in zip((x.grad, weight.grad, bias.grad), want):
+                assert got.dtype == ref.dtype and torch.equal(got, ref)
+            # one of them alone; a broadcast gradient; without weight or bias
+            fixed = x.detach()
+            alone, = torch.autograd.grad(w.layer_norm(fixed, weight.detach(), bias)[0].sum(), [bias])
+            assert torch.equal(alone, w.layer_norm_backward(torch.ones_like(fixed), fixed, weight.detach(), m, r)[2])
+            alone, = torch.autograd.grad(w.layer_norm(fixed, None, bias)[0], [bias], dy)
+            assert alone.dtype == params
+            assert torch.equal(alone, w.layer_norm_backward(dy, fixed, None, m, r)[2].to(params))
+            alone, = torch.autograd.grad(w.layer_norm(x)[0], [x], dy)
+            assert torch.equal(alone, w.layer_norm_backward(dy, fixed, None, m, r)[0])
+    # a second derivative is refused, not left out
+    x = randn(g, 4, 32).requires_grad_()
+    first, = torch.autograd.grad(w.layer_norm(x)[0].square().sum(), [x], create_graph=True)
+    with pytest.raises(RuntimeError):
+        first.sum().backward()
+
+
+def test_layer_norm_in_autograd_on_another_stream():
+    g = gen(26)
+    x, dy = hidden(g, 900, 1000, torch.bfloat16), randn(g, 900, 1000).bfloat16()
+    weight = 1 + 0.1 * randn(g, 1000)
+    y, mean, rstd = w.layer_norm(x, weight)
+    want = w.layer_norm_backward(dy, x, weight, mean, rstd)[:2]
+    torch.cuda.synchronize()
+    x.requires_grad_()
+    weight.requires_grad_()
+    s = torch.cuda.Stream()
+    for _ in range(3):
+        s.wait_stream(torch.cuda.current_stream())
+        out = w.layer_norm(x, weight, stream=s)[0]
+        torch.cuda.current_stream().wait_stream(s)
+        assert torch.equal(out, y)
+        assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, [x, weight], dy), want))
