@@ -267,6 +267,11 @@ void adamw_step(const py::list& params, const py::sequence& grads, const py::obj
                           m_scale ? m_scale->data_ptr<float>() : nullptr, v.data_ptr(),
                           v_scale ? v_scale->data_ptr<float>() : nullptr, lr, beta1, beta2, eps, weight_decay, step,
                           (const float*)ptr(grad_scale), stream_of(m)));
+    // for autograd: what was changed in place
+    for (size_t i = 0; i < n; ++i) {
+        const Tensor& p = THPVariable_Unpack(PyList_GET_ITEM(params.ptr(), (Py_ssize_t)i));
+        if (records[i].grad && !p.is_inference()) p.unsafeGetTensorImpl()->bump_version();
+    }
 }
 
 py::tuple adamw_moments(const Tensor& m, const Tensor& m_scale, const Tensor& v, const Tensor& v_scale) {

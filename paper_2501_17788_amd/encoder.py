@@ -170,8 +170,7 @@ class AdamW:
         """One step. grads: a contiguous tensor like each parameter, all of one floating type, or None for a
         parameter that this step leaves as it is. grad_scale: a float32 device tensor of one element that
         every gradient is multiplied by. The number of the step is a constant of the launched kernels: a graph
-        that captured a step repeats that number. Parameters change without autograd's notice (it counts no
-        version)."""
+        that captured a step repeats that number. autograd counts the change of a parameter as any in place."""
         args = (self.params, grads, self._table, self._dtype, self.bits, self.m, self.m_scale, self.v, self.v_scale,
                 self.lr, *self.betas, self.eps, self.weight_decay, self.steps + 1, grad_scale)
         if stream is None:

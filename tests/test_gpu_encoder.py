@@ -948,3 +948,27 @@ def test_layer_norm_in_autograd_on_another_stream():
         torch.cuda.current_stream().wait_stream(s)
         assert torch.equal(out, y)
         assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, [x, weight], dy), want))
+
+
+def test_adamw_is_seen_by_autograd():
+    """A backward pass over parameters that a step has changed since is refused, as after any change in place."""
+    for bits in (32, 8):
+        p, still = torch.ones(4, 8, device="cuda", requires_grad=True), torch.ones(8, device="cuda", requires_grad=True)
+        other = torch.ones(5, device="cuda")
+        with torch.inference_mode():
+            apart = torch.ones(5, device="cuda")  # counts no versions
+        opt = w.AdamW([p, still, other, apart], bits=bits)
+        x = torch.ones(2, 4, device="cuda", requires_grad=True)
+        stale, fine = (x @ p).sum(), (x.sum() * still).sum()
+        before = [t._version for t in (p, still, other)]
+        opt.step([torch.ones_like(p), None, torch.ones_like(other), torch.ones(5, device="cuda")])
+        assert [t._version > b for t, b in zip((p, still, other), before)] == [True, False, True]
+        assert (apart < 1).all()
+        fine.backward()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            stale.backward()
+        # a view's change is the whole tensor's
+        flat = torch.ones(20, device="cuda")
+        seen = flat._version
+        w.AdamW([flat[3:9]], bits=bits).step([torch.ones(6, device="cuda")])
+        assert flat._version > seen
