@@ -11,10 +11,14 @@ from .warp import (  # noqa: F401
 )
 
 try:
-    import torch  # noqa: F401
-except ImportError:  # the blocking search of host arrays needs no torch
-    pass
-else:
     from .encoder import (  # noqa: F401
         AdamW, QuantizedRows, layer_norm, layer_norm_backward, layer_norm_int8, linear_int8, quantize_rows,
     )
+except ImportError as e:  # search needs neither torch (for host arrays) nor the operators' binding
+    _missing = e
+
+    def __getattr__(name):
+        if name in ("AdamW", "QuantizedRows", "layer_norm", "layer_norm_backward", "layer_norm_int8", "linear_int8",
+                    "quantize_rows"):
+            raise ImportError(f"{name} needs torch and _encoder.so: {_missing}") from _missing
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

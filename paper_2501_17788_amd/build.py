@@ -83,15 +83,15 @@ def build(jobs: int | None = None) -> str:
     with ThreadPoolExecutor(jobs) as ex:
         binding = ex.submit(_compile_binding)
         objs = list(ex.map(_compile, srcs))
-        binding = binding.result()
     tmp = LIB + ".tmp"
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-Wl,--no-undefined", *objs, "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
-    if binding:
-        _link_binding(binding)
+    obj = binding.result()  # after the library, which does without it
+    if obj:
+        _link_binding(obj)
     return LIB
 
 
