@@ -50,6 +50,8 @@ def _on(stream, tensors, call, *args):
     for t in tensors:
         if t is not None and not t.is_cuda:
             raise ValueError(f"expected device tensors, got {t.device}")
+        if t is not None and t.device != stream.device:
+            raise ValueError(f"a stream of {stream.device} for tensors on {t.device}")
     with torch.cuda.stream(stream):
         for t in tensors:
             if t is not None:

@@ -225,3 +225,22 @@ def test_overlapping_tensors_are_found():
     assert _overlap([*apart, flat[49:50]]) == (3, 6)
     assert _overlap([flat[60:70], flat[0:30], flat[10:12]]) == (1, 2)
     assert _overlap([flat.view(10, 10)[3], flat[39:41]]) == (0, 1)
+
+
+def test_a_stream_of_another_device_is_refused():
+    """Its work would go to the current stream of the tensors' device, unseen by whoever waits for `stream`."""
+    from paper_2501_17788_amd import encoder
+
+    class On:  # a device tensor or a stream, as far as the check looks
+        is_cuda = True
+
+        def __init__(self, device):
+            self.device = torch.device(device)
+
+    def called(*_):
+        raise AssertionError("called")
+
+    with pytest.raises(ValueError, match="stream"):
+        encoder._on(On("cuda:1"), (None, On("cuda:0")), called)
+    with pytest.raises(ValueError, match="stream"):
+        encoder._on(On("cuda:0"), (On("cuda:0"), On("cuda:1")), called)
