@@ -16,6 +16,11 @@ constexpr int kInt8Pad = 128;  // int8 rows are padded with zeros to a multiple 
 inline int dtype_bytes(int32_t dtype) { return dtype == WARP_F32 ? 4 : 2; }
 inline bool dtype_ok(int32_t dtype) { return dtype == WARP_F32 || dtype == WARP_F16 || dtype == WARP_BF16; }
 
+// The kernel that makes the int8 product of these sizes (k: padded), by its tiles. Visible for the tests, which have to
+// reach each of them.
+enum { kSplit16x16, kSplit32x16, kSplit32x32, kTile64, kTile128, kTile256 };
+int linear_kernel(int64_t rows, int64_t n, int64_t k);
+
 // A launch's own error, without taking one that an earlier call of the process left behind.
 #define WARP_LAUNCH(...)                                                                             \
     do {                                                                                             \

@@ -4,6 +4,45 @@
 
 namespace warp {
 
+static inline int64_t cover(int64_t n, int64_t of) { return (n + of - 1) / of; }
+
+// Which kernel, by measured times (us, in a graph, operands in the caches; tokens x channels x columns).
+// Up to four 16 x 16 tiles a compute unit, a tile's columns are split among waves, in 16 x 16, 32 x 16 or 32 x 32 so
+// that there are about as many tiles as compute units: 1 x 1024 x 1024 2.8 (32 x 32 3.7, tiles of 64 x 64 4.0), 64 x
+// 1024 x 1024 3.3 (4.3), 128 x 1024 x 1024 3.9 (16 x 16 4.2, 32 x 32 4.7), 400 x 400 x 400 3.7 (64 x 64 4.2), 500 x 500
+// x 900 4.8 (5.1). Tiles of 32 x 32 no longer gain where rows are long: 64 x 4096 x 4096 10.6 (64 x 64 9.3), 512 x 512
+// x 2048 6.6 (6.0), 450 x 450 x 2000 6.7 (6.6). Where one side has no more than 16, tiles of 16 x 16 waste no rows and
+// go as far: 1 x 10,000 x 4096 9.4 (32 x 32 12.0, 64 x 64 16.4), 16 x 10,000 x 4096 13.5 (14.9, 16.7), 1 x 16,000 x
+// 2048 7.0 (7.6, 9.0), 10,000 x 16 x 4096 13.4 (14.9, 17.2); at 16 x 20,000 x 1000 64 x 64 tiles take 5.0 (8.1).
+// Else by a model of the time of each kind of tile, in hundredths of a full round of 128 x 128 tiles, 512 at once: up
+// to 256 of them, one on a compute unit, take 0.7, and a last round costs half of what it does not fill. 64 x 64 tiles
+// have no such steps and lose by long rows; 256 x 256 tiles, 256 at once, gain by them.
+//                         64 x 64  128 x 128  256 x 256
+//   1771 x 1003 x 771         6.4        8.5       21.6
+//   512 x 4096 x 4096        17.6       21.3       46.4
+//   2048 x 2048 x 2048       15.6       12.1       26.7
+//   10,000 x 800 x 800       13.8       15.0       16.8
+//   65,536 x 128 x 1024      18.1       15.8       21.2
+//   2000 x 4000 x 4000       51.6       35.1       51.3
+//   16,384 x 1024 x 1024     28.3       21.5       22.3
+//   20,000 x 1500 x 2000      102       79.7       92.6
+//   8192 x 4096 x 4096        200        138        115
+int linear_kernel(int64_t m, int64_t n, int64_t k) {
+    constexpr int64_t kUnits = 256;
+    const int64_t t16 = cover(m, 16) * cover(n, 16);
+    if (t16 <= (m <= 16 || n <= 16 ? 4 : 1) * kUnits) return kSplit16x16;
+    if (t16 <= 2 * kUnits) return kSplit32x16;
+    if (t16 <= 4 * kUnits && k <= 1024) return kSplit32x32;
+    const int64_t t64 = cover(m, 64) * cover(n, 64), t128 = cover(m, 128) * cover(n, 128);
+    const int64_t t256 = cover(m, 256) * cover(n, 256);
+    const int64_t time64 = 10 + (100 + k / 80) * t64 / 2048;
+    const int64_t time128 =
+        t128 <= kUnits ? 70 : t128 <= 2 * kUnits ? 100 : 50 * cover(t128, 2 * kUnits) + 25 * t128 / kUnits;
+    const int64_t time256 = (150 + 120000 / k) * cover(t256, kUnits);
+    if (time64 <= time128 && time64 <= time256) return kTile64;
+    return time128 <= time256 ? kTile128 : kTile256;
+}
+
 namespace {
 
 typedef int int4v __attribute__((ext_vector_type(4)));
@@ -286,45 +325,16 @@ void tiles(const LinearArgs& g, hipStream_t s) {
     hipLaunchKernelGGL((k_linear_tile<T, TM, TN, WM, WN>), dim3((uint32_t)n), dim3(64 * WM * WN), 0, s, g);
 }
 
-inline int64_t cover(int64_t n, int64_t of) { return (n + of - 1) / of; }
-
-// Which kernel, by measured times (us, in a graph, operands in the caches; tokens x channels x columns).
-// Up to four 16 x 16 tiles a compute unit, a tile's columns are split among waves, in 16 x 16, 32 x 16 or 32 x 32 so
-// that there are about as many tiles as compute units: 1 x 1024 x 1024 2.8 (32 x 32 3.7, tiles of 64 x 64 4.0), 64 x
-// 1024 x 1024 3.3 (4.3), 128 x 1024 x 1024 3.9 (16 x 16 4.2, 32 x 32 4.7), 400 x 400 x 400 3.7 (64 x 64 4.2), 500 x 500
-// x 900 4.8 (5.1). Tiles of 32 x 32 no longer gain where rows are long: 64 x 4096 x 4096 10.6 (64 x 64 9.3), 512 x 512
-// x 2048 6.6 (6.0), 450 x 450 x 2000 6.7 (6.6). Where one side has no more than 16, tiles of 16 x 16 waste no rows and
-// go as far: 1 x 10,000 x 4096 9.4 (32 x 32 12.0, 64 x 64 16.4), 16 x 10,000 x 4096 13.5 (14.9, 16.7), 1 x 16,000 x
-// 2048 7.0 (7.6, 9.0), 10,000 x 16 x 4096 13.4 (14.9, 17.2); at 16 x 20,000 x 1000 64 x 64 tiles take 5.0 (8.1).
-// Else by a model of the time of each kind of tile, in hundredths of a full round of 128 x 128 tiles, 512 at once: up
-// to 256 of them, one on a compute unit, take 0.7, and a last round costs half of what it does not fill. 64 x 64 tiles
-// have no such steps and lose by long rows; 256 x 256 tiles, 256 at once, gain by them.
-//                         64 x 64  128 x 128  256 x 256
-//   1771 x 1003 x 771         6.4        8.5       21.6
-//   512 x 4096 x 4096        17.6       21.3       46.4
-//   2048 x 2048 x 2048       15.6       12.1       26.7
-//   10,000 x 800 x 800       13.8       15.0       16.8
-//   65,536 x 128 x 1024      18.1       15.8       21.2
-//   2000 x 4000 x 4000       51.6       35.1       51.3
-//   16,384 x 1024 x 1024     28.3       21.5       22.3
-//   20,000 x 1500 x 2000      102       79.7       92.6
-//   8192 x 4096 x 4096        200        138        115
 template <typename T>
 void linear(const LinearArgs& g, hipStream_t s) {
-    constexpr int64_t kUnits = 256;
-    const int64_t m = g.rows, n = g.n, k = g.k, t16 = cover(m, 16) * cover(n, 16);
-    if (t16 <= (m <= 16 || n <= 16 ? 4 : 1) * kUnits) return split<T, 1, 1>(g, s);
-    if (t16 <= 2 * kUnits) return split<T, 2, 1>(g, s);
-    if (t16 <= 4 * kUnits && k <= 1024) return split<T, 2, 2>(g, s);
-    const int64_t t64 = cover(m, 64) * cover(n, 64), t128 = cover(m, 128) * cover(n, 128);
-    const int64_t t256 = cover(m, 256) * cover(n, 256);
-    const int64_t time64 = 10 + (100 + k / 80) * t64 / 2048;
-    const int64_t time128 =
-        t128 <= kUnits ? 70 : t128 <= 2 * kUnits ? 100 : 50 * cover(t128, 2 * kUnits) + 25 * t128 / kUnits;
-    const int64_t time256 = (150 + 120000 / k) * cover(t256, kUnits);
-    if (time64 <= time128 && time64 <= time256) tiles<T, 64, 64, 2, 2>(g, s);
-    else if (time128 <= time256) tiles<T, 128, 128, 2, 4>(g, s);
-    else tiles<T, 256, 256, 2, 4>(g, s);
+    switch (linear_kernel(g.rows, g.n, g.k)) {
+        case kSplit16x16: return split<T, 1, 1>(g, s);
+        case kSplit32x16: return split<T, 2, 1>(g, s);
+        case kSplit32x32: return split<T, 2, 2>(g, s);
+        case kTile64: return tiles<T, 64, 64, 2, 2>(g, s);
+        case kTile128: return tiles<T, 128, 128, 2, 4>(g, s);
+        default: return tiles<T, 256, 256, 2, 4>(g, s);
+    }
 }
 
 }  // namespace

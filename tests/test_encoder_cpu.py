@@ -244,3 +244,16 @@ def test_a_stream_of_another_device_is_refused():
         encoder._on(On("cuda:1"), (None, On("cuda:0")), called)
     with pytest.raises(ValueError, match="stream"):
         encoder._on(On("cuda:0"), (On("cuda:0"), On("cuda:1")), called)
+
+
+def test_product_sizes_reach_their_kernels():
+    """The sizes of the GPU tests choose the kernels that they are listed under: a change of the choice that leaves a
+    kernel without a test fails here."""
+    import product_sizes
+
+    choose = lib["_ZN4warp13linear_kernelElll"]  # int warp::linear_kernel(int64_t rows, int64_t n, int64_t k)
+    choose.argtypes, choose.restype = [ctypes.c_int64] * 3, ctypes.c_int
+    assert len(product_sizes.KERNELS) == 6
+    for number, kernel in enumerate(product_sizes.KERNELS):
+        for rows, n, cols in product_sizes.SIZES[kernel]:
+            assert choose(rows, n, -(-cols // 128) * 128) == number, (kernel, rows, n, cols)

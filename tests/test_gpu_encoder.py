@@ -972,3 +972,30 @@ def test_adamw_is_seen_by_autograd():
         seen = flat._version
         w.AdamW([flat[3:9]], bits=bits).step([torch.ones(6, device="cuda")])
         assert flat._version > seen
+
+
+def _product_cases():
+    import product_sizes
+
+    return [pytest.param(kernel, size, id=f"{kernel}: {size[0]} x {size[1]} x {size[2]}".replace(" ", ""))
+            for kernel, sizes in product_sizes.SIZES.items() for size in sizes]
+
+
+@pytest.mark.parametrize("kernel,size", _product_cases())
+def test_linear_int8_kernels(kernel, size):
+    """Every kernel of the product at sizes that are no multiples of its tiles, in every type, with a bias and without."""
+    rows, n, cols = size
+    g = gen(n)
+    a, sa = int8_rows(g, rows, cols)
+    b, sb = int8_rows(g, n, cols)
+    qa, qb = w.QuantizedRows.from_int8(a, sa), w.QuantizedRows.from_int8(b, sb)
+    acc = a.double() @ b.double().t()  # exact: below 2^53
+    scaled = acc * sb.double() * sa.double()[:, None]
+    del acc
+    for bias in (randn(g, n), None):
+        want = scaled if bias is None else scaled + bias.double()
+        for t in TYPES.values():
+            say("int8 product", kernel, size, t)
+            out = w.linear_int8(qa, qb, bias, t)
+            off = (out.double() - want).abs() - (4 * U * scaled.abs() + U * want.abs() + rounding(want, t))
+            assert out.shape == want.shape and not (off > 0).any(), (t, int((off > 0).sum()))
