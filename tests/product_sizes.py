@@ -8,6 +8,7 @@ SIZES = {
     "32 x 32 split": [(500, 509, 1000), (997, 250, 100), (33, 4999, 513)],
     "64 x 64": [(65, 4001, 4000), (1771, 1003, 771), (129, 5000, 60), (10_001, 801, 800), (65_537, 127, 1000)],
     "128 x 128": [(2041, 2047, 2000), (2001, 3999, 1900), (65_409, 127, 1000), (4090, 4083, 900)],
-    "256 x 256": [(4081, 4079, 4000), (3841, 4095, 3900), (4095, 3842, 4100), (7937, 4001, 2500), (8161, 8177, 2600), (5793, 2801, 4000)],
+    "256 x 256": [(4081, 4079, 4000), (3841, 4095, 3900), (4095, 3842, 4100), (7937, 4001, 2500),
+                  (8161, 8177, 2600), (5793, 2801, 4000)],
 }
 KERNELS = list(SIZES)  # in the order of the library's numbers

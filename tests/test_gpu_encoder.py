@@ -999,3 +999,41 @@ def test_linear_int8_kernels(kernel, size):
             out = w.linear_int8(qa, qb, bias, t)
             off = (out.double() - want).abs() - (4 * U * scaled.abs() + U * want.abs() + rounding(want, t))
             assert out.shape == want.shape and not (off > 0).any(), (t, int((off > 0).sum()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(37, 3), (5000, 100), (37, 101), (37, 256), (2100, 771), (9, 1024), (37, 2047),
+                                       (9, 3000), (700, 5001), (9, 8200), (600, 9001), (9, 16_383), (9, 16_384)])
+def test_layer_norm_backward_in_place_and_in_part(rows, cols, dtype):
+    """dx over x or over dy, either sum left out, and neither with no scratch: the bits of the ordinary call. Rows of
+    16 lanes, a wave, four and eight waves, even and ragged."""
+    from paper_2501_17788_amd import lib
+
+    t = TYPES[dtype]
+    code = {torch.float32: 0, torch.bfloat16: 2}[t]
+    g = gen(rows + cols)
+    x, dy, weight = hidden(g, rows, cols, t), randn(g, rows, cols).to(t), 1 + 0.2 * randn(g, cols)
+    _, mean, rstd = w.layer_norm(x, weight)
+    want = w.layer_norm_backward(dy, x, weight, mean, rstd)
+    need = np.zeros(1, np.int64)
+    assert lib.warp_layer_norm_backward_scratch(rows, cols, code, need.ctypes.data) == 0
+    scratch = torch.empty(int(need[0]), dtype=torch.uint8, device="cuda")
+    for place in ("x", "dy", "apart"):
+        for sums in ("both", "dw", "db", "none"):
+            say("backward", rows, cols, dtype, place, sums)
+            a, d = x.clone(), dy.clone()
+            dx = {"x": a, "dy": d, "apart": torch.empty_like(x)}[place]
+            dw, db = torch.full((2, cols), 7.0, device="cuda")
+            rc = lib.warp_layer_norm_backward(
+                d.data_ptr(), cols, a.data_ptr(), cols, rows, cols, code, weight.data_ptr(), 0, mean.data_ptr(),
+                rstd.data_ptr(), dx.data_ptr(), cols, dw.data_ptr() if sums in ("both", "dw") else None,
+                db.data_ptr() if sums in ("both", "db") else None, scratch.data_ptr() if sums != "none" else None,
+                int(need[0]) if sums != "none" else 0, torch.cuda.current_stream().cuda_stream)
+            assert rc == 0, w.last_error()
+            assert torch.equal(dx, want[0])
+            assert torch.equal(dw, want[1]) if sums in ("both", "dw") else (dw == 7).all()
+            assert torch.equal(db, want[2]) if sums in ("both", "db") else (db == 7).all()
+            if place != "x":
+                assert torch.equal(a, x)
+            if place != "dy":
+                assert torch.equal(d, dy)
