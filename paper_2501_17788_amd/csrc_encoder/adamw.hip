@@ -5,10 +5,15 @@
 // 8-bit moments. A block of 256 elements shares a scale S, its largest magnitude, and an element keeps a code c
 // of m = S sign(c) (c / 127)^2 or v = S (c / 255)^4: neighbouring codes are 2 / c (m) and 4 / c (v) apart
 // relative to their value, so values near the block's largest are kept to 1%, and v reaches down to 2e-10 of it.
-// A code counts the cutoffs that the magnitude over S reaches. A v rests on its code until one step would move it by
-// half a code: growing gradients are followed, while an element whose gradients fall and not its block's largest keeps
-// its v. The new m and v are computed without fused
+// A code counts the cutoffs that the magnitude over S reaches. The new m and v are computed without fused
 // multiply-adds, so that every step's codes follow from the formulas' 32-bit operations alone.
+//
+// A moment rests on its code until one step moves it by half the way to the next: 1 / c of an m, 2 / c of a v. A step
+// without a gradient takes 1 - b1 of an m, so with b1 = 0.9 it rests up to code 9, and 1 - b2 of a v, so with b2 = 0.999
+// it rests at every code, both while the block's largest stays. Growing gradients with noise are followed; constant ones
+// that double are not, and falling ones are not. An element whose gradient vanishes goes on moving: with noise by 0.4,
+// 3.3 and 72 lr in 2,400 steps after gradients of 1, 0.1 and 0.005 of its neighbours', by 11 and 108 lr after constant
+// ones of 1 and 0.1; a gradient that has turned below 0.5% of the block's largest does not turn its m.
 //
 // Bound by memory: 96M parameters, moments in 32 bits 467 us in fp32 (5.7 TB/s), moments in 8 bits 297 us in fp32 and
 // 168 us in bfloat16 (5.7 TB/s). There the arithmetic, some 70 operations an element, takes nearly as long: with the

@@ -88,8 +88,8 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, stream=None):
 
 
 def layer_norm_backward(dy, x, weight, mean, rstd, stream=None):
-    """Gradients (dx, dweight, dbias) of `layer_norm` for the gradient dy of its y, unknown to autograd. dweight and dbias have
-    weight's type (float32 without a weight)."""
+    """Gradients (dx, dweight, dbias) of `layer_norm` for the gradient dy of its y, unknown to autograd. dweight and
+    dbias have weight's type (float32 without a weight)."""
     if stream is None:
         return _native.layer_norm_backward(dy, x, weight, mean, rstd)
     return _on(stream, (x, dy, weight, mean, rstd), _native.layer_norm_backward, dy, x, weight, mean, rstd)
@@ -132,7 +132,12 @@ class AdamW:
 
     The moments of all tensors are two flat tensors (with 8 bits also a scale for each block of 256
     elements), each tensor's part starting at a multiple of 256. `params` are contiguous device tensors that share
-    no memory (one that a model uses twice is given once) and are updated in place."""
+    no memory (one that a model uses twice is given once) and are updated in place.
+
+    8 bits are for tensors whose gradients stay alive, within an order of magnitude among 256 neighbours. An element
+    whose gradient vanishes, or turns and is below 0.5% of its block's largest, keeps the first moment that it had (as
+    long as the largest stays) and goes on moving, by tens of lr in thousands of steps: token tables and layers with
+    dead columns belong in an optimizer of 32 bits."""
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 0.01, bits: int = 32):
