@@ -15,9 +15,10 @@
 // 3.3 and 72 lr in 2,400 steps after gradients of 1, 0.1 and 0.005 of its neighbours', by 11 and 108 lr after constant
 // ones of 1 and 0.1; a gradient that has turned below 0.5% of the block's largest does not turn its m.
 //
-// Bound by memory: 96M parameters, moments in 32 bits 467 us in fp32 (5.7 TB/s), moments in 8 bits 297 us in fp32 and
-// 168 us in bfloat16 (5.7 TB/s). There the arithmetic, some 70 operations an element, takes nearly as long: with the
-// exact square root and division in the step it was the bound (240 us).
+// Bound by memory: 96M parameters in 48 tensors, moments in 32 bits 441 us in fp32 (6.1 TB/s), moments in 8 bits 284 us
+// in fp32 (5.4 TB/s) and 164 to 204 us in bfloat16 (5.8 to 4.7 TB/s, by the card). There the arithmetic, some 70
+// operations an element, takes nearly as long: with the exact square root and division in the step it was the bound (240
+// us).
 #include <cmath>
 
 #include "encoder.h"
@@ -49,7 +50,7 @@ static_assert(sizeof(StepArgs) <= 4096, "the arguments of a launch");
 
 // V elements of which `left` are there. NT: not kept in the caches. Gradients are not read again, and moments a step
 // later; the parameters are, by the next forward pass. 96M fp32 parameters and gradients, 32-bit moments: 525 us
-// without, 467 us with.
+// without, 467 us with (on one card; 441 us on another).
 template <typename T, int V, bool NT = true>
 __device__ __forceinline__ void load_some(const T* p, int64_t left, float (&out)[V]) {
     if (left >= V) {

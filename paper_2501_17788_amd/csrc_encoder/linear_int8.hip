@@ -88,8 +88,8 @@ __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" :::
 // 20 to 16 us, also where the next kernel reads them (26 to 23.5 us with one that does), as the operands stay cached.
 //
 // Bound by power and by the loads behind the matrix cores: 8192 x 8192 by 8192 takes 418 us (2.6e15 operations a second)
-// with random values and 364 us with zeros. With results kept in the caches (437 and 376 us; 32,768 x 4096 by 4096
-// 502 us) it took 370 us without its loads (and 426 us), the matrix cores busy 61% of cycles at 1.7 GHz. No faster, of
+// with random values and 364 us with zeros, the matrix cores busy 63% of cycles at 1.6 to 1.8 GHz. With results kept in
+// the caches (437 and 376 us; 32,768 x 4096 by 4096 502 us) it took 370 us without its loads (and 426 us). No faster, of
 // 502 us: products of 32 x 32 x 32 (609), quarter steps (520), order pinned by scheduling barriers (495 with operands
 // and sums tied to registers by hand, 1450 and more where the compiler spills), tokens loaded two steps ahead (511),
 // workgroups that stay for several tiles and load the next one's first rows before they store (495 to 500), waits by

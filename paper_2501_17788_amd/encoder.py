@@ -97,7 +97,8 @@ def layer_norm_backward(dy, x, weight, mean, rstd, stream=None):
 
 def quantize_rows(x, stream=None) -> QuantizedRows:
     """Rows of x [..., cols] in 8 bits with a scale each: token activations, or a weight [n, cols] with a
-    scale for each output channel."""
+    scale for each output channel. At most 16,384 columns; wider rows that were quantised elsewhere come in through
+    `QuantizedRows.from_int8`."""
     if stream is None:
         return QuantizedRows._make(_native.quantize_rows(x))
     return QuantizedRows._make(_on(stream, (x,), _native.quantize_rows, x))
