@@ -407,10 +407,10 @@ int warp_linear_int8(const int8_t* a, int64_t a_stride, const float* a_scale, in
  *                one for each 256 of m and v): m = S * sign(c) * (c / 127)^2, v = S * (c / 255)^4. S is the block's
  *                largest magnitude (at least 2^-126); a code counts the cutoffs ((j - 1/2) / 127)^2 or
  *                ((j - 1/2) / 255)^4, j = 1, 2, ..., that the magnitude over S reaches, and is at least 1 for a
- *                v above zero, so that a step is never divided by a v that was lost. p takes the new m and v before
- *                they are coded, with a square root and a reciprocal that are off by up to 1 ulp each. A NaN or
- *                infinite gradient leaves no finite moments in its block. What fills up a tensor's last block has to
- *                stay zeros, as a step leaves it.
+ *                v above zero, so that a step is never divided by a v that was lost (code 1 stands for a number above
+ *                zero while S is at least 2^-117). p takes the new m and v before they are coded, with a square root
+ *                and a reciprocal that are off by up to 1 ulp each. A NaN or infinite gradient leaves no finite moments
+ *                in its block. What fills up a tensor's last block has to stay zeros, as a step leaves it.
  *                What 8 bits do not follow: a moment leaves its code only when one step moves it by half the way to
  *                the next, 1/c of an m and 2/c of a v. While its block's largest stays, an m whose gradient has become
  *                zero rests, with either sign, at a code of 9 or less (0.5% of the largest) if beta1 is 0.9, and a v at

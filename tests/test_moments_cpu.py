@@ -78,6 +78,12 @@ def test_codes_that_rest():
         assert np.flatnonzero(moved).tolist() == list(range(rests + 1, levels))
 
 
+def test_smallest_second_moment():
+    """Code 1 is above zero while the scale is at least 2^-117: (1 / 255)^4 is 2^-31.98, the smallest number 2^-149."""
+    assert value(np.array([1]), F(2.0 ** -117), 4)[0] > 0 and value(np.array([1]), F(2.0 ** -119), 4)[0] == 0
+    assert coded(np.pad([F(2.0 ** -117), F(2.0 ** -149)], (0, 254))[None], 4)[0][0, 1] == 1
+
+
 def test_steady_gradients():
     """Gradients whose spread varies by 1,000 inside a block: the root of v stays near it."""
     rng = np.random.default_rng(0)
