@@ -175,7 +175,8 @@ def _run_own(s):
         loss, lse = warp.cross_entropy(s["hidden"], s["table"], s["targets"], s["scale"])
         if not case["train"]:
             return loss
-        return (loss, *warp.cross_entropy_backward(s["dloss"], s["hidden"], s["table"], s["targets"], lse, s["scale"]))
+        return (loss, *warp.cross_entropy_backward(s["dloss"], s["hidden"], s["table"], s["targets"], loss, lse,
+                                                   s["scale"]))
     y = warp.linear(s["x"], s["w"], s["b"])
     if not case["train"]:
         return y
