@@ -393,6 +393,96 @@ int warp_linear_int8(const int8_t* a, int64_t a_stride, const float* a_scale, in
                      int64_t out_stride, int32_t out_dtype, void* hip_stream);
 
 /*
+ * Rows of a table by token, scaled:
+ *   out[t] = scale * table[ids[t]]
+ * A negative id (padding) gives a row of zeros, one of `vocabulary` or more a row of NaN.
+ *   ids          [tokens] whole numbers of id_bytes (4 or 8)
+ *   table        [vocabulary][cols] of dtype
+ *   out          [tokens][cols] of dtype
+ * At most 2^25 tokens and table rows and 2^20 columns (above: WARP_ENOTSUP).
+ */
+int warp_embedding(const void* ids, int32_t id_bytes, int64_t tokens, const void* table, int64_t table_stride,
+                   int64_t vocabulary, int32_t cols, int32_t dtype, float scale, void* out, int64_t out_stride,
+                   void* hip_stream);
+/*
+ * The table's gradient: dtable[v] = scale * sum over the tokens t with ids[t] = v of dy[t], every row written. A row's sum
+ * is made in an order that its tokens' order alone fixes. Ids outside the table add to nothing.
+ *   scratch      warp_embedding_backward_scratch bytes, 16-byte aligned
+ */
+int warp_embedding_backward(const void* dy, int64_t dy_stride, const void* ids, int32_t id_bytes, int64_t tokens,
+                            int64_t vocabulary, int32_t cols, int32_t dtype, float scale, void* dtable,
+                            int64_t dtable_stride, void* scratch, int64_t scratch_bytes, void* hip_stream);
+/* Host-only: bytes of scratch that the call above needs for these sizes (WARP_EINVAL for bad ones). */
+int warp_embedding_backward_scratch(int64_t tokens, int64_t vocabulary, int32_t cols, int64_t* bytes);
+
+/*
+ * Softmax cross entropy of token rows over a vocabulary whose rows are a table's; the logits are not kept:
+ *   l[t][v] = scale * hidden[t] . table[v],  lse[t] = log(sum over v of exp(l[t][v])),  loss[t] = lse[t] - l[t][target]
+ * A row with a negative target is left out: loss and lse are 0, whatever it holds. One whose target is `vocabulary` or
+ * more has NaN for both. Rows left out cost next to nothing.
+ *   targets      [tokens] whole numbers of target_bytes (4 or 8)
+ *   loss, lse    [tokens] fp32
+ *   scratch      warp_cross_entropy_scratch's `bytes`, 16-byte aligned
+ * float32 products are made of 16-bit ones that keep all digits; what an infinity enters may be NaN.
+ * At most 2^22 tokens, a vocabulary of 2^25 and 2^14 columns (above: WARP_ENOTSUP).
+ */
+int warp_cross_entropy(const void* hidden, int64_t hidden_stride, int64_t tokens, int32_t cols, int32_t dtype,
+                       const void* table, int64_t table_stride, int64_t vocabulary, const void* targets,
+                       int32_t target_bytes, float scale, float* loss, float* lse, void* scratch, int64_t scratch_bytes,
+                       void* hip_stream);
+/*
+ * Its backward pass for the gradient dloss of loss, with G[t][v] = dloss[t] * (exp(l[t][v] - lse[t]) - [v = target]):
+ *   dhidden[t] = scale * sum over v of G[t][v] table[v],  dtable[v] = scale * sum over t of G[t][v] hidden[t]
+ * For 16-bit types G, relative to the largest |dloss|, is rounded to dtype before the products. Rows that were left out
+ * have zeros in dhidden (NaN where the target is outside the vocabulary) and add to nothing, whatever dloss has there.
+ * Sums have an order that the sizes and the number of rows with a target fix.
+ *   loss, lse          [tokens] as warp_cross_entropy gave them
+ *   dhidden, dtable    like hidden and table; either may be NULL
+ *   scratch            warp_cross_entropy_scratch's `backward_bytes`, 16-byte aligned
+ */
+int warp_cross_entropy_backward(const float* dloss, const void* hidden, int64_t hidden_stride, int64_t tokens, int32_t cols,
+                                int32_t dtype, const void* table, int64_t table_stride, int64_t vocabulary,
+                                const void* targets, int32_t target_bytes, float scale, const float* loss,
+                                const float* lse, void* dhidden, int64_t dhidden_stride, void* dtable,
+                                int64_t dtable_stride, void* scratch, int64_t scratch_bytes, void* hip_stream);
+/* Host-only: bytes of scratch that the two calls above need (either may be NULL). What they need depends on the table's
+ * alignment: its address is looked at, nothing is read. */
+int warp_cross_entropy_scratch(int64_t tokens, int32_t cols, int32_t dtype, const void* table, int64_t table_stride,
+                               int64_t vocabulary, int64_t* bytes, int64_t* backward_bytes);
+
+/*
+ * A linear layer: y[r][c] = sum_j x[r][j] * weight[c][j] + bias[c].
+ *   weight       [n][cols] of dtype (x's and y's)
+ *   bias         [n] of bias_dtype (WARP_F32 or dtype) or NULL
+ *   scratch      warp_linear_scratch bytes, 16-byte aligned: copies of operands that are not 16-byte aligned rows of whole
+ *                16-byte pieces, or float32, and parts of sums where there are few rows; often none
+ * float32 products are made of 16-bit ones that keep all digits; what an infinity in x or weight enters may be NaN.
+ * WARP_ENOTSUP above 2^24 rows, 2^20 columns or channels, 2^37 elements of x or y or 2^34 of the weight.
+ */
+int warp_linear(const void* x, int64_t x_stride, int64_t rows, int32_t cols, int32_t dtype, const void* weight,
+                int64_t weight_stride, int32_t n, const void* bias, int32_t bias_dtype, void* y, int64_t y_stride,
+                void* scratch, int64_t scratch_bytes, void* hip_stream);
+int warp_linear_scratch(const void* x, int64_t x_stride, int64_t rows, int32_t cols, int32_t dtype, const void* weight,
+                        int64_t weight_stride, int32_t n, int64_t* bytes);
+/*
+ * Its backward pass where x was kept as 8-bit rows (warp_quantize_rows), a quarter or half of its bytes:
+ *   dx = dy weight,  dweight = dy^T (q * q_scale),  dbias = sum over rows of dy
+ * dx does not need x and is that of the unrounded layer; dweight is that of the rounded rows, which are rounded to dtype
+ * once more for the product (float32: not).
+ *   dy                   [rows][n] of dtype
+ *   q, q_scale           [rows] of cols columns as warp_quantize_rows writes them; not read without dweight
+ *   dx, dweight, dbias   [rows][cols], [n][cols] of dtype, [n] of dbias_dtype (WARP_F32 or dtype); each may be NULL
+ *   scratch              warp_linear_backward_scratch bytes, 16-byte aligned
+ * Limits as above.
+ */
+int warp_linear_backward(const void* dy, int64_t dy_stride, int64_t rows, int32_t n, int32_t dtype, const int8_t* q,
+                         int64_t q_stride, const float* q_scale, int32_t cols, const void* weight, int64_t weight_stride,
+                         void* dx, int64_t dx_stride, void* dweight, int64_t dweight_stride, void* dbias,
+                         int32_t dbias_dtype, void* scratch, int64_t scratch_bytes, void* hip_stream);
+int warp_linear_backward_scratch(const void* dy, int64_t dy_stride, int64_t rows, int32_t n, int32_t dtype, int32_t cols,
+                                 const void* weight, int64_t weight_stride, int64_t* bytes);
+
+/*
  * One AdamW step (decoupled weight decay) over many tensors, with t = step (1 and more):
  *   m = beta1 * m + (1 - beta1) * g,  v = beta2 * v + (1 - beta2) * g^2
  *   p = p * (1 - lr * weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)

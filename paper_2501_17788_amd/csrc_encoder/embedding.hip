@@ -1,0 +1,582 @@
+// Rows of a table by token, scaled, and the table's gradient:
+//   out[t] = scale * table[id_t],   dtable[v] = scale * sum over t with id_t = v of dy[t]
+// Both are bound by memory. The gradient's sums have a fixed order, without atomics on floats: tokens are sorted by
+// id (stably, so that a row's tokens come in order), chunks of 64 sorted tokens that belong to one row are summed on
+// their own (a common token has thousands), and each row of the table adds its chunks and what is left over of its
+// tokens. Rows without tokens are written as zeros by the same kernel: the gradient is written once.
+#include "encoder.h"
+
+namespace warp {
+
+namespace {
+
+inline int64_t cover(int64_t n, int64_t of) { return (n + of - 1) / of; }
+
+__device__ __forceinline__ int64_t id_at(const void* ids, bool wide, int64_t t) {
+    return wide ? ((const int64_t*)ids)[t] : (int64_t)((const int32_t*)ids)[t];
+}
+
+// A wave holds NV vectors of V elements of a row's column block, 64 V NV columns. A row's last vector is moved back to
+// end with the row: its first elements are its neighbour's too, and get the same values.
+template <int V>
+struct Columns {
+    int64_t at;
+    bool in;
+};
+template <int V>
+__device__ __forceinline__ Columns<V> column_of(int64_t block, int j, int nv, int lane, int64_t cols) {
+    const int64_t c = ((block * nv + j) * kWave + lane) * V;
+    return {c + V > cols ? cols - V : c, c < cols};
+}
+
+// ---------------------------------------------------------------------------- lookup
+
+struct LookupArgs {
+    const void* ids;
+    bool wide;
+    int64_t tokens, vocabulary;
+    const void* table;
+    int64_t table_stride;
+    int64_t cols;
+    float scale;
+    void* out;
+    int64_t out_stride;
+};
+
+// One wave a token.
+template <typename T, int V, int NV>
+__global__ __launch_bounds__(256) void k_lookup(LookupArgs g) {
+    const int lane = threadIdx.x & 63;
+    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= g.tokens) return;
+    const int64_t id = id_at(g.ids, g.wide, t);
+    const T* row = (const T*)g.table + id * g.table_stride;
+    T* out = (T*)g.out + t * g.out_stride;
+    const float fill = id < 0 ? 0.f : __builtin_nanf("");
+    const bool inside = id >= 0 && id < g.vocabulary;
+    Vec<T, V> x[NV];
+    Columns<V> c[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        c[j] = column_of<V>(blockIdx.y, j, NV, lane, g.cols);
+        if (c[j].in && inside) x[j] = load_vec<T, V>(row + c[j].at);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (!c[j].in) continue;
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[j].e[e] = inside ? (T)((float)x[j].e[e] * g.scale) : (T)fill;
+        store_vec<T, V>(out + c[j].at, x[j]);
+    }
+}
+
+// ---------------------------------------------------------------------------- sorting tokens by id
+
+// Stable radix sort by digits of at most 9 bits. At most 256 tiles of equal size; a tile's eight waves hold neighbouring
+// parts of it.
+constexpr int kDigits = 512, kSortThreads = 512, kSortWaves = kSortThreads / kWave;
+constexpr int kMaxTiles = 256, kTileUnit = 2048;
+constexpr int kSmall = 4096;  // so many tokens are sorted by one workgroup, in LDS
+
+struct SortPlan {
+    int64_t tokens;
+    int64_t tile;  // tokens of a tile
+    int tiles, bits, passes, digit_bits;
+};
+SortPlan sort_plan(int64_t tokens, int64_t vocabulary) {
+    SortPlan p{};
+    p.tokens = tokens;
+    p.tile = cover(cover(tokens > 0 ? tokens : 1, kMaxTiles), kTileUnit) * kTileUnit;
+    p.tiles = (int)cover(tokens, p.tile);
+    while (p.bits < 40 && (vocabulary >> p.bits)) ++p.bits;  // keys up to `vocabulary`, which stands for no row
+    p.passes = (int)cover(p.bits, 9);
+    p.digit_bits = (int)cover(p.bits, p.passes);
+    return p;
+}
+
+__device__ __forceinline__ uint32_t key_of(const void* ids, bool wide, int64_t t, int64_t vocabulary) {
+    const int64_t id = id_at(ids, wide, t);
+    return (uint32_t)(id < 0 || id >= vocabulary ? vocabulary : id);
+}
+
+__device__ __forceinline__ void clear_spans(int2* spans, int64_t vocabulary, int64_t thread, int64_t threads) {
+    for (int64_t v = thread; v < vocabulary; v += threads) spans[v] = make_int2(0, 0);
+}
+
+// Sum of s over the workgroup's threads before this one.
+__device__ __forceinline__ uint32_t sum_before(uint32_t s, uint32_t* waves) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    uint32_t x = s;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    if (lane == 63) waves[w] = x;
+    __syncthreads();
+    uint32_t before = x - s;
+    for (int i = 0; i < w; ++i) before += waves[i];
+    __syncthreads();
+    return before;
+}
+
+// Place of this lane's key among those of its wave with its digit, with next[digit] the first free place; lanes take
+// turns in their order, and next moves on.
+__device__ __forceinline__ uint32_t take_place(uint32_t digit, bool in, int digit_bits, uint32_t* next) {
+    unsigned long long same = __ballot(in);
+    for (int b = 0; b < digit_bits; ++b) {
+        const unsigned long long ones = __ballot(digit >> b & 1u);
+        same &= digit >> b & 1u ? ones : ~ones;
+    }
+    const int lane = threadIdx.x & 63;
+    const uint32_t rank = (uint32_t)__popcll(same & ((1ull << lane) - 1));
+    uint32_t place = 0;
+    if (in) place = next[digit] + rank;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (in && rank == 0) next[digit] = place + (uint32_t)__popcll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    return place;
+}
+
+struct SortArgs {
+    const void* ids;
+    bool wide;
+    int64_t tokens, vocabulary, tile;
+    int tiles, shift, digit_bits;
+    bool first;
+    const uint32_t *keys, *places;
+    uint32_t *keys_out, *places_out;
+    uint32_t* counts;  // [tile][digit]
+    int2* spans;
+};
+
+// Counts of a tile's digits; the first pass also clears the rows' spans.
+__global__ __launch_bounds__(kSortThreads) void k_token_counts(SortArgs g) {
+    __shared__ uint32_t count[kDigits];
+    count[threadIdx.x] = 0;
+    if (g.first)
+        clear_spans(g.spans, g.vocabulary, (int64_t)blockIdx.x * kSortThreads + threadIdx.x,
+                    (int64_t)gridDim.x * kSortThreads);
+    __syncthreads();
+    const int64_t start = (int64_t)blockIdx.x * g.tile;
+    const uint32_t mask = (1u << g.digit_bits) - 1;
+    for (int64_t i = threadIdx.x; i < g.tile && start + i < g.tokens; i += kSortThreads) {
+        const uint32_t key = g.first ? key_of(g.ids, g.wide, start + i, g.vocabulary) : g.keys[start + i];
+        atomicAdd(&count[key >> g.shift & mask], 1u);
+    }
+    __syncthreads();
+    g.counts[(int64_t)blockIdx.x * kDigits + threadIdx.x] = count[threadIdx.x];
+}
+
+// Tokens to their places: a digit's first place in a tile is what all tiles have of smaller digits and the tiles before
+// have of it. Every workgroup adds these up from the table of counts (at most 512 KB, in the L2s).
+__global__ __launch_bounds__(kSortThreads) void k_token_places(SortArgs g) {
+    __shared__ uint32_t next[kSortWaves][kDigits];
+    __shared__ uint32_t waves[kSortWaves];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int64_t start = (int64_t)blockIdx.x * g.tile;
+    const int64_t part = g.tile / kSortWaves;  // a multiple of 64
+    const uint32_t mask = (1u << g.digit_bits) - 1;
+    auto key_at = [&](int64_t t) { return g.first ? key_of(g.ids, g.wide, t, g.vocabulary) : g.keys[t]; };
+#pragma unroll
+    for (int i = 0; i < kSortWaves; ++i) next[i][tid] = 0;
+    __syncthreads();
+    for (int64_t i = lane; i < part; i += 64) {
+        const int64_t t = start + w * part + i;
+        if (t < g.tokens) atomicAdd(&next[w][key_at(t) >> g.shift & mask], 1u);
+    }
+    uint32_t before = 0, all = 0;
+    for (int t = 0; t < g.tiles; ++t) {
+        const uint32_t c = g.counts[(int64_t)t * kDigits + tid];
+        all += c;
+        before += t < (int)blockIdx.x ? c : 0;
+    }
+    uint32_t place = sum_before(all, waves) + before;  // (its barriers also end the counting above)
+#pragma unroll
+    for (int i = 0; i < kSortWaves; ++i) {
+        const uint32_t c = next[i][tid];
+        next[i][tid] = place;
+        place += c;
+    }
+    __syncthreads();
+    for (int64_t i = lane; i < part; i += 64) {
+        const int64_t t = start + w * part + i;
+        const bool in = t < g.tokens;
+        const uint32_t key = in ? key_at(t) : 0;
+        const uint32_t to = take_place(key >> g.shift & mask, in, g.digit_bits, next[w]);
+        if (in) {
+            g.keys_out[to] = key;
+            g.places_out[to] = g.first ? (uint32_t)t : g.places[t];
+        }
+    }
+}
+
+// Few tokens: workgroup 0 sorts them in LDS, in all passes, while the others clear the rows' spans.
+__global__ __launch_bounds__(kSortThreads) void k_sort_few(SortArgs g, int passes) {
+    if (blockIdx.x) {
+        clear_spans(g.spans, g.vocabulary, (int64_t)(blockIdx.x - 1) * kSortThreads + threadIdx.x,
+                    (int64_t)(gridDim.x - 1) * kSortThreads);
+        return;
+    }
+    __shared__ uint32_t next[kSortWaves][kDigits];
+    __shared__ uint32_t waves[kSortWaves];
+    __shared__ uint32_t key[2][kSmall], place[2][kSmall];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = (int)g.tokens;
+    const int part = (n + kSortThreads - 1) / kSortThreads * 64;  // of a wave
+    const uint32_t mask = (1u << g.digit_bits) - 1;
+    for (int i = tid; i < n; i += kSortThreads) key[0][i] = key_of(g.ids, g.wide, i, g.vocabulary), place[0][i] = i;
+    for (int p = 0; p < passes; ++p) {
+        const int from = p & 1, shift = p * g.digit_bits;
+#pragma unroll
+        for (int i = 0; i < kSortWaves; ++i) next[i][tid] = 0;
+        __syncthreads();
+        for (int i = w * part + lane; i < (w + 1) * part; i += 64)
+            if (i < n) atomicAdd(&next[w][key[from][i] >> shift & mask], 1u);
+        __syncthreads();
+        uint32_t all = 0;
+#pragma unroll
+        for (int i = 0; i < kSortWaves; ++i) all += next[i][tid];
+        uint32_t at = sum_before(all, waves);
+#pragma unroll
+        for (int i = 0; i < kSortWaves; ++i) {
+            const uint32_t c = next[i][tid];
+            next[i][tid] = at;
+            at += c;
+        }
+        __syncthreads();
+        for (int i = w * part + lane; i < (w + 1) * part; i += 64) {
+            const bool in = i < n;
+            const uint32_t k = in ? key[from][i] : 0;
+            const uint32_t to = take_place(k >> shift & mask, in, g.digit_bits, next[w]);
+            if (in) key[from ^ 1][to] = k, place[from ^ 1][to] = place[from][i];
+        }
+        __syncthreads();
+    }
+    for (int i = tid; i < n; i += kSortThreads) g.keys_out[i] = key[passes & 1][i], g.places_out[i] = place[passes & 1][i];
+}
+
+// ---------------------------------------------------------------------------- sums
+
+constexpr int kChunk = 64;  // sorted tokens of a chunk
+
+struct SumArgs {
+    const void* dy;
+    int64_t dy_stride;
+    int64_t tokens, vocabulary, cols;
+    const uint32_t *keys, *places;  // sorted
+    int2* spans;                    // of each row, its sorted tokens [x, y)
+    float* chunks;                  // [chunk][chunk_stride]
+    int64_t chunk_stride;
+    float scale;
+    void* out;
+    int64_t out_stride;
+    int64_t heavy;  // workgroups for rows with whole chunks
+};
+
+template <int V, int NV>
+struct Sums {
+    float v[NV][V] = {};
+};
+
+// Adds the rows of dy at sorted places [from, to), up to U of them under way.
+template <typename T, int V, int NV>
+__device__ __forceinline__ void add_rows(Sums<V, NV>& s, const SumArgs& g, int64_t from, int64_t to, int64_t by,
+                                         const Columns<V> (&c)[NV]) {
+    constexpr int U = 4;
+    for (int64_t i = from; i < to; i += U * by) {
+        Vec<T, V> x[U][NV];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = i + u * by;
+            if (at >= to) break;
+            const T* row = (const T*)g.dy + (int64_t)g.places[at] * g.dy_stride;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (c[j].in) x[u][j] = load_vec<T, V>(row + c[j].at);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i + u * by >= to) break;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int e = 0; e < V; ++e) s.v[j][e] += (float)x[u][j].e[e];
+        }
+    }
+}
+
+// One wave a chunk and column block: the chunk's part of the rows' spans, and its sum if all of it is one row's.
+template <typename T, int V, int NV>
+__global__ __launch_bounds__(256) void k_sum_chunks(SumArgs g) {
+    const int lane = threadIdx.x & 63;
+    const int64_t chunk = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t start = chunk * kChunk;
+    if (start >= g.tokens) return;
+    const int64_t i = start + lane;
+    const bool in = i < g.tokens;
+    const uint32_t key = in ? g.keys[i] : ~0u;
+    if (blockIdx.y == 0 && in) {
+        const uint32_t before = i ? g.keys[i - 1] : ~0u;
+        if (key != before) {
+            if (key < g.vocabulary) g.spans[key].x = (int)i;
+            if (before < g.vocabulary) g.spans[before].y = (int)i;
+        }
+        if (i + 1 == g.tokens && key < g.vocabulary) g.spans[key].y = (int)g.tokens;
+    }
+    const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane((int)key);
+    if (__ballot(key == first) != ~0ull || first >= g.vocabulary) return;
+    Columns<V> c[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) c[j] = column_of<V>(blockIdx.y, j, NV, lane, g.cols);
+    Sums<V, NV> s;
+    add_rows<T, V, NV>(s, g, start, start + kChunk, 1, c);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (c[j].in) {
+            Vec<float, V> r;
+#pragma unroll
+            for (int e = 0; e < V; ++e) r.e[e] = s.v[j][e];
+            store_vec<float, V>(g.chunks + chunk * g.chunk_stride + c[j].at, r);
+        }
+}
+
+template <typename T, int V, int NV>
+__device__ __forceinline__ void store_sums(const Sums<V, NV>& s, const SumArgs& g, int64_t row, const Columns<V> (&c)[NV]) {
+    T* out = (T*)g.out + row * g.out_stride;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (c[j].in) {
+            Vec<T, V> r;
+#pragma unroll
+            for (int e = 0; e < V; ++e) r.e[e] = (T)(s.v[j][e] * g.scale);
+            store_vec<T, V>(out + c[j].at, r);
+        }
+}
+
+// The first `heavy` workgroups: one for four chunks; each chunk that is the first whole one of a row stands for it, and
+// the workgroup's waves share the row's terms: tokens before the first whole chunk, chunks, tokens behind the last. The
+// other workgroups: one wave a row that has no whole chunk.
+template <typename T, int V, int NV>
+__global__ __launch_bounds__(256) void k_sum_rows(SumArgs g) {
+    __shared__ float joined[4][NV * V][kWave];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    Columns<V> c[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) c[j] = column_of<V>(blockIdx.y, j, NV, lane, g.cols);
+    auto whole = [&](int2 span, int64_t& from, int64_t& to) {  // whole chunks [from, to)
+        from = (span.x + kChunk - 1) / kChunk, to = span.y / kChunk;
+        return from < to;
+    };
+    int64_t from, to;
+    if ((int64_t)blockIdx.x >= g.heavy) {
+        const int64_t row = ((int64_t)blockIdx.x - g.heavy) * 4 + w;
+        if (row >= g.vocabulary) return;
+        const int2 span = g.spans[row];
+        if (whole(span, from, to)) return;
+        Sums<V, NV> s;
+        add_rows<T, V, NV>(s, g, span.x, span.y, 1, c);
+        store_sums<T, V, NV>(s, g, row, c);
+        return;
+    }
+    for (int u = 0; u < 4; ++u) {
+        const int64_t chunk = (int64_t)blockIdx.x * 4 + u;
+        if ((chunk + 1) * kChunk > g.tokens) return;
+        const uint32_t row = g.keys[chunk * kChunk];
+        if (row >= g.vocabulary) return;  // and all that follow
+        const int2 span = g.spans[row];
+        if (!whole(span, from, to) || from != chunk) continue;
+        Sums<V, NV> s;
+        add_rows<T, V, NV>(s, g, span.x + w, from * kChunk, 4, c);
+        constexpr int U = 4;
+        for (int64_t i = from + w; i < to; i += 4 * U) {
+            Vec<float, V> x[U][NV];
+#pragma unroll
+            for (int n = 0; n < U; ++n) {
+                if (i + 4 * n >= to) break;
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (c[j].in) x[n][j] = load_vec<float, V>(g.chunks + (i + 4 * n) * g.chunk_stride + c[j].at);
+            }
+#pragma unroll
+            for (int n = 0; n < U; ++n) {
+                if (i + 4 * n >= to) break;
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) s.v[j][e] += x[n][j].e[e];
+            }
+        }
+        add_rows<T, V, NV>(s, g, to * kChunk + w, span.y, 4, c);
+        __syncthreads();  // the last row's sums have been read
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) joined[w][j * V + e][lane] = s.v[j][e];
+        __syncthreads();
+        if (w == 0) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    float sum = s.v[j][e];
+#pragma unroll
+                    for (int o = 1; o < 4; ++o) sum += joined[o][j * V + e][lane];
+                    s.v[j][e] = sum;
+                }
+            store_sums<T, V, NV>(s, g, row, c);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------- launches
+
+// A wave's vectors: 16 bytes of a row each, as many as a row has up to four.
+template <typename F>
+void by_columns(int64_t cols, int wide, F f) {
+    const int64_t vectors = cover(cols, (int64_t)wide * kWave);
+    if (cols < wide) f(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, (int64_t)1);
+    else if (vectors <= 1) f(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{}, (int64_t)1);
+    else f(std::integral_constant<int, 0>{}, std::integral_constant<int, 2>{}, cover(vectors, 2));
+}
+
+template <typename T>
+void lookup(const LookupArgs& g, hipStream_t s) {
+    constexpr int W = 16 / sizeof(T);
+    by_columns(g.cols, W, [&](auto narrow, auto nv, int64_t blocks) {
+        constexpr int V = narrow.value ? 1 : W, NV = nv.value;
+        hipLaunchKernelGGL((k_lookup<T, V, NV>), dim3((uint32_t)cover(g.tokens, 4), (uint32_t)blocks), dim3(256), 0, s, g);
+    });
+}
+
+template <typename T>
+void sums(SumArgs g, hipStream_t s) {
+    constexpr int W = 16 / sizeof(T);
+    by_columns(g.cols, W, [&](auto narrow, auto nv, int64_t blocks) {
+        constexpr int V = narrow.value ? 1 : W, NV = nv.value;
+        const int64_t chunks = cover(g.tokens, kChunk);
+        if (g.tokens)
+            hipLaunchKernelGGL((k_sum_chunks<T, V, NV>), dim3((uint32_t)cover(chunks, 4), (uint32_t)blocks), dim3(256), 0, s,
+                               g);
+        g.heavy = cover(g.tokens / kChunk, 4);
+        hipLaunchKernelGGL((k_sum_rows<T, V, NV>), dim3((uint32_t)(g.heavy + cover(g.vocabulary, 4)), (uint32_t)blocks),
+                           dim3(256), 0, s, g);
+    });
+}
+
+struct BackwardScratch {
+    int64_t keys[2], places[2], counts, spans, chunks, bytes;
+};
+BackwardScratch backward_scratch(int64_t tokens, int64_t vocabulary, int64_t cols) {
+    BackwardScratch b{};
+    auto take = [&](int64_t bytes) {
+        const int64_t at = b.bytes;
+        b.bytes += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    for (int i = 0; i < 2; ++i) b.keys[i] = take(tokens * 4), b.places[i] = take(tokens * 4);
+    b.counts = take((int64_t)kMaxTiles * kDigits * 4);
+    b.spans = take(vocabulary * 8);
+    b.chunks = take(tokens / kChunk * cols * 4);
+    return b;
+}
+
+int check_embedding(const char* what, const void* ids, int32_t id_bytes, int64_t tokens, int64_t vocabulary, int64_t cols,
+                    int32_t dtype, float scale) {
+    if (tokens < 0) return fail(WARP_EINVAL, "%s: tokens must be >= 0 (got %lld)", what, (long long)tokens);
+    if (vocabulary < 1) return fail(WARP_EINVAL, "%s: vocabulary must be >= 1 (got %lld)", what, (long long)vocabulary);
+    if (cols < 1) return fail(WARP_EINVAL, "%s: cols must be >= 1 (got %lld)", what, (long long)cols);
+    if (tokens > 1 << 25 || vocabulary > 1 << 25 || cols > 1 << 20)
+        return fail(WARP_ENOTSUP, "%s: at most 2^25 tokens, 2^25 table rows and 2^20 columns (got %lld, %lld, %lld)", what,
+                    (long long)tokens, (long long)vocabulary, (long long)cols);
+    if (id_bytes != 4 && id_bytes != 8) return fail(WARP_EINVAL, "%s: ids of 4 or 8 bytes (got %d)", what, id_bytes);
+    if (!dtype_ok(dtype)) return fail(WARP_EINVAL, "%s: unknown dtype %d", what, dtype);
+    if (!(scale - scale == 0.f)) return fail(WARP_EINVAL, "%s: scale must be finite", what);
+    if (tokens && !ids) return fail(WARP_EINVAL, "%s: null pointer", what);
+    if ((uintptr_t)ids % id_bytes) return fail(WARP_EINVAL, "%s: misaligned pointer", what);
+    return WARP_OK;
+}
+int check_matrix(const char* what, const void* p, int64_t stride, int64_t rows, int64_t cols, int32_t dtype) {
+    if (rows && !p) return fail(WARP_EINVAL, "%s: null pointer", what);
+    if ((uintptr_t)p % dtype_bytes(dtype)) return fail(WARP_EINVAL, "%s: misaligned pointer", what);
+    if (rows > 1 && stride < cols)
+        return fail(WARP_EINVAL, "%s: a row stride of %lld is below %lld columns", what, (long long)stride, (long long)cols);
+    return WARP_OK;
+}
+
+}  // namespace
+
+}  // namespace warp
+
+using namespace warp;
+
+extern "C" {
+
+int warp_embedding(const void* ids, int32_t id_bytes, int64_t tokens, const void* table, int64_t table_stride,
+                   int64_t vocabulary, int32_t cols, int32_t dtype, float scale, void* out, int64_t out_stride,
+                   void* hip_stream) {
+    const char* what = "embedding";
+    int rc = check_embedding(what, ids, id_bytes, tokens, vocabulary, cols, dtype, scale);
+    if (!rc) rc = check_matrix(what, table, table_stride, vocabulary, cols, dtype);
+    if (!rc) rc = check_matrix(what, out, out_stride, tokens, cols, dtype);
+    if (!rc) rc = require_device();
+    if (rc || !tokens) return rc;
+    const LookupArgs g{ids, id_bytes == 8, tokens, vocabulary, table, table_stride, cols, scale, out, out_stride};
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (dtype == WARP_F32) WARP_LAUNCH(lookup<float>(g, s));
+    else if (dtype == WARP_F16) WARP_LAUNCH(lookup<_Float16>(g, s));
+    else WARP_LAUNCH(lookup<__bf16>(g, s));
+    return WARP_OK;
+}
+
+int warp_embedding_backward_scratch(int64_t tokens, int64_t vocabulary, int32_t cols, int64_t* bytes) {
+    if (!bytes || tokens < 0 || vocabulary < 1 || cols < 1) return fail(WARP_EINVAL, "embedding backward: bad sizes");
+    *bytes = backward_scratch(tokens, vocabulary, cols).bytes;
+    return WARP_OK;
+}
+
+int warp_embedding_backward(const void* dy, int64_t dy_stride, const void* ids, int32_t id_bytes, int64_t tokens,
+                            int64_t vocabulary, int32_t cols, int32_t dtype, float scale, void* dtable,
+                            int64_t dtable_stride, void* scratch, int64_t scratch_bytes, void* hip_stream) {
+    const char* what = "embedding backward";
+    int rc = check_embedding(what, ids, id_bytes, tokens, vocabulary, cols, dtype, scale);
+    if (!rc) rc = check_matrix(what, dy, dy_stride, tokens, cols, dtype);
+    if (!rc) rc = check_matrix(what, dtable, dtable_stride, vocabulary, cols, dtype);
+    if (rc) return rc;
+    const BackwardScratch b = backward_scratch(tokens, vocabulary, cols);
+    if (!scratch || scratch_bytes < b.bytes || (uintptr_t)scratch % 16)
+        return fail(WARP_EINVAL, "%s: needs %lld bytes of scratch, 16-byte aligned (got %lld)", what, (long long)b.bytes,
+                    (long long)(scratch ? scratch_bytes : 0));
+    rc = require_device();
+    if (rc) return rc;
+    hipStream_t s = (hipStream_t)hip_stream;
+    uint8_t* base = (uint8_t*)scratch;
+    uint32_t *keys[2], *places[2];
+    for (int i = 0; i < 2; ++i) keys[i] = (uint32_t*)(base + b.keys[i]), places[i] = (uint32_t*)(base + b.places[i]);
+    const SortPlan p = sort_plan(tokens, vocabulary);
+    SortArgs a{ids, id_bytes == 8, tokens, vocabulary, p.tile, p.tiles, 0, p.digit_bits, true, nullptr, nullptr, keys[0],
+               places[0], (uint32_t*)(base + b.counts), (int2*)(base + b.spans)};
+    int sorted = 0;
+    if (tokens <= kSmall) {
+        const int clear = (int)(cover(vocabulary, 8 * kSortThreads) < 255 ? cover(vocabulary, 8 * kSortThreads) : 255);
+        WARP_LAUNCH(hipLaunchKernelGGL(k_sort_few, dim3(1 + clear), dim3(kSortThreads), 0, s, a, p.passes));
+    } else {
+        for (int i = 0; i < p.passes; ++i) {
+            a.shift = i * p.digit_bits, a.first = i == 0;
+            a.keys = keys[(i + 1) & 1], a.places = places[(i + 1) & 1];
+            a.keys_out = keys[i & 1], a.places_out = places[i & 1];
+            WARP_LAUNCH(hipLaunchKernelGGL(k_token_counts, dim3(p.tiles), dim3(kSortThreads), 0, s, a));
+            WARP_LAUNCH(hipLaunchKernelGGL(k_token_places, dim3(p.tiles), dim3(kSortThreads), 0, s, a));
+        }
+        sorted = (p.passes - 1) & 1;
+    }
+    const SumArgs g{dy, dy_stride, tokens, vocabulary, cols, keys[sorted], places[sorted], a.spans,
+                    (float*)(base + b.chunks), cols, scale, dtable, dtable_stride, 0};
+    if (dtype == WARP_F32) WARP_LAUNCH(sums<float>(g, s));
+    else if (dtype == WARP_F16) WARP_LAUNCH(sums<_Float16>(g, s));
+    else WARP_LAUNCH(sums<__bf16>(g, s));
+    return WARP_OK;
+}
+
+}  // extern "C"

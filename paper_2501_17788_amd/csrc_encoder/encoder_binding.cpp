@@ -198,6 +198,191 @@ Tensor linear_int8(const Tensor& av, const Tensor& sa, int64_t cols, const Tenso
     return out;
 }
 
+template <typename... T>
+bool followed(const T&... tensors) {
+    return at::GradMode::is_enabled() && (tracked(tensors) || ...);
+}
+py::object node(const char* name) {  // of autograd; it calls back with gradients off
+    return py::module_::import("paper_2501_17788_amd.encoder").attr(name).attr("apply");
+}
+
+Tensor scratch_of(const Tensor& like, int64_t bytes) { return at::empty({bytes}, like.options().dtype(at::kByte)); }
+
+// Whole numbers, one for each row, in one piece.
+Tensor whole_numbers(const Tensor& t, const char* name) {
+    if (t.scalar_type() != at::kLong && t.scalar_type() != at::kInt)
+        refuse(name, " must be int64 or int32, got ", t.scalar_type());
+    return t.contiguous();
+}
+int32_t bytes_of(const Tensor& t) { return (int32_t)t.element_size(); }
+
+Rows matrix_of(const Tensor& t, const char* name, int64_t cols) {
+    if (t.dim() != 2) refuse(name, " must have two dimensions, got ", t.sizes());
+    if (cols >= 0 && t.size(1) != cols) refuse(name, " has rows of ", t.size(1), " columns, ", cols, " are needed");
+    return rows_of(t, name);
+}
+
+void same_type(const Tensor& a, const Tensor& b, const char* name, const char* other) {
+    if (a.scalar_type() != b.scalar_type()) refuse(name, " must be of ", other, "'s type ", b.scalar_type(), ", got ", a.scalar_type());
+}
+
+// leading sizes followed by one more
+std::vector<int64_t> with_last(at::IntArrayRef lead, int64_t last) {
+    std::vector<int64_t> s(lead.begin(), lead.end());
+    s.push_back(last);
+    return s;
+}
+
+Tensor embedding(const Tensor& ids, const Tensor& table, double scale) {
+    on_device(table);
+    on_device(table, ids);
+    if (followed(table))
+        return node("_Embedding")(ids, table, scale).cast<Tensor>();
+    const c10::DeviceGuard guard(table.device());
+    const Rows t = matrix_of(table, "table", -1);
+    const Tensor i = whole_numbers(ids, "ids");
+    Tensor out = at::empty(with_last(ids.sizes(), t.cols), table.options());
+    check(warp_embedding(i.const_data_ptr(), bytes_of(i), i.numel(), t.t.const_data_ptr(), t.stride, t.rows, t.cols,
+                         code(table.scalar_type()), (float)scale, out.data_ptr(), t.cols, stream_of(table)));
+    return out;
+}
+
+Tensor embedding_backward(const Tensor& dy, const Tensor& ids, int64_t vocabulary, double scale) {
+    on_device(dy);
+    on_device(dy, ids);
+    if (dy.dim() < 1 || dy.sizes().slice(0, dy.dim() - 1) != ids.sizes())
+        refuse("dy must have a row for each of the ids ", ids.sizes(), ", got ", dy.sizes());
+    const c10::DeviceGuard guard(dy.device());
+    const Rows d = rows_of(dy, "dy");
+    const Tensor i = whole_numbers(ids, "ids");
+    int64_t need = 0;
+    check(warp_embedding_backward_scratch(i.numel(), vocabulary, d.cols, &need));
+    Tensor out = at::empty({vocabulary, d.cols}, dy.options()), scratch = scratch_of(dy, need);
+    check(warp_embedding_backward(d.t.const_data_ptr(), d.stride, i.const_data_ptr(), bytes_of(i), i.numel(), vocabulary,
+                                  d.cols, code(dy.scalar_type()), (float)scale, out.data_ptr(), d.cols, scratch.data_ptr(),
+                                  need, stream_of(dy)));
+    return out;
+}
+
+// hidden rows, table and targets that fit
+struct Scores {
+    Rows h, t;
+    Tensor y;
+    Scores(const Tensor& hidden, const Tensor& table, const Tensor& targets)
+        : h(rows_of(hidden, "hidden")), t(matrix_of(table, "table", h.cols)), y(whole_numbers(targets, "targets")) {
+        same_type(table, hidden, "table", "hidden");
+        if (hidden.sizes().slice(0, hidden.dim() - 1) != targets.sizes())
+            refuse("targets must have a number for each row of hidden ", hidden.sizes(), ", got ", targets.sizes());
+    }
+};
+
+py::tuple cross_entropy(const Tensor& hidden, const Tensor& table, const Tensor& targets, double scale) {
+    on_device(hidden);
+    on_device(hidden, table);
+    on_device(hidden, targets);
+    if (followed(hidden, table))
+        return node("_CrossEntropy")(hidden, table, targets, scale);
+    const c10::DeviceGuard guard(hidden.device());
+    const Scores s(hidden, table, targets);
+    const int32_t type = code(hidden.scalar_type());
+    int64_t need = 0;
+    check(warp_cross_entropy_scratch(s.h.rows, s.h.cols, type, s.t.t.const_data_ptr(), s.t.stride, s.t.rows, &need, nullptr));
+    const auto f32 = hidden.options().dtype(at::kFloat);
+    Tensor loss = at::empty(targets.sizes(), f32), lse = at::empty(targets.sizes(), f32), scratch = scratch_of(hidden, need);
+    check(warp_cross_entropy(s.h.t.const_data_ptr(), s.h.stride, s.h.rows, s.h.cols, type, s.t.t.const_data_ptr(), s.t.stride,
+                             s.t.rows, s.y.const_data_ptr(), bytes_of(s.y), (float)scale, loss.data_ptr<float>(),
+                             lse.data_ptr<float>(), scratch.data_ptr(), need, stream_of(hidden)));
+    return py::make_tuple(loss, lse);
+}
+
+py::tuple cross_entropy_backward(const Tensor& dloss, const Tensor& hidden, const Tensor& table, const Tensor& targets,
+                                 const Tensor& loss, const Tensor& lse, double scale, bool want_hidden, bool want_table) {
+    on_device(hidden);
+    for (const Tensor* t : {&dloss, &table, &targets, &loss, &lse}) on_device(hidden, *t);
+    const c10::DeviceGuard guard(hidden.device());
+    const Scores s(hidden, table, targets);
+    for (const Tensor* t : {&dloss, &loss, &lse})
+        if (t->sizes() != targets.sizes() || t->scalar_type() != at::kFloat)
+            refuse(t == &dloss ? "dloss" : t == &loss ? "loss" : "lse", " must be float32 ", targets.sizes(), ", got ",
+                   t->scalar_type(), " ", t->sizes());
+    const int32_t type = code(hidden.scalar_type());
+    int64_t need = 0;
+    check(warp_cross_entropy_scratch(s.h.rows, s.h.cols, type, s.t.t.const_data_ptr(), s.t.stride, s.t.rows, nullptr, &need));
+    const Tensor g = dloss.contiguous(), l = loss.contiguous(), e = lse.contiguous();
+    MaybeTensor dh, dt;
+    if (want_hidden) dh = at::empty(hidden.sizes(), hidden.options());
+    if (want_table) dt = at::empty({s.t.rows, s.t.cols}, table.options());
+    Tensor scratch = scratch_of(hidden, need);
+    check(warp_cross_entropy_backward(g.const_data_ptr<float>(), s.h.t.const_data_ptr(), s.h.stride, s.h.rows, s.h.cols, type,
+                                      s.t.t.const_data_ptr(), s.t.stride, s.t.rows, s.y.const_data_ptr(), bytes_of(s.y),
+                                      (float)scale, l.const_data_ptr<float>(), e.const_data_ptr<float>(),
+                                      dh ? dh->data_ptr() : nullptr, s.h.cols, dt ? dt->data_ptr() : nullptr, s.h.cols,
+                                      scratch.data_ptr(), need, stream_of(hidden)));
+    return py::make_tuple(dh, dt);
+}
+
+Tensor linear(const Tensor& x, const Tensor& weight, const MaybeTensor& bias, const py::object& rows) {
+    on_device(x);
+    on_device(x, weight);
+    on_device(x, bias);
+    if (followed(x, weight, bias))
+        return node("_Linear")(x, weight, bias, rows).cast<Tensor>();
+    const c10::DeviceGuard guard(x.device());
+    const Rows r = rows_of(x, "x"), w = matrix_of(weight, "weight", r.cols);
+    same_type(weight, x, "weight", "x");
+    if (w.rows < 1 || w.rows > INT32_MAX) refuse("a weight of ", w.rows, " channels");
+    if (bias && (bias->dim() != 1 || bias->size(0) != w.rows ||
+                 (bias->scalar_type() != at::kFloat && bias->scalar_type() != x.scalar_type())))
+        refuse("bias must be float32 or ", x.scalar_type(), " (", w.rows, ",), got ", bias->scalar_type(), " ", bias->sizes());
+    const int32_t type = code(x.scalar_type());
+    int64_t need = 0;
+    check(warp_linear_scratch(r.t.const_data_ptr(), r.stride, r.rows, r.cols, type, w.t.const_data_ptr(), w.stride,
+                              (int32_t)w.rows, &need));
+    const MaybeTensor b = bias ? MaybeTensor(bias->contiguous()) : std::nullopt;
+    Tensor y = at::empty(with_last(x.sizes().slice(0, x.dim() - 1), w.rows), x.options()), scratch;
+    if (need) scratch = scratch_of(x, need);
+    check(warp_linear(r.t.const_data_ptr(), r.stride, r.rows, r.cols, type, w.t.const_data_ptr(), w.stride, (int32_t)w.rows,
+                      ptr(b), bias ? code(bias->scalar_type()) : WARP_F32, y.data_ptr(), w.rows,
+                      need ? scratch.data_ptr() : nullptr, need, stream_of(x)));
+    return y;
+}
+
+// dy [..., n] for the rows `values * scale` and the weight [n, cols]
+py::tuple linear_backward(const Tensor& dy, const MaybeTensor& values, const MaybeTensor& scale, const Tensor& weight,
+                          bool want_x, bool want_weight, bool want_bias, at::ScalarType bias_type) {
+    on_device(dy);
+    on_device(dy, weight);
+    on_device(dy, values);
+    on_device(dy, scale);
+    const c10::DeviceGuard guard(dy.device());
+    const Rows d = rows_of(dy, "dy"), w = matrix_of(weight, "weight", -1);
+    same_type(weight, dy, "weight", "dy");
+    if (d.cols != w.rows) refuse("dy has rows of ", d.cols, " columns for a weight of ", w.rows, " channels");
+    if (want_weight) {
+        check_int8("rows", *values, *scale, ((int64_t)w.cols + kPad - 1) / kPad * kPad);
+        if (values->size(0) != d.rows) refuse(values->size(0), " rows in 8 bits for ", d.rows, " of dy");
+    }
+    if (bias_type != at::kFloat && bias_type != dy.scalar_type())
+        refuse("dbias must be float32 or ", dy.scalar_type(), ", got ", bias_type);
+    const int32_t type = code(dy.scalar_type());
+    int64_t need = 0;
+    check(warp_linear_backward_scratch(d.t.const_data_ptr(), d.stride, d.rows, d.cols, type, w.cols, w.t.const_data_ptr(),
+                                       w.stride, &need));
+    MaybeTensor dx, dw, db;
+    if (want_x) dx = at::empty(with_last(dy.sizes().slice(0, dy.dim() - 1), w.cols), dy.options());
+    if (want_weight) dw = at::empty({w.rows, w.cols}, weight.options());
+    if (want_bias) db = at::empty({w.rows}, dy.options().dtype(bias_type));
+    Tensor scratch;
+    if (need) scratch = scratch_of(dy, need);
+    check(warp_linear_backward(d.t.const_data_ptr(), d.stride, d.rows, d.cols, type,
+                               want_weight ? (const int8_t*)values->const_data_ptr() : nullptr,
+                               want_weight ? values->stride(0) : 0, want_weight ? scale->const_data_ptr<float>() : nullptr,
+                               w.cols, w.t.const_data_ptr(), w.stride, dx ? dx->data_ptr() : nullptr, w.cols,
+                               dw ? dw->data_ptr() : nullptr, w.cols, db ? db->data_ptr() : nullptr, code(bias_type),
+                               need ? scratch.data_ptr() : nullptr, need, stream_of(dy)));
+    return py::make_tuple(dx, dw, db);
+}
+
 // The optimizer's records (warp_adamw_tensor) in a buffer that it owns, held for one call.
 struct Records {
     Py_buffer view;
@@ -299,6 +484,12 @@ PYBIND11_MODULE(_encoder, mod) {
     mod.def("quantize_rows", &quantize_rows);
     mod.def("layer_norm_int8", &layer_norm_int8);
     mod.def("linear_int8", &linear_int8);
+    mod.def("embedding", &embedding);
+    mod.def("embedding_backward", &embedding_backward);
+    mod.def("cross_entropy", &cross_entropy);
+    mod.def("cross_entropy_backward", &cross_entropy_backward);
+    mod.def("linear", &linear);
+    mod.def("linear_backward", &linear_backward);
     mod.def("adamw_step", &adamw_step);
     mod.def("adamw_moments", &adamw_moments);
 }

@@ -1,0 +1,207 @@
+// A linear layer for training that keeps its input in 8-bit rows:
+//   y = x W^T + b;  dx = dy W,  dW = dy^T (q * s),  db = sum of dy's rows
+// Bound by the matrix cores where the sizes are large; every product reads its operands as they are stored.
+#include "operands.h"
+
+namespace warp {
+
+namespace {
+
+int check_sizes(const char* what, int64_t rows, int32_t cols, int32_t n, int32_t dtype) {
+    if (rows < 0) return fail(WARP_EINVAL, "%s: rows must be >= 0 (got %lld)", what, (long long)rows);
+    if (n < 1 || cols < 1) return fail(WARP_EINVAL, "%s: n and cols must be >= 1 (got %d, %d)", what, n, cols);
+    if (rows > 1 << 24 || n > 1 << 20 || cols > 1 << 20 || (int64_t)n * cols > 1ll << 34 || rows * n > 1ll << 37 ||
+        rows * cols > 1ll << 37)
+        return fail(WARP_ENOTSUP, "%s: at most 2^24 rows, 2^20 columns and channels, and matrices of 2^37 elements (got "
+                    "%lld, %d, %d)", what, (long long)rows, cols, n);
+    if (!dtype_ok(dtype)) return fail(WARP_EINVAL, "%s: unknown dtype %d", what, dtype);
+    return WARP_OK;
+}
+int check_matrix(const char* what, const void* p, int64_t stride, int64_t rows, int64_t cols, int32_t dtype) {
+    if (rows && !p) return fail(WARP_EINVAL, "%s: null pointer", what);
+    if ((uintptr_t)p % dtype_bytes(dtype)) return fail(WARP_EINVAL, "%s: misaligned pointer", what);
+    if (rows > 1 && stride < cols)
+        return fail(WARP_EINVAL, "%s: a row stride of %lld is below %lld columns", what, (long long)stride, (long long)cols);
+    return WARP_OK;
+}
+int check_scratch(const char* what, const void* scratch, int64_t bytes, int64_t need) {
+    if (need && (!scratch || bytes < need || (uintptr_t)scratch % 16))
+        return fail(WARP_EINVAL, "%s: needs %lld bytes of scratch, 16-byte aligned (got %lld)", what, (long long)need,
+                    (long long)(scratch ? bytes : 0));
+    return WARP_OK;
+}
+
+// A product whose k range may be split: in one launch, or in parts that are joined.
+struct Product {
+    Tile tile;
+    int splits;
+    int64_t floats;
+};
+Product plan_product(int64_t m, int64_t n, int64_t k, int32_t dtype) {
+    const int64_t steps = product_steps(k, terms_of(dtype));
+    const Tile whole = whole_tile(m, n), split = split_tile(m, n, steps);
+    const int s = product_splits(m, n, steps, tile_size(split), kMaxSplits, tile_jobs(split));
+    if (s < 2 || steps < 16) return {whole, 1, 0};
+    return {split, s, part_floats(m, n, k, terms_of(dtype), split, kMaxSplits, tile_jobs(split))};
+}
+
+typedef hipError_t (*ProductCall)(const ProductArgs&, int, Tile, Finish, hipStream_t);
+
+hipError_t run_product(ProductCall call, ProductArgs g, const Product& plan, float* part, int32_t dtype, hipStream_t s) {
+    g.terms = terms_of(dtype);
+    g.splits = kMaxSplits, g.jobs = tile_jobs(plan.tile);
+    g.part = part, g.part_stride = cover_of(g.n, 4) * 4;
+    if (plan.splits == 1) return call(g, element_of(dtype), plan.tile, kStore, s);
+    const hipError_t e = call(g, element_of(dtype), plan.tile, kSum, s);
+    if (e) return e;
+    const Join j{part, g.part_stride, g.m, g.n, g.k, nullptr, nullptr, g.terms, g.splits, g.jobs, tile_size(plan.tile),
+                 nullptr, nullptr, g.m, g.out, g.out_stride, g.out_type, g.bias, g.bias_type};
+    return join_parts(j, s);
+}
+
+ProductArgs product_args(const Operand& a, const Operand& b, int64_t m, int64_t n, int64_t k, void* out, int64_t out_stride,
+                         int32_t out_type) {
+    ProductArgs g{};
+    g.a = a.p, g.a_stride = a.stride, g.a_plane = a.plane;
+    g.b = b.p, g.b_stride = b.stride, g.b_plane = b.plane;
+    g.m = m, g.n = n, g.k = k;
+    g.out = out, g.out_stride = out_stride, g.out_type = out_type;
+    return g;
+}
+
+struct Forward {
+    Space space;
+    uint16_t *x, *w;
+    float* part;
+    Product y;
+    Forward(void* base, const void* x_, int64_t x_stride, int64_t rows, int64_t cols, int32_t dtype, const void* w_,
+            int64_t w_stride, int64_t n) {
+        space.base = (uint8_t*)base;
+        y = plan_product(rows, n, cols, dtype);
+        x = space.take<uint16_t>(direct(x_, x_stride, rows, cols, dtype) ? 0 : packed_elements(rows, cols, dtype));
+        w = space.take<uint16_t>(direct(w_, w_stride, n, cols, dtype) ? 0 : packed_elements(n, cols, dtype));
+        part = space.take<float>(y.floats);
+    }
+};
+
+struct Backward {
+    Space space;
+    uint16_t *dy, *x, *w;
+    float *part, *room;
+    Product dx, dw;
+    Backward(void* base, const void* dy_, int64_t dy_stride, int64_t rows, int64_t cols, int32_t dtype, const void* w_,
+             int64_t w_stride, int64_t n) {
+        space.base = (uint8_t*)base;
+        dx = plan_product(rows, cols, n, dtype), dw = plan_product(n, cols, rows, dtype);
+        dy = space.take<uint16_t>(direct(dy_, dy_stride, rows, n, dtype) ? 0 : packed_elements(rows, n, dtype));
+        w = space.take<uint16_t>(direct(w_, w_stride, n, cols, dtype) ? 0 : packed_elements(n, cols, dtype));
+        x = space.take<uint16_t>(packed_elements(rows, cols, dtype));
+        part = space.take<float>(dx.floats > dw.floats ? dx.floats : dw.floats);
+        room = space.take<float>(column_room(rows, n));
+    }
+};
+
+#define WARP_STEP(...)                                                                                       \
+    do {                                                                                                     \
+        const hipError_t e_ = (__VA_ARGS__);                                                                 \
+        if (e_ != hipSuccess) return fail(WARP_EDEVICE, "%s: launch failed: %s", what, hipGetErrorString(e_)); \
+    } while (0)
+
+}  // namespace
+
+}  // namespace warp
+
+using namespace warp;
+
+extern "C" {
+
+int warp_linear_scratch(const void* x, int64_t x_stride, int64_t rows, int32_t cols, int32_t dtype, const void* weight,
+                        int64_t weight_stride, int32_t n, int64_t* bytes) {
+    const char* what = "linear";
+    if (!bytes) return fail(WARP_EINVAL, "%s: null pointer", what);
+    if (const int rc = check_sizes(what, rows, cols, n, dtype)) return rc;
+    *bytes = Forward(nullptr, x, x_stride, rows, cols, dtype, weight, weight_stride, n).space.used;
+    return WARP_OK;
+}
+
+int warp_linear(const void* x, int64_t x_stride, int64_t rows, int32_t cols, int32_t dtype, const void* weight,
+                int64_t weight_stride, int32_t n, const void* bias, int32_t bias_dtype, void* y, int64_t y_stride,
+                void* scratch, int64_t scratch_bytes, void* hip_stream) {
+    const char* what = "linear";
+    int rc = check_sizes(what, rows, cols, n, dtype);
+    if (!rc) rc = check_matrix(what, x, x_stride, rows, cols, dtype);
+    if (!rc) rc = check_matrix(what, weight, weight_stride, n, cols, dtype);
+    if (!rc) rc = check_matrix(what, y, y_stride, rows, n, dtype);
+    if (rc) return rc;
+    if (bias && bias_dtype != WARP_F32 && bias_dtype != dtype)
+        return fail(WARP_EINVAL, "%s: bias must be float32 or of x's type", what);
+    if (bias && (uintptr_t)bias % dtype_bytes(bias_dtype)) return fail(WARP_EINVAL, "%s: misaligned pointer", what);
+    const Forward f(scratch, x, x_stride, rows, cols, dtype, weight, weight_stride, n);
+    rc = check_scratch(what, scratch, scratch_bytes, f.space.used);
+    if (!rc) rc = require_device();
+    if (rc || !rows) return rc;
+    hipStream_t s = (hipStream_t)hip_stream;
+    hipError_t e = hipSuccess;
+    const Operand a = operand_of(x, x_stride, rows, cols, dtype, f.x, s, &e);
+    const Operand b = operand_of(weight, weight_stride, n, cols, dtype, f.w, s, &e);
+    WARP_STEP(e);
+    ProductArgs g = product_args(a, b, rows, n, cols, y, y_stride, dtype);
+    g.bias = bias, g.bias_type = bias_dtype;
+    WARP_STEP(run_product(product_along, g, f.y, f.part, dtype, s));
+    return WARP_OK;
+}
+
+int warp_linear_backward_scratch(const void* dy, int64_t dy_stride, int64_t rows, int32_t n, int32_t dtype, int32_t cols,
+                                 const void* weight, int64_t weight_stride, int64_t* bytes) {
+    const char* what = "linear backward";
+    if (!bytes) return fail(WARP_EINVAL, "%s: null pointer", what);
+    if (const int rc = check_sizes(what, rows, cols, n, dtype)) return rc;
+    *bytes = Backward(nullptr, dy, dy_stride, rows, cols, dtype, weight, weight_stride, n).space.used;
+    return WARP_OK;
+}
+
+int warp_linear_backward(const void* dy, int64_t dy_stride, int64_t rows, int32_t n, int32_t dtype, const int8_t* q,
+                         int64_t q_stride, const float* q_scale, int32_t cols, const void* weight, int64_t weight_stride,
+                         void* dx, int64_t dx_stride, void* dweight, int64_t dweight_stride, void* dbias, int32_t dbias_dtype,
+                         void* scratch, int64_t scratch_bytes, void* hip_stream) {
+    const char* what = "linear backward";
+    int rc = check_sizes(what, rows, cols, n, dtype);
+    if (!rc) rc = check_matrix(what, dy, dy_stride, rows, n, dtype);
+    if (!rc) rc = check_matrix(what, weight, weight_stride, n, cols, dtype);
+    if (!rc && dx) rc = check_matrix(what, dx, dx_stride, rows, cols, dtype);
+    if (!rc && dweight) rc = check_matrix(what, dweight, dweight_stride, n, cols, dtype);
+    if (rc) return rc;
+    if (dweight && rows) {
+        if (!q || !q_scale) return fail(WARP_EINVAL, "%s: null pointer", what);
+        if (q_stride < (cols + kInt8Pad - 1) / kInt8Pad * kInt8Pad || q_stride % 16 || (uintptr_t)q % 16 ||
+            (uintptr_t)q_scale % 4)
+            return fail(WARP_EINVAL, "%s: int8 rows need 16-byte alignment and a stride that is a multiple of 16 and at least "
+                        "%d (got %lld)", what, (cols + kInt8Pad - 1) / kInt8Pad * kInt8Pad, (long long)q_stride);
+    }
+    if (dbias && dbias_dtype != WARP_F32 && dbias_dtype != dtype)
+        return fail(WARP_EINVAL, "%s: dbias must be float32 or of dy's type", what);
+    if (dbias && (uintptr_t)dbias % dtype_bytes(dbias_dtype)) return fail(WARP_EINVAL, "%s: misaligned pointer", what);
+    const Backward w(scratch, dy, dy_stride, rows, cols, dtype, weight, weight_stride, n);
+    rc = check_scratch(what, scratch, scratch_bytes, w.space.used);
+    if (!rc) rc = require_device();
+    if (rc) return rc;
+    hipStream_t s = (hipStream_t)hip_stream;
+    hipError_t e = hipSuccess;
+    Operand d{}, t{};
+    if (rows && (dx || dweight)) d = operand_of(dy, dy_stride, rows, n, dtype, w.dy, s, &e);
+    if (rows && dx) {
+        t = operand_of(weight, weight_stride, n, cols, dtype, w.w, s, &e);
+        WARP_STEP(e);
+        WARP_STEP(run_product(product_mixed, product_args(d, t, rows, cols, n, dx, dx_stride, dtype), w.dx, w.part, dtype, s));
+    }
+    if (dweight) {  // without rows: zeros
+        WARP_STEP(unpack_int8(q, q_stride, q_scale, rows, cols, dtype, w.x, s));
+        const Operand x{w.x, packed_width(cols), rows * packed_width(cols)};
+        WARP_STEP(run_product(product_across, product_args(d, x, n, cols, rows, dweight, dweight_stride, dtype), w.dw, w.part,
+                              dtype, s));
+    }
+    if (dbias) WARP_STEP(column_sums(dy, dy_stride, rows, n, dtype, w.room, dbias, dbias_dtype, s));
+    return WARP_OK;
+}
+
+}  // extern "C"

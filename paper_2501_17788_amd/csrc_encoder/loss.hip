@@ -1,0 +1,450 @@
+// Softmax cross entropy of token rows h over a vocabulary, the rows E of a table, without keeping the logits:
+//   l_tv = scale * h_t . E_v,  lse_t = log(sum_v exp(l_tv)),  loss_t = lse_t - l_ty   (y: the row's target)
+//   G_tv = dloss_t * (exp(l_tv - lse_t) - [v = y]),  dh_t = scale * sum_v G_tv E_v,  dE_v = scale * sum_t G_tv h_t
+// Rows without a target (a negative one) are left out before any product: the others are copied next to each other, and
+// the products take their number from the device. The forward pass is one product whose tiles end in the largest logit
+// and the sum of exponentials of their rows. The backward pass goes through the vocabulary in pieces: a product makes the
+// piece's logits again and writes G in the inputs' type, two more make the piece's rows of dE from it and add to dh.
+// 8 T V d operations, where 6 T V d would do if the logits had been kept.
+//
+// Precision. The target's exponential is left out of the sums, S the rest relative to it: loss = log(1 + S) keeps its
+// digits where a token is sure, and so does the target's G, which is expm1(-loss). G is rounded to the inputs' type, as
+// matrix instructions need it (float32: three bfloat16 planes, which hold all of it). Before that it is divided by the
+// largest |dloss|, so that rows that count alike round 1 - p and not a multiple of it, and scaled to use float16's range;
+// both come back as a factor of the sums.
+#include "operands.h"
+
+namespace warp {
+
+namespace {
+
+constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kHalfScale = 32768.f;  // |G| <= 1 before it
+constexpr int64_t kPieceBytes = 512ll << 20;  // of G, and of a packed table
+constexpr int64_t kStatsBytes = 256ll << 20;
+
+// ---------------------------------------------------------------------------- rows that have a target
+
+struct SelectArgs {
+    const void* targets;
+    bool wide;
+    int64_t tokens, vocabulary;
+    const float* dloss;
+    float scale, grad_scale;
+    int32_t *list, *place, *target;  // [now] token and target; [tokens] row, -1: none, -2: target outside the vocabulary
+    int32_t* now;
+    float* factor;  // of the sums: largest |dloss| * scale / grad_scale
+    float* largest;
+};
+
+// One workgroup, eight neighbouring tokens a thread at a time.
+__global__ __launch_bounds__(1024) void k_select(SelectArgs g) {
+    constexpr int N = 8;
+    __shared__ uint32_t waves[16];
+    __shared__ uint32_t tops[16];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    int32_t count = 0;
+    uint32_t top = 0;
+    for (int64_t base = 0; base < g.tokens; base += 1024 * N) {
+        const int64_t t0 = base + (int64_t)tid * N;
+        int64_t y[N];
+        uint32_t mine = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const int64_t t = t0 + e;
+            y[e] = -1;
+            if (t < g.tokens) y[e] = g.wide ? ((const int64_t*)g.targets)[t] : (int64_t)((const int32_t*)g.targets)[t];
+            if (y[e] >= 0 && y[e] < g.vocabulary) {
+                ++mine;
+                if (g.dloss) {
+                    const uint32_t u = as_u(g.dloss[t]) & 0x7fffffffu;
+                    if (u < 0x7f800000u) top = max(top, u);
+                }
+            }
+        }
+        uint32_t x = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t v = __shfl_up(x, d);
+            if (lane >= d) x += v;
+        }
+        if (lane == 63) waves[w] = x;
+        __syncthreads();
+        int32_t at = count + (int32_t)(x - mine);
+        for (int i = 0; i < 16; ++i) {
+            if (i < w) at += (int32_t)waves[i];
+            count += (int32_t)waves[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const int64_t t = t0 + e;
+            if (t >= g.tokens) break;
+            const bool in = y[e] >= 0 && y[e] < g.vocabulary;
+            if (g.place) g.place[t] = in ? at : y[e] < 0 ? -1 : -2;
+            if (in) {
+                g.list[at] = (int32_t)t;
+                g.target[at] = (int32_t)y[e];
+                ++at;
+            }
+        }
+    }
+    top = wave_max(top);
+    if (lane == 0) tops[w] = top;
+    __syncthreads();
+    if (tid) return;
+    *g.now = count;
+    if (!g.dloss) return;
+    for (int i = 0; i < 16; ++i) top = max(top, tops[i]);
+    const float largest = top ? as_f(top) : 1.f;
+    *g.largest = largest;
+    *g.factor = largest * g.scale / g.grad_scale;
+}
+
+// ---------------------------------------------------------------------------- forward
+
+struct JoinStatsArgs {
+    const float2* stats;  // [tile][stride]
+    int64_t stride;
+    int tiles;
+    bool first, last;
+    float2* running;  // [row] of the pieces before
+    const float* of_target;
+    const int32_t* place;
+    int64_t tokens;
+    float *loss, *lse;
+};
+
+__device__ __forceinline__ float2 join_stats(float2 a, float2 b) {
+    const float top = fmaxf(a.x, b.x), from = top == -INFINITY ? 0.f : top;
+    return make_float2(top, a.y * __builtin_amdgcn_exp2f(a.x - from) + b.y * __builtin_amdgcn_exp2f(b.x - from));
+}
+
+// 64 tokens a workgroup, whose 16 waves share the tiles.
+__global__ __launch_bounds__(1024) void k_join_stats(JoinStatsArgs g) {
+    __shared__ float2 joined[16][kWave];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t t = (int64_t)blockIdx.x * kWave + lane;
+    const int32_t row = t < g.tokens ? g.place[t] : -1;
+    float2 s = make_float2(-INFINITY, 0.f);
+    if (row >= 0) {
+        if (w == 0 && !g.first) s = g.running[row];
+        constexpr int U = 4;
+        for (int i = w; i < g.tiles; i += 16 * U) {
+            float2 x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                x[u] = i + 16 * u < g.tiles ? g.stats[(i + 16 * u) * g.stride + row] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int u = 0; u < U; ++u) s = join_stats(s, x[u]);
+        }
+    }
+    joined[w][lane] = s;
+    __syncthreads();
+    if (w || t >= g.tokens) return;
+    if (row < 0) {
+        if (g.last) g.loss[t] = g.lse[t] = row == -1 ? 0.f : __builtin_nanf("");
+        return;
+    }
+    for (int i = 1; i < 16; ++i) s = join_stats(s, joined[i][lane]);
+    if (!g.last) {
+        g.running[row] = s;
+        return;
+    }
+    // the others' sum is s.y * 2^s.x, the target's term 2^y
+    const float y = g.of_target[row];
+    if (y >= s.x) {
+        const float others = s.y * __builtin_amdgcn_exp2f(s.x - y), loss = log1pf(others);
+        g.loss[t] = loss;
+        g.lse[t] = y * kLn2 + loss;
+    } else {
+        const float all = logf(s.y + __builtin_amdgcn_exp2f(y - s.x));
+        g.loss[t] = (s.x - y) * kLn2 + all;
+        g.lse[t] = s.x * kLn2 + all;
+    }
+}
+
+// ---------------------------------------------------------------------------- backward
+
+struct RowArgs {
+    const int32_t *list, *now;
+    const float *dloss, *loss, *lse, *largest;
+    float *lse2, *weight, *at_target;
+};
+__global__ __launch_bounds__(256) void k_rows(RowArgs g) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= *g.now) return;
+    const int32_t t = g.list[i];
+    const float weight = g.dloss[t] / *g.largest;
+    g.lse2[i] = g.lse[t] * kLog2E;
+    g.weight[i] = weight;
+    g.at_target[i] = weight * expm1f(-g.loss[t]);
+}
+
+// ---------------------------------------------------------------------------- sizes and scratch
+
+int check_sizes(const char* what, int64_t tokens, int64_t vocabulary, int32_t cols, int32_t dtype) {
+    if (tokens < 0) return fail(WARP_EINVAL, "%s: tokens must be >= 0 (got %lld)", what, (long long)tokens);
+    if (vocabulary < 1) return fail(WARP_EINVAL, "%s: vocabulary must be >= 1 (got %lld)", what, (long long)vocabulary);
+    if (cols < 1) return fail(WARP_EINVAL, "%s: cols must be >= 1 (got %d)", what, cols);
+    if (tokens > 1 << 22 || vocabulary > 1 << 25 || cols > 1 << 14)
+        return fail(WARP_ENOTSUP, "%s: at most 2^22 tokens, a vocabulary of 2^25 and 2^14 columns (got %lld, %lld, %d)", what,
+                    (long long)tokens, (long long)vocabulary, cols);
+    if (!dtype_ok(dtype)) return fail(WARP_EINVAL, "%s: unknown dtype %d", what, dtype);
+    return WARP_OK;
+}
+int check_matrix(const char* what, const void* p, int64_t stride, int64_t rows, int64_t cols, int32_t dtype) {
+    if (rows && !p) return fail(WARP_EINVAL, "%s: null pointer", what);
+    if ((uintptr_t)p % dtype_bytes(dtype)) return fail(WARP_EINVAL, "%s: misaligned pointer", what);
+    if (rows > 1 && stride < cols)
+        return fail(WARP_EINVAL, "%s: a row stride of %lld is below %lld columns", what, (long long)stride, (long long)cols);
+    return WARP_OK;
+}
+int check_scratch(const char* what, const void* scratch, int64_t bytes, int64_t need) {
+    if (!scratch || bytes < need || (uintptr_t)scratch % 16)
+        return fail(WARP_EINVAL, "%s: needs %lld bytes of scratch, 16-byte aligned (got %lld)", what, (long long)need,
+                    (long long)(scratch ? bytes : 0));
+    return WARP_OK;
+}
+int check_rows(const char* what, const void* targets, int32_t target_bytes, int64_t tokens, float scale, const void* loss,
+               const void* lse) {
+    if (target_bytes != 4 && target_bytes != 8)
+        return fail(WARP_EINVAL, "%s: targets of 4 or 8 bytes (got %d)", what, target_bytes);
+    if (tokens && (!targets || !loss || !lse)) return fail(WARP_EINVAL, "%s: null pointer", what);
+    if ((uintptr_t)targets % target_bytes || (uintptr_t)loss % 4 || (uintptr_t)lse % 4)
+        return fail(WARP_EINVAL, "%s: misaligned pointer", what);
+    if (!(scale - scale == 0.f)) return fail(WARP_EINVAL, "%s: scale must be finite", what);
+    return WARP_OK;
+}
+
+// Columns of a piece of the vocabulary: a multiple of 256 (the last piece is shorter).
+int64_t piece_of(int64_t vocabulary, int64_t bytes_a_column, int64_t most_bytes) {
+    int64_t p = most_bytes / bytes_a_column / 256 * 256;
+    const int64_t all = cover_of(vocabulary, 256) * 256;
+    p = p < 256 ? 256 : p > all ? all : p;
+    p = p > 1 << 20 ? 1 << 20 : p;
+    // pieces of one size
+    return cover_of(cover_of(vocabulary, cover_of(vocabulary, p)), 256) * 256;
+}
+
+struct Sizes {
+    int64_t tokens, vocabulary, cols, width;
+    int32_t dtype;
+    int planes;
+    bool packs;  // the table
+};
+Sizes sizes_of(int64_t tokens, const void* table, int64_t stride, int64_t vocabulary, int32_t cols, int32_t dtype) {
+    return {tokens, vocabulary, cols, packed_width(cols), dtype, planes_of(dtype), !direct(table, stride, vocabulary, cols, dtype)};
+}
+
+struct Forward {
+    Space space;
+    int64_t piece;
+    Tile tile;
+    uint16_t *hidden, *table;
+    int32_t *list, *place, *target, *now;
+    float2 *stats, *running;
+    float* of_target;
+    Forward(void* base, const Sizes& z) {
+        space.base = (uint8_t*)base;
+        const int64_t tokens = z.tokens > 0 ? z.tokens : 1;
+        const int64_t by_table = z.packs ? piece_of(z.vocabulary, z.width * 2 * z.planes, kPieceBytes) : 1 << 30;
+        tile = whole_tile(tokens, z.vocabulary);
+        const int64_t by_stats = piece_of(z.vocabulary, cover_of(tokens * 8, tile_size(tile)), kStatsBytes);
+        piece = by_table < by_stats ? by_table : by_stats;
+        hidden = space.take<uint16_t>(packed_elements(tokens, z.cols, z.dtype));
+        table = space.take<uint16_t>(z.packs ? packed_elements(piece, z.cols, z.dtype) : 0);
+        list = space.take<int32_t>(tokens), place = space.take<int32_t>(tokens), target = space.take<int32_t>(tokens);
+        now = space.take<int32_t>(1);
+        stats = space.take<float2>(cover_of(piece, tile_size(tile)) * tokens), running = space.take<float2>(tokens);
+        of_target = space.take<float>(tokens);
+    }
+};
+
+struct Backward {
+    Space space;
+    int64_t piece;
+    Tile logits, dh, de;
+    bool de_split;
+    uint16_t *hidden, *table, *grad;
+    int32_t *list, *place, *target, *now;
+    float *largest, *factor, *lse2, *weight, *at_target, *dh_part, *de_part;
+    Backward(void* base, const Sizes& z) {
+        space.base = (uint8_t*)base;
+        const int64_t tokens = z.tokens > 0 ? z.tokens : 1;
+        const int terms = terms_of(z.dtype);
+        piece = piece_of(z.vocabulary, tokens * 2 * z.planes, kPieceBytes);
+        if (z.packs) {
+            const int64_t by_table = piece_of(z.vocabulary, z.width * 2 * z.planes, kPieceBytes);
+            piece = by_table < piece ? by_table : piece;
+        }
+        const int64_t cols = z.vocabulary < piece ? z.vocabulary : piece;
+        logits = whole_tile(tokens, cols);
+        dh = split_tile(tokens, z.cols, product_steps(cols, terms));
+        de = whole_tile(cols, z.cols);
+        de_split = false;
+        const Tile de_other = split_tile(cols, z.cols, product_steps(tokens, terms));
+        if (product_splits(cols, z.cols, product_steps(tokens, terms), tile_size(de_other), kMaxSplits, tile_jobs(de_other)) > 1 &&
+            product_steps(tokens, terms) >= 16)
+            de_split = true, de = de_other;
+        hidden = space.take<uint16_t>(packed_elements(tokens, z.cols, z.dtype));
+        table = space.take<uint16_t>(z.packs ? packed_elements(piece, z.cols, z.dtype) : 0);
+        grad = space.take<uint16_t>(z.planes * tokens * piece);
+        list = space.take<int32_t>(tokens), place = space.take<int32_t>(tokens), target = space.take<int32_t>(tokens);
+        now = space.take<int32_t>(1);
+        largest = space.take<float>(1), factor = space.take<float>(1);
+        lse2 = space.take<float>(tokens), weight = space.take<float>(tokens), at_target = space.take<float>(tokens);
+        dh_part = space.take<float>(part_floats(tokens, z.cols, cols, terms, dh, kMaxSplits, tile_jobs(dh)));
+        de_part = space.take<float>(
+            de_split ? part_floats(cols, z.cols, tokens, terms, de, kMaxSplits, tile_jobs(de)) : 0);
+    }
+};
+
+#define WARP_STEP(...)                                                                                       \
+    do {                                                                                                     \
+        const hipError_t e_ = (__VA_ARGS__);                                                                 \
+        if (e_ != hipSuccess) return fail(WARP_EDEVICE, "%s: launch failed: %s", what, hipGetErrorString(e_)); \
+    } while (0)
+
+}  // namespace
+
+}  // namespace warp
+
+using namespace warp;
+
+extern "C" {
+
+int warp_cross_entropy_scratch(int64_t tokens, int32_t cols, int32_t dtype, const void* table, int64_t table_stride,
+                               int64_t vocabulary, int64_t* bytes, int64_t* backward_bytes) {
+    const char* what = "cross entropy";
+    if (const int rc = check_sizes(what, tokens, vocabulary, cols, dtype)) return rc;
+    const Sizes z = sizes_of(tokens, table, table_stride, vocabulary, cols, dtype);
+    if (bytes) *bytes = Forward(nullptr, z).space.used;
+    if (backward_bytes) *backward_bytes = Backward(nullptr, z).space.used;
+    return WARP_OK;
+}
+
+int warp_cross_entropy(const void* hidden, int64_t hidden_stride, int64_t tokens, int32_t cols, int32_t dtype,
+                       const void* table, int64_t table_stride, int64_t vocabulary, const void* targets,
+                       int32_t target_bytes, float scale, float* loss, float* lse, void* scratch, int64_t scratch_bytes,
+                       void* hip_stream) {
+    const char* what = "cross entropy";
+    int rc = check_sizes(what, tokens, vocabulary, cols, dtype);
+    if (!rc) rc = check_matrix(what, hidden, hidden_stride, tokens, cols, dtype);
+    if (!rc) rc = check_matrix(what, table, table_stride, vocabulary, cols, dtype);
+    if (!rc) rc = check_rows(what, targets, target_bytes, tokens, scale, loss, lse);
+    if (rc) return rc;
+    const Sizes z = sizes_of(tokens, table, table_stride, vocabulary, cols, dtype);
+    const Forward f(scratch, z);
+    rc = check_scratch(what, scratch, scratch_bytes, f.space.used);
+    if (!rc) rc = require_device();
+    if (rc || !tokens) return rc;
+    hipStream_t s = (hipStream_t)hip_stream;
+    const SelectArgs sel{targets, target_bytes == 8, tokens, vocabulary, nullptr, scale, 1.f, f.list, f.place, f.target,
+                         f.now, nullptr, nullptr};
+    WARP_LAUNCH(hipLaunchKernelGGL(k_select, dim3(1), dim3(1024), 0, s, sel));
+    WARP_STEP(pack_rows(hidden, hidden_stride, tokens, cols, dtype, f.list, f.now, f.hidden, s));
+    for (int64_t v0 = 0; v0 < vocabulary; v0 += f.piece) {
+        const int64_t n = vocabulary - v0 < f.piece ? vocabulary - v0 : f.piece;
+        const void* rows = (const uint8_t*)table + v0 * table_stride * dtype_bytes(dtype);
+        hipError_t e = hipSuccess;
+        Operand t{rows, vocabulary <= 1 ? cols : table_stride, 0};
+        if (z.packs) {
+            e = pack_rows(rows, table_stride, n, cols, dtype, nullptr, nullptr, f.table, s);
+            t = {f.table, z.width, n * z.width};
+        }
+        WARP_STEP(e);
+        ProductArgs g{};
+        g.a = f.hidden, g.a_stride = z.width, g.a_plane = tokens * z.width;
+        g.b = t.p, g.b_stride = t.stride, g.b_plane = t.plane;
+        g.m = tokens, g.n = n, g.k = cols, g.m_now = f.now, g.terms = terms_of(dtype);
+        g.to_log2 = scale * kLog2E, g.n0 = v0, g.target = f.target;
+        g.stats = f.stats, g.stats_stride = tokens, g.of_target = f.of_target;
+        WARP_STEP(product_softmax(g, element_of(dtype), false, f.tile, kStats, s));
+        const JoinStatsArgs j{f.stats, tokens, (int)cover_of(n, tile_size(f.tile)), v0 == 0, v0 + n == vocabulary, f.running,
+                              f.of_target, f.place, tokens, loss, lse};
+        WARP_LAUNCH(hipLaunchKernelGGL(k_join_stats, dim3((uint32_t)cover_of(tokens, kWave)), dim3(1024), 0, s, j));
+    }
+    return WARP_OK;
+}
+
+int warp_cross_entropy_backward(const float* dloss, const void* hidden, int64_t hidden_stride, int64_t tokens, int32_t cols,
+                                int32_t dtype, const void* table, int64_t table_stride, int64_t vocabulary,
+                                const void* targets, int32_t target_bytes, float scale, const float* loss,
+                                const float* lse, void* dhidden, int64_t dhidden_stride, void* dtable,
+                                int64_t dtable_stride, void* scratch, int64_t scratch_bytes, void* hip_stream) {
+    const char* what = "cross entropy backward";
+    int rc = check_sizes(what, tokens, vocabulary, cols, dtype);
+    if (!rc) rc = check_matrix(what, hidden, hidden_stride, tokens, cols, dtype);
+    if (!rc) rc = check_matrix(what, table, table_stride, vocabulary, cols, dtype);
+    if (!rc) rc = check_rows(what, targets, target_bytes, tokens, scale, loss, lse);
+    if (!rc && dhidden) rc = check_matrix(what, dhidden, dhidden_stride, tokens, cols, dtype);
+    if (!rc && dtable) rc = check_matrix(what, dtable, dtable_stride, vocabulary, cols, dtype);
+    if (rc) return rc;
+    if (tokens && !dloss) return fail(WARP_EINVAL, "%s: null pointer", what);
+    if ((uintptr_t)dloss % 4) return fail(WARP_EINVAL, "%s: misaligned pointer", what);
+    const Sizes z = sizes_of(tokens, table, table_stride, vocabulary, cols, dtype);
+    const Backward w(scratch, z);
+    rc = check_scratch(what, scratch, scratch_bytes, w.space.used);
+    if (!rc) rc = require_device();
+    if (rc || (!dhidden && !dtable)) return rc;
+    hipStream_t s = (hipStream_t)hip_stream;
+    const int element = element_of(dtype), terms = terms_of(dtype);
+    const float grad_scale = dtype == WARP_F16 ? kHalfScale : 1.f;
+    const SelectArgs sel{targets, target_bytes == 8, tokens, vocabulary, dloss, scale, grad_scale, w.list, w.place, w.target,
+                         w.now, w.factor, w.largest};
+    WARP_LAUNCH(hipLaunchKernelGGL(k_select, dim3(1), dim3(1024), 0, s, sel));
+    if (tokens) {
+        WARP_STEP(pack_rows(hidden, hidden_stride, tokens, cols, dtype, w.list, w.now, w.hidden, s));
+        const RowArgs r{w.list, w.now, dloss, loss, lse, w.largest, w.lse2, w.weight, w.at_target};
+        WARP_LAUNCH(hipLaunchKernelGGL(k_rows, dim3((uint32_t)cover_of(tokens, 256)), dim3(256), 0, s, r));
+    }
+    const Operand h{w.hidden, z.width, (tokens ? tokens : 1) * z.width};
+    const int64_t part_stride = cover_of(cols, 4) * 4;
+    Join dh{w.dh_part, part_stride, tokens, cols, 0, w.now, nullptr, terms, kMaxSplits, tile_jobs(w.dh), tile_size(w.dh),
+            w.factor, w.place, tokens, dhidden, dhidden_stride, dtype, nullptr, 0};
+    for (int64_t v0 = 0; v0 < vocabulary; v0 += w.piece) {
+        const int64_t n = vocabulary - v0 < w.piece ? vocabulary - v0 : w.piece;
+        const void* rows = (const uint8_t*)table + v0 * table_stride * dtype_bytes(dtype);
+        Operand t{rows, vocabulary <= 1 ? cols : table_stride, 0};
+        if (z.packs) {
+            WARP_STEP(pack_rows(rows, table_stride, n, cols, dtype, nullptr, nullptr, w.table, s));
+            t = {w.table, z.width, n * z.width};
+        }
+        ProductArgs g{};
+        g.a = h.p, g.a_stride = h.stride, g.a_plane = h.plane;
+        g.b = t.p, g.b_stride = t.stride, g.b_plane = t.plane;
+        g.m = tokens, g.n = n, g.k = cols, g.m_now = w.now, g.terms = terms;
+        g.to_log2 = scale * kLog2E, g.n0 = v0, g.target = w.target;
+        g.lse = w.lse2, g.weight = w.weight, g.at_target = w.at_target;
+        g.grad = w.grad, g.grad_stride = w.piece, g.grad_plane = tokens * w.piece, g.grad_scale = grad_scale;
+        WARP_STEP(product_softmax(g, element, z.planes == 3, w.logits, kGrad, s));
+        if (dtable) {
+            ProductArgs e{};
+            e.a = w.grad, e.a_stride = w.piece, e.a_plane = g.grad_plane;
+            e.b = h.p, e.b_stride = h.stride, e.b_plane = h.plane;
+            e.m = n, e.n = cols, e.k = tokens, e.k_now = w.now, e.terms = terms;
+            e.out = (uint8_t*)dtable + v0 * dtable_stride * dtype_bytes(dtype), e.out_stride = dtable_stride;
+            e.out_type = dtype, e.factor = w.factor;
+            e.splits = kMaxSplits, e.jobs = tile_jobs(w.de), e.part = w.de_part, e.part_stride = part_stride;
+            WARP_STEP(product_across(e, element, w.de, w.de_split ? kSum : kStore, s));
+            if (w.de_split)
+                WARP_STEP(join_parts({w.de_part, part_stride, n, cols, tokens, nullptr, w.now, terms, kMaxSplits, e.jobs,
+                                      tile_size(w.de), w.factor, nullptr, n, e.out, e.out_stride, dtype, nullptr, 0}, s));
+        }
+        if (dhidden && tokens) {
+            ProductArgs d{};
+            d.a = w.grad, d.a_stride = w.piece, d.a_plane = g.grad_plane;
+            d.b = t.p, d.b_stride = t.stride, d.b_plane = t.plane;
+            d.m = tokens, d.n = cols, d.k = n, d.m_now = w.now, d.terms = terms;
+            d.splits = kMaxSplits, d.jobs = tile_jobs(w.dh), d.part = w.dh_part, d.part_stride = part_stride;
+            d.accumulate = v0 > 0;
+            if (!v0) dh.k = n;  // the last piece, shorter, may have fewer parts: the others stay as they were
+            WARP_STEP(product_mixed(d, element, w.dh, kSum, s));
+        }
+    }
+    if (dhidden) WARP_STEP(join_parts(dh, s));
+    return WARP_OK;
+}
+
+}  // extern "C"

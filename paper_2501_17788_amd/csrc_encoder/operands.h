@@ -1,0 +1,90 @@
+// What goes into the products of product.h and what comes out: operands made ready, parts of sums joined.
+#pragma once
+
+#include "product.h"
+
+namespace warp {
+
+// Space in the caller's scratch memory, 256-byte aligned; places are counted first and have addresses once there is a base.
+struct Space {
+    uint8_t* base = nullptr;
+    int64_t used = 0;
+    template <typename T>
+    T* take(int64_t n) {
+        const int64_t at = used;
+        used += (n * (int64_t)sizeof(T) + 255) / 256 * 256;
+        return base ? (T*)(base + at) : nullptr;
+    }
+};
+
+// A matrix as the products read it.
+struct Operand {
+    const void* p = nullptr;
+    int64_t stride = 0, plane = 0;
+};
+
+inline int planes_of(int32_t dtype) { return dtype == WARP_F32 ? 3 : 1; }
+inline int terms_of(int32_t dtype) { return dtype == WARP_F32 ? 6 : 1; }
+inline int element_of(int32_t dtype) { return dtype == WARP_F16 ? WARP_F16 : WARP_BF16; }
+inline int64_t packed_width(int64_t cols) { return cover_of(cols, 64) * 64; }
+inline int64_t packed_elements(int64_t rows, int64_t cols, int32_t dtype) {
+    return planes_of(dtype) * rows * packed_width(cols);
+}
+
+// Whether the products can read a matrix where it lies: 16-bit elements, whole 16-byte pieces.
+inline bool direct(const void* p, int64_t stride, int64_t rows, int64_t cols, int32_t dtype) {
+    return dtype != WARP_F32 && (uintptr_t)p % 16 == 0 && cols % 8 == 0 && (rows <= 1 || (stride % 8 == 0 && stride <= 1 << 22));
+}
+
+// Rows (those of `list`, if given, as many as *now) as an operand of its own: padded with zeros to a multiple of 64
+// columns, float32 in planes.
+hipError_t pack_rows(const void* x, int64_t stride, int64_t rows, int64_t cols, int32_t dtype, const int32_t* list,
+                     const int32_t* now, uint16_t* out, hipStream_t s);
+// The same of 8-bit rows: q * scale, for products in `dtype`.
+hipError_t unpack_int8(const int8_t* q, int64_t q_stride, const float* scale, int64_t rows, int64_t cols, int32_t dtype,
+                       uint16_t* out, hipStream_t s);
+
+// x as an operand, copied to `room` if it cannot be read where it lies.
+inline Operand operand_of(const void* x, int64_t stride, int64_t rows, int64_t cols, int32_t dtype, uint16_t* room,
+                          hipStream_t s, hipError_t* e) {
+    if (direct(x, stride, rows, cols, dtype)) return {x, rows <= 1 ? cols : stride, 0};
+    *e = *e ? *e : pack_rows(x, stride, rows, cols, dtype, nullptr, nullptr, room, s);
+    return {room, packed_width(cols), rows * packed_width(cols)};
+}
+
+// out[r][c] = bias[c] + factor * sum of the parts of row `place[r]` (of r, without places; zero where that is negative, NaN where
+// it is below -1): what kSum products of these sizes left.
+struct Join {
+    const float* part;
+    int64_t part_stride;
+    int64_t m, n, k;
+    const int32_t *m_now, *k_now;
+    int32_t terms, splits, jobs, tile;
+    const float* factor;
+    const int32_t* place;
+    int64_t rows;
+    void* out;
+    int64_t out_stride;
+    int32_t out_type;
+    const void* bias;
+    int32_t bias_type;
+};
+hipError_t join_parts(const Join& j, hipStream_t s);
+
+// Floats that the parts of a kSum product need, whatever the present counts are.
+inline int64_t part_floats(int64_t m, int64_t n, int64_t k, int terms, Tile tile, int splits, int jobs) {
+    const int64_t t = tile_size(tile), stride = cover_of(n, 4) * 4;
+    const int64_t most = product_splits(1, 1, product_steps(k, terms), (int)t, splits, jobs);
+    // with fewer rows now there are more parts, of which about `jobs` tiles are at work
+    const int64_t whole = m * stride, parts = most * whole, bounded = jobs * t * cover_of(stride, cover_of(n, t));
+    const int64_t split = parts < bounded ? parts : bounded;
+    return whole > split ? whole : split;
+}
+
+// out = sums of x's columns, in an order that the sizes fix; `room` for column_room floats.
+inline int64_t column_chunks(int64_t rows) { return rows < 64 ? 1 : rows / 64 < 256 ? rows / 64 : 256; }
+inline int64_t column_room(int64_t rows, int64_t cols) { return column_chunks(rows) * cols; }
+hipError_t column_sums(const void* x, int64_t stride, int64_t rows, int64_t cols, int32_t dtype, float* room, void* out,
+                       int32_t out_type, hipStream_t s);
+
+}  // namespace warp

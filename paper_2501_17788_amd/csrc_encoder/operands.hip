@@ -1,0 +1,217 @@
+// Operands of the products made ready and parts of sums joined: kernels bound by memory.
+#include "operands.h"
+
+namespace warp {
+
+namespace {
+
+// Workgroups of four waves, a wave a row at a time and 512 columns of it; rows by steps of the grid.
+constexpr int kRowWaves = 4;
+constexpr int64_t kMaxRowGroups = 32768;
+dim3 row_grid(int64_t rows, int64_t width) {
+    const int64_t groups = cover_of(rows, kRowWaves);
+    return dim3((uint32_t)cover_of(width, 512), (uint32_t)(groups < kMaxRowGroups ? groups : kMaxRowGroups));
+}
+
+template <typename E, int PLANES>
+__device__ __forceinline__ void store_packed(uint16_t* out, int64_t plane, int64_t at, const float (&v)[8]) {
+    if constexpr (PLANES == 3) {
+        Vec<uint16_t, 8> p[3];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            uint16_t s[3];
+            split_f32(v[e], s);
+            p[0].e[e] = s[0], p[1].e[e] = s[1], p[2].e[e] = s[2];
+        }
+#pragma unroll
+        for (int t = 0; t < 3; ++t) store_vec<uint16_t, 8>(out + t * plane + at, p[t]);
+    } else {
+        Vec<E, 8> p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p.e[e] = (E)v[e];
+        store_vec<E, 8>((E*)out + at, p);
+    }
+}
+
+template <typename T, int PLANES>
+__global__ __launch_bounds__(64 * kRowWaves) void k_pack_rows(const T* x, int64_t stride, int64_t rows, int64_t cols,
+                                                              const int32_t* list, const int32_t* now, uint16_t* out,
+                                                              int64_t width, int64_t plane) {
+    const int64_t c = ((int64_t)blockIdx.x * kWave + (threadIdx.x & 63)) * 8;
+    if (c >= width) return;
+    const int64_t end = now ? *now : rows;
+    for (int64_t r = (int64_t)blockIdx.y * kRowWaves + (threadIdx.x >> 6); r < end; r += (int64_t)gridDim.y * kRowWaves) {
+        const T* p = x + (list ? (int64_t)list[r] : r) * stride + c;
+        float v[8];
+        if (c + 8 <= cols) {
+            const auto in = load_vec<T, 8>(p);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (float)in.e[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? (float)p[e] : 0.f;
+        }
+        store_packed<T, PLANES>(out, plane, r * width + c, v);
+    }
+}
+
+template <typename E, int PLANES>
+__global__ __launch_bounds__(64 * kRowWaves) void k_unpack_int8(const int8_t* q, int64_t q_stride, const float* scale,
+                                                                int64_t rows, int64_t cols, uint16_t* out, int64_t width,
+                                                                int64_t plane) {
+    const int64_t c = ((int64_t)blockIdx.x * kWave + (threadIdx.x & 63)) * 8;
+    if (c >= width) return;
+    for (int64_t r = (int64_t)blockIdx.y * kRowWaves + (threadIdx.x >> 6); r < rows; r += (int64_t)gridDim.y * kRowWaves) {
+        const auto in = load_vec<int8_t, 8>(q + r * q_stride + c);  // rows are padded to 128
+        const float f = scale[r];
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? (float)in.e[e] * f : 0.f;
+        store_packed<E, PLANES>(out, plane, r * width + c, v);
+    }
+}
+
+__global__ __launch_bounds__(256) void k_join_parts(Join j) {
+    const int64_t c = ((int64_t)blockIdx.x * kWave + (threadIdx.x & 63)) * 4;
+    if (c >= j.n) return;
+    const int64_t m = j.m_now ? *j.m_now : j.m, k = j.k_now ? *j.k_now : j.k;
+    const int parts = product_splits(m, j.n, product_steps(k, j.terms), j.tile, j.splits, j.jobs);
+    const float factor = j.factor ? *j.factor : 1.f;
+    float bias[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bias[e] = j.bias && c + e < j.n ? load_float(j.bias, j.bias_type, c + e) : 0.f;
+    for (int64_t r = (int64_t)blockIdx.y * kRowWaves + (threadIdx.x >> 6); r < j.rows; r += (int64_t)gridDim.y * kRowWaves) {
+        const int64_t from = j.place ? (int64_t)j.place[r] : r;
+        float4v sum = {};
+        if (from < -1) sum += __builtin_nanf("");
+        if (from >= 0) {
+            const float* p = j.part + from * j.part_stride + c;
+            for (int i = 0; i < parts; ++i) sum += *(const float4v*)(p + (int64_t)i * m * j.part_stride);
+            sum *= factor;
+        }
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = sum[e] + bias[e];
+        store_floats<4>(j.out, j.out_type, r * j.out_stride + c, v, j.n - c, false);
+    }
+}
+
+// Sums of eight neighbouring columns a lane over a chunk of rows, then of the chunks.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void k_column_parts(const T* x, int64_t stride, int64_t rows, int64_t cols, float* room) {
+    __shared__ float joined[3][V][kWave];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    int64_t c = ((int64_t)blockIdx.x * kWave + lane) * V;
+    const bool in = c < cols;
+    if (c + V > cols) c = cols - V;
+    const int64_t each = cover_of(rows, gridDim.y), first = blockIdx.y * each;
+    const int64_t end = first + each < rows ? first + each : rows;
+    float sum[V] = {};
+    constexpr int U = 4;
+    for (int64_t r = first + w; r < end; r += 4 * U) {
+        Vec<T, V> v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (in && r + 4 * u < end) v[u] = load_vec<T, V>(x + (r + 4 * u) * stride + c);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (in && r + 4 * u < end)
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[e] += (float)v[u].e[e];
+    }
+    if (w) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) joined[w - 1][e][lane] = sum[e];
+    }
+    __syncthreads();
+    if (w || !in) return;
+    Vec<float, V> out;
+#pragma unroll
+    for (int e = 0; e < V; ++e) out.e[e] = sum[e] + joined[0][e][lane] + joined[1][e][lane] + joined[2][e][lane];
+    store_vec<float, V>(room + blockIdx.y * cols + c, out);
+}
+
+__global__ __launch_bounds__(1024) void k_column_join(const float* room, int chunks, int64_t cols, void* out, int32_t type) {
+    __shared__ float joined[16][kWave];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * kWave + lane;
+    float sum = 0.f;
+    if (c < cols)
+        for (int i = w; i < chunks; i += 16) sum += room[i * cols + c];
+    joined[w][lane] = sum;
+    __syncthreads();
+    if (w || c >= cols) return;
+    float v[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[0] += joined[i][lane];
+    store_floats<1>(out, type, c, v, 1, false);
+}
+
+template <typename T>
+void column_parts(const void* x, int64_t stride, int64_t rows, int64_t cols, float* room, hipStream_t s) {
+    const uint32_t chunks = (uint32_t)column_chunks(rows);
+    if (cols < 8)
+        hipLaunchKernelGGL((k_column_parts<T, 1>), dim3(1, chunks), dim3(256), 0, s, (const T*)x, stride, rows, cols, room);
+    else
+        hipLaunchKernelGGL((k_column_parts<T, 8>), dim3((uint32_t)cover_of(cols, 512), chunks), dim3(256), 0, s, (const T*)x,
+                           stride, rows, cols, room);
+}
+
+}  // namespace
+
+hipError_t pack_rows(const void* x, int64_t stride, int64_t rows, int64_t cols, int32_t dtype, const int32_t* list,
+                     const int32_t* now, uint16_t* out, hipStream_t s) {
+    if (!rows) return hipSuccess;
+    const int64_t width = packed_width(cols), plane = rows * width;
+    const dim3 grid = row_grid(rows, width), block(64 * kRowWaves);
+    (void)hipGetLastError();
+    if (dtype == WARP_F32)
+        hipLaunchKernelGGL((k_pack_rows<float, 3>), grid, block, 0, s, (const float*)x, stride, rows, cols, list, now, out,
+                           width, plane);
+    else if (dtype == WARP_F16)
+        hipLaunchKernelGGL((k_pack_rows<_Float16, 1>), grid, block, 0, s, (const _Float16*)x, stride, rows, cols, list, now,
+                           out, width, plane);
+    else
+        hipLaunchKernelGGL((k_pack_rows<__bf16, 1>), grid, block, 0, s, (const __bf16*)x, stride, rows, cols, list, now, out,
+                           width, plane);
+    return hipGetLastError();
+}
+
+hipError_t unpack_int8(const int8_t* q, int64_t q_stride, const float* scale, int64_t rows, int64_t cols, int32_t dtype,
+                       uint16_t* out, hipStream_t s) {
+    if (!rows) return hipSuccess;
+    const int64_t width = packed_width(cols), plane = rows * width;
+    const dim3 grid = row_grid(rows, width), block(64 * kRowWaves);
+    (void)hipGetLastError();
+    if (dtype == WARP_F32)
+        hipLaunchKernelGGL((k_unpack_int8<__bf16, 3>), grid, block, 0, s, q, q_stride, scale, rows, cols, out, width, plane);
+    else if (dtype == WARP_F16)
+        hipLaunchKernelGGL((k_unpack_int8<_Float16, 1>), grid, block, 0, s, q, q_stride, scale, rows, cols, out, width, plane);
+    else
+        hipLaunchKernelGGL((k_unpack_int8<__bf16, 1>), grid, block, 0, s, q, q_stride, scale, rows, cols, out, width, plane);
+    return hipGetLastError();
+}
+
+hipError_t join_parts(const Join& j, hipStream_t s) {
+    if (!j.rows) return hipSuccess;
+    const int64_t groups = cover_of(j.rows, kRowWaves);
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(k_join_parts, dim3((uint32_t)cover_of(j.n, 256), (uint32_t)(groups < kMaxRowGroups ? groups : kMaxRowGroups)),
+                       dim3(64 * kRowWaves), 0, s, j);
+    return hipGetLastError();
+}
+
+hipError_t column_sums(const void* x, int64_t stride, int64_t rows, int64_t cols, int32_t dtype, float* room, void* out,
+                       int32_t out_type, hipStream_t s) {
+    (void)hipGetLastError();
+    if (rows) {
+        if (dtype == WARP_F32) column_parts<float>(x, stride, rows, cols, room, s);
+        else if (dtype == WARP_F16) column_parts<_Float16>(x, stride, rows, cols, room, s);
+        else column_parts<__bf16>(x, stride, rows, cols, room, s);
+    }
+    hipLaunchKernelGGL(k_column_join, dim3((uint32_t)cover_of(cols, kWave)), dim3(1024), 0, s, (const float*)room,
+                       rows ? (int)column_chunks(rows) : 0, cols, out, out_type);
+    return hipGetLastError();
+}
+
+}  // namespace warp

@@ -1,0 +1,541 @@
+// Products of matrices of 16-bit elements on the matrix cores, with what the callers do to a finished tile:
+//   C[m][n] = sum_k A(m, k) B(n, k), sums in fp32.
+// An operand's elements of one row lie together (kAlongK: tokens, weights as stored) or those of one k (kAcrossK: its
+// transpose, as stored). Operands are 16-byte aligned, their strides multiples of 8; along K a row's elements beyond k up
+// to the next multiple of 8 are zeros; across K a row is readable up to the next multiple of 8.
+//
+// float32 operands come as three planes of bfloat16, high + middle + low = x to the last bit (split_f32), and a
+// product as the six of nine products of planes that count: those left out are below 2^-23 of |a b| together.
+// (A matrix instruction for fp32 operands has a 16th of the rate; six products are 2.7 times as fast.)
+#pragma once
+
+#include "encoder.h"
+
+namespace warp {
+
+enum Layout { kAlongK, kAcrossK };
+enum Finish {
+    kStore,  // out = factor * C + bias
+    kSum,    // part[split] (+)= C, in fp32
+    kStats,  // softmax statistics of a tile's rows
+    kGrad,   // the loss's gradient for the logits
+};
+enum Tile { kT64, kT128, kT256 };
+
+struct ProductArgs {
+    const void *a, *b;
+    int64_t a_stride, b_stride;  // elements between rows as stored
+    int64_t a_plane, b_plane;    // elements between the planes of a float32 operand
+    int64_t m, n, k;
+    const int32_t *m_now, *k_now;  // device counts that take the place of m and k where they are not null
+    int32_t terms;                 // 1, or 6 products of planes
+    int32_t splits, jobs;          // at most so many parts of the k range, to have about so many tiles at work
+    // kStore
+    void* out;
+    int64_t out_stride;
+    int32_t out_type;
+    const float* factor;
+    const void* bias;
+    int32_t bias_type;
+    // kSum
+    float* part;
+    int64_t part_stride;  // a part is as many rows as there are now
+    bool accumulate;
+    // kStats and kGrad: rows are tokens, columns n0, n0 + 1, ... of the vocabulary
+    float to_log2;          // a logit in units of log 2 is to_log2 * C
+    int64_t n0;
+    const int32_t* target;  // a row's column
+    float2* stats;          // [tile column][row]: largest logit of the others than the target, sum of their exponentials
+    int64_t stats_stride;
+    float* of_target;       // [row] the target's logit
+    const float *lse, *weight, *at_target;  // [row] in units of log 2; of the row; value at the target
+    void* grad;
+    int64_t grad_stride, grad_plane;
+    float grad_scale;
+};
+
+__host__ __device__ inline int64_t cover_of(int64_t n, int64_t of) { return (n + of - 1) / of; }
+
+constexpr int kProductStep = 64;  // columns of a step: 128 bytes of a row
+
+__host__ __device__ inline int64_t product_steps(int64_t k, int terms) { return cover_of(k, kProductStep) * terms; }
+
+// Parts of the k range: so many that about `jobs` tiles are at work, of two steps at least.
+__host__ __device__ inline int product_splits(int64_t m, int64_t n, int64_t steps, int tile, int splits, int jobs) {
+    const int64_t tiles = cover_of(m, tile) * cover_of(n, tile);
+    int64_t s = tiles ? jobs / tiles : 1;
+    s = s < steps / 2 ? s : steps / 2;
+    s = s < splits ? s : splits;
+    return s < 1 ? 1 : (int)s;
+}
+inline int tile_size(Tile t) { return t == kT64 ? 64 : t == kT128 ? 128 : 256; }
+// Tiles at work at once.
+inline int tile_jobs(Tile t) { return t == kT64 ? 1024 : t == kT128 ? 512 : 256; }
+
+// Tiles of a product that is not split, and of one that may be.
+inline Tile whole_tile(int64_t m, int64_t n) {
+    if (cover_of(m, 256) * cover_of(n, 256) >= 192) return kT256;
+    return cover_of(m, 128) * cover_of(n, 128) >= 192 ? kT128 : kT64;
+}
+inline Tile split_tile(int64_t m, int64_t n, int64_t steps) {
+    if (m > 128 && n > 128 && cover_of(m, 256) * cover_of(n, 256) * steps >= 2048) return kT256;
+    return m > 64 && n > 64 && cover_of(m, 128) * cover_of(n, 128) * steps >= 1024 ? kT128 : kT64;
+}
+constexpr int kMaxSplits = 256;
+
+// x = high + middle + low, each a bfloat16 cut off towards zero: 8 + 8 + 8 bits. An infinity or a NaN stays in the
+// first.
+__host__ __device__ inline void split_f32(float x, uint16_t (&out)[3]) {
+    uint32_t u;
+    __builtin_memcpy(&u, &x, 4);
+    const bool special = (u & 0x7f800000u) == 0x7f800000u;
+    float rest = x;
+    for (int i = 0; i < 3; ++i) {
+        uint32_t v;
+        __builtin_memcpy(&v, &rest, 4);
+        v &= 0xffff0000u;
+        if (special) v = i ? 0 : u & 0x7fffff ? 0x7fc00000u : u;
+        out[i] = (uint16_t)(v >> 16);
+        float part;
+        __builtin_memcpy(&part, &v, 4);
+        rest -= part;
+    }
+}
+
+// Launches: element is WARP_F16 or WARP_BF16 (also for planes).
+hipError_t product_along(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);   // A, B along K
+hipError_t product_mixed(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);   // B across K
+hipError_t product_across(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);  // both
+hipError_t product_softmax(const ProductArgs& g, int element, bool planes, Tile tile, Finish finish, hipStream_t s);
+
+#ifdef __HIPCC__
+
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+typedef const __attribute__((address_space(1))) void product_global;
+typedef __attribute__((address_space(3))) void product_lds;
+typedef __attribute__((address_space(3))) short4v product_lds4;
+
+static __device__ uint32_t g_zeros[4];  // where pieces beyond the k range are read
+
+template <typename E>
+struct Eight {
+    typedef E type __attribute__((ext_vector_type(8)));
+};
+__device__ __forceinline__ float4v product_mfma(Eight<__bf16>::type a, Eight<__bf16>::type b, float4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float4v product_mfma(Eight<_Float16>::type a, Eight<_Float16>::type b, float4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Waits for this wave's loads into LDS, which a barrier alone does not order.
+__device__ __forceinline__ void product_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Where the 16-byte pieces of a staged operand lie in LDS.
+// Along K a row has eight pieces, in the order piece ^ key(row), so that the rows that neighbouring lanes read one
+// piece of lie in different banks. Token blocks read rows 0 .. 15 in order; a channel block j reads rows
+// 4 j + i % 4 + 4 B (i / 4), which gives a lane 4 B neighbouring columns of the result.
+// Across K a k has T / 8 pieces, two for 16 columns, in the order pair ^ pair_key(k): the transposing reads of 16 lanes
+// take 32 bytes of four k each, and lanes 16 apart take k 8 apart.
+__device__ __forceinline__ int token_piece(int row) { return row & 7; }
+template <int B>
+__device__ __forceinline__ int channel_piece(int row) { return (row & 3) | (row / (4 * B) & 1) << 2; }
+template <int T>
+__device__ __forceinline__ int pair_key(int k) { return ((k & 3) | (k >> 3 & 3) << 2) & (T / 16 - 1); }
+
+// One operand's part in a tile of T rows by 64 k, for one wave of WAVES.
+template <Layout L, int T, int WAVES, bool CHANNELS, int B>
+struct Stage {
+    static constexpr int kLoads = T / 8 / WAVES;  // of 1 KB
+    static_assert(kLoads * 8 * WAVES == T, "whole loads");
+    uint32_t off[kLoads];
+    const uint8_t* at;    // the next step's first byte
+    int64_t step_bytes;
+    const uint8_t* base;  // of plane 0
+    int lane, wave;
+
+    __device__ __forceinline__ int key(int row) const { return CHANNELS ? channel_piece<B>(row) : token_piece(row); }
+    // this lane's k within a step, in load i
+    __device__ __forceinline__ int k_of(int i) const {
+        const int unit = wave * kLoads + i;
+        if (L == kAlongK) return 8 * ((lane & 7) ^ key(unit * 8 + (lane >> 3)));
+        return (unit * 1024 + lane * 16) / (T * 2);
+    }
+    __device__ __forceinline__ void start(const void* p, int64_t stride, int64_t first, int64_t rows, int lane_, int wave_) {
+        lane = lane_, wave = wave_;
+        if (L == kAlongK) {
+            base = (const uint8_t*)p + first * stride * 2;
+            step_bytes = 2 * kProductStep;
+            const int last = (int)(rows - first < T ? rows - first : T) - 1;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int row = (wave * kLoads + i) * 8 + (lane >> 3);
+                off[i] = (uint32_t)(row < last ? row : last) * (uint32_t)(stride * 2) + 2 * k_of(i);
+            }
+        } else {
+            base = (const uint8_t*)p + first * 2;
+            step_bytes = stride * 2 * kProductStep;
+            const int64_t end = (rows - 1) / 8 * 8 - first;  // the last piece
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int k = k_of(i);
+                const int piece = ((wave * kLoads + i) * 64 + lane) & (T / 8 - 1);
+                const int64_t row = 8 * (piece ^ pair_key<T>(k) << 1);
+                off[i] = (uint32_t)k * (uint32_t)(stride * 2) + (uint32_t)(row < end ? row : end) * 2;
+            }
+        }
+    }
+    __device__ __forceinline__ void seek(int64_t plane, int64_t step) { at = base + plane * 2 + step * step_bytes; }
+    __device__ __forceinline__ void load(uint8_t* lds) const {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            __builtin_amdgcn_global_load_lds((product_global*)(at + off[i]),
+                                             (product_lds*)(lds + (wave * kLoads + i) * 1024), 16, 0, 0);
+    }
+    __device__ __forceinline__ void load_last(uint8_t* lds, int left) const {  // zeros beyond `left` k
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const uint8_t* p = k_of(i) < left ? at + off[i] : (const uint8_t*)g_zeros;
+            __builtin_amdgcn_global_load_lds((product_global*)p, (product_lds*)(lds + (wave * kLoads + i) * 1024), 16,
+                                             0, 0);
+        }
+    }
+};
+
+// Where a lane reads blocks of 16 rows of a staged operand: block i of B, half a step (32 k) at a time.
+template <typename E, Layout L, int T, bool CHANNELS, int B>
+struct Blocks {
+    typedef typename Eight<E>::type V;
+    int at;
+    __device__ __forceinline__ void start(int first, int lane) {
+        const int li = lane & 15, q = lane >> 4;
+        if (L == kAlongK) {
+            const int row = CHANNELS ? first + (li & 3) + 4 * B * (li >> 2) : first + li;
+            at = row * 128 + 16 * (q ^ (CHANNELS ? channel_piece<B>(row) : token_piece(row)));
+        } else {
+            const int k = 8 * q + (li >> 2);
+            at = k * T * 2 + ((first / 16) ^ pair_key<T>(k)) * 32 + (li & 3) * 8;
+        }
+    }
+    __device__ __forceinline__ V read(const uint8_t* lds, int i, int half) const {
+        if (L == kAlongK)
+            return *(const V*)(lds + (at ^ (64 * half)) + (CHANNELS ? 4 : 16) * i * 128);
+        const uint8_t* p = lds + (at ^ (32 * i)) + half * 32 * T * 2;
+        const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((product_lds4*)p);
+        const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((product_lds4*)(p + 4 * T * 2));
+        typedef short short8v __attribute__((ext_vector_type(8)));
+        const short8v both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(V, both);
+    }
+};
+
+template <int W>
+__device__ __forceinline__ void store_floats(void* out, int32_t type, int64_t at, const float (&v)[W], int64_t left,
+                                             bool past_caches) {
+    auto put = [&](auto t) {
+        typedef decltype(t) T;
+        T* p = (T*)out + at;
+        Vec<T, W> r;
+#pragma unroll
+        for (int e = 0; e < W; ++e) r.e[e] = (T)v[e];
+        if (left >= W) {
+            if (past_caches) stream_out<T, W>(p, r);
+            else store_vec<T, W>(p, r);
+        } else {
+#pragma unroll
+            for (int e = 0; e < W; ++e)
+                if (e < left) p[e] = r.e[e];
+        }
+    };
+    if (type == WARP_F32) put(0.f);
+    else if (type == WARP_F16) put((_Float16)0);
+    else put((__bf16)0.f);
+}
+
+__device__ __forceinline__ float load_float(const void* p, int32_t type, int64_t at) {
+    return type == WARP_F32 ? ((const float*)p)[at]
+                            : type == WARP_F16 ? (float)((const _Float16*)p)[at] : (float)((const __bf16*)p)[at];
+}
+
+// Tiles that neighbouring workgroups of an XCD work on span bands of four tiles of rows, so that its L2 serves what
+// they have in common.
+constexpr int kProductBand = 4;
+
+template <typename E, Layout LA, Layout LB, int TM, int TN, int WM, int WN, Finish F, bool PLANES>
+__global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs g) {
+    constexpr int kWaves = WM * WN;
+    constexpr int kBM = TM / WM / 16, kBN = TN / WN / 16;  // blocks of a wave
+    constexpr bool kWide = LB == kAlongK;                  // a lane holds 4 kBN neighbouring columns, else 4 in each block
+    __shared__ __attribute__((aligned(16))) uint8_t a0[TM * 128];
+    __shared__ __attribute__((aligned(16))) uint8_t a1[TM * 128];
+    __shared__ __attribute__((aligned(16))) uint8_t b0[TN * 128];
+    __shared__ __attribute__((aligned(16))) uint8_t b1[TN * 128];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int li = lane & 15, q = lane >> 4;
+    const int wm = (wave / WN) * (TM / WM), wn = (wave % WN) * (TN / WN);
+
+    const int64_t rows = g.m_now ? *g.m_now : g.m;
+    const int64_t k = g.k_now ? *g.k_now : g.k;
+    const int64_t k_steps = cover_of(k, kProductStep), steps = k_steps * g.terms;
+    const int tiles_m = (int)cover_of(rows, TM), tiles_n = (int)cover_of(g.n, TN);
+    const int splits = F == kSum ? product_splits(rows, g.n, steps, TM, g.splits, g.jobs) : 1;
+    const int tiles = tiles_m * tiles_n, total = tiles * splits;
+    // tiles of one XCD (every eighth workgroup) are neighbours
+    const int xcd = blockIdx.x & 7, per = total >> 3, more = total & 7, in_xcd = blockIdx.x >> 3;
+    if (in_xcd >= per + (xcd < more)) return;
+    const int job = xcd * per + (xcd < more ? xcd : more) + in_xcd;
+    const int split = job / tiles, tile = job % tiles;
+    const int band = tile / (kProductBand * tiles_n), in = tile - band * kProductBand * tiles_n;
+    const int wide = tiles_m - band * kProductBand < kProductBand ? tiles_m - band * kProductBand : kProductBand;
+    const int tile_n = in / wide;
+    const int64_t m0 = (int64_t)(band * kProductBand + in % wide) * TM, c0 = (int64_t)tile_n * TN;
+
+    const int64_t each = cover_of(steps, splits);
+    const int64_t first = split * each;
+    const int count = (int)(steps - first < each ? (steps > first ? steps - first : 0) : each);
+
+    Stage<LA, TM, kWaves, false, kBM> sa;
+    Stage<LB, TN, kWaves, kWide, kBN> sb;
+    sa.start(g.a, g.a_stride, m0, rows, lane, wave);
+    sb.start(g.b, g.b_stride, c0, g.n, lane, wave);
+    int term = 0;
+    int64_t kk = 0;  // step within the term
+    auto seek = [&] {
+        // planes of the terms: (0,0) (0,1) (1,0) (1,1) (0,2) (2,0)
+        sa.seek((int64_t)(0x201100 >> 4 * term & 3) * g.a_plane, kk);
+        sb.seek((int64_t)(0x021010 >> 4 * term & 3) * g.b_plane, kk);
+    };
+    if (k_steps) term = (int)(first / k_steps), kk = first % k_steps;
+    seek();
+    auto load = [&](uint8_t* la, uint8_t* lb) {
+        const int64_t left = k - kk * kProductStep;
+        if (left >= kProductStep) {
+            sa.load(la);
+            sb.load(lb);
+        } else {
+            sa.load_last(la, (int)left);
+            sb.load_last(lb, (int)left);
+        }
+        if (++kk == k_steps) {
+            kk = 0;
+            ++term;
+            seek();  // (after the last term: not used)
+        } else {
+            sa.at += sa.step_bytes;
+            sb.at += sb.step_bytes;
+        }
+    };
+
+    Blocks<E, LA, TM, false, kBM> ra;
+    Blocks<E, LB, TN, kWide, kBN> rb;
+    ra.start(wm, lane);
+    rb.start(wn, lane);
+    typedef typename Eight<E>::type V;
+    struct Part {  // a wave's operands of half a step
+        V a[kBM], b[kBN];
+    } part[2];
+    auto read = [&](Part& p, const uint8_t* la, const uint8_t* lb, int half) {
+#pragma unroll
+        for (int j = 0; j < kBN; ++j) p.b[j] = rb.read(lb, j, half);
+#pragma unroll
+        for (int i = 0; i < kBM; ++i) p.a[i] = ra.read(la, i, half);
+    };
+    float4v acc[kBM][kBN] = {};
+    auto multiply = [&](const Part& p) {
+#pragma unroll
+        for (int i = 0; i < kBM; ++i)
+#pragma unroll
+            for (int j = 0; j < kBN; ++j) acc[i][j] = product_mfma(p.b[j], p.a[i], acc[i][j]);
+    };
+    // The operands of each half step are read while the matrix cores work on the half step before it, across the
+    // barrier between steps.
+    auto step = [&](int s, const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb) {
+        product_landed();
+        __syncthreads();  // this step's rows are there, and the other buffer has been read by all
+        if (s + 1 < count) load(na, nb);
+        read(part[0], la, lb, 0);
+        if (s) multiply(part[1]);
+        read(part[1], la, lb, 1);
+        multiply(part[0]);
+    };
+    if (count) {
+        load(a0, b0);
+        step(0, a0, b0, a1, b1);
+        int s = 1;
+        for (; s + 1 < count; s += 2) {
+            step(s, a1, b1, a0, b0);
+            step(s + 1, a0, b0, a1, b1);
+        }
+        if (s < count) step(s, a1, b1, a0, b0);
+        multiply(part[1]);
+    }
+
+    // acc[i][j][e] is row m0 + wm + 16 i + li, column c0 + wn + 4 kBN q + 4 j + e (kWide) or c0 + wn + 16 j + 4 q + e
+    constexpr int kGroups = kWide ? 1 : kBN, kOut = kWide ? 4 * kBN : 4;
+    auto column = [&](int group) { return c0 + wn + (kWide ? kOut * q : 16 * group + 4 * q); };
+    if constexpr (F == kStore) {
+        const float factor = g.factor ? *g.factor : 1.f;
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u) {
+            const int64_t c = column(u);
+            if (c >= g.n) continue;
+            float bias[kOut];
+#pragma unroll
+            for (int e = 0; e < kOut; ++e) {
+                bias[e] = g.bias && c + e < g.n ? load_float(g.bias, g.bias_type, c + e) : 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < kBM; ++i) {
+                const int64_t m = m0 + wm + 16 * i + li;
+                if (m >= rows) continue;
+                float v[kOut];
+#pragma unroll
+                for (int e = 0; e < kOut; ++e) v[e] = acc[i][kWide ? e >> 2 : u][e & 3] * factor + bias[e];
+                store_floats<kOut>(g.out, g.out_type, m * g.out_stride + c, v, g.n - c, kWide);
+            }
+        }
+    } else if constexpr (F == kSum) {
+        float* out = g.part + split * rows * g.part_stride;
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u) {
+            const int64_t c = column(u);
+            if (c >= g.n) continue;
+#pragma unroll
+            for (int i = 0; i < kBM; ++i) {
+                const int64_t m = m0 + wm + 16 * i + li;
+                if (m >= rows) continue;
+                // part_stride and part are multiples of 4 floats: whole vectors, the last one into the padding
+#pragma unroll
+                for (int e = 0; e < kOut; e += 4) {
+                    if (c + e >= g.n) continue;
+                    float4v* p = (float4v*)(out + m * g.part_stride + c + e);
+                    const float4v x = acc[i][kWide ? e >> 2 : u];
+                    *p = g.accumulate ? *p + x : x;
+                }
+            }
+        }
+    } else if constexpr (F == kStats) {
+        static_assert(kWide, "rows are reduced over neighbouring columns");
+        const int64_t c = column(0);
+        __syncthreads();  // the staged operands have been read by all
+        float2* shared = (float2*)a0;  // [WN][TM]
+#pragma unroll
+        for (int i = 0; i < kBM; ++i) {
+            const int64_t m = m0 + wm + 16 * i + li;
+            float x[kOut], top = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < kOut; ++e) {
+                x[e] = acc[i][e >> 2][e & 3] * g.to_log2;
+                if (c + e >= g.n) x[e] = -INFINITY;
+            }
+            const int64_t hit = m < rows ? (int64_t)g.target[m] - g.n0 - c : -1;
+            if (hit >= 0 && hit < kOut && c + hit < g.n) {
+#pragma unroll
+                for (int e = 0; e < kOut; ++e)
+                    if (e == hit) g.of_target[m] = x[e], x[e] = -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < kOut; ++e) top = fmaxf(top, x[e]);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float from = top == -INFINITY ? 0.f : top;
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < kOut; ++e) sum += __builtin_amdgcn_exp2f(x[e] - from);
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if (q == 0) shared[(wave % WN) * TM + wm + 16 * i + li] = make_float2(top, sum);
+        }
+        __syncthreads();
+        for (int r = threadIdx.x; r < TM; r += 64 * kWaves) {
+            if (m0 + r >= rows) continue;
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < WN; ++w) top = fmaxf(top, shared[w * TM + r].x);
+            const float from = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int w = 0; w < WN; ++w) {
+                const float2 o = shared[w * TM + r];
+                sum += o.y * __builtin_amdgcn_exp2f(o.x - from);
+            }
+            g.stats[tile_n * g.stats_stride + m0 + r] = make_float2(top, sum);
+        }
+    } else {
+        static_assert(kWide, "rows are written in neighbouring columns");
+        const int64_t c = column(0);
+#pragma unroll
+        for (int i = 0; i < kBM; ++i) {
+            const int64_t m = m0 + wm + 16 * i + li;
+            if (m >= rows) continue;
+            const float lse = g.lse[m], weight = g.weight[m] * g.grad_scale;
+            const int64_t hit = (int64_t)g.target[m] - g.n0 - c;
+            float d[kOut];
+#pragma unroll
+            for (int e = 0; e < kOut; ++e) d[e] = __builtin_amdgcn_exp2f(acc[i][e >> 2][e & 3] * g.to_log2 - lse) * weight;
+            if (hit >= 0 && hit < kOut) {
+#pragma unroll
+                for (int e = 0; e < kOut; ++e)
+                    if (e == hit) d[e] = g.at_target[m] * g.grad_scale;
+            }
+            if (c + kOut > g.n) {
+#pragma unroll
+                for (int e = 0; e < kOut; ++e)
+                    if (c + e >= g.n) d[e] = 0.f;
+            }
+            if constexpr (PLANES) {
+                Vec<uint16_t, kOut> p[3];
+#pragma unroll
+                for (int e = 0; e < kOut; ++e) {
+                    uint16_t s[3];
+                    split_f32(d[e], s);
+                    p[0].e[e] = s[0], p[1].e[e] = s[1], p[2].e[e] = s[2];
+                }
+#pragma unroll
+                for (int t = 0; t < 3; ++t)
+                    store_vec<uint16_t, kOut>((uint16_t*)g.grad + t * g.grad_plane + m * g.grad_stride + c, p[t]);
+            } else {
+                Vec<E, kOut> p;
+#pragma unroll
+                for (int e = 0; e < kOut; ++e) p.e[e] = (E)d[e];
+                store_vec<E, kOut>((E*)g.grad + m * g.grad_stride + c, p);
+            }
+        }
+    }
+}
+
+// Workgroups for at most g.m rows.
+template <typename E, Layout LA, Layout LB, Finish F, bool PLANES, int TM, int TN, int WM, int WN>
+hipError_t product_launch(const ProductArgs& g, hipStream_t s) {
+    const int64_t tiles = cover_of(g.m, TM) * cover_of(g.n, TN);
+    // splits shrink as rows grow: at most `jobs` tiles, or one part of each
+    const int64_t grid = F == kSum && tiles < g.jobs ? g.jobs : tiles;
+    (void)hipGetLastError();
+    if (tiles)
+        hipLaunchKernelGGL((k_product<E, LA, LB, TM, TN, WM, WN, F, PLANES>), dim3((uint32_t)grid), dim3(64 * WM * WN), 0,
+                           s, g);
+    return hipGetLastError();
+}
+
+template <typename E, Layout LA, Layout LB, Finish F, bool PLANES = false>
+hipError_t product_tiles(const ProductArgs& g, Tile tile, hipStream_t s) {
+    switch (tile) {
+        case kT64: return product_launch<E, LA, LB, F, PLANES, 64, 64, 2, 2>(g, s);
+        case kT128: return product_launch<E, LA, LB, F, PLANES, 128, 128, 2, 4>(g, s);
+        default: return product_launch<E, LA, LB, F, PLANES, 256, 256, 2, 4>(g, s);
+    }
+}
+
+template <Layout LA, Layout LB>
+hipError_t product_any(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s) {
+    if (element == WARP_F16)
+        return finish == kSum ? product_tiles<_Float16, LA, LB, kSum>(g, tile, s)
+                              : product_tiles<_Float16, LA, LB, kStore>(g, tile, s);
+    return finish == kSum ? product_tiles<__bf16, LA, LB, kSum>(g, tile, s)
+                          : product_tiles<__bf16, LA, LB, kStore>(g, tile, s);
+}
+
+#endif  // __HIPCC__
+
+}  // namespace warp

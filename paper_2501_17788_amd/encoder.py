@@ -1,12 +1,12 @@
-"""The operators of a token encoder's head, on torch device tensors: layer norm with its gradients,
-products of 8-bit rows, and the AdamW step.
+"""The operators that train a token encoder and serve its head, on torch device tensors: table lookup, layer norm,
+linear layers and softmax cross entropy with their gradients, products of 8-bit rows, and the AdamW step.
 
 As in `warp`, everything runs in the HIP kernels behind the C ABI of include/warp.h. `_encoder.so` (from
 csrc_encoder/encoder_binding.cpp) checks tensors, allocates outputs with torch and passes pointers: a ValueError
 for tensors that do not fit, a WarpError for what the library refuses. A call works on the current stream of its
 tensors' device, or on `stream`; inputs of another stream are the caller's to wait for. Tensors have any row
 stride (a dimension's elements one after the other); leading dimensions are flattened to rows. autograd follows
-`layer_norm`; 8-bit rows and what is made of them carry no gradient.
+`embedding`, `layer_norm`, `linear` and `cross_entropy`; 8-bit rows and what is made of them carry no gradient.
 """
 from __future__ import annotations
 
@@ -117,6 +117,118 @@ def linear_int8(a: QuantizedRows, w: QuantizedRows, bias=None, dtype=torch.bfloa
     if stream is None:
         return _native.linear_int8(*a, *w, bias, dtype)
     return _on(stream, (a.values, a.scale, w.values, w.scale, bias), _native.linear_int8, *a, *w, bias, dtype)
+
+
+class _Embedding(torch.autograd.Function):
+    """What `embedding` is to autograd."""
+
+    @staticmethod
+    def forward(ctx, ids, table, scale):
+        ctx.save_for_backward(ids)
+        ctx.vocabulary, ctx.scale = table.shape[0], scale
+        return _native.embedding(ids, table, scale)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        return None, _native.embedding_backward(dy, *ctx.saved_tensors, ctx.vocabulary, ctx.scale), None
+
+
+def embedding(ids, table, scale: float = 1.0, stream=None):
+    """Rows of table [vocabulary, cols] for ids [...] (int64 or int32), times scale: [..., cols] of table's type. A negative
+    id is padding and gives zeros; one outside the table gives NaN. autograd follows the table."""
+    if stream is None:
+        return _native.embedding(ids, table, scale)
+    return _on(stream, (ids, table), _native.embedding, ids, table, scale)
+
+
+def embedding_backward(dy, ids, vocabulary: int, scale: float = 1.0, stream=None):
+    """Gradient [vocabulary, cols] of `embedding`'s table for the gradient dy [..., cols] of its rows. The sums' order is
+    the tokens': the same call gives the same bits."""
+    if stream is None:
+        return _native.embedding_backward(dy, ids, vocabulary, scale)
+    return _on(stream, (dy, ids), _native.embedding_backward, dy, ids, vocabulary, scale)
+
+
+class _CrossEntropy(torch.autograd.Function):
+    """What `cross_entropy` is to autograd. lse has no gradient, and the losses no second derivative."""
+
+    @staticmethod
+    def forward(ctx, hidden, table, targets, scale):
+        loss, lse = _native.cross_entropy(hidden, table, targets, scale)
+        # a copy: the caller may change its losses in place
+        ctx.save_for_backward(hidden, table, targets, loss.clone(), lse.clone())
+        ctx.mark_non_differentiable(lse)
+        ctx.scale = scale
+        return loss, lse
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss, _):
+        want = ctx.needs_input_grad
+        return *_native.cross_entropy_backward(dloss, *ctx.saved_tensors, ctx.scale, want[0], want[1]), None, None
+
+
+def cross_entropy(hidden, table, targets, scale: float = 1.0, stream=None):
+    """Softmax cross entropy of rows hidden [..., cols] over a vocabulary, with the logits scale * hidden . table[v] of a
+    table [vocabulary, cols]: (loss, lse), both float32 [...], lse the logarithm of the sum of the logits' exponentials.
+    The logits are never written. A row with a negative target is left out (both are 0) and costs next to nothing, so that a
+    batch with few predicted tokens needs no selection; a target outside the vocabulary gives NaN. autograd follows
+    loss."""
+    if stream is None:
+        return _native.cross_entropy(hidden, table, targets, scale)
+    return _on(stream, (hidden, table, targets), _native.cross_entropy, hidden, table, targets, scale)
+
+
+def cross_entropy_backward(dloss, hidden, table, targets, loss, lse, scale: float = 1.0, stream=None):
+    """Gradients (dhidden, dtable) of `cross_entropy` for the gradient dloss of its losses (float32), from the loss and lse
+    that it gave."""
+    args = dloss, hidden, table, targets, loss, lse
+    if stream is None:
+        return _native.cross_entropy_backward(*args, scale, True, True)
+    return _on(stream, args, _native.cross_entropy_backward, *args, scale, True, True)
+
+
+class _Linear(torch.autograd.Function):
+    """What `linear` is to autograd: of its input it keeps 8-bit rows, and those only if the weight has a gradient."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, rows):
+        y = _native.linear(x, weight, bias, None)
+        values = scale = None
+        if ctx.needs_input_grad[1]:
+            values, scale, cols = _native.quantize_rows(x) if rows is None else rows
+            if cols != x.shape[-1] or values.shape[0] != x[..., 0].numel():
+                raise ValueError(f"rows in 8 bits of {values.shape[0]} x {cols} for x {tuple(x.shape)}")
+        ctx.save_for_backward(values, scale, weight)
+        ctx.bias_type = torch.float32 if bias is None else bias.dtype
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        return *_native.linear_backward(dy, *ctx.saved_tensors, *ctx.needs_input_grad[:3], ctx.bias_type), None
+
+
+def linear(x, weight, bias=None, rows: QuantizedRows | None = None, stream=None):
+    """x [..., cols] by a weight [n, cols] of its type, plus bias [n] (float32 or of x's type): [..., n]. For autograd it
+    keeps x in 8 bits (`quantize_rows`), from which the weight's gradient is made; x's own gradient does not need x. `rows`:
+    x's 8-bit rows, where the caller has them already, as for several layers of one input."""
+    if stream is None:
+        return _native.linear(x, weight, bias, rows)
+    kept = () if rows is None else (rows.values, rows.scale)
+    return _on(stream, (x, weight, bias, *kept), _native.linear, x, weight, bias, rows)
+
+
+def linear_backward(dy, rows: QuantizedRows, weight, stream=None):
+    """Gradients (dx, dweight, dbias) of `linear` for the gradient dy of its result, from the 8-bit rows of its input. They
+    have dy's type."""
+    if rows.cols != weight.shape[-1]:
+        raise ValueError(f"rows of {rows.cols} columns for a weight {tuple(weight.shape)}")
+    args = dy, rows.values, rows.scale, weight, True, True, True, dy.dtype
+    if stream is None:
+        return _native.linear_backward(*args)
+    return _on(stream, args[:4], _native.linear_backward, *args)
 
 
 def _overlap(tensors):

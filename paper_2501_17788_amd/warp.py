@@ -28,6 +28,9 @@ EXPORTS = (
     "warp_t_prime_policy", "warp_set_scoring", "warp_build_index", "warp_search_noalloc",
     "warp_kmeans_sample_size", "warp_layer_norm", "warp_layer_norm_backward", "warp_layer_norm_backward_scratch",
     "warp_layer_norm_int8", "warp_quantize_rows", "warp_linear_int8", "warp_adamw_step", "warp_adamw_moments",
+    "warp_embedding", "warp_embedding_backward", "warp_embedding_backward_scratch", "warp_cross_entropy",
+    "warp_cross_entropy_backward", "warp_cross_entropy_scratch", "warp_linear", "warp_linear_scratch",
+    "warp_linear_backward", "warp_linear_backward_scratch",
 )
 
 
@@ -79,6 +82,18 @@ def _load() -> ctypes.CDLL:
         "warp_linear_int8": ([P, i64, P, i64, P, i64, P, i32, i32, P, P, i64, i32, P], ctypes.c_int),
         "warp_adamw_step": ([P, i32, i32, i32, i32, P, P, P, P, f64, f64, f64, f64, f64, i64, P, P], ctypes.c_int),
         "warp_adamw_moments": ([P, P, P, P, i64, P, P, P], ctypes.c_int),
+        "warp_embedding": ([P, i32, i64, P, i64, i64, i32, i32, f32, P, i64, P], ctypes.c_int),
+        "warp_embedding_backward": ([P, i64, P, i32, i64, i64, i32, i32, f32, P, i64, P, i64, P], ctypes.c_int),
+        "warp_embedding_backward_scratch": ([i64, i64, i32, P], ctypes.c_int),
+        "warp_cross_entropy": ([P, i64, i64, i32, i32, P, i64, i64, P, i32, f32, P, P, P, i64, P], ctypes.c_int),
+        "warp_cross_entropy_backward": ([P, P, i64, i64, i32, i32, P, i64, i64, P, i32, f32, P, P, P, i64, P, i64, P, i64,
+                                         P], ctypes.c_int),
+        "warp_cross_entropy_scratch": ([i64, i32, i32, P, i64, i64, P, P], ctypes.c_int),
+        "warp_linear": ([P, i64, i64, i32, i32, P, i64, i32, P, i32, P, i64, P, i64, P], ctypes.c_int),
+        "warp_linear_scratch": ([P, i64, i64, i32, i32, P, i64, i32, P], ctypes.c_int),
+        "warp_linear_backward": ([P, i64, i64, i32, i32, P, i64, P, i32, P, i64, P, i64, P, i64, P, i32, P, i64, P],
+                                 ctypes.c_int),
+        "warp_linear_backward_scratch": ([P, i64, i64, i32, i32, i32, P, i64, P], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         f = getattr(lib, name)

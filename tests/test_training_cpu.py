@@ -1,0 +1,180 @@
+"""Refusals and sizes of the operators that train a token encoder, before a device is touched."""
+import ctypes
+
+import pytest
+
+torch = pytest.importorskip("torch")
+w = pytest.importorskip("paper_2501_17788_amd")
+
+lib = w.lib
+P = 1 << 20  # an aligned address that no call below reads
+BIG = 1 << 40
+
+
+def refused(rc, code, needle):
+    assert rc == code, (rc, w.last_error())
+    assert needle in w.last_error(), w.last_error()
+
+
+def embed(**over):
+    a = dict(ids=P, id_bytes=8, tokens=4, table=P, table_stride=64, vocabulary=9, cols=64, dtype=0, scale=1.0, out=P,
+             out_stride=64, stream=None)
+    a.update(over)
+    return lib.warp_embedding(*a.values())
+
+
+def embed_back(**over):
+    a = dict(dy=P, dy_stride=64, ids=P, id_bytes=8, tokens=4, vocabulary=9, cols=64, dtype=0, scale=1.0, dtable=P,
+             dtable_stride=64, scratch=P, bytes=BIG, stream=None)
+    a.update(over)
+    return lib.warp_embedding_backward(*a.values())
+
+
+@pytest.mark.parametrize("call", [embed, embed_back])
+@pytest.mark.parametrize("over,code,needle", [
+    (dict(tokens=-1), w.EINVAL, "tokens"), (dict(vocabulary=0), w.EINVAL, "vocabulary"), (dict(cols=0), w.EINVAL, "cols"),
+    (dict(tokens=(1 << 25) + 1), w.ENOTSUP, "2^25"), (dict(vocabulary=(1 << 25) + 1), w.ENOTSUP, "2^25"),
+    (dict(cols=(1 << 20) + 1), w.ENOTSUP, "2^20"), (dict(id_bytes=2), w.EINVAL, "ids of 4 or 8"),
+    (dict(dtype=3), w.EINVAL, "dtype"), (dict(scale=float("nan")), w.EINVAL, "scale"),
+    (dict(scale=float("inf")), w.EINVAL, "scale"), (dict(ids=None), w.EINVAL, "null"), (dict(ids=P + 4), w.EINVAL, "misaligned"),
+])
+def test_embedding_refusals(call, over, code, needle):
+    refused(call(**over), code, needle)
+
+
+@pytest.mark.parametrize("over,needle", [(dict(table=None), "null"), (dict(out=None), "null"), (dict(table=P + 2), "misaligned"),
+                                         (dict(out=P + 1), "misaligned"), (dict(table_stride=63), "stride"),
+                                         (dict(out_stride=-64), "stride")])
+def test_lookup_refusals(over, needle):
+    refused(embed(**over), w.EINVAL, needle)
+
+
+@pytest.mark.parametrize("over,needle", [(dict(dy=None), "null"), (dict(dtable=None), "null"), (dict(dy=P + 2), "misaligned"),
+                                         (dict(dy_stride=0), "stride"), (dict(dtable_stride=63), "stride"),
+                                         (dict(scratch=None), "scratch"), (dict(bytes=100), "scratch"),
+                                         (dict(scratch=P + 8), "scratch")])
+def test_embedding_backward_refusals(over, needle):
+    refused(embed_back(**over), w.EINVAL, needle)
+
+
+def loss(**over):
+    a = dict(hidden=P, hidden_stride=64, tokens=4, cols=64, dtype=0, table=P, table_stride=64, vocabulary=9, targets=P,
+             target_bytes=8, scale=1.0, loss=P, lse=P, scratch=P, bytes=BIG, stream=None)
+    a.update(over)
+    return lib.warp_cross_entropy(*a.values())
+
+
+def loss_back(**over):
+    a = dict(dloss=P, hidden=P, hidden_stride=64, tokens=4, cols=64, dtype=0, table=P, table_stride=64, vocabulary=9,
+             targets=P, target_bytes=8, scale=1.0, loss=P, lse=P, dhidden=P, dhidden_stride=64, dtable=P, dtable_stride=64,
+             scratch=P, bytes=BIG, stream=None)
+    a.update(over)
+    return lib.warp_cross_entropy_backward(*a.values())
+
+
+@pytest.mark.parametrize("call", [loss, loss_back])
+@pytest.mark.parametrize("over,code,needle", [
+    (dict(tokens=-1), w.EINVAL, "tokens"), (dict(vocabulary=0), w.EINVAL, "vocabulary"), (dict(cols=0), w.EINVAL, "cols"),
+    (dict(tokens=(1 << 22) + 1), w.ENOTSUP, "2^22"), (dict(vocabulary=(1 << 25) + 1), w.ENOTSUP, "2^25"),
+    (dict(cols=(1 << 14) + 1), w.ENOTSUP, "2^14"), (dict(dtype=-1), w.EINVAL, "dtype"),
+    (dict(hidden=None), w.EINVAL, "null"), (dict(table=None), w.EINVAL, "null"), (dict(targets=None), w.EINVAL, "null"),
+    (dict(loss=None), w.EINVAL, "null"), (dict(lse=None), w.EINVAL, "null"), (dict(hidden_stride=63), w.EINVAL, "stride"),
+    (dict(table_stride=1), w.EINVAL, "stride"), (dict(hidden=P + 2), w.EINVAL, "misaligned"),
+    (dict(table=P + 1), w.EINVAL, "misaligned"), (dict(targets=P + 4), w.EINVAL, "misaligned"),
+    (dict(loss=P + 2), w.EINVAL, "misaligned"), (dict(target_bytes=1), w.EINVAL, "targets of 4 or 8"),
+    (dict(scale=float("nan")), w.EINVAL, "scale"), (dict(scratch=None), w.EINVAL, "scratch"),
+    (dict(bytes=1000), w.EINVAL, "scratch"), (dict(scratch=P + 4), w.EINVAL, "scratch"),
+])
+def test_cross_entropy_refusals(call, over, code, needle):
+    refused(call(**over), code, needle)
+
+
+@pytest.mark.parametrize("over,needle", [(dict(dloss=None), "null"), (dict(dloss=P + 1), "misaligned"),
+                                         (dict(dhidden=P + 2), "misaligned"), (dict(dtable=P + 2), "misaligned"),
+                                         (dict(dhidden_stride=8), "stride"), (dict(dtable_stride=8), "stride")])
+def test_cross_entropy_backward_refusals(over, needle):
+    refused(loss_back(**over), w.EINVAL, needle)
+
+
+def linear(**over):
+    a = dict(x=P, x_stride=64, rows=4, cols=64, dtype=0, weight=P, weight_stride=64, n=9, bias=None, bias_dtype=0, y=P,
+             y_stride=9, scratch=P, bytes=BIG, stream=None)
+    a.update(over)
+    return lib.warp_linear(*a.values())
+
+
+def linear_back(**over):
+    a = dict(dy=P, dy_stride=9, rows=4, n=9, dtype=0, q=P, q_stride=128, q_scale=P, cols=64, weight=P, weight_stride=64, dx=P,
+             dx_stride=64, dw=P, dw_stride=64, db=P, db_dtype=0, scratch=P, bytes=BIG, stream=None)
+    a.update(over)
+    return lib.warp_linear_backward(*a.values())
+
+
+@pytest.mark.parametrize("call", [linear, linear_back])
+@pytest.mark.parametrize("over,code,needle", [
+    (dict(rows=-1), w.EINVAL, "rows"), (dict(n=0), w.EINVAL, "n and cols"), (dict(cols=0), w.EINVAL, "n and cols"),
+    (dict(rows=(1 << 24) + 1), w.ENOTSUP, "2^24"), (dict(n=(1 << 20) + 1), w.ENOTSUP, "2^20"),
+    (dict(rows=1 << 24, n=1 << 14), w.ENOTSUP, "2^37"), (dict(cols=1 << 18, n=1 << 17), w.ENOTSUP, "2^37"),
+    (dict(dtype=9), w.EINVAL, "dtype"), (dict(weight=None), w.EINVAL, "null"), (dict(weight=P + 2), w.EINVAL, "misaligned"),
+    (dict(weight_stride=63), w.EINVAL, "stride"), (dict(scratch=None), w.EINVAL, "scratch"),
+    (dict(bytes=8), w.EINVAL, "scratch"), (dict(scratch=P + 1), w.EINVAL, "scratch"),
+])
+def test_linear_refusals(call, over, code, needle):
+    refused(call(**over), code, needle)
+
+
+@pytest.mark.parametrize("over,needle", [(dict(x=None), "null"), (dict(y=None), "null"), (dict(x=P + 2), "misaligned"),
+                                         (dict(x_stride=63), "stride"), (dict(y_stride=8), "stride"),
+                                         (dict(bias=P, bias_dtype=1), "bias"), (dict(bias=P, bias_dtype=7), "bias"),
+                                         (dict(bias=P + 2), "misaligned")])
+def test_linear_forward_refusals(over, needle):
+    refused(linear(**over), w.EINVAL, needle)
+
+
+@pytest.mark.parametrize("over,needle", [(dict(dy=None), "null"), (dict(dy=P + 2), "misaligned"), (dict(dy_stride=8), "stride"),
+                                         (dict(dx_stride=63), "stride"), (dict(dw_stride=63), "stride"),
+                                         (dict(dx=P + 1), "misaligned"), (dict(q=None), "null"), (dict(q_scale=None), "null"),
+                                         (dict(q_stride=64), "int8 rows"), (dict(q_stride=130), "int8 rows"),
+                                         (dict(q=P + 8), "int8 rows"), (dict(q_scale=P + 2), "int8 rows"),
+                                         (dict(db_dtype=2), "dbias"), (dict(db=P + 2), "misaligned")])
+def test_linear_backward_refusals(over, needle):
+    refused(linear_back(**over), w.EINVAL, needle)
+
+
+def test_scratch_sizes():
+    """Many rows of 16-bit operands of ordinary alignment take none; other operands a copy; more rows never take less."""
+    n = ctypes.c_int64()
+    assert not lib.warp_linear_scratch(P, 1024, 65_536, 1024, 2, P, 1024, 1024, ctypes.byref(n)) and n.value == 0
+    assert not lib.warp_linear_scratch(P + 2, 1024, 65_536, 1024, 2, P, 1024, 1024, ctypes.byref(n))
+    assert 65_536 * 1024 * 2 <= n.value < 65_536 * 1024 * 2 + 4096
+    assert not lib.warp_linear_scratch(P, 1024, 4096, 1024, 0, P, 1024, 1024, ctypes.byref(n))
+    assert n.value >= (4096 + 1024) * 1024 * 6
+    assert lib.warp_linear_scratch(P, 1024, 4096, 1024, 0, P, 1024, 1024, None) == w.EINVAL
+    assert lib.warp_linear_backward_scratch(P, 64, -1, 64, 0, 64, P, 64, ctypes.byref(n)) == w.EINVAL
+    assert lib.warp_embedding_backward_scratch(1, 0, 1, ctypes.byref(n)) == w.EINVAL
+    assert lib.warp_cross_entropy_scratch(1, 1, 0, P, 1, 0, ctypes.byref(n), None) == w.EINVAL
+    # G is never larger than a piece, whatever the vocabulary
+    sizes = []
+    for vocabulary in (100, 1000, 30_000, 250_001, 1 << 24):
+        m = ctypes.c_int64()
+        assert not lib.warp_cross_entropy_scratch(16_384, 1024, 2, P, 1024, vocabulary, ctypes.byref(n), ctypes.byref(m))
+        sizes.append(m.value)
+        assert n.value < 600 << 20
+    assert max(sizes) < 1000 << 20
+    last = 0
+    for tokens in (0, 1, 100, 16_384, 100_000):
+        assert not lib.warp_cross_entropy_scratch(tokens, 64, 1, P, 64, 5000, ctypes.byref(n), None)
+        assert n.value >= last
+        last = n.value
+
+
+def test_host_tensors_are_refused():
+    x, ids = torch.zeros(3, 8), torch.zeros(3, dtype=torch.int64)
+    rows = w.QuantizedRows(torch.zeros(3, 128, dtype=torch.int8), torch.zeros(3), 8)
+    for call in (lambda: w.embedding(ids, x), lambda: w.embedding_backward(x, ids, 3), lambda: w.linear(x, x),
+                 lambda: w.linear_backward(torch.zeros(3, 3), rows, x), lambda: w.cross_entropy(x, x, ids),
+                 lambda: w.cross_entropy_backward(ids.float(), x, x, ids, ids.float(), ids.float())):
+        with pytest.raises(ValueError, match="device tensors"):
+            call()
+    with pytest.raises(ValueError, match="columns"):
+        w.linear_backward(torch.zeros(3, 3), rows._replace(cols=9), x)
