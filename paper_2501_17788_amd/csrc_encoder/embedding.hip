@@ -4,6 +4,8 @@
 // id (stably, so that a row's tokens come in order), chunks of 64 sorted tokens that belong to one row are summed on
 // their own (a common token has thousands), and each row of the table adds its chunks and what is left over of its
 // tokens. Rows without tokens are written as zeros by the same kernel: the gradient is written once.
+#include <type_traits>
+
 #include "encoder.h"
 
 namespace warp {
@@ -41,41 +43,53 @@ struct LookupArgs {
     float scale;
     void* out;
     int64_t out_stride;
+    bool past_caches;
 };
 
-// One wave a token.
-template <typename T, int V, int NV>
+// One wave for R tokens and a block of 64 V NV columns, all its rows under way at once.
+template <typename T, int V, int NV, int R>
 __global__ __launch_bounds__(256) void k_lookup(LookupArgs g) {
     const int lane = threadIdx.x & 63;
-    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (t >= g.tokens) return;
-    const int64_t id = id_at(g.ids, g.wide, t);
-    const T* row = (const T*)g.table + id * g.table_stride;
-    T* out = (T*)g.out + t * g.out_stride;
-    const float fill = id < 0 ? 0.f : __builtin_nanf("");
-    const bool inside = id >= 0 && id < g.vocabulary;
-    Vec<T, V> x[NV];
+    const int64_t t0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * R;
+    if (t0 >= g.tokens) return;
     Columns<V> c[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        c[j] = column_of<V>(blockIdx.y, j, NV, lane, g.cols);
-        if (c[j].in && inside) x[j] = load_vec<T, V>(row + c[j].at);
+    for (int j = 0; j < NV; ++j) c[j] = column_of<V>(blockIdx.y, j, NV, lane, g.cols);
+    int64_t id[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) id[r] = id_at(g.ids, g.wide, t0 + r < g.tokens ? t0 + r : t0);
+    Vec<T, V> x[R][NV];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const bool inside = id[r] >= 0 && id[r] < g.vocabulary;
+        const T* row = (const T*)g.table + (inside ? id[r] : 0) * g.table_stride;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (c[j].in) x[r][j] = load_vec<T, V>(row + c[j].at);
     }
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        if (!c[j].in) continue;
+    for (int r = 0; r < R; ++r) {
+        if (t0 + r >= g.tokens) return;
+        const bool inside = id[r] >= 0 && id[r] < g.vocabulary;
+        const float fill = id[r] < 0 ? 0.f : __builtin_nanf("");
+        T* out = (T*)g.out + (t0 + r) * g.out_stride;
 #pragma unroll
-        for (int e = 0; e < V; ++e) x[j].e[e] = inside ? (T)((float)x[j].e[e] * g.scale) : (T)fill;
-        store_vec<T, V>(out + c[j].at, x[j]);
+        for (int j = 0; j < NV; ++j) {
+            if (!c[j].in) continue;
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[r][j].e[e] = inside ? (T)((float)x[r][j].e[e] * g.scale) : (T)fill;
+            if (g.past_caches) stream_out<T, V>(out + c[j].at, x[r][j]);
+            else store_vec<T, V>(out + c[j].at, x[r][j]);
+        }
     }
 }
 
 // ---------------------------------------------------------------------------- sorting tokens by id
 
-// Stable radix sort by digits of at most 9 bits. At most 256 tiles of equal size; a tile's eight waves hold neighbouring
+// Stable radix sort by digits of at most 9 bits. At most 128 tiles of equal size; a tile's eight waves hold neighbouring
 // parts of it.
 constexpr int kDigits = 512, kSortThreads = 512, kSortWaves = kSortThreads / kWave;
-constexpr int kMaxTiles = 256, kTileUnit = 2048;
+constexpr int kMaxTiles = 128, kTileUnit = 1024;
 constexpr int kSmall = 4096;  // so many tokens are sorted by one workgroup, in LDS
 
 struct SortPlan {
@@ -152,13 +166,15 @@ struct SortArgs {
     int2* spans;
 };
 
-// Counts of a tile's digits; the first pass also clears the rows' spans.
+// Counts of a tile's digits; in the first pass the workgroups behind the tiles' clear the rows' spans.
 __global__ __launch_bounds__(kSortThreads) void k_token_counts(SortArgs g) {
     __shared__ uint32_t count[kDigits];
+    if ((int)blockIdx.x >= g.tiles) {
+        clear_spans(g.spans, g.vocabulary, (int64_t)((int)blockIdx.x - g.tiles) * kSortThreads + threadIdx.x,
+                    (int64_t)((int)gridDim.x - g.tiles) * kSortThreads);
+        return;
+    }
     count[threadIdx.x] = 0;
-    if (g.first)
-        clear_spans(g.spans, g.vocabulary, (int64_t)blockIdx.x * kSortThreads + threadIdx.x,
-                    (int64_t)gridDim.x * kSortThreads);
     __syncthreads();
     const int64_t start = (int64_t)blockIdx.x * g.tile;
     const uint32_t mask = (1u << g.digit_bits) - 1;
@@ -188,6 +204,7 @@ __global__ __launch_bounds__(kSortThreads) void k_token_places(SortArgs g) {
         if (t < g.tokens) atomicAdd(&next[w][key_at(t) >> g.shift & mask], 1u);
     }
     uint32_t before = 0, all = 0;
+#pragma unroll 16
     for (int t = 0; t < g.tiles; ++t) {
         const uint32_t c = g.counts[(int64_t)t * kDigits + tid];
         all += c;
@@ -272,52 +289,68 @@ struct SumArgs {
     float scale;
     void* out;
     int64_t out_stride;
-    int64_t heavy;  // workgroups for rows with whole chunks
+    int64_t common;  // whole chunks
+    bool past_caches;
 };
 
-template <int V, int NV>
-struct Sums {
-    float v[NV][V] = {};
-};
-
-// Adds the rows of dy at sorted places [from, to), up to U of them under way.
-template <typename T, int V, int NV>
-__device__ __forceinline__ void add_rows(Sums<V, NV>& s, const SumArgs& g, int64_t from, int64_t to, int64_t by,
-                                         const Columns<V> (&c)[NV]) {
-    constexpr int U = 4;
-    for (int64_t i = from; i < to; i += U * by) {
-        Vec<T, V> x[U][NV];
+// Rows of dy at places that the lanes hold, U from lane `from` on, all under way at once.
+template <typename T, int V, int U>
+struct Batch {
+    Vec<T, V> x[U];
+    __device__ __forceinline__ void load(const SumArgs& g, uint32_t places, int from, Columns<V> c) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t at = i + u * by;
-            if (at >= to) break;
-            const T* row = (const T*)g.dy + (int64_t)g.places[at] * g.dy_stride;
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-                if (c[j].in) x[u][j] = load_vec<T, V>(row + c[j].at);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (i + u * by >= to) break;
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) s.v[j][e] += (float)x[u][j].e[e];
+            const uint32_t t = (uint32_t)__builtin_amdgcn_readlane((int)places, from + u);
+            if (c.in) x[u] = load_vec<T, V>((const T*)g.dy + (int64_t)t * g.dy_stride + c.at);
         }
     }
+    __device__ __forceinline__ void add(float (&sum)[V]) const {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] += (float)x[u].e[e];
+    }
+};
+// Adds those at places [from, to).
+template <typename T, int V>
+__device__ __forceinline__ void add_places(float (&sum)[V], const SumArgs& g, uint32_t places, int from, int to, Columns<V> c) {
+    auto add = [&](auto count) {
+        Batch<T, V, count.value> b;
+        b.load(g, places, from, c);
+        b.add(sum);
+        from += count.value;
+    };
+    while (to - from >= 8) add(std::integral_constant<int, 8>{});
+    if (to - from >= 4) add(std::integral_constant<int, 4>{});
+    if (to - from >= 2) add(std::integral_constant<int, 2>{});
+    if (to - from >= 1) add(std::integral_constant<int, 1>{});
 }
 
-// One wave a chunk and column block: the chunk's part of the rows' spans, and its sum if all of it is one row's.
-template <typename T, int V, int NV>
+// The sums of a workgroup's four waves, in wave 0.
+template <int V>
+__device__ __forceinline__ void join_waves(float (&sum)[V], float (&joined)[3][V][kWave]) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    __syncthreads();  // the last ones have been read
+    if (w) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) joined[w - 1][e][lane] = sum[e];
+    }
+    __syncthreads();
+    if (w) return;
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[e] += joined[0][e][lane] + joined[1][e][lane] + joined[2][e][lane];
+}
+
+// One workgroup a chunk and column block: the chunk's part of the rows' spans, and its sum if all of it is one row's.
+template <typename T, int V>
 __global__ __launch_bounds__(256) void k_sum_chunks(SumArgs g) {
-    const int lane = threadIdx.x & 63;
-    const int64_t chunk = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t start = chunk * kChunk;
-    if (start >= g.tokens) return;
+    __shared__ float joined[3][V][kWave];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t chunk = blockIdx.x, start = chunk * kChunk;
     const int64_t i = start + lane;
     const bool in = i < g.tokens;
     const uint32_t key = in ? g.keys[i] : ~0u;
-    if (blockIdx.y == 0 && in) {
+    if (blockIdx.y == 0 && w == 0 && in) {
         const uint32_t before = i ? g.keys[i - 1] : ~0u;
         if (key != before) {
             if (key < g.vocabulary) g.spans[key].x = (int)i;
@@ -327,140 +360,164 @@ __global__ __launch_bounds__(256) void k_sum_chunks(SumArgs g) {
     }
     const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane((int)key);
     if (__ballot(key == first) != ~0ull || first >= g.vocabulary) return;
-    Columns<V> c[NV];
+    const Columns<V> c = column_of<V>(blockIdx.y, 0, 1, lane, g.cols);
+    float sum[V] = {};
+    add_places<T, V>(sum, g, g.places[i], 16 * w, 16 * w + 16, c);
+    join_waves<V>(sum, joined);
+    if (w || !c.in) return;
+    Vec<float, V> r;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) c[j] = column_of<V>(blockIdx.y, j, NV, lane, g.cols);
-    Sums<V, NV> s;
-    add_rows<T, V, NV>(s, g, start, start + kChunk, 1, c);
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-        if (c[j].in) {
-            Vec<float, V> r;
-#pragma unroll
-            for (int e = 0; e < V; ++e) r.e[e] = s.v[j][e];
-            store_vec<float, V>(g.chunks + chunk * g.chunk_stride + c[j].at, r);
-        }
+    for (int e = 0; e < V; ++e) r.e[e] = sum[e];
+    store_vec<float, V>(g.chunks + chunk * g.chunk_stride + c.at, r);
 }
 
-template <typename T, int V, int NV>
-__device__ __forceinline__ void store_sums(const Sums<V, NV>& s, const SumArgs& g, int64_t row, const Columns<V> (&c)[NV]) {
-    T* out = (T*)g.out + row * g.out_stride;
+template <typename T, int V>
+__device__ __forceinline__ void store_sums(const float (&sum)[V], const SumArgs& g, int64_t row, Columns<V> c) {
+    if (!c.in) return;
+    Vec<T, V> r;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-        if (c[j].in) {
-            Vec<T, V> r;
-#pragma unroll
-            for (int e = 0; e < V; ++e) r.e[e] = (T)(s.v[j][e] * g.scale);
-            store_vec<T, V>(out + c[j].at, r);
-        }
+    for (int e = 0; e < V; ++e) r.e[e] = (T)(sum[e] * g.scale);
+    T* out = (T*)g.out + row * g.out_stride + c.at;
+    if (g.past_caches) stream_out<T, V>(out, r);
+    else store_vec<T, V>(out, r);
 }
 
-// The first `heavy` workgroups: one for four chunks; each chunk that is the first whole one of a row stands for it, and
-// the workgroup's waves share the row's terms: tokens before the first whole chunk, chunks, tokens behind the last. The
-// other workgroups: one wave a row that has no whole chunk.
-template <typename T, int V, int NV>
+// The first `common` workgroups: one for each chunk; the first whole chunk of a row stands for it, and the
+// workgroup's waves share the row's terms: tokens before that chunk, whole chunks, tokens behind the last one. The
+// other workgroups: kRows neighbouring rows a wave, those that have no whole chunk.
+constexpr int kRows = 4;
+template <typename T, int V>
 __global__ __launch_bounds__(256) void k_sum_rows(SumArgs g) {
-    __shared__ float joined[4][NV * V][kWave];
+    __shared__ float joined[3][V][kWave];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    Columns<V> c[NV];
+    const Columns<V> c = column_of<V>(blockIdx.y, 0, 1, lane, g.cols);
+    if ((int64_t)blockIdx.x >= g.common) {
+        const int64_t row0 = (((int64_t)blockIdx.x - g.common) * 4 + w) * kRows;
+        if (row0 >= g.vocabulary) return;
+        int2 span = make_int2(0, 0);
+        if (lane < kRows && row0 + lane < g.vocabulary) span = g.spans[row0 + lane];
+        // The rows' tokens as one list, which is gone through in steps of eight whatever row they belong to, the next
+        // eight under way. Lane r holds row r's end in it, and the sorted token of its entry i is i + shift.
+        const bool common = (span.x + kChunk - 1) / kChunk < span.y / kChunk;
+        const int size = common ? 0 : span.y - span.x;
+        int end = size;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) c[j] = column_of<V>(blockIdx.y, j, NV, lane, g.cols);
-    auto whole = [&](int2 span, int64_t& from, int64_t& to) {  // whole chunks [from, to)
-        from = (span.x + kChunk - 1) / kChunk, to = span.y / kChunk;
-        return from < to;
-    };
-    int64_t from, to;
-    if ((int64_t)blockIdx.x >= g.heavy) {
-        const int64_t row = ((int64_t)blockIdx.x - g.heavy) * 4 + w;
-        if (row >= g.vocabulary) return;
-        const int2 span = g.spans[row];
-        if (whole(span, from, to)) return;
-        Sums<V, NV> s;
-        add_rows<T, V, NV>(s, g, span.x, span.y, 1, c);
-        store_sums<T, V, NV>(s, g, row, c);
+        for (int d = 1; d < kRows; d <<= 1) {
+            const int before = __shfl_up(end, d);
+            if (lane >= d) end += before;
+        }
+        const int shift = span.x - (end - size);
+        const unsigned long long skipped = __ballot(common || row0 + lane >= g.vocabulary);
+        const int total = __builtin_amdgcn_readlane(end, kRows - 1);
+        auto places_of = [&](int base) {  // 64 entries
+            const int i = base + lane;
+            int at = i + __builtin_amdgcn_readlane(shift, 0);
+#pragma unroll
+            for (int r = 1; r < kRows; ++r)
+                if (i >= __builtin_amdgcn_readlane(end, r - 1)) at = i + __builtin_amdgcn_readlane(shift, r);
+            return i < total ? g.places[at] : 0;  // behind the end token 0, which is not added
+        };
+        constexpr int U = 8;
+        Batch<T, V, U> now, next;
+        uint32_t places = places_of(0);
+        float sum[V] = {};
+        if (total) now.load(g, places, 0, c);
+        int i = 0, r = 0;
+        auto finish = [&] {  // rows that end at entry i
+            while (r < kRows && __builtin_amdgcn_readlane(end, r) == i) {
+                if (!(skipped >> r & 1)) store_sums<T, V>(sum, g, row0 + r, c);
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[e] = 0.f;
+                ++r;
+            }
+        };
+        finish();
+        while (i < total) {
+            const int ahead = i + U;
+            if (ahead < total) {
+                if (ahead % kChunk == 0) places = places_of(ahead);
+                next.load(g, places, ahead % kChunk, c);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (i >= total) break;
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[e] += (float)now.x[u].e[e];
+                ++i;
+                finish();
+            }
+            now = next;
+        }
         return;
     }
-    for (int u = 0; u < 4; ++u) {
-        const int64_t chunk = (int64_t)blockIdx.x * 4 + u;
-        if ((chunk + 1) * kChunk > g.tokens) return;
-        const uint32_t row = g.keys[chunk * kChunk];
-        if (row >= g.vocabulary) return;  // and all that follow
-        const int2 span = g.spans[row];
-        if (!whole(span, from, to) || from != chunk) continue;
-        Sums<V, NV> s;
-        add_rows<T, V, NV>(s, g, span.x + w, from * kChunk, 4, c);
-        constexpr int U = 4;
-        for (int64_t i = from + w; i < to; i += 4 * U) {
-            Vec<float, V> x[U][NV];
+    const int64_t chunk = blockIdx.x;
+    const uint32_t row = g.keys[chunk * kChunk];
+    if (row >= g.vocabulary) return;
+    const int2 span = g.spans[row];
+    const int first = (span.x + kChunk - 1) / kChunk, end = span.y / kChunk;  // whole chunks
+    if (first != chunk || first >= end) return;
+    float sum[V] = {};
+    const int before = first * kChunk - span.x, behind = span.y - end * kChunk;  // below 64 each
+    uint32_t places = lane < before ? g.places[span.x + lane] : 0;
+    add_places<T, V>(sum, g, places, before * w / 4, before * (w + 1) / 4, c);
+    auto add = [&](int i, auto count) {
+        constexpr int U = count.value;
+        Vec<float, V> x[U];
 #pragma unroll
-            for (int n = 0; n < U; ++n) {
-                if (i + 4 * n >= to) break;
+        for (int u = 0; u < U; ++u)
+            if (c.in) x[u] = load_vec<float, V>(g.chunks + (int64_t)(i + 4 * u) * g.chunk_stride + c.at);
 #pragma unroll
-                for (int j = 0; j < NV; ++j)
-                    if (c[j].in) x[n][j] = load_vec<float, V>(g.chunks + (i + 4 * n) * g.chunk_stride + c[j].at);
-            }
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int n = 0; n < U; ++n) {
-                if (i + 4 * n >= to) break;
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) s.v[j][e] += x[n][j].e[e];
-            }
-        }
-        add_rows<T, V, NV>(s, g, to * kChunk + w, span.y, 4, c);
-        __syncthreads();  // the last row's sums have been read
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int e = 0; e < V; ++e) joined[w][j * V + e][lane] = s.v[j][e];
-        __syncthreads();
-        if (w == 0) {
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    float sum = s.v[j][e];
-#pragma unroll
-                    for (int o = 1; o < 4; ++o) sum += joined[o][j * V + e][lane];
-                    s.v[j][e] = sum;
-                }
-            store_sums<T, V, NV>(s, g, row, c);
-        }
-    }
+            for (int e = 0; e < V; ++e) sum[e] += x[u].e[e];
+    };
+    int i = first + w;
+    for (; i + 12 < end; i += 16) add(i, std::integral_constant<int, 4>{});
+    for (; i < end; i += 4) add(i, std::integral_constant<int, 1>{});
+    places = lane < behind ? g.places[end * kChunk + lane] : 0;
+    add_places<T, V>(sum, g, places, behind * w / 4, behind * (w + 1) / 4, c);
+    join_waves<V>(sum, joined);
+    if (!w) store_sums<T, V>(sum, g, row, c);
 }
 
 // ---------------------------------------------------------------------------- launches
 
-// A wave's vectors: 16 bytes of a row each, as many as a row has up to four.
+// Vectors of 16 bytes, or single elements where a row is shorter.
 template <typename F>
-void by_columns(int64_t cols, int wide, F f) {
-    const int64_t vectors = cover(cols, (int64_t)wide * kWave);
-    if (cols < wide) f(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, (int64_t)1);
-    else if (vectors <= 1) f(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{}, (int64_t)1);
-    else f(std::integral_constant<int, 0>{}, std::integral_constant<int, 2>{}, cover(vectors, 2));
+void by_width(int64_t cols, int wide, F f) {
+    if (cols < wide) f(std::true_type{}, (int64_t)1);
+    else f(std::false_type{}, cover(cols, (int64_t)wide * kWave));
 }
 
+// Results of more than the last-level cache holds pass it by.
+constexpr int64_t kCached = 256ll << 20;
+
 template <typename T>
-void lookup(const LookupArgs& g, hipStream_t s) {
+void lookup(LookupArgs g, hipStream_t s) {
     constexpr int W = 16 / sizeof(T);
-    by_columns(g.cols, W, [&](auto narrow, auto nv, int64_t blocks) {
-        constexpr int V = narrow.value ? 1 : W, NV = nv.value;
-        hipLaunchKernelGGL((k_lookup<T, V, NV>), dim3((uint32_t)cover(g.tokens, 4), (uint32_t)blocks), dim3(256), 0, s, g);
+    g.past_caches = g.tokens * g.cols * (int64_t)sizeof(T) > kCached;
+    by_width(g.cols, W, [&](auto narrow, int64_t blocks) {
+        constexpr int V = narrow.value ? 1 : W;
+        if (g.tokens < 4096)
+            hipLaunchKernelGGL((k_lookup<T, V, 1, 1>), dim3((uint32_t)cover(g.tokens, 4), (uint32_t)blocks), dim3(256), 0, s,
+                               g);
+        else
+            hipLaunchKernelGGL((k_lookup<T, V, 2, 4>), dim3((uint32_t)cover(g.tokens, 16), (uint32_t)cover(blocks, 2)),
+                               dim3(256), 0, s, g);
     });
 }
 
 template <typename T>
 void sums(SumArgs g, hipStream_t s) {
     constexpr int W = 16 / sizeof(T);
-    by_columns(g.cols, W, [&](auto narrow, auto nv, int64_t blocks) {
-        constexpr int V = narrow.value ? 1 : W, NV = nv.value;
-        const int64_t chunks = cover(g.tokens, kChunk);
+    g.common = g.tokens / kChunk;
+    g.past_caches = g.vocabulary * g.cols * (int64_t)sizeof(T) > kCached;
+    by_width(g.cols, W, [&](auto narrow, int64_t blocks) {
+        constexpr int V = narrow.value ? 1 : W;
         if (g.tokens)
-            hipLaunchKernelGGL((k_sum_chunks<T, V, NV>), dim3((uint32_t)cover(chunks, 4), (uint32_t)blocks), dim3(256), 0, s,
-                               g);
-        g.heavy = cover(g.tokens / kChunk, 4);
-        hipLaunchKernelGGL((k_sum_rows<T, V, NV>), dim3((uint32_t)(g.heavy + cover(g.vocabulary, 4)), (uint32_t)blocks),
+            hipLaunchKernelGGL((k_sum_chunks<T, V>), dim3((uint32_t)cover(g.tokens, kChunk), (uint32_t)blocks), dim3(256), 0,
+                               s, g);
+        hipLaunchKernelGGL((k_sum_rows<T, V>), dim3((uint32_t)(g.common + cover(g.vocabulary, 4 * kRows)), (uint32_t)blocks),
                            dim3(256), 0, s, g);
     });
 }
@@ -522,7 +579,7 @@ int warp_embedding(const void* ids, int32_t id_bytes, int64_t tokens, const void
     if (!rc) rc = check_matrix(what, out, out_stride, tokens, cols, dtype);
     if (!rc) rc = require_device();
     if (rc || !tokens) return rc;
-    const LookupArgs g{ids, id_bytes == 8, tokens, vocabulary, table, table_stride, cols, scale, out, out_stride};
+    const LookupArgs g{ids, id_bytes == 8, tokens, vocabulary, table, table_stride, cols, scale, out, out_stride, false};
     hipStream_t s = (hipStream_t)hip_stream;
     if (dtype == WARP_F32) WARP_LAUNCH(lookup<float>(g, s));
     else if (dtype == WARP_F16) WARP_LAUNCH(lookup<_Float16>(g, s));
@@ -558,21 +615,21 @@ int warp_embedding_backward(const void* dy, int64_t dy_stride, const void* ids, 
     SortArgs a{ids, id_bytes == 8, tokens, vocabulary, p.tile, p.tiles, 0, p.digit_bits, true, nullptr, nullptr, keys[0],
                places[0], (uint32_t*)(base + b.counts), (int2*)(base + b.spans)};
     int sorted = 0;
+    const int clear = (int)(cover(vocabulary, 8 * kSortThreads) < 255 ? cover(vocabulary, 8 * kSortThreads) : 255);
     if (tokens <= kSmall) {
-        const int clear = (int)(cover(vocabulary, 8 * kSortThreads) < 255 ? cover(vocabulary, 8 * kSortThreads) : 255);
         WARP_LAUNCH(hipLaunchKernelGGL(k_sort_few, dim3(1 + clear), dim3(kSortThreads), 0, s, a, p.passes));
     } else {
         for (int i = 0; i < p.passes; ++i) {
             a.shift = i * p.digit_bits, a.first = i == 0;
             a.keys = keys[(i + 1) & 1], a.places = places[(i + 1) & 1];
             a.keys_out = keys[i & 1], a.places_out = places[i & 1];
-            WARP_LAUNCH(hipLaunchKernelGGL(k_token_counts, dim3(p.tiles), dim3(kSortThreads), 0, s, a));
+            WARP_LAUNCH(hipLaunchKernelGGL(k_token_counts, dim3(p.tiles + (i ? 0 : clear)), dim3(kSortThreads), 0, s, a));
             WARP_LAUNCH(hipLaunchKernelGGL(k_token_places, dim3(p.tiles), dim3(kSortThreads), 0, s, a));
         }
         sorted = (p.passes - 1) & 1;
     }
     const SumArgs g{dy, dy_stride, tokens, vocabulary, cols, keys[sorted], places[sorted], a.spans,
-                    (float*)(base + b.chunks), cols, scale, dtable, dtable_stride, 0};
+                    (float*)(base + b.chunks), cols, scale, dtable, dtable_stride, 0, false};
     if (dtype == WARP_F32) WARP_LAUNCH(sums<float>(g, s));
     else if (dtype == WARP_F16) WARP_LAUNCH(sums<_Float16>(g, s));
     else WARP_LAUNCH(sums<__bf16>(g, s));

@@ -37,57 +37,63 @@ struct SelectArgs {
     float* largest;
 };
 
-// One workgroup, eight neighbouring tokens a thread at a time.
+// One workgroup: turns of eight times 1024 neighbouring tokens, whose loads and stores are in one piece a wave.
 __global__ __launch_bounds__(1024) void k_select(SelectArgs g) {
     constexpr int N = 8;
-    __shared__ uint32_t waves[16];
+    __shared__ int32_t waves[N][16];
     __shared__ uint32_t tops[16];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     int32_t count = 0;
     uint32_t top = 0;
     for (int64_t base = 0; base < g.tokens; base += 1024 * N) {
-        const int64_t t0 = base + (int64_t)tid * N;
+        const int64_t t0 = base + tid;
         int64_t y[N];
-        uint32_t mine = 0;
+        uint32_t d[N] = {};
+        auto at = [&](int e) { return t0 + 1024 * e < g.tokens ? t0 + 1024 * e : g.tokens - 1; };
+        if (g.wide) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] = ((const int64_t*)g.targets)[at(e)];
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] = ((const int32_t*)g.targets)[at(e)];
+        }
+        if (g.dloss) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) d[e] = as_u(g.dloss[at(e)]) & 0x7fffffffu;
+        }
+        int32_t rank[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const int64_t t = t0 + e;
-            y[e] = -1;
-            if (t < g.tokens) y[e] = g.wide ? ((const int64_t*)g.targets)[t] : (int64_t)((const int32_t*)g.targets)[t];
-            if (y[e] >= 0 && y[e] < g.vocabulary) {
-                ++mine;
-                if (g.dloss) {
-                    const uint32_t u = as_u(g.dloss[t]) & 0x7fffffffu;
-                    if (u < 0x7f800000u) top = max(top, u);
-                }
-            }
+            const bool in = t0 + 1024 * e < g.tokens && y[e] >= 0 && y[e] < g.vocabulary;
+            const unsigned long long all = __ballot(in);
+            rank[e] = in ? (int32_t)__popcll(all & ((1ull << lane) - 1)) : -1;
+            if (lane == 0) waves[e][w] = (int32_t)__popcll(all);
+            if (in && d[e] < 0x7f800000u) top = max(top, d[e]);
         }
-        uint32_t x = mine;
+        __syncthreads();
+        // this lane's count of the turn's waves before it and behind it: 128 numbers, two a lane
+        const int32_t a = waves[lane >> 3][2 * lane & 15], b = waves[lane >> 3][(2 * lane & 15) + 1];
+        int32_t x = a + b;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t v = __shfl_up(x, d);
-            if (lane >= d) x += v;
+        for (int s = 1; s < 64; s <<= 1) {
+            const int32_t v = __shfl_up(x, s);
+            if (lane >= s) x += v;
         }
-        if (lane == 63) waves[w] = x;
-        __syncthreads();
-        int32_t at = count + (int32_t)(x - mine);
-        for (int i = 0; i < 16; ++i) {
-            if (i < w) at += (int32_t)waves[i];
-            count += (int32_t)waves[i];
-        }
-        __syncthreads();
+        const int32_t before = x - a - b;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const int64_t t = t0 + e;
-            if (t >= g.tokens) break;
-            const bool in = y[e] >= 0 && y[e] < g.vocabulary;
-            if (g.place) g.place[t] = in ? at : y[e] < 0 ? -1 : -2;
-            if (in) {
-                g.list[at] = (int32_t)t;
-                g.target[at] = (int32_t)y[e];
-                ++at;
+            const int32_t pair = __builtin_amdgcn_readlane(before, 8 * e + (w >> 1));
+            const int32_t first = count + pair + (w & 1 ? __builtin_amdgcn_readlane(a, 8 * e + (w >> 1)) : 0);
+            const int64_t t = t0 + 1024 * e;
+            if (t >= g.tokens) continue;
+            g.place[t] = rank[e] >= 0 ? first + rank[e] : y[e] < 0 ? -1 : -2;
+            if (rank[e] >= 0) {
+                g.list[first + rank[e]] = (int32_t)t;
+                g.target[first + rank[e]] = (int32_t)y[e];
             }
         }
+        count += __builtin_amdgcn_readlane(x, 63);
+        __syncthreads();  // before the next turn's counts
     }
     top = wave_max(top);
     if (lane == 0) tops[w] = top;

@@ -71,24 +71,47 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_unpack_int8(const int8_t* q,
     }
 }
 
-__global__ __launch_bounds__(256) void k_join_parts(Join j) {
-    const int64_t c = ((int64_t)blockIdx.x * kWave + (threadIdx.x & 63)) * 4;
-    if (c >= j.n) return;
+// A wave 256 columns of one row. Few rows of many parts: the four waves of a workgroup share a row's parts.
+template <bool SHARED>
+__global__ __launch_bounds__(64 * kRowWaves) void k_join_parts(Join j) {
+    __shared__ float4v joined[SHARED ? kRowWaves : 1][kWave];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t c = ((int64_t)blockIdx.x * kWave + lane) * 4;
     const int64_t m = j.m_now ? *j.m_now : j.m, k = j.k_now ? *j.k_now : j.k;
     const int parts = product_splits(m, j.n, product_steps(k, j.terms), j.tile, j.splits, j.jobs);
     const float factor = j.factor ? *j.factor : 1.f;
     float bias[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) bias[e] = j.bias && c + e < j.n ? load_float(j.bias, j.bias_type, c + e) : 0.f;
-    for (int64_t r = (int64_t)blockIdx.y * kRowWaves + (threadIdx.x >> 6); r < j.rows; r += (int64_t)gridDim.y * kRowWaves) {
+    const int64_t plane = m * j.part_stride;
+    const int by = SHARED ? kRowWaves : 1;
+    for (int64_t r = (int64_t)blockIdx.y * (kRowWaves / by) + (SHARED ? 0 : w); r < j.rows;
+         r += (int64_t)gridDim.y * (kRowWaves / by)) {
         const int64_t from = j.place ? (int64_t)j.place[r] : r;
         float4v sum = {};
-        if (from < -1) sum += __builtin_nanf("");
-        if (from >= 0) {
+        if (from >= 0 && c < j.n) {
             const float* p = j.part + from * j.part_stride + c;
-            for (int i = 0; i < parts; ++i) sum += *(const float4v*)(p + (int64_t)i * m * j.part_stride);
-            sum *= factor;
+            int i = SHARED ? w : 0;
+            for (; i + 7 * by < parts; i += 8 * by) {
+                float4v x[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) x[u] = *(const float4v*)(p + (int64_t)(i + u * by) * plane);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) sum += x[u];
+            }
+            for (; i < parts; i += by) sum += *(const float4v*)(p + (int64_t)i * plane);
         }
+        if constexpr (SHARED) {
+            __syncthreads();  // the last row's have been read
+            joined[w][lane] = sum;
+            __syncthreads();
+            if (w) continue;
+#pragma unroll
+            for (int i = 1; i < kRowWaves; ++i) sum += joined[i][lane];
+        }
+        if (c >= j.n) continue;
+        sum *= factor;
+        if (from < -1) sum += __builtin_nanf("");
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = sum[e] + bias[e];
@@ -194,10 +217,14 @@ hipError_t unpack_int8(const int8_t* q, int64_t q_stride, const float* scale, in
 
 hipError_t join_parts(const Join& j, hipStream_t s) {
     if (!j.rows) return hipSuccess;
+    const uint32_t x = (uint32_t)cover_of(j.n, 256);
     const int64_t groups = cover_of(j.rows, kRowWaves);
     (void)hipGetLastError();
-    hipLaunchKernelGGL(k_join_parts, dim3((uint32_t)cover_of(j.n, 256), (uint32_t)(groups < kMaxRowGroups ? groups : kMaxRowGroups)),
-                       dim3(64 * kRowWaves), 0, s, j);
+    if (j.rows * x <= 2048)
+        hipLaunchKernelGGL(k_join_parts<true>, dim3(x, (uint32_t)j.rows), dim3(64 * kRowWaves), 0, s, j);
+    else
+        hipLaunchKernelGGL(k_join_parts<false>, dim3(x, (uint32_t)(groups < kMaxRowGroups ? groups : kMaxRowGroups)),
+                           dim3(64 * kRowWaves), 0, s, j);
     return hipGetLastError();
 }
 

@@ -9,6 +9,8 @@
 // (A matrix instruction for fp32 operands has a 16th of the rate; six products are 2.7 times as fast.)
 #pragma once
 
+#include <type_traits>
+
 #include "encoder.h"
 
 namespace warp {
@@ -35,7 +37,7 @@ struct ProductArgs {
     int64_t out_stride;
     int32_t out_type;
     const float* factor;
-    const void* bias;
+    const void* bias;  // only where B lies along K
     int32_t bias_type;
     // kSum
     float* part;
@@ -222,7 +224,9 @@ struct Blocks {
     __device__ __forceinline__ V read(const uint8_t* lds, int i, int half) const {
         if (L == kAlongK)
             return *(const V*)(lds + (at ^ (64 * half)) + (CHANNELS ? 4 : 16) * i * 128);
-        const uint8_t* p = lds + (at ^ (32 * i)) + half * 32 * T * 2;
+        int place = at;
+        asm volatile("" : "+v"(place));  // kept from computing all blocks' addresses ahead, which takes registers
+        const uint8_t* p = lds + (place ^ (32 * i)) + half * 32 * T * 2;
         const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((product_lds4*)p);
         const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((product_lds4*)(p + 4 * T * 2));
         typedef short short8v __attribute__((ext_vector_type(8)));
@@ -257,6 +261,30 @@ __device__ __forceinline__ void store_floats(void* out, int32_t type, int64_t at
 __device__ __forceinline__ float load_float(const void* p, int32_t type, int64_t at) {
     return type == WARP_F32 ? ((const float*)p)[at]
                             : type == WARP_F16 ? (float)((const _Float16*)p)[at] : (float)((const __bf16*)p)[at];
+}
+
+// From block j's columns 4 q + e in lane (li, q) to block q's (of two blocks: 4 (2 (q / 2) + j) + e of block q % 2).
+template <int B>
+__device__ __forceinline__ void neighbours(float4v (&x)[B]) {
+    auto swap = [&](int a, int b, auto far) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t u = as_u(x[a][e]), v = as_u(x[b][e]);
+            if constexpr (far.value) {
+                const auto r = __builtin_amdgcn_permlane32_swap(u, v, false, false);
+                x[a][e] = as_f(r[0]), x[b][e] = as_f(r[1]);
+            } else {
+                const auto r = __builtin_amdgcn_permlane16_swap(u, v, false, false);
+                x[a][e] = as_f(r[0]), x[b][e] = as_f(r[1]);
+            }
+        }
+    };
+    if constexpr (B == 4) {
+        swap(0, 2, std::true_type{});
+        swap(1, 3, std::true_type{});
+        swap(2, 3, std::false_type{});
+    }
+    swap(0, 1, std::false_type{});
 }
 
 // Tiles that neighbouring workgroups of an XCD work on span bands of four tiles of rows, so that its L2 serves what
@@ -372,53 +400,45 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs g) {
         multiply(part[1]);
     }
 
-    // acc[i][j][e] is row m0 + wm + 16 i + li, column c0 + wn + 4 kBN q + 4 j + e (kWide) or c0 + wn + 16 j + 4 q + e
-    constexpr int kGroups = kWide ? 1 : kBN, kOut = kWide ? 4 * kBN : 4;
-    auto column = [&](int group) { return c0 + wn + (kWide ? kOut * q : 16 * group + 4 * q); };
+    // acc[i][j][e] is row m0 + wm + 16 i + li, column c0 + wn + 4 kBN q + 4 j + e of channels in their own order; else column
+    // 16 j + 4 q + e of the wave's, which an exchange between lanes 16 and 32 apart turns into 4 kBN neighbours a lane.
+    constexpr int kOut = 4 * kBN;
+    if constexpr (!kWide) {
+#pragma unroll
+        for (int i = 0; i < kBM; ++i) neighbours<kBN>(acc[i]);
+    }
+    const int64_t c = c0 + wn + (kWide || kBN == 4 ? kOut * q : 16 * (q & 1) + 8 * (q >> 1));
     if constexpr (F == kStore) {
+        if (c >= g.n) return;
         const float factor = g.factor ? *g.factor : 1.f;
+        float bias[kOut];
 #pragma unroll
-        for (int u = 0; u < kGroups; ++u) {
-            const int64_t c = column(u);
-            if (c >= g.n) continue;
-            float bias[kOut];
+        for (int e = 0; e < kOut; ++e)
+            bias[e] = kWide && g.bias && c + e < g.n ? load_float(g.bias, g.bias_type, c + e) : 0.f;
 #pragma unroll
-            for (int e = 0; e < kOut; ++e) {
-                bias[e] = g.bias && c + e < g.n ? load_float(g.bias, g.bias_type, c + e) : 0.f;
-            }
+        for (int i = 0; i < kBM; ++i) {
+            const int64_t m = m0 + wm + 16 * i + li;
+            if (m >= rows) continue;
+            float v[kOut];
 #pragma unroll
-            for (int i = 0; i < kBM; ++i) {
-                const int64_t m = m0 + wm + 16 * i + li;
-                if (m >= rows) continue;
-                float v[kOut];
-#pragma unroll
-                for (int e = 0; e < kOut; ++e) v[e] = acc[i][kWide ? e >> 2 : u][e & 3] * factor + bias[e];
-                store_floats<kOut>(g.out, g.out_type, m * g.out_stride + c, v, g.n - c, kWide);
-            }
+            for (int e = 0; e < kOut; ++e) v[e] = acc[i][e >> 2][e & 3] * factor + bias[e];
+            store_floats<kOut>(g.out, g.out_type, m * g.out_stride + c, v, g.n - c, true);
         }
     } else if constexpr (F == kSum) {
         float* out = g.part + split * rows * g.part_stride;
 #pragma unroll
-        for (int u = 0; u < kGroups; ++u) {
-            const int64_t c = column(u);
-            if (c >= g.n) continue;
+        for (int i = 0; i < kBM; ++i) {
+            const int64_t m = m0 + wm + 16 * i + li;
+            if (m >= rows) continue;
+            // part_stride and part are multiples of 4 floats: whole vectors, the last one into the padding
 #pragma unroll
-            for (int i = 0; i < kBM; ++i) {
-                const int64_t m = m0 + wm + 16 * i + li;
-                if (m >= rows) continue;
-                // part_stride and part are multiples of 4 floats: whole vectors, the last one into the padding
-#pragma unroll
-                for (int e = 0; e < kOut; e += 4) {
-                    if (c + e >= g.n) continue;
-                    float4v* p = (float4v*)(out + m * g.part_stride + c + e);
-                    const float4v x = acc[i][kWide ? e >> 2 : u];
-                    *p = g.accumulate ? *p + x : x;
-                }
+            for (int j = 0; j < kBN; ++j) {
+                if (c + 4 * j >= g.n) continue;
+                float4v* p = (float4v*)(out + m * g.part_stride + c + 4 * j);
+                *p = g.accumulate ? *p + acc[i][j] : acc[i][j];
             }
         }
     } else if constexpr (F == kStats) {
-        static_assert(kWide, "rows are reduced over neighbouring columns");
-        const int64_t c = column(0);
         __syncthreads();  // the staged operands have been read by all
         float2* shared = (float2*)a0;  // [WN][TM]
 #pragma unroll
@@ -463,8 +483,6 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs g) {
             g.stats[tile_n * g.stats_stride + m0 + r] = make_float2(top, sum);
         }
     } else {
-        static_assert(kWide, "rows are written in neighbouring columns");
-        const int64_t c = column(0);
 #pragma unroll
         for (int i = 0; i < kBM; ++i) {
             const int64_t m = m0 + wm + 16 * i + li;
