@@ -34,16 +34,14 @@ int check_scratch(const char* what, const void* scratch, int64_t bytes, int64_t 
 // A product whose k range may be split: in one launch, or in parts that are joined.
 struct Product {
     Tile tile;
-    int splits;
+    bool split;
     int64_t floats;
+    Product(int64_t m, int64_t n, int64_t k, int32_t dtype) {
+        const ProductPlan p = plan_product(m, n, product_steps(k, terms_of(dtype)), true);
+        tile = p.tile, split = p.split;
+        floats = split ? part_floats(m, n, k, terms_of(dtype), tile, kMaxSplits, tile_jobs(tile)) : 0;
+    }
 };
-Product plan_product(int64_t m, int64_t n, int64_t k, int32_t dtype) {
-    const int64_t steps = product_steps(k, terms_of(dtype));
-    const Tile whole = whole_tile(m, n), split = split_tile(m, n, steps);
-    const int s = product_splits(m, n, steps, tile_size(split), kMaxSplits, tile_jobs(split));
-    if (s < 2 || steps < 16) return {whole, 1, 0};
-    return {split, s, part_floats(m, n, k, terms_of(dtype), split, kMaxSplits, tile_jobs(split))};
-}
 
 typedef hipError_t (*ProductCall)(const ProductArgs&, int, Tile, Finish, hipStream_t);
 
@@ -51,8 +49,9 @@ hipError_t run_product(ProductCall call, ProductArgs g, const Product& plan, flo
     g.terms = terms_of(dtype);
     g.splits = kMaxSplits, g.jobs = tile_jobs(plan.tile);
     g.part = part, g.part_stride = cover_of(g.n, 4) * 4;
-    if (plan.splits == 1) return call(g, element_of(dtype), plan.tile, kStore, s);
-    const hipError_t e = call(g, element_of(dtype), plan.tile, kSum, s);
+    if (!plan.split) return call(g, element_of(dtype), plan.tile, kStore, s);
+    const hipError_t e = g.b_scale ? product_bytes(g, element_of(dtype), plan.tile, s)
+                                   : call(g, element_of(dtype), plan.tile, kSum, s);
     if (e) return e;
     const Join j{part, g.part_stride, g.m, g.n, g.k, nullptr, nullptr, g.terms, g.splits, g.jobs, tile_size(plan.tile),
                  nullptr, nullptr, g.m, g.out, g.out_stride, g.out_type, g.bias, g.bias_type};
@@ -75,29 +74,45 @@ struct Forward {
     float* part;
     Product y;
     Forward(void* base, const void* x_, int64_t x_stride, int64_t rows, int64_t cols, int32_t dtype, const void* w_,
-            int64_t w_stride, int64_t n) {
+            int64_t w_stride, int64_t n)
+        : y(rows, n, cols, dtype) {
         space.base = (uint8_t*)base;
-        y = plan_product(rows, n, cols, dtype);
         x = space.take<uint16_t>(direct(x_, x_stride, rows, cols, dtype) ? 0 : packed_elements(rows, cols, dtype));
         w = space.take<uint16_t>(direct(w_, w_stride, n, cols, dtype) ? 0 : packed_elements(n, cols, dtype));
         part = space.take<float>(y.floats);
     }
 };
 
+// Few output channels: every 8-bit row is read by one or two tiles, so that the product takes it as it is. With more,
+// rows are unpacked once, to be read by loads that pass no registers (65,536 x 1024 by 128: 45 us instead of 36 for unpacking
+// and 43 for the product; 32,768 x 4096 by 4096, in tiles of 128: 1500 us instead of 65 and 933).
+inline bool takes_bytes(int64_t n, int32_t dtype) { return dtype != WARP_F32 && n <= 256; }
+
 struct Backward {
     Space space;
     uint16_t *dy, *x, *w;
     float *part, *room;
     Product dx, dw;
+    bool bytes;
+    int64_t sums;  // parts of dbias
     Backward(void* base, const void* dy_, int64_t dy_stride, int64_t rows, int64_t cols, int32_t dtype, const void* w_,
-             int64_t w_stride, int64_t n) {
+             int64_t w_stride, int64_t n)
+        : dx(rows, cols, n, dtype), dw(n, cols, rows, dtype) {
         space.base = (uint8_t*)base;
-        dx = plan_product(rows, cols, n, dtype), dw = plan_product(n, cols, rows, dtype);
         dy = space.take<uint16_t>(direct(dy_, dy_stride, rows, n, dtype) ? 0 : packed_elements(rows, n, dtype));
         w = space.take<uint16_t>(direct(w_, w_stride, n, cols, dtype) ? 0 : packed_elements(n, cols, dtype));
-        x = space.take<uint16_t>(packed_elements(rows, cols, dtype));
+        bytes = takes_bytes(n, dtype);
+        sums = 0;
+        if (bytes) {
+            const int64_t steps = product_steps(rows, 1);
+            dw.tile = plan_product(n, cols, steps, true, kT128).tile, dw.split = true;
+            dw.floats = part_floats(n, cols, rows, 1, dw.tile, kMaxSplits, tile_jobs(dw.tile));
+            sums = product_splits(n, cols, steps, tile_size(dw.tile), kMaxSplits, tile_jobs(dw.tile)) *
+                   cover_of(cols, tile_size(dw.tile));
+        }
+        x = space.take<uint16_t>(bytes ? 0 : packed_elements(rows, cols, dtype));
         part = space.take<float>(dx.floats > dw.floats ? dx.floats : dw.floats);
-        room = space.take<float>(column_room(rows, n));
+        room = space.take<float>(sums * n > column_room(rows, n) ? sums * n : column_room(rows, n));
     }
 };
 
@@ -194,13 +209,19 @@ int warp_linear_backward(const void* dy, int64_t dy_stride, int64_t rows, int32_
         WARP_STEP(e);
         WARP_STEP(run_product(product_mixed, product_args(d, t, rows, cols, n, dx, dx_stride, dtype), w.dx, w.part, dtype, s));
     }
-    if (dweight) {  // without rows: zeros
+    const bool bytes = dweight && w.bytes && rows;
+    if (bytes) {
+        ProductArgs g = product_args(d, {q, q_stride, 0}, n, cols, rows, dweight, dweight_stride, dtype);
+        g.b_scale = q_scale, g.sums = dbias ? w.room : nullptr;
+        WARP_STEP(run_product(nullptr, g, w.dw, w.part, dtype, s));
+        if (dbias) WARP_STEP(join_columns(w.room, w.sums, n, dbias, dbias_dtype, s));
+    } else if (dweight) {  // without rows: zeros
         WARP_STEP(unpack_int8(q, q_stride, q_scale, rows, cols, dtype, w.x, s));
         const Operand x{w.x, packed_width(cols), rows * packed_width(cols)};
         WARP_STEP(run_product(product_across, product_args(d, x, n, cols, rows, dweight, dweight_stride, dtype), w.dw, w.part,
                               dtype, s));
     }
-    if (dbias) WARP_STEP(column_sums(dy, dy_stride, rows, n, dtype, w.room, dbias, dbias_dtype, s));
+    if (dbias && !bytes) WARP_STEP(column_sums(dy, dy_stride, rows, n, dtype, w.room, dbias, dbias_dtype, s));
     return WARP_OK;
 }
 

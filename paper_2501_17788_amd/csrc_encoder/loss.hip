@@ -255,7 +255,7 @@ struct Forward {
         space.base = (uint8_t*)base;
         const int64_t tokens = z.tokens > 0 ? z.tokens : 1;
         const int64_t by_table = z.packs ? piece_of(z.vocabulary, z.width * 2 * z.planes, kPieceBytes) : 1 << 30;
-        tile = whole_tile(tokens, z.vocabulary);
+        tile = plan_product(tokens, z.vocabulary, product_steps(z.cols, terms_of(z.dtype)), false).tile;
         const int64_t by_stats = piece_of(z.vocabulary, cover_of(tokens * 8, tile_size(tile)), kStatsBytes);
         piece = by_table < by_stats ? by_table : by_stats;
         hidden = space.take<uint16_t>(packed_elements(tokens, z.cols, z.dtype));
@@ -285,14 +285,10 @@ struct Backward {
             piece = by_table < piece ? by_table : piece;
         }
         const int64_t cols = z.vocabulary < piece ? z.vocabulary : piece;
-        logits = whole_tile(tokens, cols);
-        dh = split_tile(tokens, z.cols, product_steps(cols, terms));
-        de = whole_tile(cols, z.cols);
-        de_split = false;
-        const Tile de_other = split_tile(cols, z.cols, product_steps(tokens, terms));
-        if (product_splits(cols, z.cols, product_steps(tokens, terms), tile_size(de_other), kMaxSplits, tile_jobs(de_other)) > 1 &&
-            product_steps(tokens, terms) >= 16)
-            de_split = true, de = de_other;
+        logits = plan_product(tokens, cols, product_steps(z.cols, terms), false).tile;
+        dh = plan_product(tokens, z.cols, product_steps(cols, terms), true).tile;
+        const ProductPlan e = plan_product(cols, z.cols, product_steps(tokens, terms), true);
+        de = e.tile, de_split = e.split;
         hidden = space.take<uint16_t>(packed_elements(tokens, z.cols, z.dtype));
         table = space.take<uint16_t>(z.packs ? packed_elements(piece, z.cols, z.dtype) : 0);
         grad = space.take<uint16_t>(z.planes * tokens * piece);

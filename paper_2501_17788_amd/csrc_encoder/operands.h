@@ -84,6 +84,7 @@ inline int64_t part_floats(int64_t m, int64_t n, int64_t k, int terms, Tile tile
 // out = sums of x's columns, in an order that the sizes fix; `room` for column_room floats.
 inline int64_t column_chunks(int64_t rows) { return rows < 64 ? 1 : rows / 64 < 256 ? rows / 64 : 256; }
 inline int64_t column_room(int64_t rows, int64_t cols) { return column_chunks(rows) * cols; }
+hipError_t join_columns(const float* room, int64_t chunks, int64_t cols, void* out, int32_t out_type, hipStream_t s);
 hipError_t column_sums(const void* x, int64_t stride, int64_t rows, int64_t cols, int32_t dtype, float* room, void* out,
                        int32_t out_type, hipStream_t s);
 

@@ -154,19 +154,23 @@ __global__ __launch_bounds__(256) void k_column_parts(const T* x, int64_t stride
     store_vec<float, V>(room + blockIdx.y * cols + c, out);
 }
 
-__global__ __launch_bounds__(1024) void k_column_join(const float* room, int chunks, int64_t cols, void* out, int32_t type) {
-    __shared__ float joined[16][kWave];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * kWave + lane;
+// 16 columns a workgroup, 64 parts of each side by side.
+__global__ __launch_bounds__(1024) void k_join_columns(const float* room, int64_t chunks, int64_t cols, void* out,
+                                                       int32_t type) {
+    __shared__ float joined[64][17];
+    const int col = threadIdx.x & 15, part = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 16 + col;
     float sum = 0.f;
-    if (c < cols)
-        for (int i = w; i < chunks; i += 16) sum += room[i * cols + c];
-    joined[w][lane] = sum;
+    if (c < cols) {
+#pragma unroll 8
+        for (int64_t i = part; i < chunks; i += 64) sum += room[i * cols + c];
+    }
+    joined[part][col] = sum;
     __syncthreads();
-    if (w || c >= cols) return;
+    if (part || c >= cols) return;
     float v[1] = {0.f};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[0] += joined[i][lane];
+    for (int i = 0; i < 64; ++i) v[0] += joined[i][col];
     store_floats<1>(out, type, c, v, 1, false);
 }
 
@@ -236,8 +240,13 @@ hipError_t column_sums(const void* x, int64_t stride, int64_t rows, int64_t cols
         else if (dtype == WARP_F16) column_parts<_Float16>(x, stride, rows, cols, room, s);
         else column_parts<__bf16>(x, stride, rows, cols, room, s);
     }
-    hipLaunchKernelGGL(k_column_join, dim3((uint32_t)cover_of(cols, kWave)), dim3(1024), 0, s, (const float*)room,
-                       rows ? (int)column_chunks(rows) : 0, cols, out, out_type);
+    return join_columns(room, rows ? column_chunks(rows) : 0, cols, out, out_type, s);
+}
+
+hipError_t join_columns(const float* room, int64_t chunks, int64_t cols, void* out, int32_t out_type, hipStream_t s) {
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(k_join_columns, dim3((uint32_t)cover_of(cols, 16)), dim3(1024), 0, s, room, chunks, cols, out,
+                       out_type);
     return hipGetLastError();
 }
 

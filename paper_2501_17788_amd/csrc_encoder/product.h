@@ -32,6 +32,9 @@ struct ProductArgs {
     const int32_t *m_now, *k_now;  // device counts that take the place of m and k where they are not null
     int32_t terms;                 // 1, or 6 products of planes
     int32_t splits, jobs;          // at most so many parts of the k range, to have about so many tiles at work
+    // 8-bit rows in the place of b (across K): b_stride bytes apart, a scale for each
+    const float* b_scale;
+    float* sums;  // [split][tile column][m]: parts of the sums of A's columns over k; may be null
     // kStore
     void* out;
     int64_t out_stride;
@@ -74,16 +77,57 @@ inline int tile_size(Tile t) { return t == kT64 ? 64 : t == kT128 ? 128 : 256; }
 // Tiles at work at once.
 inline int tile_jobs(Tile t) { return t == kT64 ? 1024 : t == kT128 ? 512 : 256; }
 
-// Tiles of a product that is not split, and of one that may be.
-inline Tile whole_tile(int64_t m, int64_t n) {
-    if (cover_of(m, 256) * cover_of(n, 256) >= 192) return kT256;
-    return cover_of(m, 128) * cover_of(n, 128) >= 192 ? kT128 : kT64;
+// How a product is made: its tiles, and whether its k range is split.
+struct ProductPlan {
+    Tile tile;
+    bool split;
+};
+// The faster one by a model of measured times, in ns. `jobs` tiles of `steps` steps take rounds of as many as are at work at
+// once, the last one less where it leaves compute units to fewer. Their bytes take time too: operands from memory at 5 TB/s and
+// again for each tile at 20 (unless the caches hold them), results at 5.5, less for short pieces of rows; a quarter of the
+// shorter of both times is not hidden behind the longer. Parts are written and read once more, at 4 TB/s, by a launch of
+// its own. Measured (us, 16-bit elements, operands in the caches; whole | in parts):
+//                           64 x 64      128 x 128    256 x 256
+//   1 x 1024 x 1024        7.0 | 6.5    10.5 | 7.2   23.5 | 9.1
+//   1024 x 1024 x 1024     8.1 | 18     11.9 | 24    26.7 | 28
+//   1024 x 1024 x 4096      33 | 25       42 | 27      87 | 43
+//   8192 x 1024 x 1024      27            22           30
+//   65,536 x 128 x 1024     31            25           31
+//   2048 x 4096 x 4096      97            65           94
+//   4096 x 4096 x 4096     192           129          111
+//   128 x 1024 x 65,536    465 | 44      603 | 39    1403 | 54
+//   4096 x 1024 x 65,536  1266           819 | 614   1533 | 490
+inline int64_t product_time(Tile t, int64_t jobs, int64_t steps) {
+    const int64_t at_once = tile_jobs(t), full = jobs / at_once, rest = jobs % at_once;
+    if (t == kT64)
+        return full * (650 * steps + 2200) + (!rest ? 0 : rest <= 256 ? 460 * steps + 1000 : rest <= 512 ? 500 * steps + 1500
+                                                                                                         : 800 * steps + 2500);
+    if (t == kT128) return full * (1000 * steps + 3500) + (!rest ? 0 : rest <= 256 ? 600 * steps + 3000 : 1000 * steps + 3500);
+    return full * (1600 * steps + 9000) + (!rest ? 0 : rest <= 160 ? 1350 * steps + 6000 : 1600 * steps + 9000);
 }
-inline Tile split_tile(int64_t m, int64_t n, int64_t steps) {
-    if (m > 128 && n > 128 && cover_of(m, 256) * cover_of(n, 256) * steps >= 2048) return kT256;
-    return m > 64 && n > 64 && cover_of(m, 128) * cover_of(n, 128) * steps >= 1024 ? kT128 : kT64;
+inline int64_t product_traffic(Tile t, int64_t m, int64_t n, int64_t steps) {
+    const int64_t size = tile_size(t), a = m * steps * 128, b = n * steps * 128, cached = 4 << 20;
+    const int64_t loads = a * (a > cached ? cover_of(n, size) : 1) + b * (b > cached ? cover_of(m, size) : 1);
+    return (a + b) / 5000 + loads / 20000 + m * n * 2 * (96 + size) / size / 5500;
 }
 constexpr int kMaxSplits = 256;
+inline ProductPlan plan_product(int64_t m, int64_t n, int64_t steps, bool may_split, Tile largest = kT256) {
+    ProductPlan best{kT64, false};
+    int64_t least = INT64_MAX;
+    for (const Tile t : {kT64, kT128, kT256}) {
+        if (t > largest) break;
+        const int64_t tiles = cover_of(m, tile_size(t)) * cover_of(n, tile_size(t));
+        const int64_t traffic = product_traffic(t, m, n, steps);
+        auto both = [&](int64_t time) { return time > traffic ? time + traffic / 4 : traffic + time / 4; };
+        const int64_t whole = both(product_time(t, tiles, steps));
+        if (whole < least) least = whole, best = {t, false};
+        const int splits = may_split ? product_splits(m, n, steps, tile_size(t), kMaxSplits, tile_jobs(t)) : 1;
+        if (splits < 2) continue;
+        const int64_t parts = both(product_time(t, tiles * splits, cover_of(steps, splits))) + 5500 + m * n * splits / 500;
+        if (parts < least) least = parts, best = {t, true};
+    }
+    return best;
+}
 
 // x = high + middle + low, each a bfloat16 cut off towards zero: 8 + 8 + 8 bits. An infinity or a NaN stays in the
 // first.
@@ -108,6 +152,7 @@ __host__ __device__ inline void split_f32(float x, uint16_t (&out)[3]) {
 hipError_t product_along(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);   // A, B along K
 hipError_t product_mixed(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);   // B across K
 hipError_t product_across(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);  // both
+hipError_t product_bytes(const ProductArgs& g, int element, Tile tile, hipStream_t s);  // both; b of 8 bits; kSum, to kT128
 hipError_t product_softmax(const ProductArgs& g, int element, bool planes, Tile tile, Finish finish, hipStream_t s);
 
 #ifdef __HIPCC__
@@ -206,6 +251,40 @@ struct Stage {
     }
 };
 
+// The same for 8-bit rows across K, which pass registers: 16 bytes a thread, times their row's scale, rounded to E.
+template <typename E, int T>
+struct ByteStage {
+    const int8_t* at;
+    const float* scale;
+    int64_t step_bytes;
+    int k, place;
+    typedef int int4v __attribute__((ext_vector_type(4)));
+    int4v data;
+    float factor;
+    __device__ __forceinline__ void start(const void* p, int64_t stride, const float* scales, int64_t first, int64_t step) {
+        constexpr int kPairs = T / 16;
+        k = threadIdx.x / kPairs;
+        const int pair = threadIdx.x % kPairs;
+        at = (const int8_t*)p + (step * kProductStep + k) * stride + first + 16 * pair;
+        scale = scales + step * kProductStep + k;
+        step_bytes = stride * kProductStep;
+        place = k * T * 2 + (pair ^ pair_key<T>(k)) * 32;
+    }
+    __device__ __forceinline__ void load(int64_t left) {
+        data = int4v{}, factor = 0.f;
+        if (k < left) data = *(const int4v*)at, factor = *scale;
+        at += step_bytes;
+        scale += kProductStep;
+    }
+    __device__ __forceinline__ void put(uint8_t* lds) const {
+        typename Eight<E>::type v[2];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e >> 3][e & 7] = (E)((float)(int8_t)(data[e >> 2] >> 8 * (e & 3)) * factor);
+        *(typename Eight<E>::type*)(lds + place) = v[0];
+        *(typename Eight<E>::type*)(lds + place + 16) = v[1];
+    }
+};
+
 // Where a lane reads blocks of 16 rows of a staged operand: block i of B, half a step (32 k) at a time.
 template <typename E, Layout L, int T, bool CHANNELS, int B>
 struct Blocks {
@@ -291,8 +370,10 @@ __device__ __forceinline__ void neighbours(float4v (&x)[B]) {
 // they have in common.
 constexpr int kProductBand = 4;
 
-template <typename E, Layout LA, Layout LB, int TM, int TN, int WM, int WN, Finish F, bool PLANES>
-__global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs g) {
+enum Kind { kPlain, kPlanes, kBytes };  // G in planes of a float32; B of 8 bits
+
+template <typename E, Layout LA, Layout LB, int TM, int TN, int WM, int WN, Finish F, Kind KIND>
+__global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(ProductArgs g) {
     constexpr int kWaves = WM * WN;
     constexpr int kBM = TM / WM / 16, kBN = TN / WN / 16;  // blocks of a wave
     constexpr bool kWide = LB == kAlongK;                  // a lane holds 4 kBN neighbouring columns, else 4 in each block
@@ -327,24 +408,27 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs g) {
     Stage<LA, TM, kWaves, false, kBM> sa;
     Stage<LB, TN, kWaves, kWide, kBN> sb;
     sa.start(g.a, g.a_stride, m0, rows, lane, wave);
-    sb.start(g.b, g.b_stride, c0, g.n, lane, wave);
+    ByteStage<E, TN> bytes;
+    if constexpr (KIND == kBytes) bytes.start(g.b, g.b_stride, g.b_scale, c0, first);
+    else sb.start(g.b, g.b_stride, c0, g.n, lane, wave);
     int term = 0;
     int64_t kk = 0;  // step within the term
     auto seek = [&] {
         // planes of the terms: (0,0) (0,1) (1,0) (1,1) (0,2) (2,0)
         sa.seek((int64_t)(0x201100 >> 4 * term & 3) * g.a_plane, kk);
-        sb.seek((int64_t)(0x021010 >> 4 * term & 3) * g.b_plane, kk);
+        if constexpr (KIND != kBytes) sb.seek((int64_t)(0x021010 >> 4 * term & 3) * g.b_plane, kk);
     };
     if (k_steps) term = (int)(first / k_steps), kk = first % k_steps;
     seek();
     auto load = [&](uint8_t* la, uint8_t* lb) {
         const int64_t left = k - kk * kProductStep;
+        if constexpr (KIND == kBytes) bytes.load(left);
         if (left >= kProductStep) {
             sa.load(la);
-            sb.load(lb);
+            if constexpr (KIND != kBytes) sb.load(lb);
         } else {
             sa.load_last(la, (int)left);
-            sb.load_last(lb, (int)left);
+            if constexpr (KIND != kBytes) sb.load_last(lb, (int)left);
         }
         if (++kk == k_steps) {
             kk = 0;
@@ -352,7 +436,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs g) {
             seek();  // (after the last term: not used)
         } else {
             sa.at += sa.step_bytes;
-            sb.at += sb.step_bytes;
+            if constexpr (KIND != kBytes) sb.at += sb.step_bytes;
         }
     };
 
@@ -377,6 +461,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs g) {
 #pragma unroll
             for (int j = 0; j < kBN; ++j) acc[i][j] = product_mfma(p.b[j], p.a[i], acc[i][j]);
     };
+    V ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (E)1.f;
+    float4v totals[kBM] = {};
+    int turn = (int)(first % tiles_n);
     // The operands of each half step are read while the matrix cores work on the half step before it, across the
     // barrier between steps.
     auto step = [&](int s, const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb) {
@@ -387,9 +476,21 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs g) {
         if (s) multiply(part[1]);
         read(part[1], la, lb, 1);
         multiply(part[0]);
+        if constexpr (KIND == kBytes) {
+            // sums of A's columns: products by ones, of steps that the workgroups of a row of tiles take in turn
+            if (g.sums && wave % WN == 0 && turn == tile_n) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < kBM; ++i) totals[i] = product_mfma(ones, part[h].a[i], totals[i]);
+            }
+            turn = turn + 1 == tiles_n ? 0 : turn + 1;
+            if (s + 1 < count) bytes.put(nb);
+        }
     };
     if (count) {
         load(a0, b0);
+        if constexpr (KIND == kBytes) bytes.put(b0);
         step(0, a0, b0, a1, b1);
         int s = 1;
         for (; s + 1 < count; s += 2) {
@@ -426,6 +527,15 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs g) {
         }
     } else if constexpr (F == kSum) {
         float* out = g.part + split * rows * g.part_stride;
+        if constexpr (KIND == kBytes) {
+            if (g.sums && wave % WN == 0 && q == 0) {
+#pragma unroll
+                for (int i = 0; i < kBM; ++i) {
+                    const int64_t m = m0 + wm + 16 * i + li;
+                    if (m < rows) g.sums[((int64_t)split * tiles_n + tile_n) * rows + m] = totals[i][0];
+                }
+            }
+        }
 #pragma unroll
         for (int i = 0; i < kBM; ++i) {
             const int64_t m = m0 + wm + 16 * i + li;
@@ -502,7 +612,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs g) {
                 for (int e = 0; e < kOut; ++e)
                     if (c + e >= g.n) d[e] = 0.f;
             }
-            if constexpr (PLANES) {
+            if constexpr (KIND == kPlanes) {
                 Vec<uint16_t, kOut> p[3];
 #pragma unroll
                 for (int e = 0; e < kOut; ++e) {
@@ -524,24 +634,26 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(ProductArgs g) {
 }
 
 // Workgroups for at most g.m rows.
-template <typename E, Layout LA, Layout LB, Finish F, bool PLANES, int TM, int TN, int WM, int WN>
+template <typename E, Layout LA, Layout LB, Finish F, Kind KIND, int TM, int TN, int WM, int WN>
 hipError_t product_launch(const ProductArgs& g, hipStream_t s) {
     const int64_t tiles = cover_of(g.m, TM) * cover_of(g.n, TN);
     // splits shrink as rows grow: at most `jobs` tiles, or one part of each
     const int64_t grid = F == kSum && tiles < g.jobs ? g.jobs : tiles;
     (void)hipGetLastError();
     if (tiles)
-        hipLaunchKernelGGL((k_product<E, LA, LB, TM, TN, WM, WN, F, PLANES>), dim3((uint32_t)grid), dim3(64 * WM * WN), 0,
+        hipLaunchKernelGGL((k_product<E, LA, LB, TM, TN, WM, WN, F, KIND>), dim3((uint32_t)grid), dim3(64 * WM * WN), 0,
                            s, g);
     return hipGetLastError();
 }
 
-template <typename E, Layout LA, Layout LB, Finish F, bool PLANES = false>
+template <typename E, Layout LA, Layout LB, Finish F, Kind KIND = kPlain>
 hipError_t product_tiles(const ProductArgs& g, Tile tile, hipStream_t s) {
     switch (tile) {
-        case kT64: return product_launch<E, LA, LB, F, PLANES, 64, 64, 2, 2>(g, s);
-        case kT128: return product_launch<E, LA, LB, F, PLANES, 128, 128, 2, 4>(g, s);
-        default: return product_launch<E, LA, LB, F, PLANES, 256, 256, 2, 4>(g, s);
+        case kT64: return product_launch<E, LA, LB, F, KIND, 64, 64, 2, 2>(g, s);
+        case kT128: return product_launch<E, LA, LB, F, KIND, 128, 128, 2, 4>(g, s);
+        default:
+            if constexpr (KIND == kBytes) return hipErrorInvalidValue;
+            else return product_launch<E, LA, LB, F, KIND, 256, 256, 2, 4>(g, s);
     }
 }
 

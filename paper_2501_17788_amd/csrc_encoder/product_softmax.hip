@@ -7,7 +7,7 @@ hipError_t product_softmax(const ProductArgs& g, int element, bool planes, Tile 
     if (finish == kStats)
         return element == WARP_F16 ? product_tiles<_Float16, kAlongK, kAlongK, kStats>(g, tile, s)
                                    : product_tiles<__bf16, kAlongK, kAlongK, kStats>(g, tile, s);
-    if (planes) return product_tiles<__bf16, kAlongK, kAlongK, kGrad, true>(g, tile, s);
+    if (planes) return product_tiles<__bf16, kAlongK, kAlongK, kGrad, kPlanes>(g, tile, s);
     return element == WARP_F16 ? product_tiles<_Float16, kAlongK, kAlongK, kGrad>(g, tile, s)
                                : product_tiles<__bf16, kAlongK, kAlongK, kGrad>(g, tile, s);
 }
