@@ -77,9 +77,11 @@ __device__ __forceinline__ int token_key(int row) { return row & 7; }
 template <int BN>
 __device__ __forceinline__ int channel_key(int row) { return (row & 3) | (row / (4 * BN) & 1) << 2; }
 
-// Waits for this wave's loads into LDS. A barrier alone orders no loads that pass no registers: without this wait it
-// would be the compiler's choice whether other waves find the rows there behind the barrier.
-__device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Waits for this wave's loads into LDS and for its reads of LDS. A barrier alone orders no loads that pass no registers:
+// without this wait it would be the compiler's choice whether other waves find the rows there behind the barrier. Nor does
+// it end reads whose registers are needed later only (the tiles of 128 x 128 had some under way across it): another wave's
+// loads behind the barrier may come before them where two kernels share a compute unit.
+__device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 // A workgroup makes a tile of TM tokens by TN channels with WM x WN waves. Each K step's rows are copied to LDS
 // by loads that pass no registers, into one of two buffers, while the matrix cores work on the other. The two
