@@ -37,9 +37,9 @@ struct SelectArgs {
     float* largest;
 };
 
-// One workgroup: turns of eight times 1024 neighbouring tokens, whose loads and stores are in one piece a wave.
+// One workgroup: turns of sixteen times 1024 neighbouring tokens, whose loads and stores are in one piece a wave.
 __global__ __launch_bounds__(1024) void k_select(SelectArgs g) {
-    constexpr int N = 8;
+    constexpr int N = 16;
     __shared__ int32_t waves[N][16];
     __shared__ uint32_t tops[16];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -71,19 +71,20 @@ __global__ __launch_bounds__(1024) void k_select(SelectArgs g) {
             if (in && d[e] < 0x7f800000u) top = max(top, d[e]);
         }
         __syncthreads();
-        // this lane's count of the turn's waves before it and behind it: 128 numbers, two a lane
-        const int32_t a = waves[lane >> 3][2 * lane & 15], b = waves[lane >> 3][(2 * lane & 15) + 1];
-        int32_t x = a + b;
+        // the turn's tokens before each wave of each 1024: 256 numbers, four a lane
+        const int4 n = ((const int4*)waves)[lane];
+        const int32_t mine = n.x + n.y + n.z + n.w;
+        int32_t x = mine;
 #pragma unroll
         for (int s = 1; s < 64; s <<= 1) {
             const int32_t v = __shfl_up(x, s);
             if (lane >= s) x += v;
         }
-        const int32_t before = x - a - b;
+        const int part = w & 3;
+        const int32_t before = x - mine + (part > 0 ? n.x : 0) + (part > 1 ? n.y : 0) + (part > 2 ? n.z : 0);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const int32_t pair = __builtin_amdgcn_readlane(before, 8 * e + (w >> 1));
-            const int32_t first = count + pair + (w & 1 ? __builtin_amdgcn_readlane(a, 8 * e + (w >> 1)) : 0);
+            const int32_t first = count + __builtin_amdgcn_readlane(before, 4 * e + (w >> 2));
             const int64_t t = t0 + 1024 * e;
             if (t >= g.tokens) continue;
             g.place[t] = rank[e] >= 0 ? first + rank[e] : y[e] < 0 ? -1 : -2;
@@ -223,6 +224,10 @@ int check_rows(const char* what, const void* targets, int32_t target_bytes, int6
     return WARP_OK;
 }
 
+// Not zero, by which what lies outside the vocabulary, minus infinity, could not be multiplied: the smallest number has no
+// effect on logits below 2^100 either.
+float to_log2(float scale) { return scale ? scale * kLog2E : 1.17549435e-38f; }
+
 // Columns of a piece of the vocabulary: a multiple of 256 (the last piece is shorter).
 int64_t piece_of(int64_t vocabulary, int64_t bytes_a_column, int64_t most_bytes) {
     int64_t p = most_bytes / bytes_a_column / 256 * 256;
@@ -360,7 +365,7 @@ int warp_cross_entropy(const void* hidden, int64_t hidden_stride, int64_t tokens
         g.a = f.hidden, g.a_stride = z.width, g.a_plane = tokens * z.width;
         g.b = t.p, g.b_stride = t.stride, g.b_plane = t.plane;
         g.m = tokens, g.n = n, g.k = cols, g.m_now = f.now, g.terms = terms_of(dtype);
-        g.to_log2 = scale * kLog2E, g.n0 = v0, g.target = f.target;
+        g.to_log2 = to_log2(scale), g.n0 = v0, g.target = f.target;
         g.stats = f.stats, g.stats_stride = tokens, g.of_target = f.of_target;
         WARP_STEP(product_softmax(g, element_of(dtype), false, f.tile, kStats, s));
         const JoinStatsArgs j{f.stats, tokens, (int)cover_of(n, tile_size(f.tile)), v0 == 0, v0 + n == vocabulary, f.running,
@@ -417,7 +422,7 @@ int warp_cross_entropy_backward(const float* dloss, const void* hidden, int64_t 
         g.a = h.p, g.a_stride = h.stride, g.a_plane = h.plane;
         g.b = t.p, g.b_stride = t.stride, g.b_plane = t.plane;
         g.m = tokens, g.n = n, g.k = cols, g.m_now = w.now, g.terms = terms;
-        g.to_log2 = scale * kLog2E, g.n0 = v0, g.target = w.target;
+        g.to_log2 = to_log2(scale), g.n0 = v0, g.target = w.target;
         g.lse = w.lse2, g.weight = w.weight, g.at_target = w.at_target;
         g.grad = w.grad, g.grad_stride = w.piece, g.grad_plane = tokens * w.piece, g.grad_scale = grad_scale;
         WARP_STEP(product_softmax(g, element, z.planes == 3, w.logits, kGrad, s));

@@ -47,7 +47,7 @@ struct ProductArgs {
     int64_t part_stride;  // a part is as many rows as there are now
     bool accumulate;
     // kStats and kGrad: rows are tokens, columns n0, n0 + 1, ... of the vocabulary
-    float to_log2;          // a logit in units of log 2 is to_log2 * C
+    float to_log2;          // a logit in units of log 2 is to_log2 * C; not zero
     int64_t n0;
     const int32_t* target;  // a row's column
     float2* stats;          // [tile column][row]: largest logit of the others than the target, sum of their exponentials
@@ -164,7 +164,7 @@ typedef const __attribute__((address_space(1))) void product_global;
 typedef __attribute__((address_space(3))) void product_lds;
 typedef __attribute__((address_space(3))) short4v product_lds4;
 
-static __device__ uint32_t g_zeros[4];  // where pieces beyond the k range are read
+static __device__ __attribute__((aligned(16))) uint32_t g_zeros[4];  // where pieces beyond the k range are read
 
 template <typename E>
 struct Eight {
@@ -177,8 +177,10 @@ __device__ __forceinline__ float4v product_mfma(Eight<_Float16>::type a, Eight<_
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-// Waits for this wave's loads into LDS, which a barrier alone does not order.
-__device__ __forceinline__ void product_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Waits for this wave's loads into LDS and for its reads of LDS, before a barrier behind which other waves read the ones
+// and load over the others. A barrier alone orders neither: the compiler leaves reads under way across it, whose registers
+// are needed only later, and where two kernels shared a compute unit, loads have come before such reads.
+__device__ __forceinline__ void product_landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 // Where the 16-byte pieces of a staged operand lie in LDS.
 // Along K a row has eight pieces, in the order piece ^ key(row), so that the rows that neighbouring lanes read one
@@ -498,8 +500,21 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
             step(s + 1, a0, b0, a1, b1);
         }
         if (s < count) step(s, a1, b1, a0, b0);
-        multiply(part[1]);
     }
+    // What the tile's rows have is on its way during the last products: behind the first store it would be waited for row
+    // by row.
+    int64_t column_hit[kBM];
+    float row_lse[kBM], row_weight[kBM];
+    if constexpr (F == kStats || F == kGrad) {
+#pragma unroll
+        for (int i = 0; i < kBM; ++i) {
+            const int64_t at = m0 + wm + 16 * i + li, m = at < rows ? at : rows - 1;
+            column_hit[i] = (int64_t)g.target[m] - g.n0 - (c0 + wn + 4 * kBN * q);
+            if (at >= rows) column_hit[i] = -1;
+            if constexpr (F == kGrad) row_lse[i] = g.lse[m], row_weight[i] = g.weight[m] * g.grad_scale;
+        }
+    }
+    if (count) multiply(part[1]);
 
     // acc[i][j][e] is row m0 + wm + 16 i + li, column c0 + wn + 4 kBN q + 4 j + e of channels in their own order; else column
     // 16 j + 4 q + e of the wave's, which an exchange between lanes 16 and 32 apart turns into 4 kBN neighbours a lane.
@@ -551,29 +566,41 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
     } else if constexpr (F == kStats) {
         __syncthreads();  // the staged operands have been read by all
         float2* shared = (float2*)a0;  // [WN][TM]
+        const bool whole = c0 + TN <= g.n;  // of all lanes
 #pragma unroll
         for (int i = 0; i < kBM; ++i) {
             const int64_t m = m0 + wm + 16 * i + li;
-            float x[kOut], top = -INFINITY;
+            float x[kOut];
 #pragma unroll
-            for (int e = 0; e < kOut; ++e) {
-                x[e] = acc[i][e >> 2][e & 3] * g.to_log2;
-                if (c + e >= g.n) x[e] = -INFINITY;
+            for (int e = 0; e < kOut; ++e) x[e] = acc[i][e >> 2][e & 3];
+            // what does not count is as far down as it goes
+            const float down = g.to_log2 < 0.f ? INFINITY : -INFINITY;
+            if (!whole) {
+#pragma unroll
+                for (int e = 0; e < kOut; ++e)
+                    if (c + e >= g.n) x[e] = down;
             }
-            const int64_t hit = m < rows ? (int64_t)g.target[m] - g.n0 - c : -1;
+            const int64_t hit = column_hit[i];
             if (hit >= 0 && hit < kOut && c + hit < g.n) {
 #pragma unroll
                 for (int e = 0; e < kOut; ++e)
-                    if (e == hit) g.of_target[m] = x[e], x[e] = -INFINITY;
+                    if (e == hit) g.of_target[m] = x[e] * g.to_log2, x[e] = down;
             }
+            float top = x[0];
+            if (g.to_log2 < 0.f) {
 #pragma unroll
-            for (int e = 0; e < kOut; ++e) top = fmaxf(top, x[e]);
+                for (int e = 1; e < kOut; ++e) top = fminf(top, x[e]);
+            } else {
+#pragma unroll
+                for (int e = 1; e < kOut; ++e) top = fmaxf(top, x[e]);
+            }
+            top *= g.to_log2;
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float from = top == -INFINITY ? 0.f : top;
             float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < kOut; ++e) sum += __builtin_amdgcn_exp2f(x[e] - from);
+            for (int e = 0; e < kOut; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], g.to_log2, -from));
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
             if (q == 0) shared[(wave % WN) * TM + wm + 16 * i + li] = make_float2(top, sum);
@@ -597,17 +624,18 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
         for (int i = 0; i < kBM; ++i) {
             const int64_t m = m0 + wm + 16 * i + li;
             if (m >= rows) continue;
-            const float lse = g.lse[m], weight = g.weight[m] * g.grad_scale;
-            const int64_t hit = (int64_t)g.target[m] - g.n0 - c;
+            const int64_t hit = column_hit[i];
             float d[kOut];
 #pragma unroll
-            for (int e = 0; e < kOut; ++e) d[e] = __builtin_amdgcn_exp2f(acc[i][e >> 2][e & 3] * g.to_log2 - lse) * weight;
+            for (int e = 0; e < kOut; ++e)
+                d[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][e >> 2][e & 3], g.to_log2, -row_lse[i])) * row_weight[i];
             if (hit >= 0 && hit < kOut) {
+                const float at = g.at_target[m] * g.grad_scale;
 #pragma unroll
                 for (int e = 0; e < kOut; ++e)
-                    if (e == hit) d[e] = g.at_target[m] * g.grad_scale;
+                    if (e == hit) d[e] = at;
             }
-            if (c + kOut > g.n) {
+            if (c0 + TN > g.n) {
 #pragma unroll
                 for (int e = 0; e < kOut; ++e)
                     if (c + e >= g.n) d[e] = 0.f;

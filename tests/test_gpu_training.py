@@ -726,6 +726,39 @@ def test_captured_in_two_graphs(dtype):
                 assert torch.equal(a, b), (k, i)
 
 
+def test_products_side_by_side():
+    """Products on two streams at once, whose workgroups share compute units: the same bits as alone. Loads into LDS that
+    came before another wave's reads showed here, in one call of ten."""
+    g = gen(50)
+    x = [randn(g, 6000, 136) for _ in range(2)]
+    weight = randn(g, 3000, 136)
+    q, wq = [w.quantize_rows(t) for t in x], w.quantize_rows(weight)
+    targets = torch.randint(0, 3000, (6000,), generator=g, device="cuda")
+    dy = randn(g, 6000, 3000)
+
+    def work(i):
+        out = [w.linear_int8(q[i], wq), w.linear(x[i], weight), *w.cross_entropy(x[i], weight, targets, 0.1)]
+        out += w.linear_backward(dy, q[i], weight)[:2]
+        return out + list(w.cross_entropy_backward(targets.float(), x[i], weight, targets, *out[2:4], 0.1))
+
+    want = [work(i) for i in range(2)]
+    graphs, outs = [], []
+    for i in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(work(i))
+        graphs.append(graph)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for k in range(40):
+        torch.cuda.synchronize()
+        for graph, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert all(torch.equal(u, v) for u, v in zip(a, b)), k
+
+
 def test_outputs_alone_are_written():
     """C calls into the middle of larger buffers: what lies around the results stays."""
     lib, g = w.lib, gen(47)
