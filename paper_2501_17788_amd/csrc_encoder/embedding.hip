@@ -1,9 +1,10 @@
 // Rows of a table by token, scaled, and the table's gradient:
 //   out[t] = scale * table[id_t],   dtable[v] = scale * sum over t with id_t = v of dy[t]
 // Both are bound by memory. The gradient's sums have a fixed order, without atomics on floats: tokens are sorted by
-// id (stably, so that a row's tokens come in order), chunks of 64 sorted tokens that belong to one row are summed on
-// their own (a common token has thousands), and each row of the table adds its chunks and what is left over of its
-// tokens. Rows without tokens are written as zeros by the same kernel: the gradient is written once.
+// id (stably, so that a row's tokens come in order) and summed in chunks of 32 sorted tokens, whatever rows these belong
+// to. A row whose tokens lie in one chunk is written from there; one that goes on in another leaves a part in each, and
+// those are added last, together with the zeros of the rows without tokens: the gradient is written once, and a
+// common token's thousands are as many waves' work.
 #include <type_traits>
 
 #include "encoder.h"
@@ -276,7 +277,8 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_few(SortArgs g, int passe
 
 // ---------------------------------------------------------------------------- sums
 
-constexpr int kChunk = 64;  // sorted tokens of a chunk
+constexpr int kChunk = 32;  // sorted tokens of a chunk
+constexpr int kFew = 8;     // parts that one wave adds
 
 struct SumArgs {
     const void* dy;
@@ -284,12 +286,14 @@ struct SumArgs {
     int64_t tokens, vocabulary, cols;
     const uint32_t *keys, *places;  // sorted
     int2* spans;                    // of each row, its sorted tokens [x, y)
-    float* chunks;                  // [chunk][chunk_stride]
-    int64_t chunk_stride;
+    // [chunk][2][part_stride]: sums of the chunk's tokens of a row that came before, and of one that began there and goes on
+    float* parts;
+    int64_t part_stride;
     float scale;
     void* out;
     int64_t out_stride;
-    int64_t common;  // whole chunks
+    int32_t blocks;  // of columns
+    int64_t common;  // workgroups for rows of many parts
     bool past_caches;
 };
 
@@ -301,75 +305,28 @@ struct Batch {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint32_t t = (uint32_t)__builtin_amdgcn_readlane((int)places, from + u);
-            if (c.in) x[u] = load_vec<T, V>((const T*)g.dy + (int64_t)t * g.dy_stride + c.at);
+            x[u] = load_vec<T, V>((const T*)g.dy + (int64_t)t * g.dy_stride + (c.in ? c.at : 0));
         }
     }
-    __device__ __forceinline__ void add(float (&sum)[V]) const {
+    // Waits for all of them at once: behind a store that not every wave makes, each use of a loaded value would wait for
+    // all loads and stores under way.
+    __device__ __forceinline__ void arrive() {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int e = 0; e < V; ++e) sum[e] += (float)x[u].e[e];
+        for (int u = 0; u < U; ++u) {
+            if constexpr (V == 1) {
+                uint32_t v = 0;
+                __builtin_memcpy(&v, &x[u], sizeof(x[u]));
+                asm volatile("" : "+v"(v));
+                __builtin_memcpy(&x[u], &v, sizeof(x[u]));
+            } else {
+                typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+                uint4v v = __builtin_bit_cast(uint4v, x[u]);
+                asm volatile("" : "+v"(v));
+                x[u] = __builtin_bit_cast(Vec<T, V>, v);
+            }
+        }
     }
 };
-// Adds those at places [from, to).
-template <typename T, int V>
-__device__ __forceinline__ void add_places(float (&sum)[V], const SumArgs& g, uint32_t places, int from, int to, Columns<V> c) {
-    auto add = [&](auto count) {
-        Batch<T, V, count.value> b;
-        b.load(g, places, from, c);
-        b.add(sum);
-        from += count.value;
-    };
-    while (to - from >= 8) add(std::integral_constant<int, 8>{});
-    if (to - from >= 4) add(std::integral_constant<int, 4>{});
-    if (to - from >= 2) add(std::integral_constant<int, 2>{});
-    if (to - from >= 1) add(std::integral_constant<int, 1>{});
-}
-
-// The sums of a workgroup's four waves, in wave 0.
-template <int V>
-__device__ __forceinline__ void join_waves(float (&sum)[V], float (&joined)[3][V][kWave]) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    __syncthreads();  // the last ones have been read
-    if (w) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) joined[w - 1][e][lane] = sum[e];
-    }
-    __syncthreads();
-    if (w) return;
-#pragma unroll
-    for (int e = 0; e < V; ++e) sum[e] += joined[0][e][lane] + joined[1][e][lane] + joined[2][e][lane];
-}
-
-// One workgroup a chunk and column block: the chunk's part of the rows' spans, and its sum if all of it is one row's.
-template <typename T, int V>
-__global__ __launch_bounds__(256) void k_sum_chunks(SumArgs g) {
-    __shared__ float joined[3][V][kWave];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t chunk = blockIdx.x, start = chunk * kChunk;
-    const int64_t i = start + lane;
-    const bool in = i < g.tokens;
-    const uint32_t key = in ? g.keys[i] : ~0u;
-    if (blockIdx.y == 0 && w == 0 && in) {
-        const uint32_t before = i ? g.keys[i - 1] : ~0u;
-        if (key != before) {
-            if (key < g.vocabulary) g.spans[key].x = (int)i;
-            if (before < g.vocabulary) g.spans[before].y = (int)i;
-        }
-        if (i + 1 == g.tokens && key < g.vocabulary) g.spans[key].y = (int)g.tokens;
-    }
-    const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane((int)key);
-    if (__ballot(key == first) != ~0ull || first >= g.vocabulary) return;
-    const Columns<V> c = column_of<V>(blockIdx.y, 0, 1, lane, g.cols);
-    float sum[V] = {};
-    add_places<T, V>(sum, g, g.places[i], 16 * w, 16 * w + 16, c);
-    join_waves<V>(sum, joined);
-    if (w || !c.in) return;
-    Vec<float, V> r;
-#pragma unroll
-    for (int e = 0; e < V; ++e) r.e[e] = sum[e];
-    store_vec<float, V>(g.chunks + chunk * g.chunk_stride + c.at, r);
-}
 
 template <typename T, int V>
 __device__ __forceinline__ void store_sums(const float (&sum)[V], const SumArgs& g, int64_t row, Columns<V> c) {
@@ -382,102 +339,126 @@ __device__ __forceinline__ void store_sums(const float (&sum)[V], const SumArgs&
     else store_vec<T, V>(out, r);
 }
 
-// The first `common` workgroups: one for each chunk; the first whole chunk of a row stands for it, and the
-// workgroup's waves share the row's terms: tokens before that chunk, whole chunks, tokens behind the last one. The
-// other workgroups: kRows neighbouring rows a wave, those that have no whole chunk.
-constexpr int kRows = 4;
+// One wave a chunk and column block (those of a chunk are neighbours), half of its rows under way while the other half is
+// added; and the chunk's part of the rows' spans.
 template <typename T, int V>
-__global__ __launch_bounds__(256) void k_sum_rows(SumArgs g) {
-    __shared__ float joined[3][V][kWave];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const Columns<V> c = column_of<V>(blockIdx.y, 0, 1, lane, g.cols);
-    if ((int64_t)blockIdx.x >= g.common) {
-        const int64_t row0 = (((int64_t)blockIdx.x - g.common) * 4 + w) * kRows;
-        if (row0 >= g.vocabulary) return;
-        int2 span = make_int2(0, 0);
-        if (lane < kRows && row0 + lane < g.vocabulary) span = g.spans[row0 + lane];
-        // The rows' tokens as one list, which is gone through in steps of eight whatever row they belong to, the next
-        // eight under way. Lane r holds row r's end in it, and the sorted token of its entry i is i + shift.
-        const bool common = (span.x + kChunk - 1) / kChunk < span.y / kChunk;
-        const int size = common ? 0 : span.y - span.x;
-        int end = size;
-#pragma unroll
-        for (int d = 1; d < kRows; d <<= 1) {
-            const int before = __shfl_up(end, d);
-            if (lane >= d) end += before;
-        }
-        const int shift = span.x - (end - size);
-        const unsigned long long skipped = __ballot(common || row0 + lane >= g.vocabulary);
-        const int total = __builtin_amdgcn_readlane(end, kRows - 1);
-        auto places_of = [&](int base) {  // 64 entries
-            const int i = base + lane;
-            int at = i + __builtin_amdgcn_readlane(shift, 0);
-#pragma unroll
-            for (int r = 1; r < kRows; ++r)
-                if (i >= __builtin_amdgcn_readlane(end, r - 1)) at = i + __builtin_amdgcn_readlane(shift, r);
-            return i < total ? g.places[at] : 0;  // behind the end token 0, which is not added
-        };
-        constexpr int U = 8;
-        Batch<T, V, U> now, next;
-        uint32_t places = places_of(0);
-        float sum[V] = {};
-        if (total) now.load(g, places, 0, c);
-        int i = 0, r = 0;
-        auto finish = [&] {  // rows that end at entry i
-            while (r < kRows && __builtin_amdgcn_readlane(end, r) == i) {
-                if (!(skipped >> r & 1)) store_sums<T, V>(sum, g, row0 + r, c);
-#pragma unroll
-                for (int e = 0; e < V; ++e) sum[e] = 0.f;
-                ++r;
-            }
-        };
-        finish();
-        while (i < total) {
-            const int ahead = i + U;
-            if (ahead < total) {
-                if (ahead % kChunk == 0) places = places_of(ahead);
-                next.load(g, places, ahead % kChunk, c);
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (i >= total) break;
-#pragma unroll
-                for (int e = 0; e < V; ++e) sum[e] += (float)now.x[u].e[e];
-                ++i;
-                finish();
-            }
-            now = next;
-        }
-        return;
+__global__ __launch_bounds__(256) void k_sum_chunks(SumArgs g) {
+    const int lane = threadIdx.x & 63;
+    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), chunk = wave / g.blocks, start = chunk * kChunk;
+    const int block = (int)(wave % g.blocks);
+    if (start >= g.tokens) return;
+    const int64_t i = start + lane;
+    const bool in = lane < kChunk && i < g.tokens;
+    const uint32_t key = in ? g.keys[i] : ~0u;
+    const uint32_t before = in && i ? g.keys[i - 1] : ~0u, behind = in && i + 1 < g.tokens ? g.keys[i + 1] : ~0u;
+    const uint32_t places = in ? g.places[i] : 0;
+    if (block == 0 && in && key < g.vocabulary) {
+        if (key != before) g.spans[key].x = (int)i;
+        if (key != behind) g.spans[key].y = (int)i + 1;
     }
-    const int64_t chunk = blockIdx.x;
-    const uint32_t row = g.keys[chunk * kChunk];
-    if (row >= g.vocabulary) return;
-    const int2 span = g.spans[row];
-    const int first = (span.x + kChunk - 1) / kChunk, end = span.y / kChunk;  // whole chunks
-    if (first != chunk || first >= end) return;
+    const int total = (int)__popcll(__ballot(in && key < g.vocabulary));  // the others come last
+    if (!total) return;
+    const unsigned long long ends = __ballot(in && key != behind);
+    bool open = __builtin_amdgcn_readfirstlane((int)(key == before));  // the row's sum began in another chunk
+    const Columns<V> c = column_of<V>(block, 0, 1, lane, g.cols);
+    auto store_part = [&](const float (&sum)[V], int which) {
+        if (!c.in) return;
+        Vec<float, V> r;
+#pragma unroll
+        for (int e = 0; e < V; ++e) r.e[e] = sum[e];
+        store_vec<float, V>(g.parts + (2 * chunk + which) * g.part_stride + c.at, r);
+    };
+    constexpr int U = 16;
+    Batch<T, V, U> half[2];
     float sum[V] = {};
-    const int before = first * kChunk - span.x, behind = span.y - end * kChunk;  // below 64 each
-    uint32_t places = lane < before ? g.places[span.x + lane] : 0;
-    add_places<T, V>(sum, g, places, before * w / 4, before * (w + 1) / 4, c);
+    half[0].load(g, places, 0, c);  // lanes behind the end hold a place too, whose row is not added
+    auto add = [&](const Batch<T, V, U>& b, int at) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (at + u >= total) break;
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] += (float)b.x[u].e[e];
+            if (!(ends >> (at + u) & 1)) continue;
+            if (open) store_part(sum, 0);
+            else store_sums<T, V>(sum, g, __builtin_amdgcn_readlane((int)key, at + u), c);
+            open = false;
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] = 0.f;
+        }
+    };
+    half[0].arrive();
+    if (total > U) half[1].load(g, places, U, c);
+    add(half[0], 0);
+    if (total > U) {
+        half[1].arrive();
+        add(half[1], U);
+    }
+    if (!(ends >> (total - 1) & 1)) store_part(sum, open ? 0 : 1);
+}
+
+// Adds a row's parts, those of chunks first, first + 1, ... last: one a wave, every `by`th from `from` on.
+template <int V>
+__device__ __forceinline__ void add_parts(float (&sum)[V], const SumArgs& g, int first, int last, int from, int by, Columns<V> c) {
     auto add = [&](int i, auto count) {
         constexpr int U = count.value;
         Vec<float, V> x[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (c.in) x[u] = load_vec<float, V>(g.chunks + (int64_t)(i + 4 * u) * g.chunk_stride + c.at);
+        for (int u = 0; u < U; ++u) {
+            const int64_t chunk = i + by * u;
+            if (c.in) x[u] = load_vec<float, V>(g.parts + (2 * chunk + (chunk == first)) * g.part_stride + c.at);
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int e = 0; e < V; ++e) sum[e] += x[u].e[e];
     };
-    int i = first + w;
-    for (; i + 12 < end; i += 16) add(i, std::integral_constant<int, 4>{});
-    for (; i < end; i += 4) add(i, std::integral_constant<int, 1>{});
-    places = lane < behind ? g.places[end * kChunk + lane] : 0;
-    add_places<T, V>(sum, g, places, behind * w / 4, behind * (w + 1) / 4, c);
-    join_waves<V>(sum, joined);
-    if (!w) store_sums<T, V>(sum, g, row, c);
+    int i = first + from;
+    for (; i + 3 * by <= last; i += 4 * by) add(i, std::integral_constant<int, 4>{});
+    for (; i <= last; i += by) add(i, std::integral_constant<int, 1>{});
+}
+
+// The first `common` workgroups: one for each chunk; the second one of a row that has many stands for it, and the
+// workgroup's waves share its parts. The others: kRows neighbouring rows a wave, those without tokens and those of few
+// parts.
+constexpr int kRows = 4;
+template <typename T, int V>
+__global__ __launch_bounds__(256) void k_finish_rows(SumArgs g) {
+    __shared__ float joined[3][V][kWave];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const Columns<V> c = column_of<V>(blockIdx.y, 0, 1, lane, g.cols);
+    if ((int64_t)blockIdx.x >= g.common) {
+        const int64_t row0 = (((int64_t)blockIdx.x - g.common) * 4 + w) * kRows;
+        int2 span = make_int2(0, 0);
+        if (lane < kRows && row0 + lane < g.vocabulary) span = g.spans[row0 + lane];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            if (row0 + r >= g.vocabulary) return;
+            const int from = __builtin_amdgcn_readlane(span.x, r), to = __builtin_amdgcn_readlane(span.y, r);
+            const int first = from / kChunk, last = (to - 1) / kChunk;
+            if (from < to && (first == last || last - first >= kFew)) continue;
+            float sum[V] = {};
+            if (from < to) add_parts<V>(sum, g, first, last, 0, 1, c);
+            store_sums<T, V>(sum, g, row0 + r, c);
+        }
+        return;
+    }
+    const int chunk = (int)blockIdx.x;
+    const uint32_t row = g.keys[(int64_t)chunk * kChunk];
+    if (row >= g.vocabulary) return;
+    const int2 span = g.spans[row];
+    const int first = span.x / kChunk, last = (span.y - 1) / kChunk;
+    if (chunk != first + 1 || last - first < kFew) return;
+    float sum[V] = {};
+    add_parts<V>(sum, g, first, last, w, 4, c);
+    if (w) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) joined[w - 1][e][lane] = sum[e];
+    }
+    __syncthreads();
+    if (w) return;
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[e] += joined[0][e][lane] + joined[1][e][lane] + joined[2][e][lane];
+    store_sums<T, V>(sum, g, row, c);
 }
 
 // ---------------------------------------------------------------------------- launches
@@ -510,20 +491,21 @@ void lookup(LookupArgs g, hipStream_t s) {
 template <typename T>
 void sums(SumArgs g, hipStream_t s) {
     constexpr int W = 16 / sizeof(T);
-    g.common = g.tokens / kChunk;
+    g.blocks = 1;
+    g.common = g.tokens > kFew * kChunk ? cover(g.tokens, kChunk) : 0;
     g.past_caches = g.vocabulary * g.cols * (int64_t)sizeof(T) > kCached;
     by_width(g.cols, W, [&](auto narrow, int64_t blocks) {
         constexpr int V = narrow.value ? 1 : W;
+        g.blocks = (int32_t)blocks;
         if (g.tokens)
-            hipLaunchKernelGGL((k_sum_chunks<T, V>), dim3((uint32_t)cover(g.tokens, kChunk), (uint32_t)blocks), dim3(256), 0,
-                               s, g);
-        hipLaunchKernelGGL((k_sum_rows<T, V>), dim3((uint32_t)(g.common + cover(g.vocabulary, 4 * kRows)), (uint32_t)blocks),
+            hipLaunchKernelGGL((k_sum_chunks<T, V>), dim3((uint32_t)cover(cover(g.tokens, kChunk) * blocks, 4)), dim3(256), 0, s, g);
+        hipLaunchKernelGGL((k_finish_rows<T, V>), dim3((uint32_t)(g.common + cover(g.vocabulary, 4 * kRows)), (uint32_t)blocks),
                            dim3(256), 0, s, g);
     });
 }
 
 struct BackwardScratch {
-    int64_t keys[2], places[2], counts, spans, chunks, bytes;
+    int64_t keys[2], places[2], counts, spans, parts, bytes;
 };
 BackwardScratch backward_scratch(int64_t tokens, int64_t vocabulary, int64_t cols) {
     BackwardScratch b{};
@@ -535,7 +517,7 @@ BackwardScratch backward_scratch(int64_t tokens, int64_t vocabulary, int64_t col
     for (int i = 0; i < 2; ++i) b.keys[i] = take(tokens * 4), b.places[i] = take(tokens * 4);
     b.counts = take((int64_t)kMaxTiles * kDigits * 4);
     b.spans = take(vocabulary * 8);
-    b.chunks = take(tokens / kChunk * cols * 4);
+    b.parts = take(cover(tokens, kChunk) * 2 * cols * 4);
     return b;
 }
 
@@ -629,7 +611,7 @@ int warp_embedding_backward(const void* dy, int64_t dy_stride, const void* ids, 
         sorted = (p.passes - 1) & 1;
     }
     const SumArgs g{dy, dy_stride, tokens, vocabulary, cols, keys[sorted], places[sorted], a.spans,
-                    (float*)(base + b.chunks), cols, scale, dtable, dtable_stride, 0, false};
+                    (float*)(base + b.parts), cols, scale, dtable, dtable_stride, 0, 0, false};
     if (dtype == WARP_F32) WARP_LAUNCH(sums<float>(g, s));
     else if (dtype == WARP_F16) WARP_LAUNCH(sums<_Float16>(g, s));
     else WARP_LAUNCH(sums<__bf16>(g, s));
