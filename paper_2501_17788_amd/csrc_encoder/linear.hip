@@ -35,10 +35,10 @@ int check_scratch(const char* what, const void* scratch, int64_t bytes, int64_t 
 struct Product {
     Tile tile;
     bool split;
-    int64_t floats;
-    Product(int64_t m, int64_t n, int64_t k, int32_t dtype) {
-        const ProductPlan p = plan_product(m, n, product_steps(k, terms_of(dtype)), true);
-        tile = p.tile, split = p.split;
+    int64_t floats, time;
+    Product(int64_t m, int64_t n, int64_t k, int32_t dtype, Tile largest = kT256) {
+        const ProductPlan p = plan_product(m, n, product_steps(k, terms_of(dtype)), true, largest);
+        tile = p.tile, split = p.split, time = p.time;
         floats = split ? part_floats(m, n, k, terms_of(dtype), tile, kMaxSplits, tile_jobs(tile)) : 0;
     }
 };
@@ -49,10 +49,10 @@ hipError_t run_product(ProductCall call, ProductArgs g, const Product& plan, flo
     g.terms = terms_of(dtype);
     g.splits = kMaxSplits, g.jobs = tile_jobs(plan.tile);
     g.part = part, g.part_stride = cover_of(g.n, 4) * 4;
-    if (!plan.split) return call(g, element_of(dtype), plan.tile, kStore, s);
-    const hipError_t e = g.b_scale ? product_bytes(g, element_of(dtype), plan.tile, s)
-                                   : call(g, element_of(dtype), plan.tile, kSum, s);
-    if (e) return e;
+    const Finish finish = plan.split ? kSum : kStore;
+    const hipError_t e = g.b_scale ? product_bytes(g, element_of(dtype), plan.tile, finish, s)
+                                   : call(g, element_of(dtype), plan.tile, finish, s);
+    if (e || !plan.split) return e;
     const Join j{part, g.part_stride, g.m, g.n, g.k, nullptr, nullptr, g.terms, g.splits, g.jobs, tile_size(plan.tile),
                  nullptr, nullptr, g.m, g.out, g.out_stride, g.out_type, g.bias, g.bias_type};
     return join_parts(j, s);
@@ -73,20 +73,28 @@ struct Forward {
     uint16_t *x, *w;
     float* part;
     Product y;
+    bool few;
     Forward(void* base, const void* x_, int64_t x_stride, int64_t rows, int64_t cols, int32_t dtype, const void* w_,
             int64_t w_stride, int64_t n)
         : y(rows, n, cols, dtype) {
         space.base = (uint8_t*)base;
+        few = rows <= kFewRows && dtype != WARP_F32;
+        if (few) y.floats = 0;
         x = space.take<uint16_t>(direct(x_, x_stride, rows, cols, dtype) ? 0 : packed_elements(rows, cols, dtype));
         w = space.take<uint16_t>(direct(w_, w_stride, n, cols, dtype) ? 0 : packed_elements(n, cols, dtype));
         part = space.take<float>(y.floats);
     }
 };
 
-// Few output channels: every 8-bit row is read by one or two tiles, so that the product takes it as it is. With more,
-// rows are unpacked once, to be read by loads that pass no registers (65,536 x 1024 by 128: 45 us instead of 36 for unpacking
-// and 43 for the product; 32,768 x 4096 by 4096, in tiles of 128: 1500 us instead of 65 and 933).
-inline bool takes_bytes(int64_t n, int32_t dtype) { return dtype != WARP_F32 && n <= 256; }
+// Whether dweight's product takes the 8-bit rows as they are, and dbias with them, or has them unpacked and dy summed
+// first. Its loads pass registers then, and tiles are 128 x 128 at most: an eighth more time for each; the other way
+// reads and writes the rows and reads dy once more, with three launches. `direct`, `packed`: the products' times, ns.
+// us for dweight and dbias, as they are | unpacked: 1 x 1024 by 1024 9.4 | 15.9, 1771 x 768 by 1000 19.4 | 30.9, 65,536 x 1024 by
+// 128 45 | 96, by 512 112 | 172, by 1024 188 | 222, 16,384 x 1024 by 1024 67 | 72, 32,768 x 2048 by 2048 351 | 314, 4096 x 4096 by
+// 4096 168 | 133, 32,768 x 4096 by 4096 1344 | 990.
+inline bool takes_bytes(int64_t rows, int64_t n, int64_t cols, int32_t dtype, int64_t direct, int64_t packed) {
+    return dtype != WARP_F32 && direct + direct / 8 + 5000 < packed + rows * cols * 3 / 5000 + rows * n * 2 / 5000 + 12000;
+}
 
 struct Backward {
     Space space;
@@ -101,14 +109,14 @@ struct Backward {
         space.base = (uint8_t*)base;
         dy = space.take<uint16_t>(direct(dy_, dy_stride, rows, n, dtype) ? 0 : packed_elements(rows, n, dtype));
         w = space.take<uint16_t>(direct(w_, w_stride, n, cols, dtype) ? 0 : packed_elements(n, cols, dtype));
-        bytes = takes_bytes(n, dtype);
+        const Product direct_dw(n, cols, rows, dtype, kT128);
+        bytes = takes_bytes(rows, n, cols, dtype, direct_dw.time, dw.time);
         sums = 0;
         if (bytes) {
-            const int64_t steps = product_steps(rows, 1);
-            dw.tile = plan_product(n, cols, steps, true, kT128).tile, dw.split = true;
-            dw.floats = part_floats(n, cols, rows, 1, dw.tile, kMaxSplits, tile_jobs(dw.tile));
-            sums = product_splits(n, cols, steps, tile_size(dw.tile), kMaxSplits, tile_jobs(dw.tile)) *
-                   cover_of(cols, tile_size(dw.tile));
+            dw = direct_dw;
+            sums = dw.split ? product_splits(n, cols, product_steps(rows, 1), tile_size(dw.tile), kMaxSplits, tile_jobs(dw.tile))
+                            : 1;
+            sums *= cover_of(cols, tile_size(dw.tile));
         }
         x = space.take<uint16_t>(bytes ? 0 : packed_elements(rows, cols, dtype));
         part = space.take<float>(dx.floats > dw.floats ? dx.floats : dw.floats);
@@ -162,7 +170,8 @@ int warp_linear(const void* x, int64_t x_stride, int64_t rows, int32_t cols, int
     WARP_STEP(e);
     ProductArgs g = product_args(a, b, rows, n, cols, y, y_stride, dtype);
     g.bias = bias, g.bias_type = bias_dtype;
-    WARP_STEP(run_product(product_along, g, f.y, f.part, dtype, s));
+    if (f.few) WARP_STEP(product_few(g, element_of(dtype), s));
+    else WARP_STEP(run_product(product_along, g, f.y, f.part, dtype, s));
     return WARP_OK;
 }
 

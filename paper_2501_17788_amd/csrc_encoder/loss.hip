@@ -37,10 +37,10 @@ struct SelectArgs {
     float* largest;
 };
 
-// One workgroup: turns of sixteen times 1024 neighbouring tokens, whose loads and stores are in one piece a wave.
+// One workgroup: turns of eight times 1024 neighbouring tokens, whose loads and stores are in one piece a wave.
 __global__ __launch_bounds__(1024) void k_select(SelectArgs g) {
-    constexpr int N = 16;
-    __shared__ int32_t waves[N][16];
+    constexpr int N = 8;
+    __shared__ __attribute__((aligned(8))) int32_t waves[N][16];
     __shared__ uint32_t tops[16];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     int32_t count = 0;
@@ -71,20 +71,19 @@ __global__ __launch_bounds__(1024) void k_select(SelectArgs g) {
             if (in && d[e] < 0x7f800000u) top = max(top, d[e]);
         }
         __syncthreads();
-        // the turn's tokens before each wave of each 1024: 256 numbers, four a lane
-        const int4 n = ((const int4*)waves)[lane];
-        const int32_t mine = n.x + n.y + n.z + n.w;
+        // the turn's tokens before each wave of each 1024: 128 numbers, two a lane
+        const int2 n = ((const int2*)waves)[lane];
+        const int32_t mine = n.x + n.y;
         int32_t x = mine;
 #pragma unroll
         for (int s = 1; s < 64; s <<= 1) {
             const int32_t v = __shfl_up(x, s);
             if (lane >= s) x += v;
         }
-        const int part = w & 3;
-        const int32_t before = x - mine + (part > 0 ? n.x : 0) + (part > 1 ? n.y : 0) + (part > 2 ? n.z : 0);
+        const int32_t before = x - mine + (w & 1 ? n.x : 0);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const int32_t first = count + __builtin_amdgcn_readlane(before, 4 * e + (w >> 2));
+            const int32_t first = count + __builtin_amdgcn_readlane(before, 8 * e + (w >> 1));
             const int64_t t = t0 + 1024 * e;
             if (t >= g.tokens) continue;
             g.place[t] = rank[e] >= 0 ? first + rank[e] : y[e] < 0 ? -1 : -2;
@@ -108,6 +107,66 @@ __global__ __launch_bounds__(1024) void k_select(SelectArgs g) {
     *g.factor = largest * g.scale / g.grad_scale;
 }
 
+// Up to 64 tokens, in one launch: a workgroup for each, whose waves all look at all targets; it packs its own row, and the
+// first one writes what k_select and k_rows write.
+constexpr int kFewTokens = 64;
+struct FewArgs {
+    SelectArgs select;
+    const void* hidden;
+    int64_t hidden_stride, cols, width, plane;
+    uint16_t* packed;
+    const float *loss, *lse;  // of the forward pass, with dloss
+    float *lse2, *weight, *at_target;
+};
+template <typename T, int PLANES>
+__global__ __launch_bounds__(256) void k_take_few(FewArgs f) {
+    const SelectArgs& g = f.select;
+    const int lane = threadIdx.x & 63, me = (int)blockIdx.x;
+    int64_t y = -1;
+    if (lane < g.tokens) y = g.wide ? ((const int64_t*)g.targets)[lane] : (int64_t)((const int32_t*)g.targets)[lane];
+    const bool in = y >= 0 && y < g.vocabulary;
+    const unsigned long long all = __ballot(in);
+    const int rank = (int)__popcll(all & ((1ull << lane) - 1));
+    if (me == 0 && threadIdx.x < 64) {
+        if (lane < g.tokens) g.place[lane] = in ? rank : y < 0 ? -1 : -2;
+        if (in) g.list[rank] = lane, g.target[rank] = (int32_t)y;
+        if (lane == 0) *g.now = (int32_t)__popcll(all);
+        if (g.dloss) {
+            const float d = in ? g.dloss[lane] : 0.f;
+            const uint32_t u = as_u(d) & 0x7fffffffu, top = wave_max(u < 0x7f800000u ? u : 0u);
+            const float largest = top ? as_f(top) : 1.f;
+            if (lane == 0) *g.largest = largest, *g.factor = largest * g.scale / g.grad_scale;
+            if (in) {
+                const float weight = d / largest;
+                f.lse2[rank] = f.lse[lane] * kLog2E;
+                f.weight[rank] = weight;
+                f.at_target[rank] = weight * expm1f(-f.loss[lane]);
+            }
+        }
+    }
+    if (!(all >> me & 1)) return;
+    const int64_t row = __builtin_amdgcn_readlane(rank, me);
+    const T* x = (const T*)f.hidden + me * f.hidden_stride;
+    for (int64_t c = (int64_t)threadIdx.x * 8; c < f.width; c += 8 * 256) {
+        float v[8];
+        if (c + 8 <= f.cols) {
+            const auto r = load_vec<T, 8>(x + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (float)r.e[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = c + e < f.cols ? (float)x[c + e] : 0.f;
+        }
+        store_packed<T, PLANES>(f.packed, f.plane, row * f.width + c, v);
+    }
+}
+void take_few(const FewArgs& f, int32_t dtype, hipStream_t s) {
+    const dim3 grid((uint32_t)f.select.tokens), block(256);
+    if (dtype == WARP_F32) hipLaunchKernelGGL((k_take_few<float, 3>), grid, block, 0, s, f);
+    else if (dtype == WARP_F16) hipLaunchKernelGGL((k_take_few<_Float16, 1>), grid, block, 0, s, f);
+    else hipLaunchKernelGGL((k_take_few<__bf16, 1>), grid, block, 0, s, f);
+}
+
 // ---------------------------------------------------------------------------- forward
 
 struct JoinStatsArgs {
@@ -127,38 +186,21 @@ __device__ __forceinline__ float2 join_stats(float2 a, float2 b) {
     return make_float2(top, a.y * __builtin_amdgcn_exp2f(a.x - from) + b.y * __builtin_amdgcn_exp2f(b.x - from));
 }
 
-// 64 tokens a workgroup, whose 16 waves share the tiles.
-__global__ __launch_bounds__(1024) void k_join_stats(JoinStatsArgs g) {
-    __shared__ float2 joined[16][kWave];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t t = (int64_t)blockIdx.x * kWave + lane;
-    const int32_t row = t < g.tokens ? g.place[t] : -1;
-    float2 s = make_float2(-INFINITY, 0.f);
-    if (row >= 0) {
-        if (w == 0 && !g.first) s = g.running[row];
-        constexpr int U = 4;
-        for (int i = w; i < g.tiles; i += 16 * U) {
-            float2 x[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                x[u] = i + 16 * u < g.tiles ? g.stats[(i + 16 * u) * g.stride + row] : make_float2(-INFINITY, 0.f);
-#pragma unroll
-            for (int u = 0; u < U; ++u) s = join_stats(s, x[u]);
-        }
-    }
-    joined[w][lane] = s;
-    __syncthreads();
-    if (w || t >= g.tokens) return;
+// Lane k's and lane k ^ d's.
+__device__ __forceinline__ float2 join_lanes(float2 s, int d) {
+    return join_stats(s, make_float2(__shfl_xor(s.x, d), __shfl_xor(s.y, d)));
+}
+
+// The row's loss from the others' sum, s.y * 2^s.x, and the target's term, 2^y.
+__device__ __forceinline__ void store_loss(const JoinStatsArgs& g, int64_t t, int32_t row, float2 s) {
     if (row < 0) {
         if (g.last) g.loss[t] = g.lse[t] = row == -1 ? 0.f : __builtin_nanf("");
         return;
     }
-    for (int i = 1; i < 16; ++i) s = join_stats(s, joined[i][lane]);
     if (!g.last) {
         g.running[row] = s;
         return;
     }
-    // the others' sum is s.y * 2^s.x, the target's term 2^y
     const float y = g.of_target[row];
     if (y >= s.x) {
         const float others = s.y * __builtin_amdgcn_exp2f(s.x - y), loss = log1pf(others);
@@ -169,6 +211,41 @@ __global__ __launch_bounds__(1024) void k_join_stats(JoinStatsArgs g) {
         g.loss[t] = (s.x - y) * kLn2 + all;
         g.lse[t] = s.x * kLn2 + all;
     }
+}
+
+// 64 tokens a workgroup, whose 16 waves share the tiles; of few tokens one, whose lanes share them too.
+template <bool FEW>
+__global__ __launch_bounds__(1024) void k_join_stats(JoinStatsArgs g) {
+    __shared__ float2 joined[16][FEW ? 1 : kWave];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t t = FEW ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kWave + lane;
+    const int32_t row = t < g.tokens ? g.place[t] : -1;
+    float2 s = make_float2(-INFINITY, 0.f);
+    if (row >= 0) {
+        if ((FEW ? threadIdx.x : w) == 0 && !g.first) s = g.running[row];
+        constexpr int U = FEW ? 1 : 4;
+        const int from = FEW ? (int)threadIdx.x : w, by = FEW ? 1024 : 16;
+        for (int i = from; i < g.tiles; i += by * U) {
+            float2 x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                x[u] = i + by * u < g.tiles ? g.stats[(i + by * u) * g.stride + row] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int u = 0; u < U; ++u) s = join_stats(s, x[u]);
+        }
+    }
+    if constexpr (FEW) {
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) s = join_lanes(s, d);
+        if (lane == 0) joined[w][0] = s;
+    } else {
+        joined[w][lane] = s;
+    }
+    __syncthreads();
+    if ((FEW ? threadIdx.x : w) || t >= g.tokens) return;
+    if (row >= 0)
+        for (int i = 1; i < 16; ++i) s = join_stats(s, joined[i][FEW ? 0 : lane]);
+    store_loss(g, t, row, s);
 }
 
 // ---------------------------------------------------------------------------- backward
@@ -349,8 +426,14 @@ int warp_cross_entropy(const void* hidden, int64_t hidden_stride, int64_t tokens
     hipStream_t s = (hipStream_t)hip_stream;
     const SelectArgs sel{targets, target_bytes == 8, tokens, vocabulary, nullptr, scale, 1.f, f.list, f.place, f.target,
                          f.now, nullptr, nullptr};
-    WARP_LAUNCH(hipLaunchKernelGGL(k_select, dim3(1), dim3(1024), 0, s, sel));
-    WARP_STEP(pack_rows(hidden, hidden_stride, tokens, cols, dtype, f.list, f.now, f.hidden, s));
+    const bool few = tokens <= kFewTokens;
+    if (few) {
+        WARP_LAUNCH(take_few({sel, hidden, hidden_stride, cols, z.width, tokens * z.width, f.hidden, nullptr, nullptr, nullptr,
+                              nullptr, nullptr}, dtype, s));
+    } else {
+        WARP_LAUNCH(hipLaunchKernelGGL(k_select, dim3(1), dim3(1024), 0, s, sel));
+        WARP_STEP(pack_rows(hidden, hidden_stride, tokens, cols, dtype, f.list, f.now, f.hidden, s));
+    }
     for (int64_t v0 = 0; v0 < vocabulary; v0 += f.piece) {
         const int64_t n = vocabulary - v0 < f.piece ? vocabulary - v0 : f.piece;
         const void* rows = (const uint8_t*)table + v0 * table_stride * dtype_bytes(dtype);
@@ -370,7 +453,8 @@ int warp_cross_entropy(const void* hidden, int64_t hidden_stride, int64_t tokens
         WARP_STEP(product_softmax(g, element_of(dtype), false, f.tile, kStats, s));
         const JoinStatsArgs j{f.stats, tokens, (int)cover_of(n, tile_size(f.tile)), v0 == 0, v0 + n == vocabulary, f.running,
                               f.of_target, f.place, tokens, loss, lse};
-        WARP_LAUNCH(hipLaunchKernelGGL(k_join_stats, dim3((uint32_t)cover_of(tokens, kWave)), dim3(1024), 0, s, j));
+        if (few) WARP_LAUNCH(hipLaunchKernelGGL(k_join_stats<true>, dim3((uint32_t)tokens), dim3(1024), 0, s, j));
+        else WARP_LAUNCH(hipLaunchKernelGGL(k_join_stats<false>, dim3((uint32_t)cover_of(tokens, kWave)), dim3(1024), 0, s, j));
     }
     return WARP_OK;
 }
@@ -400,8 +484,13 @@ int warp_cross_entropy_backward(const float* dloss, const void* hidden, int64_t 
     const float grad_scale = dtype == WARP_F16 ? kHalfScale : 1.f;
     const SelectArgs sel{targets, target_bytes == 8, tokens, vocabulary, dloss, scale, grad_scale, w.list, w.place, w.target,
                          w.now, w.factor, w.largest};
-    WARP_LAUNCH(hipLaunchKernelGGL(k_select, dim3(1), dim3(1024), 0, s, sel));
-    if (tokens) {
+    if (tokens && tokens <= kFewTokens) {
+        WARP_LAUNCH(take_few({sel, hidden, hidden_stride, cols, z.width, tokens * z.width, w.hidden, loss, lse, w.lse2, w.weight,
+                              w.at_target}, dtype, s));
+    } else {
+        WARP_LAUNCH(hipLaunchKernelGGL(k_select, dim3(1), dim3(1024), 0, s, sel));
+    }
+    if (tokens > kFewTokens) {
         WARP_STEP(pack_rows(hidden, hidden_stride, tokens, cols, dtype, w.list, w.now, w.hidden, s));
         const RowArgs r{w.list, w.now, dloss, loss, lse, w.largest, w.lse2, w.weight, w.at_target};
         WARP_LAUNCH(hipLaunchKernelGGL(k_rows, dim3((uint32_t)cover_of(tokens, 256)), dim3(256), 0, s, r));

@@ -36,6 +36,29 @@ inline bool direct(const void* p, int64_t stride, int64_t rows, int64_t cols, in
     return dtype != WARP_F32 && (uintptr_t)p % 16 == 0 && cols % 8 == 0 && (rows <= 1 || (stride % 8 == 0 && stride <= 1 << 22));
 }
 
+#ifdef __HIPCC__
+// Eight elements of an operand.
+template <typename E, int PLANES>
+__device__ __forceinline__ void store_packed(uint16_t* out, int64_t plane, int64_t at, const float (&v)[8]) {
+    if constexpr (PLANES == 3) {
+        Vec<uint16_t, 8> p[3];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            uint16_t s[3];
+            split_f32(v[e], s);
+            p[0].e[e] = s[0], p[1].e[e] = s[1], p[2].e[e] = s[2];
+        }
+#pragma unroll
+        for (int t = 0; t < 3; ++t) store_vec<uint16_t, 8>(out + t * plane + at, p[t]);
+    } else {
+        Vec<E, 8> p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p.e[e] = (E)v[e];
+        store_vec<E, 8>((E*)out + at, p);
+    }
+}
+#endif
+
 // Rows (those of `list`, if given, as many as *now) as an operand of its own: padded with zeros to a multiple of 64
 // columns, float32 in planes.
 hipError_t pack_rows(const void* x, int64_t stride, int64_t rows, int64_t cols, int32_t dtype, const int32_t* list,

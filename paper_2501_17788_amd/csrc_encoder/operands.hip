@@ -13,26 +13,6 @@ dim3 row_grid(int64_t rows, int64_t width) {
     return dim3((uint32_t)cover_of(width, 512), (uint32_t)(groups < kMaxRowGroups ? groups : kMaxRowGroups));
 }
 
-template <typename E, int PLANES>
-__device__ __forceinline__ void store_packed(uint16_t* out, int64_t plane, int64_t at, const float (&v)[8]) {
-    if constexpr (PLANES == 3) {
-        Vec<uint16_t, 8> p[3];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            uint16_t s[3];
-            split_f32(v[e], s);
-            p[0].e[e] = s[0], p[1].e[e] = s[1], p[2].e[e] = s[2];
-        }
-#pragma unroll
-        for (int t = 0; t < 3; ++t) store_vec<uint16_t, 8>(out + t * plane + at, p[t]);
-    } else {
-        Vec<E, 8> p;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p.e[e] = (E)v[e];
-        store_vec<E, 8>((E*)out + at, p);
-    }
-}
-
 template <typename T, int PLANES>
 __global__ __launch_bounds__(64 * kRowWaves) void k_pack_rows(const T* x, int64_t stride, int64_t rows, int64_t cols,
                                                               const int32_t* list, const int32_t* now, uint16_t* out,

@@ -81,6 +81,7 @@ inline int tile_jobs(Tile t) { return t == kT64 ? 1024 : t == kT128 ? 512 : 256;
 struct ProductPlan {
     Tile tile;
     bool split;
+    int64_t time;  // by the model below
 };
 // The faster one by a model of measured times, in ns. `jobs` tiles of `steps` steps take rounds of as many as are at work at
 // once, the last one less where it leaves compute units to fewer. Their bytes take time too: operands from memory at 5 TB/s and
@@ -112,19 +113,18 @@ inline int64_t product_traffic(Tile t, int64_t m, int64_t n, int64_t steps) {
 }
 constexpr int kMaxSplits = 256;
 inline ProductPlan plan_product(int64_t m, int64_t n, int64_t steps, bool may_split, Tile largest = kT256) {
-    ProductPlan best{kT64, false};
-    int64_t least = INT64_MAX;
+    ProductPlan best{kT64, false, INT64_MAX};
     for (const Tile t : {kT64, kT128, kT256}) {
         if (t > largest) break;
         const int64_t tiles = cover_of(m, tile_size(t)) * cover_of(n, tile_size(t));
         const int64_t traffic = product_traffic(t, m, n, steps);
         auto both = [&](int64_t time) { return time > traffic ? time + traffic / 4 : traffic + time / 4; };
         const int64_t whole = both(product_time(t, tiles, steps));
-        if (whole < least) least = whole, best = {t, false};
+        if (whole < best.time) best = {t, false, whole};
         const int splits = may_split ? product_splits(m, n, steps, tile_size(t), kMaxSplits, tile_jobs(t)) : 1;
         if (splits < 2) continue;
         const int64_t parts = both(product_time(t, tiles * splits, cover_of(steps, splits))) + 5500 + m * n * splits / 500;
-        if (parts < least) least = parts, best = {t, true};
+        if (parts < best.time) best = {t, true, parts};
     }
     return best;
 }
@@ -152,7 +152,9 @@ __host__ __device__ inline void split_f32(float x, uint16_t (&out)[3]) {
 hipError_t product_along(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);   // A, B along K
 hipError_t product_mixed(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);   // B across K
 hipError_t product_across(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);  // both
-hipError_t product_bytes(const ProductArgs& g, int element, Tile tile, hipStream_t s);  // both; b of 8 bits; kSum, to kT128
+constexpr int kFewRows = 32;
+hipError_t product_few(const ProductArgs& g, int element, hipStream_t s);  // both along K; kStore of up to kFewRows rows
+hipError_t product_bytes(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);  // b of 8 bits; to kT128
 hipError_t product_softmax(const ProductArgs& g, int element, bool planes, Tile tile, Finish finish, hipStream_t s);
 
 #ifdef __HIPCC__
@@ -524,6 +526,15 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
         for (int i = 0; i < kBM; ++i) neighbours<kBN>(acc[i]);
     }
     const int64_t c = c0 + wn + (kWide || kBN == 4 ? kOut * q : 16 * (q & 1) + 8 * (q >> 1));
+    if constexpr (KIND == kBytes) {
+        if (g.sums && wave % WN == 0 && q == 0) {
+#pragma unroll
+            for (int i = 0; i < kBM; ++i) {
+                const int64_t m = m0 + wm + 16 * i + li;
+                if (m < rows) g.sums[((int64_t)split * tiles_n + tile_n) * rows + m] = totals[i][0];
+            }
+        }
+    }
     if constexpr (F == kStore) {
         if (c >= g.n) return;
         const float factor = g.factor ? *g.factor : 1.f;
@@ -542,15 +553,6 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
         }
     } else if constexpr (F == kSum) {
         float* out = g.part + split * rows * g.part_stride;
-        if constexpr (KIND == kBytes) {
-            if (g.sums && wave % WN == 0 && q == 0) {
-#pragma unroll
-                for (int i = 0; i < kBM; ++i) {
-                    const int64_t m = m0 + wm + 16 * i + li;
-                    if (m < rows) g.sums[((int64_t)split * tiles_n + tile_n) * rows + m] = totals[i][0];
-                }
-            }
-        }
 #pragma unroll
         for (int i = 0; i < kBM; ++i) {
             const int64_t m = m0 + wm + 16 * i + li;

@@ -7,9 +7,12 @@ hipError_t product_across(const ProductArgs& g, int element, Tile tile, Finish f
     return product_any<kAcrossK, kAcrossK>(g, element, tile, finish, s);
 }
 
-hipError_t product_bytes(const ProductArgs& g, int element, Tile tile, hipStream_t s) {
-    return element == WARP_F16 ? product_tiles<_Float16, kAcrossK, kAcrossK, kSum, kBytes>(g, tile, s)
-                               : product_tiles<__bf16, kAcrossK, kAcrossK, kSum, kBytes>(g, tile, s);
+hipError_t product_bytes(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s) {
+    if (element == WARP_F16)
+        return finish == kSum ? product_tiles<_Float16, kAcrossK, kAcrossK, kSum, kBytes>(g, tile, s)
+                              : product_tiles<_Float16, kAcrossK, kAcrossK, kStore, kBytes>(g, tile, s);
+    return finish == kSum ? product_tiles<__bf16, kAcrossK, kAcrossK, kSum, kBytes>(g, tile, s)
+                          : product_tiles<__bf16, kAcrossK, kAcrossK, kStore, kBytes>(g, tile, s);
 }
 
 }  // namespace warp
