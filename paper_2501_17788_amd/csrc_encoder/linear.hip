@@ -164,10 +164,10 @@ int warp_linear(const void* x, int64_t x_stride, int64_t rows, int32_t cols, int
     if (!rc) rc = require_device();
     if (rc || !rows) return rc;
     hipStream_t s = (hipStream_t)hip_stream;
-    hipError_t e = hipSuccess;
-    const Operand a = operand_of(x, x_stride, rows, cols, dtype, f.x, s, &e);
-    const Operand b = operand_of(weight, weight_stride, n, cols, dtype, f.w, s, &e);
-    WARP_STEP(e);
+    PackRows pack_x, pack_w;
+    const Operand a = operand_of(x, x_stride, rows, cols, dtype, f.x, &pack_x);
+    const Operand b = operand_of(weight, weight_stride, n, cols, dtype, f.w, &pack_w);
+    WARP_STEP(pack_rows(pack_x, pack_w, dtype, s));
     ProductArgs g = product_args(a, b, rows, n, cols, y, y_stride, dtype);
     g.bias = bias, g.bias_type = bias_dtype;
     if (f.few) WARP_STEP(product_few(g, element_of(dtype), s));
@@ -210,12 +210,12 @@ int warp_linear_backward(const void* dy, int64_t dy_stride, int64_t rows, int32_
     if (!rc) rc = require_device();
     if (rc) return rc;
     hipStream_t s = (hipStream_t)hip_stream;
-    hipError_t e = hipSuccess;
+    PackRows pack_dy, pack_w;
     Operand d{}, t{};
-    if (rows && (dx || dweight)) d = operand_of(dy, dy_stride, rows, n, dtype, w.dy, s, &e);
+    if (rows && (dx || dweight)) d = operand_of(dy, dy_stride, rows, n, dtype, w.dy, &pack_dy);
+    if (rows && dx) t = operand_of(weight, weight_stride, n, cols, dtype, w.w, &pack_w);
+    WARP_STEP(pack_rows(pack_dy, pack_w, dtype, s));
     if (rows && dx) {
-        t = operand_of(weight, weight_stride, n, cols, dtype, w.w, s, &e);
-        WARP_STEP(e);
         WARP_STEP(run_product(product_mixed, product_args(d, t, rows, cols, n, dx, dx_stride, dtype), w.dx, w.part, dtype, s));
     }
     const bool bytes = dweight && w.bytes && rows;

@@ -432,7 +432,7 @@ int warp_cross_entropy(const void* hidden, int64_t hidden_stride, int64_t tokens
                               nullptr, nullptr}, dtype, s));
     } else {
         WARP_LAUNCH(hipLaunchKernelGGL(k_select, dim3(1), dim3(1024), 0, s, sel));
-        WARP_STEP(pack_rows(hidden, hidden_stride, tokens, cols, dtype, f.list, f.now, f.hidden, s));
+        WARP_STEP(pack_rows({hidden, hidden_stride, tokens, cols, f.list, f.now, f.hidden}, {}, dtype, s));
     }
     for (int64_t v0 = 0; v0 < vocabulary; v0 += f.piece) {
         const int64_t n = vocabulary - v0 < f.piece ? vocabulary - v0 : f.piece;
@@ -440,7 +440,7 @@ int warp_cross_entropy(const void* hidden, int64_t hidden_stride, int64_t tokens
         hipError_t e = hipSuccess;
         Operand t{rows, vocabulary <= 1 ? cols : table_stride, 0};
         if (z.packs) {
-            e = pack_rows(rows, table_stride, n, cols, dtype, nullptr, nullptr, f.table, s);
+            e = pack_rows({rows, table_stride, n, cols, nullptr, nullptr, f.table}, {}, dtype, s);
             t = {f.table, z.width, n * z.width};
         }
         WARP_STEP(e);
@@ -491,7 +491,7 @@ int warp_cross_entropy_backward(const float* dloss, const void* hidden, int64_t 
         WARP_LAUNCH(hipLaunchKernelGGL(k_select, dim3(1), dim3(1024), 0, s, sel));
     }
     if (tokens > kFewTokens) {
-        WARP_STEP(pack_rows(hidden, hidden_stride, tokens, cols, dtype, w.list, w.now, w.hidden, s));
+        WARP_STEP(pack_rows({hidden, hidden_stride, tokens, cols, w.list, w.now, w.hidden}, {}, dtype, s));
         const RowArgs r{w.list, w.now, dloss, loss, lse, w.largest, w.lse2, w.weight, w.at_target};
         WARP_LAUNCH(hipLaunchKernelGGL(k_rows, dim3((uint32_t)cover_of(tokens, 256)), dim3(256), 0, s, r));
     }
@@ -504,7 +504,7 @@ int warp_cross_entropy_backward(const float* dloss, const void* hidden, int64_t 
         const void* rows = (const uint8_t*)table + v0 * table_stride * dtype_bytes(dtype);
         Operand t{rows, vocabulary <= 1 ? cols : table_stride, 0};
         if (z.packs) {
-            WARP_STEP(pack_rows(rows, table_stride, n, cols, dtype, nullptr, nullptr, w.table, s));
+            WARP_STEP(pack_rows({rows, table_stride, n, cols, nullptr, nullptr, w.table}, {}, dtype, s));
             t = {w.table, z.width, n * z.width};
         }
         ProductArgs g{};

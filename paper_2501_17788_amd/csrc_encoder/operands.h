@@ -26,7 +26,7 @@ struct Operand {
 inline int planes_of(int32_t dtype) { return dtype == WARP_F32 ? 3 : 1; }
 inline int terms_of(int32_t dtype) { return dtype == WARP_F32 ? 6 : 1; }
 inline int element_of(int32_t dtype) { return dtype == WARP_F16 ? WARP_F16 : WARP_BF16; }
-inline int64_t packed_width(int64_t cols) { return cover_of(cols, 64) * 64; }
+__host__ __device__ inline int64_t packed_width(int64_t cols) { return cover_of(cols, 64) * 64; }
 inline int64_t packed_elements(int64_t rows, int64_t cols, int32_t dtype) {
     return planes_of(dtype) * rows * packed_width(cols);
 }
@@ -59,19 +59,24 @@ __device__ __forceinline__ void store_packed(uint16_t* out, int64_t plane, int64
 }
 #endif
 
-// Rows (those of `list`, if given, as many as *now) as an operand of its own: padded with zeros to a multiple of 64
-// columns, float32 in planes.
-hipError_t pack_rows(const void* x, int64_t stride, int64_t rows, int64_t cols, int32_t dtype, const int32_t* list,
-                     const int32_t* now, uint16_t* out, hipStream_t s);
+// Rows (those of `list`, if given, as many as *now) that become an operand of their own: padded with zeros to a multiple of
+// 64 columns, float32 in planes. Two matrices in one launch; none where rows is 0.
+struct PackRows {
+    const void* x = nullptr;
+    int64_t stride = 0, rows = 0, cols = 0;
+    const int32_t *list = nullptr, *now = nullptr;
+    uint16_t* out = nullptr;
+};
+hipError_t pack_rows(const PackRows& a, const PackRows& b, int32_t dtype, hipStream_t s);
 // The same of 8-bit rows: q * scale, for products in `dtype`.
 hipError_t unpack_int8(const int8_t* q, int64_t q_stride, const float* scale, int64_t rows, int64_t cols, int32_t dtype,
                        uint16_t* out, hipStream_t s);
 
-// x as an operand, copied to `room` if it cannot be read where it lies.
+// x as an operand: where it lies, or in `room`, for which `job` is then what has to be packed.
 inline Operand operand_of(const void* x, int64_t stride, int64_t rows, int64_t cols, int32_t dtype, uint16_t* room,
-                          hipStream_t s, hipError_t* e) {
+                          PackRows* job) {
     if (direct(x, stride, rows, cols, dtype)) return {x, rows <= 1 ? cols : stride, 0};
-    *e = *e ? *e : pack_rows(x, stride, rows, cols, dtype, nullptr, nullptr, room, s);
+    *job = {x, stride, rows, cols, nullptr, nullptr, room};
     return {room, packed_width(cols), rows * packed_width(cols)};
 }
 

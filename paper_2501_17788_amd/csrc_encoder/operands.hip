@@ -13,25 +13,29 @@ dim3 row_grid(int64_t rows, int64_t width) {
     return dim3((uint32_t)cover_of(width, 512), (uint32_t)(groups < kMaxRowGroups ? groups : kMaxRowGroups));
 }
 
+// One matrix for each blockIdx.z.
+struct PackJobs {
+    PackRows m[2];
+};
 template <typename T, int PLANES>
-__global__ __launch_bounds__(64 * kRowWaves) void k_pack_rows(const T* x, int64_t stride, int64_t rows, int64_t cols,
-                                                              const int32_t* list, const int32_t* now, uint16_t* out,
-                                                              int64_t width, int64_t plane) {
+__global__ __launch_bounds__(64 * kRowWaves) void k_pack_rows(PackJobs jobs) {
+    const PackRows& j = jobs.m[blockIdx.z];
+    const int64_t width = packed_width(j.cols), plane = j.rows * width;
     const int64_t c = ((int64_t)blockIdx.x * kWave + (threadIdx.x & 63)) * 8;
     if (c >= width) return;
-    const int64_t end = now ? *now : rows;
+    const int64_t end = j.now ? *j.now : j.rows;
     for (int64_t r = (int64_t)blockIdx.y * kRowWaves + (threadIdx.x >> 6); r < end; r += (int64_t)gridDim.y * kRowWaves) {
-        const T* p = x + (list ? (int64_t)list[r] : r) * stride + c;
+        const T* p = (const T*)j.x + (j.list ? (int64_t)j.list[r] : r) * j.stride + c;
         float v[8];
-        if (c + 8 <= cols) {
+        if (c + 8 <= j.cols) {
             const auto in = load_vec<T, 8>(p);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = (float)in.e[e];
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? (float)p[e] : 0.f;
+            for (int e = 0; e < 8; ++e) v[e] = c + e < j.cols ? (float)p[e] : 0.f;
         }
-        store_packed<T, PLANES>(out, plane, r * width + c, v);
+        store_packed<T, PLANES>(j.out, plane, r * width + c, v);
     }
 }
 
@@ -166,21 +170,20 @@ void column_parts(const void* x, int64_t stride, int64_t rows, int64_t cols, flo
 
 }  // namespace
 
-hipError_t pack_rows(const void* x, int64_t stride, int64_t rows, int64_t cols, int32_t dtype, const int32_t* list,
-                     const int32_t* now, uint16_t* out, hipStream_t s) {
-    if (!rows) return hipSuccess;
-    const int64_t width = packed_width(cols), plane = rows * width;
-    const dim3 grid = row_grid(rows, width), block(64 * kRowWaves);
+hipError_t pack_rows(const PackRows& a, const PackRows& b, int32_t dtype, hipStream_t s) {
+    PackJobs jobs{{a.rows ? a : b, b}};
+    const int count = !!a.rows + !!b.rows;
+    if (!count) return hipSuccess;
+    dim3 grid = row_grid(jobs.m[0].rows, packed_width(jobs.m[0].cols));
+    if (count == 2) {
+        const dim3 other = row_grid(b.rows, packed_width(b.cols));
+        grid = dim3(grid.x > other.x ? grid.x : other.x, grid.y > other.y ? grid.y : other.y, 2);
+    }
+    const dim3 block(64 * kRowWaves);
     (void)hipGetLastError();
-    if (dtype == WARP_F32)
-        hipLaunchKernelGGL((k_pack_rows<float, 3>), grid, block, 0, s, (const float*)x, stride, rows, cols, list, now, out,
-                           width, plane);
-    else if (dtype == WARP_F16)
-        hipLaunchKernelGGL((k_pack_rows<_Float16, 1>), grid, block, 0, s, (const _Float16*)x, stride, rows, cols, list, now,
-                           out, width, plane);
-    else
-        hipLaunchKernelGGL((k_pack_rows<__bf16, 1>), grid, block, 0, s, (const __bf16*)x, stride, rows, cols, list, now, out,
-                           width, plane);
+    if (dtype == WARP_F32) hipLaunchKernelGGL((k_pack_rows<float, 3>), grid, block, 0, s, jobs);
+    else if (dtype == WARP_F16) hipLaunchKernelGGL((k_pack_rows<_Float16, 1>), grid, block, 0, s, jobs);
+    else hipLaunchKernelGGL((k_pack_rows<__bf16, 1>), grid, block, 0, s, jobs);
     return hipGetLastError();
 }
 
