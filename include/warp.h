@@ -399,7 +399,7 @@ int warp_linear_int8(const int8_t* a, int64_t a_stride, const float* a_scale, in
  *   ids          [tokens] whole numbers of id_bytes (4 or 8)
  *   table        [vocabulary][cols] of dtype
  *   out          [tokens][cols] of dtype
- * At most 2^25 tokens and table rows and 2^20 columns (above: WARP_ENOTSUP).
+ * At most 2^25 tokens and table rows, 2^20 columns and 2^37 elements of the table or of out (above: WARP_ENOTSUP).
  */
 int warp_embedding(const void* ids, int32_t id_bytes, int64_t tokens, const void* table, int64_t table_stride,
                    int64_t vocabulary, int32_t cols, int32_t dtype, float scale, void* out, int64_t out_stride,
@@ -457,7 +457,7 @@ int warp_cross_entropy_scratch(int64_t tokens, int32_t cols, int32_t dtype, cons
  *   scratch      warp_linear_scratch bytes, 16-byte aligned: copies of operands that are not 16-byte aligned rows of whole
  *                16-byte pieces, or float32, and parts of sums where there are few rows; often none
  * float32 products are made of 16-bit ones that keep all digits; what an infinity in x or weight enters may be NaN.
- * WARP_ENOTSUP above 2^24 rows, 2^20 columns or channels, 2^37 elements of x or y or 2^34 of the weight.
+ * WARP_ENOTSUP above 2^24 rows, 2^20 columns or channels, 2^36 elements of x or y or 2^34 of the weight.
  */
 int warp_linear(const void* x, int64_t x_stride, int64_t rows, int32_t cols, int32_t dtype, const void* weight,
                 int64_t weight_stride, int32_t n, const void* bias, int32_t bias_dtype, void* y, int64_t y_stride,

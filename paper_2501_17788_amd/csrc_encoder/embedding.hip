@@ -521,14 +521,18 @@ BackwardScratch backward_scratch(int64_t tokens, int64_t vocabulary, int64_t col
     return b;
 }
 
-int check_embedding(const char* what, const void* ids, int32_t id_bytes, int64_t tokens, int64_t vocabulary, int64_t cols,
-                    int32_t dtype, float scale) {
+int check_sizes(const char* what, int64_t tokens, int64_t vocabulary, int64_t cols) {
     if (tokens < 0) return fail(WARP_EINVAL, "%s: tokens must be >= 0 (got %lld)", what, (long long)tokens);
     if (vocabulary < 1) return fail(WARP_EINVAL, "%s: vocabulary must be >= 1 (got %lld)", what, (long long)vocabulary);
     if (cols < 1) return fail(WARP_EINVAL, "%s: cols must be >= 1 (got %lld)", what, (long long)cols);
-    if (tokens > 1 << 25 || vocabulary > 1 << 25 || cols > 1 << 20)
-        return fail(WARP_ENOTSUP, "%s: at most 2^25 tokens, 2^25 table rows and 2^20 columns (got %lld, %lld, %lld)", what,
-                    (long long)tokens, (long long)vocabulary, (long long)cols);
+    if (tokens > 1 << 25 || vocabulary > 1 << 25 || cols > 1 << 20 || tokens * cols > 1ll << 37 || vocabulary * cols > 1ll << 37)
+        return fail(WARP_ENOTSUP, "%s: at most 2^25 tokens, 2^25 table rows, 2^20 columns and 2^37 elements (got %lld, %lld, "
+                    "%lld)", what, (long long)tokens, (long long)vocabulary, (long long)cols);
+    return WARP_OK;
+}
+int check_embedding(const char* what, const void* ids, int32_t id_bytes, int64_t tokens, int64_t vocabulary, int64_t cols,
+                    int32_t dtype, float scale) {
+    if (const int rc = check_sizes(what, tokens, vocabulary, cols)) return rc;
     if (id_bytes != 4 && id_bytes != 8) return fail(WARP_EINVAL, "%s: ids of 4 or 8 bytes (got %d)", what, id_bytes);
     if (!dtype_ok(dtype)) return fail(WARP_EINVAL, "%s: unknown dtype %d", what, dtype);
     if (!(scale - scale == 0.f)) return fail(WARP_EINVAL, "%s: scale must be finite", what);
@@ -570,7 +574,9 @@ int warp_embedding(const void* ids, int32_t id_bytes, int64_t tokens, const void
 }
 
 int warp_embedding_backward_scratch(int64_t tokens, int64_t vocabulary, int32_t cols, int64_t* bytes) {
-    if (!bytes || tokens < 0 || vocabulary < 1 || cols < 1) return fail(WARP_EINVAL, "embedding backward: bad sizes");
+    const char* what = "embedding backward";
+    if (!bytes) return fail(WARP_EINVAL, "%s: null pointer", what);
+    if (const int rc = check_sizes(what, tokens, vocabulary, cols)) return rc;
     *bytes = backward_scratch(tokens, vocabulary, cols).bytes;
     return WARP_OK;
 }

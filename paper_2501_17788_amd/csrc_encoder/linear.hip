@@ -10,10 +10,10 @@ namespace {
 int check_sizes(const char* what, int64_t rows, int32_t cols, int32_t n, int32_t dtype) {
     if (rows < 0) return fail(WARP_EINVAL, "%s: rows must be >= 0 (got %lld)", what, (long long)rows);
     if (n < 1 || cols < 1) return fail(WARP_EINVAL, "%s: n and cols must be >= 1 (got %d, %d)", what, n, cols);
-    if (rows > 1 << 24 || n > 1 << 20 || cols > 1 << 20 || (int64_t)n * cols > 1ll << 34 || rows * n > 1ll << 37 ||
-        rows * cols > 1ll << 37)
-        return fail(WARP_ENOTSUP, "%s: at most 2^24 rows, 2^20 columns and channels, and matrices of 2^37 elements (got "
-                    "%lld, %d, %d)", what, (long long)rows, cols, n);
+    if (rows > 1 << 24 || n > 1 << 20 || cols > 1 << 20 || (int64_t)n * cols > 1ll << 34 || rows * n > 1ll << 36 ||
+        rows * cols > 1ll << 36)
+        return fail(WARP_ENOTSUP, "%s: at most 2^24 rows, 2^20 columns and channels, and matrices of 2^36 elements (weights: "
+                    "2^34; got %lld, %d, %d)", what, (long long)rows, cols, n);
     if (!dtype_ok(dtype)) return fail(WARP_EINVAL, "%s: unknown dtype %d", what, dtype);
     return WARP_OK;
 }
@@ -131,6 +131,16 @@ struct Backward {
     } while (0)
 
 }  // namespace
+
+int product_choice(int64_t m, int64_t n, int64_t k, int dtype, bool bytes) {
+    Product p(m, n, k, dtype);
+    if (bytes) {
+        const Product direct(m, n, k, dtype, kT128);
+        if (!takes_bytes(k, m, n, dtype, direct.time, p.time)) return -1;
+        p = direct;
+    }
+    return p.tile + 4 * p.split;
+}
 
 }  // namespace warp
 

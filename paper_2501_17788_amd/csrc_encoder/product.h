@@ -117,6 +117,7 @@ inline ProductPlan plan_product(int64_t m, int64_t n, int64_t steps, bool may_sp
     for (const Tile t : {kT64, kT128, kT256}) {
         if (t > largest) break;
         const int64_t tiles = cover_of(m, tile_size(t)) * cover_of(n, tile_size(t));
+        if (t != largest && tiles >= 1 << 22) continue;  // a grid has at most 2^32 threads
         const int64_t traffic = product_traffic(t, m, n, steps);
         auto both = [&](int64_t time) { return time > traffic ? time + traffic / 4 : traffic + time / 4; };
         const int64_t whole = both(product_time(t, tiles, steps));
@@ -128,6 +129,10 @@ inline ProductPlan plan_product(int64_t m, int64_t n, int64_t steps, bool may_sp
     }
     return best;
 }
+
+// What a linear layer's products choose, for the tests, which have to reach each kernel: the tile, plus 4 where the k range
+// is split; with `bytes` that of 8-bit rows as they are, -1 where they are unpacked.
+int product_choice(int64_t m, int64_t n, int64_t k, int dtype, bool bytes);
 
 // x = high + middle + low, each a bfloat16 cut off towards zero: 8 + 8 + 8 bits. An infinity or a NaN stays in the
 // first.

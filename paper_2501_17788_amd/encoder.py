@@ -198,8 +198,9 @@ class _Linear(torch.autograd.Function):
         values = scale = None
         if ctx.needs_input_grad[1]:
             values, scale, cols = _native.quantize_rows(x) if rows is None else rows
-            if cols != x.shape[-1] or values.shape[0] != x[..., 0].numel():
-                raise ValueError(f"rows in 8 bits of {values.shape[0]} x {cols} for x {tuple(x.shape)}")
+            count = x.numel() // x.shape[-1]
+            if cols != x.shape[-1] or values.shape[0] != count or values.dtype != torch.int8 or scale.shape != (count,):
+                raise ValueError(f"rows in 8 bits of {tuple(values.shape)}, {cols} columns, for x {tuple(x.shape)}")
         ctx.save_for_backward(values, scale, weight)
         ctx.bias_type = torch.float32 if bias is None else bias.dtype
         return y

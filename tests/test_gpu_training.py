@@ -15,6 +15,8 @@ import math
 import numpy as np
 import pytest
 
+import product_plans
+
 torch = pytest.importorskip("torch")
 w = pytest.importorskip("paper_2501_17788_amd")
 
@@ -224,13 +226,8 @@ def test_linear(rows, cols, n, dtype):
     close(db, dy64.sum(0), rows * U * sizes + rounding(dy64.sum(0), dtype), "dbias")
 
 
-# tiles of 64, 128 and 256, sums in one part and in several, ragged in every size
-LARGER = [(2000, 1003, 771), (2500, 520, 4100), (4097, 4099, 136), (300, 5000, 640), (20_001, 256, 128), (1, 9000, 4096),
-          (3, 70, 9000), (9000, 70, 3), (513, 2049, 2100), (50_001, 8, 8), (8, 50_001, 16), (5000, 3001, 1500)]
-
-
 @ALL
-@pytest.mark.parametrize("rows,cols,n", LARGER)
+@pytest.mark.parametrize("rows,cols,n", product_plans.SIZES)
 def test_linear_of_whole_numbers(rows, cols, n, dtype):
     """Every sum is exact, and so is its rounding."""
     g = gen(rows + cols + n)

@@ -35,6 +35,7 @@ def embed_back(**over):
     (dict(tokens=-1), w.EINVAL, "tokens"), (dict(vocabulary=0), w.EINVAL, "vocabulary"), (dict(cols=0), w.EINVAL, "cols"),
     (dict(tokens=(1 << 25) + 1), w.ENOTSUP, "2^25"), (dict(vocabulary=(1 << 25) + 1), w.ENOTSUP, "2^25"),
     (dict(cols=(1 << 20) + 1), w.ENOTSUP, "2^20"), (dict(id_bytes=2), w.EINVAL, "ids of 4 or 8"),
+    (dict(tokens=1 << 25, cols=1 << 13), w.ENOTSUP, "2^37"), (dict(vocabulary=1 << 25, cols=1 << 13), w.ENOTSUP, "2^37"),
     (dict(dtype=3), w.EINVAL, "dtype"), (dict(scale=float("nan")), w.EINVAL, "scale"),
     (dict(scale=float("inf")), w.EINVAL, "scale"), (dict(ids=None), w.EINVAL, "null"), (dict(ids=P + 4), w.EINVAL, "misaligned"),
 ])
@@ -114,7 +115,7 @@ def linear_back(**over):
 @pytest.mark.parametrize("over,code,needle", [
     (dict(rows=-1), w.EINVAL, "rows"), (dict(n=0), w.EINVAL, "n and cols"), (dict(cols=0), w.EINVAL, "n and cols"),
     (dict(rows=(1 << 24) + 1), w.ENOTSUP, "2^24"), (dict(n=(1 << 20) + 1), w.ENOTSUP, "2^20"),
-    (dict(rows=1 << 24, n=1 << 14), w.ENOTSUP, "2^37"), (dict(cols=1 << 18, n=1 << 17), w.ENOTSUP, "2^37"),
+    (dict(rows=1 << 24, n=1 << 14), w.ENOTSUP, "2^36"), (dict(cols=1 << 18, n=1 << 17), w.ENOTSUP, "2^34"),
     (dict(dtype=9), w.EINVAL, "dtype"), (dict(weight=None), w.EINVAL, "null"), (dict(weight=P + 2), w.EINVAL, "misaligned"),
     (dict(weight_stride=63), w.EINVAL, "stride"), (dict(scratch=None), w.EINVAL, "scratch"),
     (dict(bytes=8), w.EINVAL, "scratch"), (dict(scratch=P + 1), w.EINVAL, "scratch"),
@@ -152,6 +153,7 @@ def test_scratch_sizes():
     assert lib.warp_linear_scratch(P, 1024, 4096, 1024, 0, P, 1024, 1024, None) == w.EINVAL
     assert lib.warp_linear_backward_scratch(P, 64, -1, 64, 0, 64, P, 64, ctypes.byref(n)) == w.EINVAL
     assert lib.warp_embedding_backward_scratch(1, 0, 1, ctypes.byref(n)) == w.EINVAL
+    assert lib.warp_embedding_backward_scratch(1, 1 << 60, 1, ctypes.byref(n)) == w.ENOTSUP
     assert lib.warp_cross_entropy_scratch(1, 1, 0, P, 1, 0, ctypes.byref(n), None) == w.EINVAL
     # G is never larger than a piece, whatever the vocabulary
     sizes = []
@@ -178,3 +180,25 @@ def test_host_tensors_are_refused():
             call()
     with pytest.raises(ValueError, match="columns"):
         w.linear_backward(torch.zeros(3, 3), rows._replace(cols=9), x)
+
+
+def test_product_sizes_reach_their_kernels():
+    """The sizes of the GPU tests choose the products that they are listed under: a change of the choice that leaves one
+    without a test fails here."""
+    import product_plans
+
+    choose = lib["_ZN4warp14product_choiceElllib"]  # int warp::product_choice(int64_t m, int64_t n, int64_t k, int dtype, bool bytes)
+    choose.argtypes, choose.restype = [ctypes.c_int64] * 3 + [ctypes.c_int, ctypes.c_bool], ctypes.c_int
+    seen = set()
+    for rows, cols, n in product_plans.SIZES:
+        for dtype in (0, 1, 2):
+            if dtype == 0 or rows > 32:
+                seen.add(("y", choose(rows, n, cols, dtype, False)))
+            else:
+                seen.add(("y", "few"))
+            seen.add(("dx", choose(rows, cols, n, dtype, False)))
+            packed, direct = choose(n, cols, rows, dtype, False), choose(n, cols, rows, dtype, True)
+            seen.add(("dweight", direct + 10 if direct >= 0 else packed))
+    want = {(name, tile + 4 * split) for name in ("y", "dx", "dweight") for tile in range(3) for split in (0, 1)}
+    want |= {("y", "few")} | {("dweight", 10 + tile + 4 * split) for tile in range(2) for split in (0, 1)}
+    assert want <= seen, sorted(want - seen, key=str)
