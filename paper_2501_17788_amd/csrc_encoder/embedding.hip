@@ -91,7 +91,9 @@ __global__ __launch_bounds__(256) void k_lookup(LookupArgs g) {
 // parts of it.
 constexpr int kDigits = 512, kSortThreads = 512, kSortWaves = kSortThreads / kWave;
 constexpr int kMaxTiles = 128, kTileUnit = 1024;
-constexpr int kSmall = 4096;  // so many tokens are sorted by one workgroup, in LDS
+// So many tokens are sorted by one workgroup, in LDS: the whole gradient of 4096 into 9973 rows of 64 columns takes 28 us
+// this way and 29 by tiles, of 8192 39 and 31, of 500 rows 2000 tokens 16 and 18.
+constexpr int kSmall = 4096;
 
 struct SortPlan {
     int64_t tokens;

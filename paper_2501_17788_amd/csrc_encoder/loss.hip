@@ -37,6 +37,66 @@ struct SelectArgs {
     float* largest;
 };
 
+// Up to 2^17 tokens: a workgroup for each 1024, which counts the rows before its own by itself (16,384 tokens 8 us; by one
+// workgroup 13). The last one has seen all of them.
+constexpr int64_t kSelectWide = 1 << 17;
+__global__ __launch_bounds__(1024) void k_select_wide(SelectArgs g) {
+    constexpr int U = 8;
+    __shared__ int32_t waves[2][16];
+    __shared__ uint32_t tops[16];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int64_t base = (int64_t)blockIdx.x * 1024;
+    const bool last = blockIdx.x == gridDim.x - 1;
+    auto target = [&](int64_t t) { return g.wide ? ((const int64_t*)g.targets)[t] : (int64_t)((const int32_t*)g.targets)[t]; };
+    int32_t mine = 0;  // of this thread's tokens before the workgroup's
+    uint32_t top = 0;
+    for (int64_t t0 = tid; t0 < base; t0 += 1024 * U) {
+        int64_t y[U];
+        uint32_t d[U] = {};
+#pragma unroll
+        for (int u = 0; u < U; ++u) y[u] = t0 + 1024 * u < base ? target(t0 + 1024 * u) : -1;
+        if (last && g.dloss) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) d[u] = t0 + 1024 * u < base ? as_u(g.dloss[t0 + 1024 * u]) & 0x7fffffffu : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool in = y[u] >= 0 && y[u] < g.vocabulary;
+            mine += in;
+            if (in && d[u] < 0x7f800000u) top = max(top, d[u]);
+        }
+    }
+    const int64_t t = base + tid;
+    const int64_t y = t < g.tokens ? target(t) : -1;
+    const bool in = y >= 0 && y < g.vocabulary;
+    if (last && in && g.dloss) {
+        const uint32_t d = as_u(g.dloss[t]) & 0x7fffffffu;
+        if (d < 0x7f800000u) top = max(top, d);
+    }
+    const unsigned long long all = __ballot(in);
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) mine += __shfl_xor(mine, s);
+    top = wave_max(top);
+    if (lane == 0) waves[0][w] = mine, waves[1][w] = (int32_t)__popcll(all), tops[w] = top;
+    __syncthreads();
+    int32_t first = 0, count = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        first += waves[0][i] + (i < w ? waves[1][i] : 0);
+        count += waves[0][i] + waves[1][i];
+    }
+    const int32_t row = first + (int32_t)__popcll(all & ((1ull << lane) - 1));
+    if (t < g.tokens) g.place[t] = in ? row : y < 0 ? -1 : -2;
+    if (in) g.list[row] = (int32_t)t, g.target[row] = (int32_t)y;
+    if (!last || tid) return;
+    *g.now = count;
+    if (!g.dloss) return;
+    for (int i = 0; i < 16; ++i) top = max(top, tops[i]);
+    const float largest = top ? as_f(top) : 1.f;
+    *g.largest = largest;
+    *g.factor = largest * g.scale / g.grad_scale;
+}
+
 // One workgroup: turns of eight times 1024 neighbouring tokens, whose loads and stores are in one piece a wave.
 __global__ __launch_bounds__(1024) void k_select(SelectArgs g) {
     constexpr int N = 8;
@@ -105,6 +165,13 @@ __global__ __launch_bounds__(1024) void k_select(SelectArgs g) {
     const float largest = top ? as_f(top) : 1.f;
     *g.largest = largest;
     *g.factor = largest * g.scale / g.grad_scale;
+}
+
+void select(const SelectArgs& g, hipStream_t s) {
+    if (g.tokens && g.tokens <= kSelectWide)
+        hipLaunchKernelGGL(k_select_wide, dim3((uint32_t)cover_of(g.tokens, 1024)), dim3(1024), 0, s, g);
+    else
+        hipLaunchKernelGGL(k_select, dim3(1), dim3(1024), 0, s, g);
 }
 
 // Up to 64 tokens, in one launch: a workgroup for each, whose waves all look at all targets; it packs its own row, and the
@@ -431,7 +498,7 @@ int warp_cross_entropy(const void* hidden, int64_t hidden_stride, int64_t tokens
         WARP_LAUNCH(take_few({sel, hidden, hidden_stride, cols, z.width, tokens * z.width, f.hidden, nullptr, nullptr, nullptr,
                               nullptr, nullptr}, dtype, s));
     } else {
-        WARP_LAUNCH(hipLaunchKernelGGL(k_select, dim3(1), dim3(1024), 0, s, sel));
+        WARP_LAUNCH(select(sel, s));
         WARP_STEP(pack_rows({hidden, hidden_stride, tokens, cols, f.list, f.now, f.hidden}, {}, dtype, s));
     }
     for (int64_t v0 = 0; v0 < vocabulary; v0 += f.piece) {
@@ -488,7 +555,7 @@ int warp_cross_entropy_backward(const float* dloss, const void* hidden, int64_t 
         WARP_LAUNCH(take_few({sel, hidden, hidden_stride, cols, z.width, tokens * z.width, w.hidden, loss, lse, w.lse2, w.weight,
                               w.at_target}, dtype, s));
     } else {
-        WARP_LAUNCH(hipLaunchKernelGGL(k_select, dim3(1), dim3(1024), 0, s, sel));
+        WARP_LAUNCH(select(sel, s));
     }
     if (tokens > kFewTokens) {
         WARP_STEP(pack_rows({hidden, hidden_stride, tokens, cols, w.list, w.now, w.hidden}, {}, dtype, s));

@@ -49,9 +49,14 @@ def rounding(v, dtype):
 
 
 def close(got, want, tol, what):
+    """Within tol; NaN for NaN; and an infinity of the right sign where a value within tol rounds to it: from 65,520 on in
+    float16, whose largest number is 65,504 in steps of 32."""
+    half = got.dtype == torch.float16
     got, want = got.detach().double(), want.double()
     assert got.shape == want.shape, (what, got.shape, want.shape)
     bad = ~((got - want).abs() <= tol) & ~(got.isnan() & want.isnan())
+    if half:
+        bad &= ~(got.isinf() & (got.sign() == want.sign()) & (want.abs() + tol >= 65_520))
     if bad.any():
         i = torch.nonzero(bad.reshape(-1))[0].item()
         raise AssertionError(f"{what}: {int(bad.sum())} of {bad.numel()} values are off, the first at {i}: "
@@ -404,7 +409,7 @@ def test_cross_entropy(tokens, vocabulary, cols, dtype):
 @ALL
 def test_cross_entropy_of_larger_sizes(dtype):
     """Tiles of 128 and 256, many parts of a sum."""
-    for tokens, vocabulary, cols in ((2100, 3001, 136), (400, 30_011, 72), (5000, 130, 64), (9, 100_003, 24)):
+    for tokens, vocabulary, cols in ((2100, 3001, 136), (400, 30_011, 72), (5000, 130, 64), (9, 100_003, 24), (140_001, 50, 8)):
         g = gen(tokens)
         hidden, table, targets = scores(g, tokens, vocabulary, cols, dtype)
         targets[::3] = -1
