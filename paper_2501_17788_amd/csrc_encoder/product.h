@@ -207,9 +207,8 @@ struct Stage {
     static constexpr int kLoads = T / 8 / WAVES;  // of 1 KB
     static_assert(kLoads * 8 * WAVES == T, "whole loads");
     uint32_t off[kLoads];
-    const uint8_t* at;    // the next step's first byte
+    const uint8_t* at;  // the next step's first byte, of plane 0
     int64_t step_bytes;
-    const uint8_t* base;  // of plane 0
     int lane, wave;
 
     __device__ __forceinline__ int key(int row) const { return CHANNELS ? channel_piece<B>(row) : token_piece(row); }
@@ -222,7 +221,7 @@ struct Stage {
     __device__ __forceinline__ void start(const void* p, int64_t stride, int64_t first, int64_t rows, int lane_, int wave_) {
         lane = lane_, wave = wave_;
         if (L == kAlongK) {
-            base = (const uint8_t*)p + first * stride * 2;
+            at = (const uint8_t*)p + first * stride * 2;
             step_bytes = 2 * kProductStep;
             const int last = (int)(rows - first < T ? rows - first : T) - 1;
 #pragma unroll
@@ -231,7 +230,7 @@ struct Stage {
                 off[i] = (uint32_t)(row < last ? row : last) * (uint32_t)(stride * 2) + 2 * k_of(i);
             }
         } else {
-            base = (const uint8_t*)p + first * 2;
+            at = (const uint8_t*)p + first * 2;
             step_bytes = stride * 2 * kProductStep;
             const int64_t end = (rows - 1) / 8 * 8 - first;  // the last piece
 #pragma unroll
@@ -243,17 +242,18 @@ struct Stage {
             }
         }
     }
-    __device__ __forceinline__ void seek(int64_t plane, int64_t step) { at = base + plane * 2 + step * step_bytes; }
-    __device__ __forceinline__ void load(uint8_t* lds) const {
+    __device__ __forceinline__ void load(uint8_t* lds, int64_t plane) const {
+        const uint8_t* from = at + 2 * plane;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            __builtin_amdgcn_global_load_lds((product_global*)(at + off[i]),
+            __builtin_amdgcn_global_load_lds((product_global*)(from + off[i]),
                                              (product_lds*)(lds + (wave * kLoads + i) * 1024), 16, 0, 0);
     }
-    __device__ __forceinline__ void load_last(uint8_t* lds, int left) const {  // zeros beyond `left` k
+    __device__ __forceinline__ void load_last(uint8_t* lds, int64_t plane, int left) const {  // zeros beyond `left` k
+        const uint8_t* from = at + 2 * plane;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const uint8_t* p = k_of(i) < left ? at + off[i] : (const uint8_t*)g_zeros;
+            const uint8_t* p = k_of(i) < left ? from + off[i] : (const uint8_t*)g_zeros;
             __builtin_amdgcn_global_load_lds((product_global*)p, (product_lds*)(lds + (wave * kLoads + i) * 1024), 16,
                                              0, 0);
         }
@@ -396,7 +396,7 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
 
     const int64_t rows = g.m_now ? *g.m_now : g.m;
     const int64_t k = g.k_now ? *g.k_now : g.k;
-    const int64_t k_steps = cover_of(k, kProductStep), steps = k_steps * g.terms;
+    const int64_t steps = product_steps(k, g.terms);
     const int tiles_m = (int)cover_of(rows, TM), tiles_n = (int)cover_of(g.n, TN);
     const int splits = F == kSum ? product_splits(rows, g.n, steps, TM, g.splits, g.jobs) : 1;
     const int tiles = tiles_m * tiles_n, total = tiles * splits;
@@ -417,36 +417,34 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
     Stage<LA, TM, kWaves, false, kBM> sa;
     Stage<LB, TN, kWaves, kWide, kBN> sb;
     sa.start(g.a, g.a_stride, m0, rows, lane, wave);
+    // a step's 64 k go through all terms before the next ones: their planes are in the caches then
+    int64_t kk = g.terms == 1 ? first : first / g.terms;
+    int term = g.terms == 1 ? 0 : (int)(first % g.terms);
     ByteStage<E, TN> bytes;
-    if constexpr (KIND == kBytes) bytes.start(g.b, g.b_stride, g.b_scale, c0, first);
-    else sb.start(g.b, g.b_stride, c0, g.n, lane, wave);
-    int term = 0;
-    int64_t kk = 0;  // step within the term
-    auto seek = [&] {
-        // planes of the terms: (0,0) (0,1) (1,0) (1,1) (0,2) (2,0)
-        sa.seek((int64_t)(0x201100 >> 4 * term & 3) * g.a_plane, kk);
-        if constexpr (KIND != kBytes) sb.seek((int64_t)(0x021010 >> 4 * term & 3) * g.b_plane, kk);
-    };
-    if (k_steps) term = (int)(first / k_steps), kk = first % k_steps;
-    seek();
+    if constexpr (KIND == kBytes) {
+        bytes.start(g.b, g.b_stride, g.b_scale, c0, first);
+    } else {
+        sb.start(g.b, g.b_stride, c0, g.n, lane, wave);
+        sb.at += kk * sb.step_bytes;
+    }
+    sa.at += kk * sa.step_bytes;
     auto load = [&](uint8_t* la, uint8_t* lb) {
+        // planes of the terms: (0,0) (0,1) (1,0) (1,1) (0,2) (2,0)
+        const int64_t plane_a = (int64_t)(0x201100 >> 4 * term & 3) * g.a_plane, plane_b = (int64_t)(0x021010 >> 4 * term & 3) * g.b_plane;
         const int64_t left = k - kk * kProductStep;
         if constexpr (KIND == kBytes) bytes.load(left);
         if (left >= kProductStep) {
-            sa.load(la);
-            if constexpr (KIND != kBytes) sb.load(lb);
+            sa.load(la, plane_a);
+            if constexpr (KIND != kBytes) sb.load(lb, plane_b);
         } else {
-            sa.load_last(la, (int)left);
-            if constexpr (KIND != kBytes) sb.load_last(lb, (int)left);
+            sa.load_last(la, plane_a, (int)left);
+            if constexpr (KIND != kBytes) sb.load_last(lb, plane_b, (int)left);
         }
-        if (++kk == k_steps) {
-            kk = 0;
-            ++term;
-            seek();  // (after the last term: not used)
-        } else {
-            sa.at += sa.step_bytes;
-            if constexpr (KIND != kBytes) sb.at += sb.step_bytes;
-        }
+        if (++term < g.terms) return;
+        term = 0;
+        ++kk;
+        sa.at += sa.step_bytes;
+        if constexpr (KIND != kBytes) sb.at += sb.step_bytes;
     };
 
     Blocks<E, LA, TM, false, kBM> ra;
