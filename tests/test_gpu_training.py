@@ -432,6 +432,10 @@ def test_cross_entropy_in_pieces():
     r = Loss64(hidden[rows], table, targets[rows], float(np.float32(0.3)))
     close(loss[rows], r.want_loss, r.e_loss, "pieces of statistics")
     assert not loss[targets < 0].any() and not lse[targets < 0].any()
+    # a table that is packed piece by piece, whose rows are no whole pieces of 16 bytes
+    hidden, table, targets = scores(g, 70, 300_001, 1025, torch.bfloat16)
+    targets[:5] = torch.tensor([0, 300_000, 150_015, 150_016, -1], device="cuda")
+    check_loss(hidden, table, targets, 0.02, torch.ones(70, device="cuda"), "pieces of a packed table")
 
 
 @ALL
