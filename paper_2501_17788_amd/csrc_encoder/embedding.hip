@@ -5,6 +5,9 @@
 // to. A row whose tokens lie in one chunk is written from there; one that goes on in another leaves a part in each, and
 // those are added last, together with the zeros of the rows without tokens: the gradient is written once, and a
 // common token's thousands are as many waves' work.
+// A training step's 131,072 tokens (30% padding), 32,128 rows of 1024 bf16: lookup 67 us, 5.0 TB/s of the output and the table;
+// gradient 120 us: sorting 32, chunks 73, the rest 15. Sorting by rows' own counts instead needs the counts' prefix sums and
+// atomics that fix no order.
 #include <type_traits>
 
 #include "encoder.h"
@@ -47,7 +50,8 @@ struct LookupArgs {
     bool past_caches;
 };
 
-// One wave for R tokens and a block of 64 V NV columns, all its rows under way at once.
+// One wave for R tokens and a block of 64 V NV columns, all its rows under way at once: a row's address has to wait for its
+// id. 32 rows of 768 take 2.6 us, an empty launch's time.
 template <typename T, int V, int NV, int R>
 __global__ __launch_bounds__(256) void k_lookup(LookupArgs g) {
     const int lane = threadIdx.x & 63;
@@ -88,7 +92,7 @@ __global__ __launch_bounds__(256) void k_lookup(LookupArgs g) {
 // ---------------------------------------------------------------------------- sorting tokens by id
 
 // Stable radix sort by digits of at most 9 bits. At most 128 tiles of equal size; a tile's eight waves hold neighbouring
-// parts of it.
+// parts of it. Bound by latency: a pass over 131,072 tokens takes 5 us for the counts and 11 for the places.
 constexpr int kDigits = 512, kSortThreads = 512, kSortWaves = kSortThreads / kWave;
 constexpr int kMaxTiles = 128, kTileUnit = 1024;
 // So many tokens are sorted by one workgroup, in LDS: the whole gradient of 4096 into 9973 rows of 64 columns takes 28 us
@@ -342,7 +346,8 @@ __device__ __forceinline__ void store_sums(const float (&sum)[V], const SumArgs&
 }
 
 // One wave a chunk and column block (those of a chunk are neighbours), half of its rows under way while the other half is
-// added; and the chunk's part of the rows' spans.
+// added; and the chunk's part of the rows' spans. Bound by memory where rows come in the tokens' order, which sorting
+// scatters: 91,750 rows of 2 KB take 73 us (2.6 TB/s), as long as an indexed copy of them in this order.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void k_sum_chunks(SumArgs g) {
     const int lane = threadIdx.x & 63;
@@ -421,7 +426,7 @@ __device__ __forceinline__ void add_parts(float (&sum)[V], const SumArgs& g, int
 
 // The first `common` workgroups: one for each chunk; the second one of a row that has many stands for it, and the
 // workgroup's waves share its parts. The others: kRows neighbouring rows a wave, those without tokens and those of few
-// parts.
+// parts. 250,001 rows of 768 fp16, of which 8192 tokens reach few: 72 us, 5.3 TB/s of zeros.
 constexpr int kRows = 4;
 template <typename T, int V>
 __global__ __launch_bounds__(256) void k_finish_rows(SumArgs g) {

@@ -1,5 +1,5 @@
-// Shared by the kernels of the token encoder's head (norm.hip, linear_int8.hip, adamw.hip): element
-// types, vectors of any element alignment, wave reductions, and the checks of their C entry points.
+// Shared by the token encoder's kernels: element types, vectors of any element alignment, wave
+// reductions, and the checks of their C entry points.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -202,6 +202,13 @@ template <typename... T>
 bool followed(const T&... tensors) {
     return at::GradMode::is_enabled() && (tracked(tensors) || ...);
 }
+
+// Whether a leaf's gradients are added on the default stream, where a graph that was made there lives.
+bool adds_on_default_stream(const Tensor& leaf) {
+    const auto node = torch::autograd::impl::try_get_grad_accumulator(leaf);
+    const auto stream = node ? node->stream() : std::nullopt;
+    return stream && stream->id() == c10::hip::getDefaultHIPStream(leaf.get_device()).id();
+}
 py::object node(const char* name) {  // of autograd; it calls back with gradients off
     return py::module_::import("paper_2501_17788_amd.encoder").attr(name).attr("apply");
 }
@@ -484,6 +491,7 @@ PYBIND11_MODULE(_encoder, mod) {
     mod.def("quantize_rows", &quantize_rows);
     mod.def("layer_norm_int8", &layer_norm_int8);
     mod.def("linear_int8", &linear_int8);
+    mod.def("adds_on_default_stream", &adds_on_default_stream);
     mod.def("embedding", &embedding);
     mod.def("embedding_backward", &embedding_backward);
     mod.def("cross_entropy", &cross_entropy);

@@ -376,11 +376,24 @@ __device__ __forceinline__ void neighbours(float4v (&x)[B]) {
 }
 
 // Tiles that neighbouring workgroups of an XCD work on span bands of four tiles of rows, so that its L2 serves what
-// they have in common.
+// they have in common (bands of two and eight are as fast).
 constexpr int kProductBand = 4;
 
 enum Kind { kPlain, kPlanes, kBytes };  // G in planes of a float32; B of 8 bits
 
+// One tile by four waves (64 x 64) or eight: a step's rows of A and B are loaded into one pair of buffers in LDS, past the
+// registers, while the matrix cores work on the other. 256 x 256 has the fewest bytes from LDS and from memory for an
+// operation, and one workgroup on a compute unit; the smaller tiles are for sizes that would leave compute units idle or
+// round up too far (plan_product).
+// Large products are bound by the matrix cores, busy 54 to 60% of the time at 1.9 to 2.0 GHz, and by what keeps them from
+// work: a copy whose rows all came from the caches ran 3 to 5% faster, one without results 4% (k = 8192) to 16% (1024). No
+// read of LDS has a bank conflict. bf16, us (and those of a library's product):
+//                               both along K    B across K     both across K
+//   8192 x 8192 by 8192           851  (767)     915  (873)      945  (991)
+//   16,384 x 32,128 by 1024      1028  (942)    1056 (1085)     1090 (1185)
+// Not faster: workgroups that stay for several tiles, the next one's first rows on their way (8192^3: 863); four waves of
+// 128 x 128 each (1640 to 1790: accumulators are moved between registers); loads behind the reads, wave priorities and
+// groups of instructions fixed by hints (spilled registers, 1.5 times slower and more).
 template <typename E, Layout LA, Layout LB, int TM, int TN, int WM, int WN, Finish F, Kind KIND>
 __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(ProductArgs g) {
     constexpr int kWaves = WM * WN;
@@ -569,6 +582,7 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
             }
         }
     } else if constexpr (F == kStats) {
+        // 16,384 tokens by 32,128 rows of 1024: 1011 us, a little less than with the logits written (1028)
         __syncthreads();  // the staged operands have been read by all
         float2* shared = (float2*)a0;  // [WN][TM]
         const bool whole = c0 + TN <= g.n;  // of all lanes

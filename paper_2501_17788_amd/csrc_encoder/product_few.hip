@@ -6,7 +6,8 @@ namespace warp {
 namespace {
 
 // A workgroup makes 16 columns of all rows (16 BM at most): its eight waves share the k range, 32 at a time and four such
-// steps under way, straight from memory, and their sums meet in LDS in a fixed order.
+// steps under way, straight from memory, and their sums meet in LDS in a fixed order. 1 x 1024 by 1024 takes 3.7 us, little
+// more than an empty launch; tiles of 64 x 64 with the k range in parts took 8.3 with the launch that joined them.
 constexpr int kFewWaves = 8;
 template <typename E, int BM>
 __global__ __launch_bounds__(64 * kFewWaves) void k_product_few(ProductArgs g) {

@@ -59,6 +59,14 @@ def _on(stream, tensors, call, *args):
         return call(*args)
 
 
+def _refuse_capture(ctx):
+    """Refuses a backward pass under capture whose leaves' gradients would be added on the default stream, since a graph
+    made there lives: a stream under capture cannot be joined with it, and trying ends the process."""
+    if torch.cuda.is_current_stream_capturing() and any(
+            hasattr(f, "variable") and _native.adds_on_default_stream(f.variable) for f, _ in ctx.next_functions):
+        raise RuntimeError("a backward pass cannot be captured while a graph of the same leaves from outside the capture lives")
+
+
 class _LayerNorm(torch.autograd.Function):
     """What `layer_norm` is to autograd. The statistics have no gradient, and y no second derivative."""
 
@@ -73,6 +81,7 @@ class _LayerNorm(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy, *_):
+        _refuse_capture(ctx)
         x, weight, mean, rstd = ctx.saved_tensors
         dx, dw, db = _native.layer_norm_backward(dy, x, weight, mean, rstd)
         return dx, None if weight is None else dw, None if ctx.bias_type is None else db.to(ctx.bias_type), None
@@ -131,6 +140,7 @@ class _Embedding(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
+        _refuse_capture(ctx)
         return None, _native.embedding_backward(dy, *ctx.saved_tensors, ctx.vocabulary, ctx.scale), None
 
 
@@ -165,6 +175,7 @@ class _CrossEntropy(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dloss, _):
+        _refuse_capture(ctx)
         want = ctx.needs_input_grad
         return *_native.cross_entropy_backward(dloss, *ctx.saved_tensors, ctx.scale, want[0], want[1]), None, None
 
@@ -208,6 +219,7 @@ class _Linear(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
+        _refuse_capture(ctx)
         return *_native.linear_backward(dy, *ctx.saved_tensors, *ctx.needs_input_grad[:3], ctx.bias_type), None
 
 

@@ -10,6 +10,7 @@ size.
 """
 from __future__ import annotations
 
+import gc
 import math
 
 import numpy as np
@@ -730,6 +731,45 @@ def test_captured_in_two_graphs(dtype):
         for (work, _), out in zip(made, outs):
             for i, (a, b) in enumerate(zip(out, work())):
                 assert torch.equal(a, b), (k, i)
+
+
+@pytest.mark.parametrize("name", ["embedding", "linear", "cross_entropy", "layer_norm"])
+def test_captured_backward_of_leaves_in_use(name):
+    """A backward pass under capture is refused while an eager graph of its leaves lives; afterwards it is captured, and
+    replays give what eager passes give."""
+    g = gen(60)
+    leaf = randn(g, 97, 64).requires_grad_() if name != "layer_norm" else (1 + 0.1 * randn(g, 64)).requires_grad_()
+    x, ids = randn(g, 70, 64), torch.randint(-1, 97, (70,), generator=g, device="cuda")
+    out = {"embedding": lambda: w.embedding(ids, leaf), "linear": lambda: w.linear(x, leaf),
+           "cross_entropy": lambda: w.cross_entropy(x, leaf, ids)[0], "layer_norm": lambda: w.layer_norm(x, leaf)[0]}[name]
+    dy = torch.randn(out().shape, generator=g, device="cuda")
+    lives = out()
+    torch.cuda.synchronize()
+    say("refused capture of", name)
+    with pytest.raises(RuntimeError, match="cannot be captured"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            out().backward(dy)
+    assert leaf.grad is None
+    lives.backward(dy)  # the eager graph is whole
+    assert leaf.grad is not None
+    leaf.grad = None
+    del lives
+    gc.collect()  # the refused graph, which the error's traceback held
+    torch.cuda.synchronize()
+    say("capture of", name)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out().backward(dy)
+    got = leaf.grad
+    for k in range(3):
+        x.copy_(randn(g, 70, 64))
+        dy.copy_(torch.randn(dy.shape, generator=g, device="cuda"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        with torch.no_grad():
+            kept = got.clone()
+        assert torch.equal(kept, torch.autograd.grad(out(), leaf, dy)[0]), k
 
 
 def test_products_side_by_side():
