@@ -43,19 +43,30 @@ struct Product {
         tile = p.tile, split = p.split, time = p.time;
         floats = split ? part_floats(m, n, k, terms_of(dtype), tile, kMaxSplits, tile_jobs(tile)) : 0;
     }
+    Product(int64_t m, int64_t n, int64_t k) : tile(tile_f32(m, n)), time(0) {  // float32 without planes: steps of 32
+        split = tile == kT64 && product_splits(m, n, cover_of(k, 32), 64, kMaxSplits, tile_jobs(tile)) > 1;
+        floats = split ? part_floats(m, n, 2 * k, 1, tile, kMaxSplits, tile_jobs(tile)) : 0;
+    }
 };
+
+// float32 rows that are multiplied as they are, without planes: the matrix instructions for them have a 16th of the rate, but nothing has
+// to be packed. us, as they are | in planes: 64 x 4096 by
+// 4096 29 | 63, 256 85 | 105, 384 118 | 136, 1024 by 1024 10 | 22, 25 | 28, 25 | 30, 771 by 3001 (packed, as rows of whole pieces) 25 | 24,
+// 32 | 33, 39 | 36; 800 x 4096 by 4096 297 | 214.
+constexpr int kWholeRows = 384;
 
 typedef hipError_t (*ProductCall)(const ProductArgs&, int, Tile, Finish, hipStream_t);
 
-hipError_t run_product(ProductCall call, ProductArgs g, const Product& plan, float* part, int32_t dtype, hipStream_t s) {
-    g.terms = terms_of(dtype);
+hipError_t run_product(ProductCall call, ProductArgs g, const Product& plan, float* part, int32_t dtype, hipStream_t s,
+                       bool whole = false) {
+    g.terms = whole ? 1 : terms_of(dtype);
     g.splits = kMaxSplits, g.jobs = tile_jobs(plan.tile);
     g.part = part, g.part_stride = cover_of(g.n, 4) * 4;
     const Finish finish = plan.split ? kSum : kStore;
     const hipError_t e = g.b_scale ? product_bytes(g, element_of(dtype), plan.tile, finish, s)
-                                   : call(g, element_of(dtype), plan.tile, finish, s);
+                                   : call(g, whole ? dtype : element_of(dtype), plan.tile, finish, s);
     if (e || !plan.split) return e;
-    const Join j{part, g.part_stride, g.m, g.n, g.k, nullptr, nullptr, g.terms, g.splits, g.jobs, tile_size(plan.tile),
+    const Join j{part, g.part_stride, g.m, g.n, whole ? 2 * g.k : g.k, nullptr, nullptr, g.terms, g.splits, g.jobs, tile_size(plan.tile),
                  nullptr, nullptr, g.m, g.out, g.out_stride, g.out_type, g.bias, g.bias_type};
     return join_parts(j, s);
 }
@@ -75,15 +86,21 @@ struct Forward {
     uint16_t *x, *w;
     float* part;
     Product y;
-    bool few;
+    bool few, whole;  // float32 without planes
     Forward(void* base, const void* x_, int64_t x_stride, int64_t rows, int64_t cols, int32_t dtype, const void* w_,
             int64_t w_stride, int64_t n)
         : y(rows, n, cols, dtype) {
         space.base = (uint8_t*)base;
-        few = rows <= kFewRows && dtype != WARP_F32;
+        few = rows <= kFewRows;
+        whole = !few && dtype == WARP_F32 && rows <= kWholeRows;
         if (few) y.floats = 0;
-        x = space.take<uint16_t>(direct(x_, x_stride, rows, cols, dtype) ? 0 : packed_elements(rows, cols, dtype));
-        w = space.take<uint16_t>(direct(w_, w_stride, n, cols, dtype) ? 0 : packed_elements(n, cols, dtype));
+        if (whole) y = Product(rows, n, cols);
+        auto room = [&](const void* p, int64_t stride, int64_t count) {
+            if (few || (whole ? direct_f32 : direct)(p, stride, count, cols, dtype)) return (int64_t)0;
+            return whole ? 2 * count * packed_width(cols) : packed_elements(count, cols, dtype);
+        };
+        x = space.take<uint16_t>(room(x_, x_stride, rows));
+        w = space.take<uint16_t>(room(w_, w_stride, n));
         part = space.take<float>(y.floats);
     }
 };
@@ -98,19 +115,31 @@ inline bool takes_bytes(int64_t rows, int64_t n, int64_t cols, int32_t dtype, in
     return dtype != WARP_F32 && direct + direct / 8 + 5000 < packed + rows * cols * 3 / 5000 + rows * n * 2 / 5000 + 12000;
 }
 
+// dx of few rows by the weight where it lies, dweight of few float32 rows. us for both, dbias and the 8-bit rows, so | by tiles in
+// planes: 16 x 4096 by 4096 40 | 157, 32 53 | 157, 64 76 | 168, 771 by 3001 30 | 45, 41 | 45, 38 | 44, 16 x 1024 by 1024 21 | 32.
+inline bool few_dx(int64_t rows, int32_t dtype) { return rows <= (dtype == WARP_F32 ? 2 * kFewRows : kFewRows); }
+inline bool takes_outer(int64_t rows, int64_t n, int64_t cols, int32_t dtype) {
+    return dtype == WARP_F32 && rows && rows <= (n * cols < 1 << 23 ? kOuter / 2 : kOuter);
+}
+
 struct Backward {
     Space space;
     uint16_t *dy, *x, *w;
     float *part, *room;
     Product dx, dw;
-    bool bytes;
-    int64_t sums;  // parts of dbias
+    bool bytes, few, outer;  // dx of few rows, dweight over few
+    int64_t sums;     // parts of dbias
+    int parts;        // of dx of few rows
     Backward(void* base, const void* dy_, int64_t dy_stride, int64_t rows, int64_t cols, int32_t dtype, const void* w_,
              int64_t w_stride, int64_t n)
         : dx(rows, cols, n, dtype), dw(n, cols, rows, dtype) {
         space.base = (uint8_t*)base;
-        dy = space.take<uint16_t>(direct(dy_, dy_stride, rows, n, dtype) ? 0 : packed_elements(rows, n, dtype));
-        w = space.take<uint16_t>(direct(w_, w_stride, n, cols, dtype) ? 0 : packed_elements(n, cols, dtype));
+        few = few_dx(rows, dtype);
+        outer = takes_outer(rows, n, cols, dtype);
+        dy = space.take<uint16_t>((few && outer) || direct(dy_, dy_stride, rows, n, dtype) ? 0 : packed_elements(rows, n, dtype));
+        parts = few ? few_parts(rows, cols, n, dtype) : 0;
+        if (few) dx.floats = parts * rows * cover_of(cols, 4) * 4;
+        w = space.take<uint16_t>(few || direct(w_, w_stride, n, cols, dtype) ? 0 : packed_elements(n, cols, dtype));
         const Product direct_dw(n, cols, rows, dtype, kT128);
         bytes = takes_bytes(rows, n, cols, dtype, direct_dw.time, dw.time);
         sums = 0;
@@ -120,7 +149,8 @@ struct Backward {
                             : 1;
             sums *= cover_of(cols, tile_size(dw.tile));
         }
-        x = space.take<uint16_t>(bytes ? 0 : packed_elements(rows, cols, dtype));
+        x = space.take<uint16_t>(bytes || outer ? 0 : packed_elements(rows, cols, dtype));
+        if (outer) dw.floats = 0;
         part = space.take<float>(dx.floats > dw.floats ? dx.floats : dw.floats);
         room = space.take<float>(sums * n > column_room(rows, n) ? sums * n : column_room(rows, n));
     }
@@ -176,14 +206,20 @@ int warp_linear(const void* x, int64_t x_stride, int64_t rows, int32_t cols, int
     if (!rc) rc = require_device();
     if (rc || !rows) return rc;
     hipStream_t s = (hipStream_t)hip_stream;
+    if (f.few) {
+        ProductArgs g = product_args({x, rows <= 1 ? cols : x_stride, 0}, {weight, n <= 1 ? cols : weight_stride, 0}, rows, n, cols, y,
+                                     y_stride, dtype);
+        g.bias = bias, g.bias_type = bias_dtype;
+        WARP_STEP(product_few(g, dtype, false, kStore, 1, s));
+        return WARP_OK;
+    }
     PackRows pack_x, pack_w;
-    const Operand a = operand_of(x, x_stride, rows, cols, dtype, f.x, &pack_x);
-    const Operand b = operand_of(weight, weight_stride, n, cols, dtype, f.w, &pack_w);
+    const Operand a = operand_of(x, x_stride, rows, cols, dtype, f.x, &pack_x, f.whole);
+    const Operand b = operand_of(weight, weight_stride, n, cols, dtype, f.w, &pack_w, f.whole);
     WARP_STEP(pack_rows(pack_x, pack_w, dtype, s));
     ProductArgs g = product_args(a, b, rows, n, cols, y, y_stride, dtype);
     g.bias = bias, g.bias_type = bias_dtype;
-    if (f.few) WARP_STEP(product_few(g, element_of(dtype), s));
-    else WARP_STEP(run_product(product_along, g, f.y, f.part, dtype, s));
+    WARP_STEP(run_product(product_along, g, f.y, f.part, dtype, s, f.whole));
     return WARP_OK;
 }
 
@@ -224,14 +260,26 @@ int warp_linear_backward(const void* dy, int64_t dy_stride, int64_t rows, int32_
     hipStream_t s = (hipStream_t)hip_stream;
     PackRows pack_dy, pack_w;
     Operand d{}, t{};
-    if (rows && (dx || dweight)) d = operand_of(dy, dy_stride, rows, n, dtype, w.dy, &pack_dy);
-    if (rows && dx) t = operand_of(weight, weight_stride, n, cols, dtype, w.w, &pack_w);
+    if (rows && ((dx && !w.few) || (dweight && !w.outer))) d = operand_of(dy, dy_stride, rows, n, dtype, w.dy, &pack_dy);
+    if (rows && dx && !w.few) t = operand_of(weight, weight_stride, n, cols, dtype, w.w, &pack_w);
     WARP_STEP(pack_rows(pack_dy, pack_w, dtype, s));
-    if (rows && dx) {
+    if (rows && dx && w.few) {
+        ProductArgs g = product_args({dy, rows <= 1 ? n : dy_stride, 0}, {weight, n <= 1 ? cols : weight_stride, 0}, rows, cols, n, dx,
+                                     dx_stride, dtype);
+        g.part = w.part, g.part_stride = cover_of(cols, 4) * 4;
+        WARP_STEP(product_few(g, dtype, false, kSum, w.parts, s));
+        Join j{w.part, g.part_stride, rows, cols, n, nullptr, nullptr, 0, 0, 0, 0, nullptr, nullptr, rows, dx, dx_stride, dtype,
+               nullptr, 0};
+        j.parts = w.parts;
+        WARP_STEP(join_parts(j, s));
+    } else if (rows && dx) {
         WARP_STEP(run_product(product_mixed, product_args(d, t, rows, cols, n, dx, dx_stride, dtype), w.dx, w.part, dtype, s));
     }
     const bool bytes = dweight && w.bytes && rows;
-    if (bytes) {
+    if (dweight && w.outer) {
+        WARP_STEP(product_outer({dy, q, rows <= 1 ? n : dy_stride, 0, q_stride, 0, q_scale, n, cols, rows, nullptr, nullptr, (float*)dweight,
+                                 dweight_stride, (float*)dbias}, s));
+    } else if (bytes) {
         ProductArgs g = product_args(d, {q, q_stride, 0}, n, cols, rows, dweight, dweight_stride, dtype);
         g.b_scale = q_scale, g.sums = dbias ? w.room : nullptr;
         WARP_STEP(run_product(nullptr, g, w.dw, w.part, dtype, s));
@@ -242,7 +290,7 @@ int warp_linear_backward(const void* dy, int64_t dy_stride, int64_t rows, int32_
         WARP_STEP(run_product(product_across, product_args(d, x, n, cols, rows, dweight, dweight_stride, dtype), w.dw, w.part,
                               dtype, s));
     }
-    if (dbias && !bytes) WARP_STEP(column_sums(dy, dy_stride, rows, n, dtype, w.room, dbias, dbias_dtype, s));
+    if (dbias && !bytes && !(dweight && w.outer)) WARP_STEP(column_sums(dy, dy_stride, rows, n, dtype, w.room, dbias, dbias_dtype, s));
     return WARP_OK;
 }
 

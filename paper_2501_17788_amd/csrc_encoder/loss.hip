@@ -388,10 +388,22 @@ struct Sizes {
     int64_t tokens, vocabulary, cols, width;
     int32_t dtype;
     int planes;
+    bool few;    // rows: the table is read where it lies
     bool packs;  // the table
+    bool whole;  // the forward pass's float32 without planes
 };
-Sizes sizes_of(int64_t tokens, const void* table, int64_t stride, int64_t vocabulary, int32_t cols, int32_t dtype) {
-    return {tokens, vocabulary, cols, packed_width(cols), dtype, planes_of(dtype), !direct(table, stride, vocabulary, cols, dtype)};
+Sizes sizes_of(int64_t tokens, const void* table, int64_t stride, int64_t vocabulary, int32_t cols, int32_t dtype, bool back) {
+    // us with the table where it lies | by tiles. 16 tokens in 16 bits: forward, 5000 rows of 4096 18 | 40, 32,128 of 768 19 | 18,
+    // 100,001 of 1023 (packed for tiles) 135 | 146, 200,001 of 65 40 | 58; backward 43 | 64, 46 | 44, 516 | 403, 79 | 87. 32 tokens in
+    // float32, forward 49 | 210, 41 | 88, 167 | 364, 91 | 104, both passes 201 | 504, 194 | 261, 748 | 1275, 286 | 296.
+    const bool few = dtype == WARP_F32 ? tokens <= kFewRows
+                                       : tokens <= kFewRows / 2 && (vocabulary <= 16384 || (cols % 8 && !back));
+    // The forward pass in float32 as it is | in planes: 64 tokens 40 | 89, 33 | 61, 312 | 401, 92 | 210, 79 | 103 (tables of 768 x
+    // 32,128, 128 x 100,001, 1023, 4096 x 5000, 65 x 200,001), 100 tokens 73 | 103, 58 | 79, 445 | 398, 93 | 213, 113 | 129, 200 tokens
+    // 121 | 123, 88 | 90, 711 | 468, 153 | 213, 161 | 163.
+    const bool whole = !back && !few && dtype == WARP_F32 && tokens <= 128;
+    const bool packs = !few && !(whole ? direct_f32 : direct)(table, stride, vocabulary, cols, dtype);
+    return {tokens, vocabulary, cols, packed_width(cols), dtype, planes_of(dtype), few, packs, whole};
 }
 
 struct Forward {
@@ -407,13 +419,15 @@ struct Forward {
         const int64_t tokens = z.tokens > 0 ? z.tokens : 1;
         const int64_t by_table = z.packs ? piece_of(z.vocabulary, z.width * 2 * z.planes, kPieceBytes) : 1 << 30;
         tile = plan_product(tokens, z.vocabulary, product_steps(z.cols, terms_of(z.dtype)), false).tile;
-        const int64_t by_stats = piece_of(z.vocabulary, cover_of(tokens * 8, tile_size(tile)), kStatsBytes);
+        if (z.whole) tile = tile_f32(tokens, z.vocabulary);
+        const int64_t columns = z.few ? 16 : tile_size(tile);
+        const int64_t by_stats = piece_of(z.vocabulary, cover_of(tokens * 8, columns), kStatsBytes);
         piece = by_table < by_stats ? by_table : by_stats;
         hidden = space.take<uint16_t>(packed_elements(tokens, z.cols, z.dtype));
         table = space.take<uint16_t>(z.packs ? packed_elements(piece, z.cols, z.dtype) : 0);
         list = space.take<int32_t>(tokens), place = space.take<int32_t>(tokens), target = space.take<int32_t>(tokens);
         now = space.take<int32_t>(1);
-        stats = space.take<float2>(cover_of(piece, tile_size(tile)) * tokens), running = space.take<float2>(tokens);
+        stats = space.take<float2>(cover_of(piece, columns) * tokens), running = space.take<float2>(tokens);
         of_target = space.take<float>(tokens);
     }
 };
@@ -422,7 +436,8 @@ struct Backward {
     Space space;
     int64_t piece;
     Tile logits, dh, de;
-    bool de_split;
+    bool de_split, outer;
+    int dh_parts;  // of few rows
     uint16_t *hidden, *table, *grad;
     int32_t *list, *place, *target, *now;
     float *largest, *factor, *lse2, *weight, *at_target, *dh_part, *de_part;
@@ -439,7 +454,8 @@ struct Backward {
         logits = plan_product(tokens, cols, product_steps(z.cols, terms), false).tile;
         dh = plan_product(tokens, z.cols, product_steps(cols, terms), true).tile;
         const ProductPlan e = plan_product(cols, z.cols, product_steps(tokens, terms), true);
-        de = e.tile, de_split = e.split;
+        outer = z.dtype == WARP_F32 && tokens <= kFewRows;
+        de = e.tile, de_split = !outer && e.split;
         hidden = space.take<uint16_t>(packed_elements(tokens, z.cols, z.dtype));
         table = space.take<uint16_t>(z.packs ? packed_elements(piece, z.cols, z.dtype) : 0);
         grad = space.take<uint16_t>(z.planes * tokens * piece);
@@ -447,7 +463,9 @@ struct Backward {
         now = space.take<int32_t>(1);
         largest = space.take<float>(1), factor = space.take<float>(1);
         lse2 = space.take<float>(tokens), weight = space.take<float>(tokens), at_target = space.take<float>(tokens);
-        dh_part = space.take<float>(part_floats(tokens, z.cols, cols, terms, dh, kMaxSplits, tile_jobs(dh)));
+        dh_parts = z.few ? few_parts(tokens, z.cols, cols, z.dtype) : 0;
+        dh_part = space.take<float>(z.few ? dh_parts * tokens * cover_of(z.cols, 4) * 4
+                                          : part_floats(tokens, z.cols, cols, terms, dh, kMaxSplits, tile_jobs(dh)));
         de_part = space.take<float>(
             de_split ? part_floats(cols, z.cols, tokens, terms, de, kMaxSplits, tile_jobs(de)) : 0);
     }
@@ -471,9 +489,9 @@ int warp_cross_entropy_scratch(int64_t tokens, int32_t cols, int32_t dtype, cons
                                int64_t vocabulary, int64_t* bytes, int64_t* backward_bytes) {
     const char* what = "cross entropy";
     if (const int rc = check_sizes(what, tokens, vocabulary, cols, dtype)) return rc;
-    const Sizes z = sizes_of(tokens, table, table_stride, vocabulary, cols, dtype);
-    if (bytes) *bytes = Forward(nullptr, z).space.used;
-    if (backward_bytes) *backward_bytes = Backward(nullptr, z).space.used;
+    auto sizes = [&](bool back) { return sizes_of(tokens, table, table_stride, vocabulary, cols, dtype, back); };
+    if (bytes) *bytes = Forward(nullptr, sizes(false)).space.used;
+    if (backward_bytes) *backward_bytes = Backward(nullptr, sizes(true)).space.used;
     return WARP_OK;
 }
 
@@ -487,7 +505,7 @@ int warp_cross_entropy(const void* hidden, int64_t hidden_stride, int64_t tokens
     if (!rc) rc = check_matrix(what, table, table_stride, vocabulary, cols, dtype);
     if (!rc) rc = check_rows(what, targets, target_bytes, tokens, scale, loss, lse);
     if (rc) return rc;
-    const Sizes z = sizes_of(tokens, table, table_stride, vocabulary, cols, dtype);
+    const Sizes z = sizes_of(tokens, table, table_stride, vocabulary, cols, dtype, false);
     const Forward f(scratch, z);
     rc = check_scratch(what, scratch, scratch_bytes, f.space.used);
     if (!rc) rc = require_device();
@@ -496,12 +514,13 @@ int warp_cross_entropy(const void* hidden, int64_t hidden_stride, int64_t tokens
     const SelectArgs sel{targets, target_bytes == 8, tokens, vocabulary, nullptr, scale, 1.f, f.list, f.place, f.target,
                          f.now, nullptr, nullptr};
     const bool few = tokens <= kFewTokens;
-    if (few) {
+    if (z.few) {  // all rows, the others' results unused
+    } else if (few && !z.whole) {
         WARP_LAUNCH(take_few({sel, hidden, hidden_stride, cols, z.width, tokens * z.width, f.hidden, nullptr, nullptr, nullptr,
                               nullptr, nullptr}, dtype, s));
     } else {
         WARP_LAUNCH(select(sel, s));
-        WARP_STEP(pack_rows({hidden, hidden_stride, tokens, cols, f.list, f.now, f.hidden}, {}, dtype, s));
+        WARP_STEP(pack_rows({hidden, hidden_stride, tokens, cols, f.list, f.now, f.hidden, z.whole}, {}, dtype, s));
     }
     for (int64_t v0 = 0; v0 < vocabulary; v0 += f.piece) {
         const int64_t n = vocabulary - v0 < f.piece ? vocabulary - v0 : f.piece;
@@ -509,7 +528,7 @@ int warp_cross_entropy(const void* hidden, int64_t hidden_stride, int64_t tokens
         hipError_t e = hipSuccess;
         Operand t{rows, vocabulary <= 1 ? cols : table_stride, 0};
         if (z.packs) {
-            e = pack_rows({rows, table_stride, n, cols, nullptr, nullptr, f.table}, {}, dtype, s);
+            e = pack_rows({rows, table_stride, n, cols, nullptr, nullptr, f.table, z.whole}, {}, dtype, s);
             t = {f.table, z.width, n * z.width};
         }
         WARP_STEP(e);
@@ -519,8 +538,16 @@ int warp_cross_entropy(const void* hidden, int64_t hidden_stride, int64_t tokens
         g.m = tokens, g.n = n, g.k = cols, g.m_now = f.now, g.terms = terms_of(dtype);
         g.to_log2 = to_log2(scale), g.n0 = v0, g.target = f.target;
         g.stats = f.stats, g.stats_stride = tokens, g.of_target = f.of_target;
-        WARP_STEP(product_softmax(g, element_of(dtype), false, f.tile, kStats, s));
-        const JoinStatsArgs j{f.stats, tokens, (int)cover_of(n, tile_size(f.tile)), v0 == 0, v0 + n == vocabulary, f.running,
+        if (z.few) {
+            g.a = hidden, g.a_stride = tokens <= 1 ? cols : hidden_stride, g.m_now = nullptr;
+            g.targets = targets, g.wide = target_bytes == 8, g.vocabulary = vocabulary, g.place = f.place;
+        }
+        if (z.whole) g.terms = 1;
+        if (z.few) WARP_STEP(product_few(g, dtype, false, kStats, 1, s));
+        else if (z.whole) WARP_STEP(product_softmax(g, WARP_F32, false, f.tile, kStats, s));
+        else WARP_STEP(product_softmax(g, element_of(dtype), false, f.tile, kStats, s));
+        const int64_t columns = !z.few ? tile_size(f.tile) : few_wide(n) ? 32 : 16;
+        const JoinStatsArgs j{f.stats, tokens, (int)cover_of(n, columns), v0 == 0, v0 + n == vocabulary, f.running,
                               f.of_target, f.place, tokens, loss, lse};
         if (few) WARP_LAUNCH(hipLaunchKernelGGL(k_join_stats<true>, dim3((uint32_t)tokens), dim3(1024), 0, s, j));
         else WARP_LAUNCH(hipLaunchKernelGGL(k_join_stats<false>, dim3((uint32_t)cover_of(tokens, kWave)), dim3(1024), 0, s, j));
@@ -543,7 +570,7 @@ int warp_cross_entropy_backward(const float* dloss, const void* hidden, int64_t 
     if (rc) return rc;
     if (tokens && !dloss) return fail(WARP_EINVAL, "%s: null pointer", what);
     if ((uintptr_t)dloss % 4) return fail(WARP_EINVAL, "%s: misaligned pointer", what);
-    const Sizes z = sizes_of(tokens, table, table_stride, vocabulary, cols, dtype);
+    const Sizes z = sizes_of(tokens, table, table_stride, vocabulary, cols, dtype, true);
     const Backward w(scratch, z);
     rc = check_scratch(what, scratch, scratch_bytes, w.space.used);
     if (!rc) rc = require_device();
@@ -567,7 +594,7 @@ int warp_cross_entropy_backward(const float* dloss, const void* hidden, int64_t 
     const Operand h{w.hidden, z.width, (tokens ? tokens : 1) * z.width};
     const int64_t part_stride = cover_of(cols, 4) * 4;
     Join dh{w.dh_part, part_stride, tokens, cols, 0, w.now, nullptr, terms, kMaxSplits, tile_jobs(w.dh), tile_size(w.dh),
-            w.factor, w.place, tokens, dhidden, dhidden_stride, dtype, nullptr, 0};
+            w.factor, w.place, tokens, dhidden, dhidden_stride, dtype, nullptr, 0, w.dh_parts};
     for (int64_t v0 = 0; v0 < vocabulary; v0 += w.piece) {
         const int64_t n = vocabulary - v0 < w.piece ? vocabulary - v0 : w.piece;
         const void* rows = (const uint8_t*)table + v0 * table_stride * dtype_bytes(dtype);
@@ -583,14 +610,18 @@ int warp_cross_entropy_backward(const float* dloss, const void* hidden, int64_t 
         g.to_log2 = to_log2(scale), g.n0 = v0, g.target = w.target;
         g.lse = w.lse2, g.weight = w.weight, g.at_target = w.at_target;
         g.grad = w.grad, g.grad_stride = w.piece, g.grad_plane = tokens * w.piece, g.grad_scale = grad_scale;
-        WARP_STEP(product_softmax(g, element, z.planes == 3, w.logits, kGrad, s));
-        if (dtable) {
+        if (z.few) WARP_STEP(product_few(g, dtype, z.planes == 3, kGrad, 1, s));
+        else WARP_STEP(product_softmax(g, element, z.planes == 3, w.logits, kGrad, s));
+        void* rows_out = dtable ? (uint8_t*)dtable + v0 * dtable_stride * dtype_bytes(dtype) : nullptr;
+        if (dtable && w.outer) {
+            WARP_STEP(product_outer({w.grad, h.p, w.piece, g.grad_plane, h.stride, h.plane, nullptr, n, cols, tokens, w.now,
+                                     w.factor, (float*)rows_out, dtable_stride, nullptr}, s));
+        } else if (dtable) {
             ProductArgs e{};
             e.a = w.grad, e.a_stride = w.piece, e.a_plane = g.grad_plane;
             e.b = h.p, e.b_stride = h.stride, e.b_plane = h.plane;
             e.m = n, e.n = cols, e.k = tokens, e.k_now = w.now, e.terms = terms;
-            e.out = (uint8_t*)dtable + v0 * dtable_stride * dtype_bytes(dtype), e.out_stride = dtable_stride;
-            e.out_type = dtype, e.factor = w.factor;
+            e.out = rows_out, e.out_stride = dtable_stride, e.out_type = dtype, e.factor = w.factor;
             e.splits = kMaxSplits, e.jobs = tile_jobs(w.de), e.part = w.de_part, e.part_stride = part_stride;
             WARP_STEP(product_across(e, element, w.de, w.de_split ? kSum : kStore, s));
             if (w.de_split)
@@ -605,7 +636,8 @@ int warp_cross_entropy_backward(const float* dloss, const void* hidden, int64_t 
             d.splits = kMaxSplits, d.jobs = tile_jobs(w.dh), d.part = w.dh_part, d.part_stride = part_stride;
             d.accumulate = v0 > 0;
             if (!v0) dh.k = n;  // the last piece, shorter, may have fewer parts: the others stay as they were
-            WARP_STEP(product_mixed(d, element, w.dh, kSum, s));
+            if (z.few) WARP_STEP(product_few(d, dtype, z.planes == 3, kSum, w.dh_parts, s));
+            else WARP_STEP(product_mixed(d, element, w.dh, kSum, s));
         }
     }
     if (dhidden) WARP_STEP(join_parts(dh, s));

@@ -36,6 +36,15 @@ inline bool direct(const void* p, int64_t stride, int64_t rows, int64_t cols, in
     return dtype != WARP_F32 && (uintptr_t)p % 16 == 0 && cols % 8 == 0 && (rows <= 1 || (stride % 8 == 0 && stride <= 1 << 22));
 }
 
+// The same for float32 products along K without planes.
+inline bool direct_f32(const void* p, int64_t stride, int64_t rows, int64_t cols, int32_t dtype) {
+    return dtype == WARP_F32 && (uintptr_t)p % 16 == 0 && cols % 4 == 0 && (rows <= 1 || (stride % 4 == 0 && stride <= 1 << 21));
+}
+// Tiles of 128 load half as much, where there are enough of them.
+inline Tile tile_f32(int64_t m, int64_t n) {
+    return m <= 64 || cover_of(m, 128) * cover_of(n, 128) < 256 ? kT64 : kT128;
+}
+
 #ifdef __HIPCC__
 // Eight elements of an operand.
 template <typename E, int PLANES>
@@ -66,17 +75,18 @@ struct PackRows {
     int64_t stride = 0, rows = 0, cols = 0;
     const int32_t *list = nullptr, *now = nullptr;
     uint16_t* out = nullptr;
+    bool whole = false;  // float32 as it is
 };
 hipError_t pack_rows(const PackRows& a, const PackRows& b, int32_t dtype, hipStream_t s);
 // The same of 8-bit rows: q * scale, for products in `dtype`.
 hipError_t unpack_int8(const int8_t* q, int64_t q_stride, const float* scale, int64_t rows, int64_t cols, int32_t dtype,
                        uint16_t* out, hipStream_t s);
 
-// x as an operand: where it lies, or in `room`, for which `job` is then what has to be packed.
+// x as an operand: where it lies, or in `room`, for which `job` is then what has to be packed. `whole`: float32 without planes.
 inline Operand operand_of(const void* x, int64_t stride, int64_t rows, int64_t cols, int32_t dtype, uint16_t* room,
-                          PackRows* job) {
-    if (direct(x, stride, rows, cols, dtype)) return {x, rows <= 1 ? cols : stride, 0};
-    *job = {x, stride, rows, cols, nullptr, nullptr, room};
+                          PackRows* job, bool whole = false) {
+    if (whole ? direct_f32(x, stride, rows, cols, dtype) : direct(x, stride, rows, cols, dtype)) return {x, rows <= 1 ? cols : stride, 0};
+    *job = {x, stride, rows, cols, nullptr, nullptr, room, whole};
     return {room, packed_width(cols), rows * packed_width(cols)};
 }
 
@@ -96,8 +106,36 @@ struct Join {
     int32_t out_type;
     const void* bias;
     int32_t bias_type;
+    int32_t parts = 0;  // where they were made by product_few
 };
 hipError_t join_parts(const Join& j, hipStream_t s);
+
+// Products of few rows (product_few): whether those along K are made of 32 columns a wave or 16, and in how many parts those across K
+// are made, to have 512 workgroups.
+constexpr int kFewRows = 32;  // most that one load of the other operand serves
+inline bool few_wide(int64_t n) { return n > 8192; }
+inline int few_parts(int64_t m, int64_t n, int64_t k, int32_t dtype) {
+    if (!m) return 1;
+    const bool f32 = dtype == WARP_F32;
+    const int64_t tiles = cover_of(m, m <= 16 ? 16 : 32) * cover_of(n, f32 ? 64 : 128);
+    const int64_t most = cover_of(k, f32 ? 128 : 256), parts = 512 / tiles;
+    return (int)(parts < 1 ? 1 : parts < most ? parts : most);
+}
+
+// float32 products over at most kOuter k, both operands across K: in planes, or A a float32 and B 8-bit rows with scales.
+constexpr int kOuter = 64;
+struct OuterArgs {
+    const void *a, *b;
+    int64_t a_stride, a_plane, b_stride, b_plane;
+    const float* b_scale;
+    int64_t m, n, k;
+    const int32_t* k_now;
+    const float* factor;
+    float* out;
+    int64_t out_stride;
+    float* sums;  // of A's columns, or null
+};
+hipError_t product_outer(const OuterArgs& g, hipStream_t s);
 
 // Floats that the parts of a kSum product need, whatever the present counts are.
 inline int64_t part_floats(int64_t m, int64_t n, int64_t k, int terms, Tile tile, int splits, int jobs) {

@@ -63,7 +63,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_join_parts(Join j) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int64_t c = ((int64_t)blockIdx.x * kWave + lane) * 4;
     const int64_t m = j.m_now ? *j.m_now : j.m, k = j.k_now ? *j.k_now : j.k;
-    const int parts = product_splits(m, j.n, product_steps(k, j.terms), j.tile, j.splits, j.jobs);
+    const int parts = j.parts ? j.parts : product_splits(m, j.n, product_steps(k, j.terms), j.tile, j.splits, j.jobs);
     const float factor = j.factor ? *j.factor : 1.f;
     float bias[4];
 #pragma unroll
@@ -182,7 +182,8 @@ hipError_t pack_rows(const PackRows& a, const PackRows& b, int32_t dtype, hipStr
     }
     const dim3 block(64 * kRowWaves);
     (void)hipGetLastError();
-    if (dtype == WARP_F32) hipLaunchKernelGGL((k_pack_rows<float, 3>), grid, block, 0, s, jobs);
+    if (jobs.m[0].whole) hipLaunchKernelGGL((k_pack_rows<float, 1>), grid, block, 0, s, jobs);
+    else if (dtype == WARP_F32) hipLaunchKernelGGL((k_pack_rows<float, 3>), grid, block, 0, s, jobs);
     else if (dtype == WARP_F16) hipLaunchKernelGGL((k_pack_rows<_Float16, 1>), grid, block, 0, s, jobs);
     else hipLaunchKernelGGL((k_pack_rows<__bf16, 1>), grid, block, 0, s, jobs);
     return hipGetLastError();

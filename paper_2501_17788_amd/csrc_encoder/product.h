@@ -1,4 +1,4 @@
-// Products of matrices of 16-bit elements on the matrix cores, with what the callers do to a finished tile:
+// Products of matrices on the matrix cores, most of them of 16-bit elements, with what the callers do to a finished tile:
 //   C[m][n] = sum_k A(m, k) B(n, k), sums in fp32.
 // An operand's elements of one row lie together (kAlongK: tokens, weights as stored) or those of one k (kAcrossK: its
 // transpose, as stored). Operands are 16-byte aligned, their strides multiples of 8; along K a row's elements beyond k up
@@ -6,7 +6,8 @@
 //
 // float32 operands come as three planes of bfloat16, high + middle + low = x to the last bit (split_f32), and a
 // product as the six of nine products of planes that count: those left out are below 2^-23 of |a b| together.
-// (A matrix instruction for fp32 operands has a 16th of the rate; six products are 2.7 times as fast.)
+// (A matrix instruction for fp32 operands has a 16th of the rate; six products are 2.7 times as fast.) Where there are few
+// rows, for which packing a whole weight would take longer than the product, they are multiplied as they are.
 #pragma once
 
 #include <type_traits>
@@ -53,6 +54,11 @@ struct ProductArgs {
     float2* stats;          // [tile column][row]: largest logit of the others than the target, sum of their exponentials
     int64_t stats_stride;
     float* of_target;       // [row] the target's logit
+    // instead of `target`, of few rows: the tokens' own targets, by which a row's place becomes its number, -1 or -2
+    const void* targets;
+    bool wide;
+    int64_t vocabulary;
+    int32_t* place;
     const float *lse, *weight, *at_target;  // [row] in units of log 2; of the row; value at the target
     void* grad;
     int64_t grad_stride, grad_plane;
@@ -153,12 +159,13 @@ __host__ __device__ inline void split_f32(float x, uint16_t (&out)[3]) {
     }
 }
 
-// Launches: element is WARP_F16 or WARP_BF16 (also for planes).
+// Launches: element is WARP_F16 or WARP_BF16 (also for planes), along K and for kStats also WARP_F32 (up to kT128).
 hipError_t product_along(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);   // A, B along K
 hipError_t product_mixed(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);   // B across K
 hipError_t product_across(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);  // both
-constexpr int kFewRows = 32;
-hipError_t product_few(const ProductArgs& g, int element, hipStream_t s);  // both along K; kStore of up to kFewRows rows
+// Operands as they are, of any alignment, A along K (with `planes` a float32 in planes). B along K: kStore, kStats or kGrad; across K:
+// kSum in `parts` parts.
+hipError_t product_few(const ProductArgs& g, int32_t dtype, bool planes, Finish finish, int parts, hipStream_t s);
 hipError_t product_bytes(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);  // b of 8 bits; to kT128
 hipError_t product_softmax(const ProductArgs& g, int element, bool planes, Tile tile, Finish finish, hipStream_t s);
 
@@ -179,6 +186,15 @@ struct Eight {
 };
 __device__ __forceinline__ float4v product_mfma(Eight<__bf16>::type a, Eight<__bf16>::type b, float4v c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+template <>
+struct Eight<float> {  // four of them
+    typedef float4v type;
+};
+__device__ __forceinline__ float4v product_mfma(float4v a, float4v b, float4v c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    return c;
 }
 __device__ __forceinline__ float4v product_mfma(Eight<_Float16>::type a, Eight<_Float16>::type b, float4v c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -201,9 +217,10 @@ __device__ __forceinline__ int channel_piece(int row) { return (row & 3) | (row 
 template <int T>
 __device__ __forceinline__ int pair_key(int k) { return ((k & 3) | (k >> 3 & 3) << 2) & (T / 16 - 1); }
 
-// One operand's part in a tile of T rows by 64 k, for one wave of WAVES.
-template <Layout L, int T, int WAVES, bool CHANNELS, int B>
+// One operand's part in a tile of T rows by 128 bytes of k, of S each, for one wave of WAVES.
+template <Layout L, int T, int WAVES, bool CHANNELS, int B, int S>
 struct Stage {
+    static_assert(L == kAlongK || S == 2, "across K two blocks of 16-bit elements are read at once");
     static constexpr int kLoads = T / 8 / WAVES;  // of 1 KB
     static_assert(kLoads * 8 * WAVES == T, "whole loads");
     uint32_t off[kLoads];
@@ -215,19 +232,19 @@ struct Stage {
     // this lane's k within a step, in load i
     __device__ __forceinline__ int k_of(int i) const {
         const int unit = wave * kLoads + i;
-        if (L == kAlongK) return 8 * ((lane & 7) ^ key(unit * 8 + (lane >> 3)));
+        if (L == kAlongK) return 16 / S * ((lane & 7) ^ key(unit * 8 + (lane >> 3)));
         return (unit * 1024 + lane * 16) / (T * 2);
     }
     __device__ __forceinline__ void start(const void* p, int64_t stride, int64_t first, int64_t rows, int lane_, int wave_) {
         lane = lane_, wave = wave_;
         if (L == kAlongK) {
-            at = (const uint8_t*)p + first * stride * 2;
-            step_bytes = 2 * kProductStep;
+            at = (const uint8_t*)p + first * stride * S;
+            step_bytes = 128;
             const int last = (int)(rows - first < T ? rows - first : T) - 1;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int row = (wave * kLoads + i) * 8 + (lane >> 3);
-                off[i] = (uint32_t)(row < last ? row : last) * (uint32_t)(stride * 2) + 2 * k_of(i);
+                off[i] = (uint32_t)(row < last ? row : last) * (uint32_t)(stride * S) + S * k_of(i);
             }
         } else {
             at = (const uint8_t*)p + first * 2;
@@ -409,7 +426,8 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
 
     const int64_t rows = g.m_now ? *g.m_now : g.m;
     const int64_t k = g.k_now ? *g.k_now : g.k;
-    const int64_t steps = product_steps(k, g.terms);
+    constexpr int kStep = 128 / sizeof(E);
+    const int64_t steps = cover_of(k, kStep) * g.terms;
     const int tiles_m = (int)cover_of(rows, TM), tiles_n = (int)cover_of(g.n, TN);
     const int splits = F == kSum ? product_splits(rows, g.n, steps, TM, g.splits, g.jobs) : 1;
     const int tiles = tiles_m * tiles_n, total = tiles * splits;
@@ -427,8 +445,8 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
     const int64_t first = split * each;
     const int count = (int)(steps - first < each ? (steps > first ? steps - first : 0) : each);
 
-    Stage<LA, TM, kWaves, false, kBM> sa;
-    Stage<LB, TN, kWaves, kWide, kBN> sb;
+    Stage<LA, TM, kWaves, false, kBM, sizeof(E)> sa;
+    Stage<LB, TN, kWaves, kWide, kBN, sizeof(E)> sb;
     sa.start(g.a, g.a_stride, m0, rows, lane, wave);
     // a step's 64 k go through all terms before the next ones: their planes are in the caches then
     int64_t kk = g.terms == 1 ? first : first / g.terms;
@@ -444,9 +462,9 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
     auto load = [&](uint8_t* la, uint8_t* lb) {
         // planes of the terms: (0,0) (0,1) (1,0) (1,1) (0,2) (2,0)
         const int64_t plane_a = (int64_t)(0x201100 >> 4 * term & 3) * g.a_plane, plane_b = (int64_t)(0x021010 >> 4 * term & 3) * g.b_plane;
-        const int64_t left = k - kk * kProductStep;
+        const int64_t left = k - kk * kStep;
         if constexpr (KIND == kBytes) bytes.load(left);
-        if (left >= kProductStep) {
+        if (left >= kStep) {
             sa.load(la, plane_a);
             if constexpr (KIND != kBytes) sb.load(lb, plane_b);
         } else {
@@ -699,7 +717,7 @@ hipError_t product_tiles(const ProductArgs& g, Tile tile, hipStream_t s) {
         case kT64: return product_launch<E, LA, LB, F, KIND, 64, 64, 2, 2>(g, s);
         case kT128: return product_launch<E, LA, LB, F, KIND, 128, 128, 2, 4>(g, s);
         default:
-            if constexpr (KIND == kBytes) return hipErrorInvalidValue;
+            if constexpr (KIND == kBytes || sizeof(E) == 4) return hipErrorInvalidValue;
             else return product_launch<E, LA, LB, F, KIND, 256, 256, 2, 4>(g, s);
     }
 }

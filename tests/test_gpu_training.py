@@ -233,7 +233,7 @@ def test_linear(rows, cols, n, dtype):
 
 
 @ALL
-@pytest.mark.parametrize("rows,cols,n", product_plans.SIZES)
+@pytest.mark.parametrize("rows,cols,n", product_plans.SIZES + product_plans.FEW)
 def test_linear_of_whole_numbers(rows, cols, n, dtype):
     """Every sum is exact, and so is its rounding."""
     g = gen(rows + cols + n)
@@ -405,6 +405,27 @@ def test_cross_entropy(tokens, vocabulary, cols, dtype):
     check_loss(hidden, table, some, cols ** -0.5, dloss, "some")
     b = check_loss(shifted(hidden), shifted(table), targets.int(), cols ** -0.5, dloss, "shifted")
     assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@ALL
+@pytest.mark.parametrize("tokens", [1, 15, 16, 17, 32, 33, 64, 65, 128, 129])
+def test_cross_entropy_of_few_tokens(tokens, dtype):
+    """On both sides of the numbers of tokens that choose between the kernels; vocabularies of both of their widths."""
+    for vocabulary, cols in ((5, 1), (33, 260), (300, 1030), (8200, 129), (16_500, 64), (17_000, 33)):
+        g = gen(tokens + vocabulary)
+        hidden, table, targets = scores(g, tokens, vocabulary, cols, dtype)
+        if tokens > 2:
+            targets[1], targets[2] = -1, vocabulary
+        dloss = torch.full((tokens,), 1000.0 if dtype == torch.float16 else 1.0, device="cuda")
+        say("cross entropy of few", tokens, vocabulary, cols, dtype)
+        a = check_loss(hidden, table, targets, cols ** -0.5, dloss, (tokens, vocabulary))
+        b = check_loss(shifted(hidden), shifted(table), targets.int(), -cols ** -0.5, dloss, (tokens, vocabulary, "negative"))
+        assert torch.isfinite(a[0]).sum() == torch.isfinite(b[0]).sum() >= tokens - 1
+        if tokens > 2:  # what a row that is left out holds is in no result
+            hidden[1] = math.nan
+            loss, lse = w.cross_entropy(hidden, table, targets, cols ** -0.5)
+            c = (loss, lse, *w.cross_entropy_backward(dloss, hidden, table, targets, loss, lse, cols ** -0.5))
+            assert all(torch.equal(x.nan_to_num(7.0), y.nan_to_num(7.0)) for x, y in zip(a, c))
 
 
 @ALL

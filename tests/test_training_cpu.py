@@ -117,8 +117,8 @@ def linear_back(**over):
     (dict(rows=(1 << 24) + 1), w.ENOTSUP, "2^24"), (dict(n=(1 << 20) + 1), w.ENOTSUP, "2^20"),
     (dict(rows=1 << 24, n=1 << 14), w.ENOTSUP, "2^36"), (dict(cols=1 << 18, n=1 << 17), w.ENOTSUP, "2^34"),
     (dict(dtype=9), w.EINVAL, "dtype"), (dict(weight=None), w.EINVAL, "null"), (dict(weight=P + 2), w.EINVAL, "misaligned"),
-    (dict(weight_stride=63), w.EINVAL, "stride"), (dict(scratch=None), w.EINVAL, "scratch"),
-    (dict(bytes=8), w.EINVAL, "scratch"), (dict(scratch=P + 1), w.EINVAL, "scratch"),
+    (dict(weight_stride=63), w.EINVAL, "stride"), (dict(rows=400, scratch=None), w.EINVAL, "scratch"),
+    (dict(rows=400, bytes=8), w.EINVAL, "scratch"), (dict(rows=400, scratch=P + 1), w.EINVAL, "scratch"),
 ])
 def test_linear_refusals(call, over, code, needle):
     refused(call(**over), code, needle)
@@ -192,13 +192,11 @@ def test_product_sizes_reach_their_kernels():
     seen = set()
     for rows, cols, n in product_plans.SIZES:
         for dtype in (0, 1, 2):
-            if dtype == 0 or rows > 32:
-                seen.add(("y", choose(rows, n, cols, dtype, False)))
-            else:
-                seen.add(("y", "few"))
-            seen.add(("dx", choose(rows, cols, n, dtype, False)))
+            few, whole, outer = rows <= 32, dtype == 0 and rows <= 384, dtype == 0 and rows <= 32
+            seen.add(("y", "few" if few else "whole" if whole else choose(rows, n, cols, dtype, False)))
+            seen.add(("dx", "few" if rows <= (64 if dtype == 0 else 32) else choose(rows, cols, n, dtype, False)))
             packed, direct = choose(n, cols, rows, dtype, False), choose(n, cols, rows, dtype, True)
-            seen.add(("dweight", direct + 10 if direct >= 0 else packed))
+            seen.add(("dweight", "outer" if outer else direct + 10 if direct >= 0 else packed))
     want = {(name, tile + 4 * split) for name in ("y", "dx", "dweight") for tile in range(3) for split in (0, 1)}
-    want |= {("y", "few")} | {("dweight", 10 + tile + 4 * split) for tile in range(2) for split in (0, 1)}
+    want |= {("y", "few"), ("y", "whole"), ("dx", "few"), ("dweight", "outer")} | {("dweight", 10 + tile + 4 * split) for tile in range(2) for split in (0, 1)}
     assert want <= seen, sorted(want - seen, key=str)
