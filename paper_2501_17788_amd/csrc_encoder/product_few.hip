@@ -95,7 +95,7 @@ __global__ __launch_bounds__(64 * few_waves<LB>()) void k_product_few(ProductArg
     static_assert(LB == kAlongK || BN == W, "a lane's pieces across K are of W blocks");
     typedef typename Piece<T>::type V;
     __shared__ float sums[kWaves][16 * BM][kCols + 1];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, q = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, q = lane >> 4;
     const int sharing = LB == kAlongK ? g.splits : kWaves, group = wave / sharing, mine = wave % sharing;
     const int64_t tile = (int64_t)blockIdx.x * (kWaves / sharing) + group;
     const int64_t c0 = tile * kCols, m0 = (int64_t)blockIdx.y * 16 * BM;
@@ -123,8 +123,10 @@ __global__ __launch_bounds__(64 * few_waves<LB>()) void k_product_few(ProductArg
         constexpr int U = BM + BN <= 2 ? 2 : 1;
         for (int64_t k = first + 4 * kStep * mine; k < end; k += U * 4 * kStep * sharing) {
             V a[U][BM][4], b[U][BN][4];
+            const int under_way = k + 4 * kStep * sharing < end ? U : 1;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                if (u >= under_way) break;
                 const int64_t at = k + u * 4 * kStep * sharing + W * piece;
 #pragma unroll
                 for (int j = 0; j < BN; ++j)
@@ -140,6 +142,7 @@ __global__ __launch_bounds__(64 * few_waves<LB>()) void k_product_few(ProductArg
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                if (u >= under_way) break;
 #pragma unroll
                 for (int j = 0; j < BN; ++j) quad_transpose(b[u][j]);
 #pragma unroll
