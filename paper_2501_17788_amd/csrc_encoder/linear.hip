@@ -52,7 +52,8 @@ struct Product {
 // float32 rows that are multiplied as they are, without planes: the matrix instructions for them have a 16th of the rate, but nothing has
 // to be packed. us, as they are | in planes: 64 x 4096 by
 // 4096 29 | 63, 256 85 | 105, 384 118 | 136, 1024 by 1024 10 | 22, 25 | 28, 25 | 30, 771 by 3001 (packed, as rows of whole pieces) 25 | 24,
-// 32 | 33, 39 | 36; 800 x 4096 by 4096 297 | 214.
+// 32 | 33, 39 | 36; 800 x 4096 by 4096 297 | 214. With gradients, 65 x 4096 by 4096 144 | 232, 200 251 | 330, 384 363 | 406, 771 by 3001
+// 75 | 73, 90 | 98, 115 | 116.
 constexpr int kWholeRows = 384;
 
 typedef hipError_t (*ProductCall)(const ProductArgs&, int, Tile, Finish, hipStream_t);
@@ -128,6 +129,7 @@ struct Backward {
     float *part, *room;
     Product dx, dw;
     bool bytes, few, outer;  // dx of few rows, dweight over few
+    bool whole;              // float32 without planes
     int64_t sums;     // parts of dbias
     int parts;        // of dx of few rows
     Backward(void* base, const void* dy_, int64_t dy_stride, int64_t rows, int64_t cols, int32_t dtype, const void* w_,
@@ -136,10 +138,16 @@ struct Backward {
         space.base = (uint8_t*)base;
         few = few_dx(rows, dtype);
         outer = takes_outer(rows, n, cols, dtype);
-        dy = space.take<uint16_t>((few && outer) || direct(dy_, dy_stride, rows, n, dtype) ? 0 : packed_elements(rows, n, dtype));
+        whole = dtype == WARP_F32 && rows > kFewRows && rows <= kWholeRows;
+        if (whole) dx = Product(rows, cols, n), dw = Product(n, cols, rows);
+        auto room_of = [&](const void* p, int64_t stride, int64_t count, int64_t width) {
+            if ((whole ? direct_f32 : direct)(p, stride, count, width, dtype)) return (int64_t)0;
+            return whole ? 2 * count * packed_width(width) : packed_elements(count, width, dtype);
+        };
+        dy = space.take<uint16_t>(few && outer ? 0 : room_of(dy_, dy_stride, rows, n));
         parts = few ? few_parts(rows, cols, n, dtype) : 0;
         if (few) dx.floats = parts * rows * cover_of(cols, 4) * 4;
-        w = space.take<uint16_t>(few || direct(w_, w_stride, n, cols, dtype) ? 0 : packed_elements(n, cols, dtype));
+        w = space.take<uint16_t>(few ? 0 : room_of(w_, w_stride, n, cols));
         const Product direct_dw(n, cols, rows, dtype, kT128);
         bytes = takes_bytes(rows, n, cols, dtype, direct_dw.time, dw.time);
         sums = 0;
@@ -260,8 +268,8 @@ int warp_linear_backward(const void* dy, int64_t dy_stride, int64_t rows, int32_
     hipStream_t s = (hipStream_t)hip_stream;
     PackRows pack_dy, pack_w;
     Operand d{}, t{};
-    if (rows && ((dx && !w.few) || (dweight && !w.outer))) d = operand_of(dy, dy_stride, rows, n, dtype, w.dy, &pack_dy);
-    if (rows && dx && !w.few) t = operand_of(weight, weight_stride, n, cols, dtype, w.w, &pack_w);
+    if (rows && ((dx && !w.few) || (dweight && !w.outer))) d = operand_of(dy, dy_stride, rows, n, dtype, w.dy, &pack_dy, w.whole);
+    if (rows && dx && !w.few) t = operand_of(weight, weight_stride, n, cols, dtype, w.w, &pack_w, w.whole);
     WARP_STEP(pack_rows(pack_dy, pack_w, dtype, s));
     if (rows && dx && w.few) {
         ProductArgs g = product_args({dy, rows <= 1 ? n : dy_stride, 0}, {weight, n <= 1 ? cols : weight_stride, 0}, rows, cols, n, dx,
@@ -273,7 +281,8 @@ int warp_linear_backward(const void* dy, int64_t dy_stride, int64_t rows, int32_
         j.parts = w.parts;
         WARP_STEP(join_parts(j, s));
     } else if (rows && dx) {
-        WARP_STEP(run_product(product_mixed, product_args(d, t, rows, cols, n, dx, dx_stride, dtype), w.dx, w.part, dtype, s));
+        WARP_STEP(run_product(product_mixed, product_args(d, t, rows, cols, n, dx, dx_stride, dtype), w.dx, w.part, dtype, s,
+                              w.whole));
     }
     const bool bytes = dweight && w.bytes && rows;
     if (dweight && w.outer) {
@@ -285,10 +294,10 @@ int warp_linear_backward(const void* dy, int64_t dy_stride, int64_t rows, int32_
         WARP_STEP(run_product(nullptr, g, w.dw, w.part, dtype, s));
         if (dbias) WARP_STEP(join_columns(w.room, w.sums, n, dbias, dbias_dtype, s));
     } else if (dweight) {  // without rows: zeros
-        WARP_STEP(unpack_int8(q, q_stride, q_scale, rows, cols, dtype, w.x, s));
+        WARP_STEP(unpack_int8(q, q_stride, q_scale, rows, cols, dtype, w.x, s, w.whole));
         const Operand x{w.x, packed_width(cols), rows * packed_width(cols)};
         WARP_STEP(run_product(product_across, product_args(d, x, n, cols, rows, dweight, dweight_stride, dtype), w.dw, w.part,
-                              dtype, s));
+                              dtype, s, w.whole));
     }
     if (dbias && !bytes && !(dweight && w.outer)) WARP_STEP(column_sums(dy, dy_stride, rows, n, dtype, w.room, dbias, dbias_dtype, s));
     return WARP_OK;

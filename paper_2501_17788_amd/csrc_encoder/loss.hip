@@ -390,7 +390,7 @@ struct Sizes {
     int planes;
     bool few;    // rows: the table is read where it lies
     bool packs;  // the table
-    bool whole;  // the forward pass's float32 without planes
+    bool whole;  // float32 without planes
 };
 Sizes sizes_of(int64_t tokens, const void* table, int64_t stride, int64_t vocabulary, int32_t cols, int32_t dtype, bool back) {
     // us with the table where it lies | by tiles. 16 tokens in 16 bits: forward, 5000 rows of 4096 18 | 40, 32,128 of 768 19 | 18,
@@ -398,10 +398,11 @@ Sizes sizes_of(int64_t tokens, const void* table, int64_t stride, int64_t vocabu
     // float32, forward 49 | 210, 41 | 88, 167 | 364, 91 | 104, both passes 201 | 504, 194 | 261, 748 | 1275, 286 | 296.
     const bool few = dtype == WARP_F32 ? tokens <= kFewRows
                                        : tokens <= kFewRows / 2 && (vocabulary <= 16384 || (cols % 8 && !back));
-    // The forward pass in float32 as it is | in planes: 64 tokens 40 | 89, 33 | 61, 312 | 401, 92 | 210, 79 | 103 (tables of 768 x
-    // 32,128, 128 x 100,001, 1023, 4096 x 5000, 65 x 200,001), 100 tokens 73 | 103, 58 | 79, 445 | 398, 93 | 213, 113 | 129, 200 tokens
-    // 121 | 123, 88 | 90, 711 | 468, 153 | 213, 161 | 163.
-    const bool whole = !back && !few && dtype == WARP_F32 && tokens <= 128;
+    // More float32 tokens as they are | in planes, both passes: 64 tokens 164 | 300, 120 | 192, 1144 | 1346, 249 | 522, 272 | 336
+    // (tables of 768 x 32,128, 128 x 100,001, 1023, 4096 x 5000, 65 x 200,001), 100 tokens 276 | 335, 200 | 234, 1494 | 1656, 294 | 510,
+    // 394 | 448; the forward pass of 200 121 | 123, 88 | 90, 711 | 468, 153 | 213, 161 | 163, of 400 224 | 164, 143 | 134, 1120 | 724,
+    // 236 | 259, 249 | 226.
+    const bool whole = !few && dtype == WARP_F32 && tokens <= (vocabulary <= 16384 ? 256 : 128);
     const bool packs = !few && !(whole ? direct_f32 : direct)(table, stride, vocabulary, cols, dtype);
     return {tokens, vocabulary, cols, packed_width(cols), dtype, planes_of(dtype), few, packs, whole};
 }
@@ -454,8 +455,9 @@ struct Backward {
         logits = plan_product(tokens, cols, product_steps(z.cols, terms), false).tile;
         dh = plan_product(tokens, z.cols, product_steps(cols, terms), true).tile;
         const ProductPlan e = plan_product(cols, z.cols, product_steps(tokens, terms), true);
+        if (z.whole) logits = tile_f32(tokens, cols), dh = tile_f32(tokens, z.cols);
         outer = z.dtype == WARP_F32 && tokens <= kFewRows;
-        de = e.tile, de_split = !outer && e.split;
+        de = z.whole ? tile_f32(cols, z.cols) : e.tile, de_split = !outer && !z.whole && e.split;
         hidden = space.take<uint16_t>(packed_elements(tokens, z.cols, z.dtype));
         table = space.take<uint16_t>(z.packs ? packed_elements(piece, z.cols, z.dtype) : 0);
         grad = space.take<uint16_t>(z.planes * tokens * piece);
@@ -465,7 +467,7 @@ struct Backward {
         lse2 = space.take<float>(tokens), weight = space.take<float>(tokens), at_target = space.take<float>(tokens);
         dh_parts = z.few ? few_parts(tokens, z.cols, cols, z.dtype) : 0;
         dh_part = space.take<float>(z.few ? dh_parts * tokens * cover_of(z.cols, 4) * 4
-                                          : part_floats(tokens, z.cols, cols, terms, dh, kMaxSplits, tile_jobs(dh)));
+                                          : part_floats(tokens, z.cols, z.whole ? 2 * cols : cols, z.whole ? 1 : terms, dh, kMaxSplits, tile_jobs(dh)));
         de_part = space.take<float>(
             de_split ? part_floats(cols, z.cols, tokens, terms, de, kMaxSplits, tile_jobs(de)) : 0);
     }
@@ -576,18 +578,19 @@ int warp_cross_entropy_backward(const float* dloss, const void* hidden, int64_t 
     if (!rc) rc = require_device();
     if (rc || (!dhidden && !dtable)) return rc;
     hipStream_t s = (hipStream_t)hip_stream;
-    const int element = element_of(dtype), terms = terms_of(dtype);
+    const int element = z.whole ? (int)WARP_F32 : element_of(dtype), terms = z.whole ? 1 : terms_of(dtype);
     const float grad_scale = dtype == WARP_F16 ? kHalfScale : 1.f;
     const SelectArgs sel{targets, target_bytes == 8, tokens, vocabulary, dloss, scale, grad_scale, w.list, w.place, w.target,
                          w.now, w.factor, w.largest};
-    if (tokens && tokens <= kFewTokens) {
+    const bool few = tokens <= kFewTokens && !z.whole;
+    if (tokens && few) {
         WARP_LAUNCH(take_few({sel, hidden, hidden_stride, cols, z.width, tokens * z.width, w.hidden, loss, lse, w.lse2, w.weight,
                               w.at_target}, dtype, s));
     } else {
         WARP_LAUNCH(select(sel, s));
     }
-    if (tokens > kFewTokens) {
-        WARP_STEP(pack_rows({hidden, hidden_stride, tokens, cols, w.list, w.now, w.hidden}, {}, dtype, s));
+    if (!few) {
+        WARP_STEP(pack_rows({hidden, hidden_stride, tokens, cols, w.list, w.now, w.hidden, z.whole}, {}, dtype, s));
         const RowArgs r{w.list, w.now, dloss, loss, lse, w.largest, w.lse2, w.weight, w.at_target};
         WARP_LAUNCH(hipLaunchKernelGGL(k_rows, dim3((uint32_t)cover_of(tokens, 256)), dim3(256), 0, s, r));
     }
@@ -600,7 +603,7 @@ int warp_cross_entropy_backward(const float* dloss, const void* hidden, int64_t 
         const void* rows = (const uint8_t*)table + v0 * table_stride * dtype_bytes(dtype);
         Operand t{rows, vocabulary <= 1 ? cols : table_stride, 0};
         if (z.packs) {
-            WARP_STEP(pack_rows({rows, table_stride, n, cols, nullptr, nullptr, w.table}, {}, dtype, s));
+            WARP_STEP(pack_rows({rows, table_stride, n, cols, nullptr, nullptr, w.table, z.whole}, {}, dtype, s));
             t = {w.table, z.width, n * z.width};
         }
         ProductArgs g{};
@@ -635,7 +638,7 @@ int warp_cross_entropy_backward(const float* dloss, const void* hidden, int64_t 
             d.m = tokens, d.n = cols, d.k = n, d.m_now = w.now, d.terms = terms;
             d.splits = kMaxSplits, d.jobs = tile_jobs(w.dh), d.part = w.dh_part, d.part_stride = part_stride;
             d.accumulate = v0 > 0;
-            if (!v0) dh.k = n;  // the last piece, shorter, may have fewer parts: the others stay as they were
+            if (!v0) dh.k = z.whole ? 2 * n : n;  // the last piece, shorter, may have fewer parts: the others stay as they were
             if (z.few) WARP_STEP(product_few(d, dtype, z.planes == 3, kSum, w.dh_parts, s));
             else WARP_STEP(product_mixed(d, element, w.dh, kSum, s));
         }

@@ -36,7 +36,7 @@ inline bool direct(const void* p, int64_t stride, int64_t rows, int64_t cols, in
     return dtype != WARP_F32 && (uintptr_t)p % 16 == 0 && cols % 8 == 0 && (rows <= 1 || (stride % 8 == 0 && stride <= 1 << 22));
 }
 
-// The same for float32 products along K without planes.
+// The same for float32 products without planes.
 inline bool direct_f32(const void* p, int64_t stride, int64_t rows, int64_t cols, int32_t dtype) {
     return dtype == WARP_F32 && (uintptr_t)p % 16 == 0 && cols % 4 == 0 && (rows <= 1 || (stride % 4 == 0 && stride <= 1 << 21));
 }
@@ -80,7 +80,7 @@ struct PackRows {
 hipError_t pack_rows(const PackRows& a, const PackRows& b, int32_t dtype, hipStream_t s);
 // The same of 8-bit rows: q * scale, for products in `dtype`.
 hipError_t unpack_int8(const int8_t* q, int64_t q_stride, const float* scale, int64_t rows, int64_t cols, int32_t dtype,
-                       uint16_t* out, hipStream_t s);
+                       uint16_t* out, hipStream_t s, bool whole = false);
 
 // x as an operand: where it lies, or in `room`, for which `job` is then what has to be packed. `whole`: float32 without planes.
 inline Operand operand_of(const void* x, int64_t stride, int64_t rows, int64_t cols, int32_t dtype, uint16_t* room,

@@ -190,12 +190,14 @@ hipError_t pack_rows(const PackRows& a, const PackRows& b, int32_t dtype, hipStr
 }
 
 hipError_t unpack_int8(const int8_t* q, int64_t q_stride, const float* scale, int64_t rows, int64_t cols, int32_t dtype,
-                       uint16_t* out, hipStream_t s) {
+                       uint16_t* out, hipStream_t s, bool whole) {
     if (!rows) return hipSuccess;
     const int64_t width = packed_width(cols), plane = rows * width;
     const dim3 grid = row_grid(rows, width), block(64 * kRowWaves);
     (void)hipGetLastError();
-    if (dtype == WARP_F32)
+    if (whole)
+        hipLaunchKernelGGL((k_unpack_int8<float, 1>), grid, block, 0, s, q, q_stride, scale, rows, cols, out, width, plane);
+    else if (dtype == WARP_F32)
         hipLaunchKernelGGL((k_unpack_int8<__bf16, 3>), grid, block, 0, s, q, q_stride, scale, rows, cols, out, width, plane);
     else if (dtype == WARP_F16)
         hipLaunchKernelGGL((k_unpack_int8<_Float16, 1>), grid, block, 0, s, q, q_stride, scale, rows, cols, out, width, plane);

@@ -1,7 +1,7 @@
 // Products of matrices on the matrix cores, most of them of 16-bit elements, with what the callers do to a finished tile:
 //   C[m][n] = sum_k A(m, k) B(n, k), sums in fp32.
 // An operand's elements of one row lie together (kAlongK: tokens, weights as stored) or those of one k (kAcrossK: its
-// transpose, as stored). Operands are 16-byte aligned, their strides multiples of 8; along K a row's elements beyond k up
+// transpose, as stored). Operands are 16-byte aligned, their strides multiples of 8 (float32: 4); along K a row's elements beyond k up
 // to the next multiple of 8 are zeros; across K a row is readable up to the next multiple of 8.
 //
 // float32 operands come as three planes of bfloat16, high + middle + low = x to the last bit (split_f32), and a
@@ -159,7 +159,7 @@ __host__ __device__ inline void split_f32(float x, uint16_t (&out)[3]) {
     }
 }
 
-// Launches: element is WARP_F16 or WARP_BF16 (also for planes), along K and for kStats also WARP_F32 (up to kT128).
+// Launches: element is WARP_F16 or WARP_BF16 (also for planes), or WARP_F32 up to kT128.
 hipError_t product_along(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);   // A, B along K
 hipError_t product_mixed(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);   // B across K
 hipError_t product_across(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);  // both
@@ -210,17 +210,18 @@ __device__ __forceinline__ void product_landed() { asm volatile("s_waitcnt vmcnt
 // piece of lie in different banks. Token blocks read rows 0 .. 15 in order; a channel block j reads rows
 // 4 j + i % 4 + 4 B (i / 4), which gives a lane 4 B neighbouring columns of the result.
 // Across K a k has T / 8 pieces, two for 16 columns, in the order pair ^ pair_key(k): the transposing reads of 16 lanes
-// take 32 bytes of four k each, and lanes 16 apart take k 8 apart.
+// take 32 bytes of four k each, and lanes 16 apart take k 8 apart. A float32's k has T / 4 pieces, in the order piece ^
+// float_key(k): 16 lanes read 16 neighbours of one k, lanes 16 apart take k four apart.
 __device__ __forceinline__ int token_piece(int row) { return row & 7; }
 template <int B>
 __device__ __forceinline__ int channel_piece(int row) { return (row & 3) | (row / (4 * B) & 1) << 2; }
+__device__ __forceinline__ int float_key(int k) { return (k >> 2 & 3) * 4; }
 template <int T>
 __device__ __forceinline__ int pair_key(int k) { return ((k & 3) | (k >> 3 & 3) << 2) & (T / 16 - 1); }
 
 // One operand's part in a tile of T rows by 128 bytes of k, of S each, for one wave of WAVES.
 template <Layout L, int T, int WAVES, bool CHANNELS, int B, int S>
 struct Stage {
-    static_assert(L == kAlongK || S == 2, "across K two blocks of 16-bit elements are read at once");
     static constexpr int kLoads = T / 8 / WAVES;  // of 1 KB
     static_assert(kLoads * 8 * WAVES == T, "whole loads");
     uint32_t off[kLoads];
@@ -233,7 +234,7 @@ struct Stage {
     __device__ __forceinline__ int k_of(int i) const {
         const int unit = wave * kLoads + i;
         if (L == kAlongK) return 16 / S * ((lane & 7) ^ key(unit * 8 + (lane >> 3)));
-        return (unit * 1024 + lane * 16) / (T * 2);
+        return (unit * 1024 + lane * 16) / (T * S);
     }
     __device__ __forceinline__ void start(const void* p, int64_t stride, int64_t first, int64_t rows, int lane_, int wave_) {
         lane = lane_, wave = wave_;
@@ -247,15 +248,16 @@ struct Stage {
                 off[i] = (uint32_t)(row < last ? row : last) * (uint32_t)(stride * S) + S * k_of(i);
             }
         } else {
-            at = (const uint8_t*)p + first * 2;
-            step_bytes = stride * 2 * kProductStep;
-            const int64_t end = (rows - 1) / 8 * 8 - first;  // the last piece
+            constexpr int W = 16 / S;
+            at = (const uint8_t*)p + first * S;
+            step_bytes = stride * 128;
+            const int64_t end = (rows - 1) / W * W - first;  // the last piece
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int k = k_of(i);
-                const int piece = ((wave * kLoads + i) * 64 + lane) & (T / 8 - 1);
-                const int64_t row = 8 * (piece ^ pair_key<T>(k) << 1);
-                off[i] = (uint32_t)k * (uint32_t)(stride * 2) + (uint32_t)(row < end ? row : end) * 2;
+                const int piece = ((wave * kLoads + i) * 64 + lane) & (T / W - 1);
+                const int64_t row = W * (piece ^ (S == 4 ? float_key(k) : pair_key<T>(k) << 1));
+                off[i] = (uint32_t)k * (uint32_t)(stride * S) + (uint32_t)(row < end ? row : end) * S;
             }
         }
     }
@@ -321,6 +323,8 @@ struct Blocks {
         if (L == kAlongK) {
             const int row = CHANNELS ? first + (li & 3) + 4 * B * (li >> 2) : first + li;
             at = row * 128 + 16 * (q ^ (CHANNELS ? channel_piece<B>(row) : token_piece(row)));
+        } else if (sizeof(E) == 4) {
+            at = 4 * q * T * 4 + ((first / 16) ^ q) * 64 + li * 4;
         } else {
             const int k = 8 * q + (li >> 2);
             at = k * T * 2 + ((first / 16) ^ pair_key<T>(k)) * 32 + (li & 3) * 8;
@@ -329,6 +333,13 @@ struct Blocks {
     __device__ __forceinline__ V read(const uint8_t* lds, int i, int half) const {
         if (L == kAlongK)
             return *(const V*)(lds + (at ^ (64 * half)) + (CHANNELS ? 4 : 16) * i * 128);
+        if constexpr (L == kAcrossK && sizeof(E) == 4) {
+            const uint8_t* p = lds + (at ^ (64 * i)) + half * 16 * T * 4;
+            V v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = *(const float*)(p + e * T * 4);
+            return v;
+        }
         int place = at;
         asm volatile("" : "+v"(place));  // kept from computing all blocks' addresses ahead, which takes registers
         const uint8_t* p = lds + (place ^ (32 * i)) + half * 32 * T * 2;

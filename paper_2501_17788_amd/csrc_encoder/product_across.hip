@@ -4,6 +4,9 @@
 namespace warp {
 
 hipError_t product_across(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s) {
+    if (element == WARP_F32)
+        return finish == kSum ? product_tiles<float, kAcrossK, kAcrossK, kSum>(g, tile, s)
+                              : product_tiles<float, kAcrossK, kAcrossK, kStore>(g, tile, s);
     return product_any<kAcrossK, kAcrossK>(g, element, tile, finish, s);
 }
 

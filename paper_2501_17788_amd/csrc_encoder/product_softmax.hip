@@ -4,7 +4,9 @@
 namespace warp {
 
 hipError_t product_softmax(const ProductArgs& g, int element, bool planes, Tile tile, Finish finish, hipStream_t s) {
-    if (element == WARP_F32) return product_tiles<float, kAlongK, kAlongK, kStats>(g, tile, s);
+    if (element == WARP_F32)
+        return finish == kStats ? product_tiles<float, kAlongK, kAlongK, kStats>(g, tile, s)
+                                : product_tiles<float, kAlongK, kAlongK, kGrad>(g, tile, s);
     if (finish == kStats)
         return element == WARP_F16 ? product_tiles<_Float16, kAlongK, kAlongK, kStats>(g, tile, s)
                                    : product_tiles<__bf16, kAlongK, kAlongK, kStats>(g, tile, s);

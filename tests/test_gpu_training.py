@@ -408,7 +408,7 @@ def test_cross_entropy(tokens, vocabulary, cols, dtype):
 
 
 @ALL
-@pytest.mark.parametrize("tokens", [1, 15, 16, 17, 32, 33, 64, 65, 128, 129])
+@pytest.mark.parametrize("tokens", [1, 15, 16, 17, 32, 33, 64, 65, 128, 129, 256, 257])
 def test_cross_entropy_of_few_tokens(tokens, dtype):
     """On both sides of the numbers of tokens that choose between the kernels; vocabularies of both of their widths."""
     for vocabulary, cols in ((5, 1), (33, 260), (300, 1030), (8200, 129), (16_500, 64), (17_000, 33)):

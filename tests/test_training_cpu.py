@@ -194,9 +194,9 @@ def test_product_sizes_reach_their_kernels():
         for dtype in (0, 1, 2):
             few, whole, outer = rows <= 32, dtype == 0 and rows <= 384, dtype == 0 and rows <= 32
             seen.add(("y", "few" if few else "whole" if whole else choose(rows, n, cols, dtype, False)))
-            seen.add(("dx", "few" if rows <= (64 if dtype == 0 else 32) else choose(rows, cols, n, dtype, False)))
+            seen.add(("dx", "few" if rows <= (64 if dtype == 0 else 32) else "whole" if whole else choose(rows, cols, n, dtype, False)))
             packed, direct = choose(n, cols, rows, dtype, False), choose(n, cols, rows, dtype, True)
-            seen.add(("dweight", "outer" if outer else direct + 10 if direct >= 0 else packed))
+            seen.add(("dweight", "outer" if outer else "whole" if whole else direct + 10 if direct >= 0 else packed))
     want = {(name, tile + 4 * split) for name in ("y", "dx", "dweight") for tile in range(3) for split in (0, 1)}
-    want |= {("y", "few"), ("y", "whole"), ("dx", "few"), ("dweight", "outer")} | {("dweight", 10 + tile + 4 * split) for tile in range(2) for split in (0, 1)}
+    want |= {("y", "few"), ("y", "whole"), ("dx", "few"), ("dx", "whole"), ("dweight", "outer"), ("dweight", "whole")} | {("dweight", 10 + tile + 4 * split) for tile in range(2) for split in (0, 1)}
     assert want <= seen, sorted(want - seen, key=str)
