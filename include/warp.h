@@ -423,7 +423,8 @@ int warp_embedding_backward_scratch(int64_t tokens, int64_t vocabulary, int32_t 
  *   targets      [tokens] whole numbers of target_bytes (4 or 8)
  *   loss, lse    [tokens] fp32
  *   scratch      warp_cross_entropy_scratch's `bytes`, 16-byte aligned
- * float32 products are made of 16-bit ones that keep all digits; what an infinity enters may be NaN.
+ * float32 products of many rows are made of 16-bit ones that keep all digits, of operands down to 2^-110 (of smaller ones what lies
+ * below 2^-133 counts as zero); what an infinity enters may be NaN.
  * At most 2^22 tokens, a vocabulary of 2^25 and 2^14 columns (above: WARP_ENOTSUP).
  */
 int warp_cross_entropy(const void* hidden, int64_t hidden_stride, int64_t tokens, int32_t cols, int32_t dtype,
@@ -456,7 +457,7 @@ int warp_cross_entropy_scratch(int64_t tokens, int32_t cols, int32_t dtype, cons
  *   bias         [n] of bias_dtype (WARP_F32 or dtype) or NULL
  *   scratch      warp_linear_scratch bytes, 16-byte aligned: copies of operands that are not 16-byte aligned rows of whole
  *                16-byte pieces, or float32, and parts of sums where there are few rows; often none
- * float32 products are made of 16-bit ones that keep all digits; what an infinity in x or weight enters may be NaN.
+ * float32 as for the loss; what an infinity in x or weight enters may be NaN.
  * WARP_ENOTSUP above 2^24 rows, 2^20 columns or channels, 2^36 elements of x or y or 2^34 of the weight.
  */
 int warp_linear(const void* x, int64_t x_stride, int64_t rows, int32_t cols, int32_t dtype, const void* weight,

@@ -141,7 +141,7 @@ inline ProductPlan plan_product(int64_t m, int64_t n, int64_t steps, bool may_sp
 int product_choice(int64_t m, int64_t n, int64_t k, int dtype, bool bytes);
 
 // x = high + middle + low, each a bfloat16 cut off towards zero: 8 + 8 + 8 bits. An infinity or a NaN stays in the
-// first.
+// first. Below 2^-110 the last bits of x are below bfloat16's smallest number, 2^-133, and lost.
 __host__ __device__ inline void split_f32(float x, uint16_t (&out)[3]) {
     uint32_t u;
     __builtin_memcpy(&u, &x, 4);

@@ -291,6 +291,20 @@ def test_float32_products_keep_their_digits():
                   rounding(want, torch.float32), (k, by))
 
 
+@pytest.mark.parametrize("rows", [1, 20, 40, 300, 500, 3000])
+def test_float32_products_of_tiny_values(rows):
+    """Subnormal operands: in planes each loses less than 2^-133."""
+    g = gen(rows)
+    x, weight = 1e-40 * randn(g, rows, 64), 1e10 * randn(g, 72, 64)
+    want, sizes = x.double() @ weight.double().t(), x.double().abs() @ weight.double().abs().t()
+    lost = 0.0 if rows <= 300 else 2.0 ** -133
+    close(w.linear(x, weight), want, (12 * 64 + 3) * U * sizes + lost * weight.double().abs().sum(1), "y")
+    dy = 1e-40 * randn(g, rows, 72)
+    want, sizes = dy.double() @ weight.double(), dy.double().abs() @ weight.double().abs()
+    dx, _, _ = w.linear_backward(dy, w.quantize_rows(torch.ones(rows, 64, device="cuda")), weight)
+    close(dx, want, (12 * 72 + 3) * U * sizes + lost * weight.double().abs().sum(0), "dx")
+
+
 def test_linear_past_32_bits():
     """x and y of more than 2^31 elements: the last rows equal those of a call on them alone."""
     g = gen(12)
