@@ -49,10 +49,10 @@ struct Product {
     }
 };
 
-// float32 rows that are multiplied as they are, without planes: the matrix instructions for them have a 16th of the rate, but nothing has
-// to be packed. us, as they are | in planes: 64 x 4096 by
-// 4096 29 | 63, 256 85 | 105, 384 118 | 136, 1024 by 1024 10 | 22, 25 | 28, 25 | 30, 771 by 3001 (packed, as rows of whole pieces) 25 | 24,
-// 32 | 33, 39 | 36; 800 x 4096 by 4096 297 | 214. With gradients, 65 x 4096 by 4096 144 | 232, 200 251 | 330, 384 363 | 406, 771 by 3001
+// Most float32 rows that are multiplied as they are, without planes: the matrix instructions for them have a 16th of the
+// rate, but nothing has to be packed. us, as they are | in planes, for 64, 256 and 384 rows: 4096 by 4096 29 | 63, 85 | 105,
+// 118 | 136, 1024 by 1024 10 | 22, 25 | 28, 25 | 30, 771 by 3001 (copied to rows of whole pieces) 25 | 24, 32 | 33, 39 | 36; for 800
+// rows 4096 by 4096 297 | 214. With gradients, 65, 200 and 384 rows: 4096 by 4096 144 | 232, 251 | 330, 363 | 406, 771 by 3001
 // 75 | 73, 90 | 98, 115 | 116.
 constexpr int kWholeRows = 384;
 
@@ -153,9 +153,9 @@ struct Backward {
         sums = 0;
         if (bytes) {
             dw = direct_dw;
-            sums = dw.split ? product_splits(n, cols, product_steps(rows, 1), tile_size(dw.tile), kMaxSplits, tile_jobs(dw.tile))
-                            : 1;
-            sums *= cover_of(cols, tile_size(dw.tile));
+            if (dw.split)
+                sums = product_splits(n, cols, product_steps(rows, 1), tile_size(dw.tile), kMaxSplits, tile_jobs(dw.tile)) *
+                       cover_of(cols, tile_size(dw.tile));
         }
         x = space.take<uint16_t>(bytes || outer ? 0 : packed_elements(rows, cols, dtype));
         if (outer) dw.floats = 0;
@@ -290,9 +290,11 @@ int warp_linear_backward(const void* dy, int64_t dy_stride, int64_t rows, int32_
                                  dweight_stride, (float*)dbias}, s));
     } else if (bytes) {
         ProductArgs g = product_args(d, {q, q_stride, 0}, n, cols, rows, dweight, dweight_stride, dtype);
-        g.b_scale = q_scale, g.sums = dbias ? w.room : nullptr;
+        g.b_scale = q_scale;
+        if (dbias && w.dw.split) g.sums = w.room;
+        else g.all_sums = dbias, g.sums_type = dbias_dtype;
         WARP_STEP(run_product(nullptr, g, w.dw, w.part, dtype, s));
-        if (dbias) WARP_STEP(join_columns(w.room, w.sums, n, dbias, dbias_dtype, s));
+        if (g.sums) WARP_STEP(join_columns(w.room, w.sums, n, dbias, dbias_dtype, s));
     } else if (dweight) {  // without rows: zeros
         WARP_STEP(unpack_int8(q, q_stride, q_scale, rows, cols, dtype, w.x, s, w.whole));
         const Operand x{w.x, packed_width(cols), rows * packed_width(cols)};

@@ -36,6 +36,8 @@ struct ProductArgs {
     // 8-bit rows in the place of b (across K): b_stride bytes apart, a scale for each
     const float* b_scale;
     float* sums;  // [split][tile column][m]: parts of the sums of A's columns over k; may be null
+    void* all_sums;  // [m]: the sums themselves, of kStore products; may be null
+    int32_t sums_type;
     // kStore
     void* out;
     int64_t out_stride;
@@ -526,8 +528,9 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
         read(part[1], la, lb, 1);
         multiply(part[0]);
         if constexpr (KIND == kBytes) {
-            // sums of A's columns: products by ones, of steps that the workgroups of a row of tiles take in turn
-            if (g.sums && wave % WN == 0 && turn == tile_n) {
+            // sums of A's columns: products by ones, of steps that the workgroups of a row of tiles take in turn, or all by the
+            // first one, which saves the launch that adds them
+            if ((F == kStore ? g.all_sums && tile_n == 0 : g.sums && turn == tile_n) && wave % WN == 0) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -572,11 +575,14 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
     }
     const int64_t c = c0 + wn + (kWide || kBN == 4 ? kOut * q : 16 * (q & 1) + 8 * (q >> 1));
     if constexpr (KIND == kBytes) {
-        if (g.sums && wave % WN == 0 && q == 0) {
+        if ((F == kStore ? g.all_sums && tile_n == 0 : g.sums != nullptr) && wave % WN == 0 && q == 0) {
 #pragma unroll
             for (int i = 0; i < kBM; ++i) {
                 const int64_t m = m0 + wm + 16 * i + li;
-                if (m < rows) g.sums[((int64_t)split * tiles_n + tile_n) * rows + m] = totals[i][0];
+                if (m >= rows) continue;
+                const float v[1] = {totals[i][0]};
+                if constexpr (F == kStore) store_floats<1>(g.all_sums, g.sums_type, m, v, 1, false);
+                else g.sums[((int64_t)split * tiles_n + tile_n) * rows + m] = v[0];
             }
         }
     }
