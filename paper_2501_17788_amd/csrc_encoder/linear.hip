@@ -130,7 +130,7 @@ struct Backward {
     Product dx, dw;
     bool bytes, few, outer;  // dx of few rows, dweight over few
     bool whole;              // float32 without planes
-    int64_t sums;     // parts of dbias
+    int64_t sums;     // parts of dbias; none where it comes with dweight
     int parts;        // of dx of few rows
     Backward(void* base, const void* dy_, int64_t dy_stride, int64_t rows, int64_t cols, int32_t dtype, const void* w_,
              int64_t w_stride, int64_t n)
@@ -154,8 +154,10 @@ struct Backward {
         if (bytes) {
             dw = direct_dw;
             if (dw.split)
-                sums = product_splits(n, cols, product_steps(rows, 1), tile_size(dw.tile), kMaxSplits, tile_jobs(dw.tile)) *
-                       cover_of(cols, tile_size(dw.tile));
+                sums = product_splits(n, cols, product_steps(rows, 1), tile_size(dw.tile), kMaxSplits, tile_jobs(dw.tile));
+            else
+                sums = dw.tile == kT64 ? 0 : 1;
+            sums *= cover_of(cols, tile_size(dw.tile));
         }
         x = space.take<uint16_t>(bytes || outer ? 0 : packed_elements(rows, cols, dtype));
         if (outer) dw.floats = 0;
@@ -291,7 +293,7 @@ int warp_linear_backward(const void* dy, int64_t dy_stride, int64_t rows, int32_
     } else if (bytes) {
         ProductArgs g = product_args(d, {q, q_stride, 0}, n, cols, rows, dweight, dweight_stride, dtype);
         g.b_scale = q_scale;
-        if (dbias && w.dw.split) g.sums = w.room;
+        if (dbias && w.sums) g.sums = w.room;
         else g.all_sums = dbias, g.sums_type = dbias_dtype;
         WARP_STEP(run_product(nullptr, g, w.dw, w.part, dtype, s));
         if (g.sums) WARP_STEP(join_columns(w.room, w.sums, n, dbias, dbias_dtype, s));

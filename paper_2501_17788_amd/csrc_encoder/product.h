@@ -36,7 +36,7 @@ struct ProductArgs {
     // 8-bit rows in the place of b (across K): b_stride bytes apart, a scale for each
     const float* b_scale;
     float* sums;  // [split][tile column][m]: parts of the sums of A's columns over k; may be null
-    void* all_sums;  // [m]: the sums themselves, of kStore products; may be null
+    void* all_sums;  // [m]: the sums themselves, of kStore products in tiles of 64; may be null
     int32_t sums_type;
     // kStore
     void* out;
@@ -428,6 +428,7 @@ template <typename E, Layout LA, Layout LB, int TM, int TN, int WM, int WN, Fini
 __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(ProductArgs g) {
     constexpr int kWaves = WM * WN;
     constexpr int kBM = TM / WM / 16, kBN = TN / WN / 16;  // blocks of a wave
+    constexpr bool kAllSums = F == kStore && TM == 64;
     constexpr bool kWide = LB == kAlongK;                  // a lane holds 4 kBN neighbouring columns, else 4 in each block
     __shared__ __attribute__((aligned(16))) uint8_t a0[TM * 128];
     __shared__ __attribute__((aligned(16))) uint8_t a1[TM * 128];
@@ -529,8 +530,9 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
         multiply(part[0]);
         if constexpr (KIND == kBytes) {
             // sums of A's columns: products by ones, of steps that the workgroups of a row of tiles take in turn, or all by the
-            // first one, which saves the launch that adds them
-            if ((F == kStore ? g.all_sums && tile_n == 0 : g.sums && turn == tile_n) && wave % WN == 0) {
+            // first one, which saves the launch that adds them (62 -> 59 us where that is one of six; tiles of 128, by which
+            // it would take 57 instead of 42 for 3000 x 2048 by 2048, take turns)
+            if ((kAllSums ? g.all_sums && tile_n == 0 : g.sums && turn == tile_n) && wave % WN == 0) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -575,13 +577,13 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
     }
     const int64_t c = c0 + wn + (kWide || kBN == 4 ? kOut * q : 16 * (q & 1) + 8 * (q >> 1));
     if constexpr (KIND == kBytes) {
-        if ((F == kStore ? g.all_sums && tile_n == 0 : g.sums != nullptr) && wave % WN == 0 && q == 0) {
+        if ((kAllSums ? g.all_sums && tile_n == 0 : g.sums != nullptr) && wave % WN == 0 && q == 0) {
 #pragma unroll
             for (int i = 0; i < kBM; ++i) {
                 const int64_t m = m0 + wm + 16 * i + li;
                 if (m >= rows) continue;
                 const float v[1] = {totals[i][0]};
-                if constexpr (F == kStore) store_floats<1>(g.all_sums, g.sums_type, m, v, 1, false);
+                if constexpr (kAllSums) store_floats<1>(g.all_sums, g.sums_type, m, v, 1, false);
                 else g.sums[((int64_t)split * tiles_n + tile_n) * rows + m] = v[0];
             }
         }
