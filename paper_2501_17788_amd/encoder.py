@@ -7,6 +7,8 @@ for tensors that do not fit, a WarpError for what the library refuses. A call wo
 tensors' device, or on `stream`; inputs of another stream are the caller's to wait for. Tensors have any row
 stride (a dimension's elements one after the other); leading dimensions are flattened to rows. autograd follows
 `embedding`, `layer_norm`, `linear` and `cross_entropy`; 8-bit rows and what is made of them carry no gradient.
+Calls can be captured into graphs; a backward pass only while no graph of the same leaves from outside the capture lives
+(a RuntimeError).
 """
 from __future__ import annotations
 
