@@ -35,7 +35,7 @@ struct SelectArgs {
     float scale, grad_scale;
     int32_t *list, *place, *target;  // [now] token and target; [tokens] row, -1: none, -2: target outside the vocabulary
     int32_t* now;
-    float* factor;  // of the sums: largest |dloss| * scale / grad_scale
+    float* factor;  // of the sums: largest |dloss| * scale / grad_scale; written without tokens too, whose dloss may be null
     float* largest;
 };
 
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(1024) void k_select_wide(SelectArgs g) {
     if (in) g.list[row] = (int32_t)t, g.target[row] = (int32_t)y;
     if (!last || tid) return;
     *g.now = count;
-    if (!g.dloss) return;
+    if (!g.factor) return;
     for (int i = 0; i < 16; ++i) top = max(top, tops[i]);
     const float largest = top ? as_f(top) : 1.f;
     *g.largest = largest;
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(1024) void k_select(SelectArgs g) {
     __syncthreads();
     if (tid) return;
     *g.now = count;
-    if (!g.dloss) return;
+    if (!g.factor) return;
     for (int i = 0; i < 16; ++i) top = max(top, tops[i]);
     const float largest = top ? as_f(top) : 1.f;
     *g.largest = largest;

@@ -885,3 +885,46 @@ def test_outputs_alone_are_written():
             assert not lib.warp_cross_entropy_backward(P(dloss), P(x), cols, 5, cols, 0, P(table), cols, 30, P(ids), 8, 1.0,
                                                        P(loss), P(lse), *to[0], *to[1], P(scratch), 1 << 28, stream)
             check(rows, cols, want[part])
+
+
+@ALL
+def test_scratch_is_written_before_it_is_read(dtype):
+    """C calls whose scratch holds NaN (bytes of 255) or zeros give the same bits; without tokens or rows, gradients of zeros."""
+    lib, g, code = w.lib, gen(48), {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}[dtype]
+    stream = torch.cuda.current_stream().cuda_stream
+    room = torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    P = lambda t: t.data_ptr()  # noqa: E731
+
+    def both(call, *shapes):
+        got = []
+        for fill in (0, 255):
+            room.fill_(fill)
+            out = [torch.full(s, 7.0, dtype=t, device="cuda") for s, t in shapes]
+            assert not call(*out), w.last_error()
+            got.append(out)
+        for a, b in zip(*got):
+            assert torch.equal(a, b)
+        return got[0]
+
+    for tokens, vocabulary, cols in ((0, 300, 72), (0, 9, 5), (1, 300, 72), (20, 40, 24), (90, 300, 72), (700, 2000, 136)):
+        say("scratch", tokens, vocabulary, cols, dtype)
+        x, table, dloss = randn(g, tokens, cols).to(dtype), randn(g, vocabulary, cols).to(dtype), randn(g, tokens)
+        for kept in (True, False):
+            ids = torch.randint(-1, vocabulary, (tokens,), generator=g, device="cuda") if kept else torch.full((tokens,), -1).cuda()
+            loss, lse = both(lambda a, b: lib.warp_cross_entropy(P(x), cols, tokens, cols, code, P(table), cols, vocabulary, P(ids),
+                                                                 8, 0.1, P(a), P(b), P(room), 1 << 26, stream),
+                             ((tokens,), torch.float32), ((tokens,), torch.float32))
+            dh, dt = both(lambda a, b: lib.warp_cross_entropy_backward(
+                P(dloss), P(x), cols, tokens, cols, code, P(table), cols, vocabulary, P(ids), 8, 0.1, P(loss), P(lse), P(a), cols, P(b),
+                cols, P(room), 1 << 26, stream), ((tokens, cols), dtype), ((vocabulary, cols), dtype))
+            de, = both(lambda a: lib.warp_embedding_backward(P(x), cols, P(ids), 8, tokens, vocabulary, cols, code, 1.0, P(a), cols,
+                                                             P(room), 1 << 26, stream), ((vocabulary, cols), dtype))
+            if not tokens or not kept:
+                assert not dh.any() and not dt.any() and not de.any()
+        dy, q = randn(g, tokens, vocabulary).to(dtype), w.quantize_rows(x)
+        both(lambda a: lib.warp_linear(P(x), cols, tokens, cols, code, P(table), cols, vocabulary, None, 0, P(a), vocabulary, P(room),
+                                       1 << 26, stream), ((tokens, vocabulary), dtype))
+        dx, dw, db = both(lambda a, b, c: lib.warp_linear_backward(
+            P(dy), vocabulary, tokens, vocabulary, code, P(q.values), q.values.stride(0), P(q.scale), cols, P(table), cols, P(a), cols,
+            P(b), cols, P(c), code, P(room), 1 << 26, stream), ((tokens, cols), dtype), ((vocabulary, cols), dtype), ((vocabulary,), dtype))
+        assert tokens or not (dw.any() or db.any())
