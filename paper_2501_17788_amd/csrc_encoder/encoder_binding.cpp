@@ -1,6 +1,7 @@
 // The Python binding of the token encoder's operators: checks torch tensors, allocates outputs and calls the C
 // functions of warp.h on the current stream of the tensors' device. Native because a small call's time is the host's:
 // layer norm of 32 rows takes 10.2 us through ctypes and 6 us through this, 3.5 us of either being the launch.
+#include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/extension.h>
@@ -85,14 +86,25 @@ Params params_of(const Tensor& x, const MaybeTensor& weight, const MaybeTensor& 
 Tensor like(const Tensor& x) { return x.is_contiguous() ? at::empty_like(x) : at::empty(x.sizes(), x.options()); }
 
 bool tracked(const MaybeTensor& t) { return t && t->requires_grad(); }
+// Whether forward-mode differentiation follows t: by a tangent, which a tensor without a gradient can have too.
+bool has_tangent(const MaybeTensor& t) {
+    return t && c10::AutogradState::get_tls_state().get_fw_grad_mode() && t->_fw_grad(0).defined();
+}
+// Calls that autograd follows go through its node, which refuses tangents; it calls back with both modes off.
+template <typename... T>
+bool followed(const T&... tensors) {
+    return (at::GradMode::is_enabled() && (tracked(tensors) || ...)) || (has_tangent(tensors) || ...);
+}
+py::object node(const char* name) {
+    return py::module_::import("paper_2501_17788_amd.encoder").attr(name).attr("apply");
+}
 
 py::tuple layer_norm(const Tensor& x, const MaybeTensor& weight, const MaybeTensor& bias, double eps) {
     on_device(x);
     on_device(x, weight);
     on_device(x, bias);
-    // autograd's node, which calls this again with gradients off
-    if (at::GradMode::is_enabled() && (x.requires_grad() || tracked(weight) || tracked(bias)))
-        return py::module_::import("paper_2501_17788_amd.encoder").attr("_LayerNorm").attr("apply")(x, weight, bias, eps);
+    if (followed(x, weight, bias))
+        return node("_LayerNorm")(x, weight, bias, eps);
     const c10::DeviceGuard guard(x.device());
     const Rows r = rows_of(x, "x");
     const Params p = params_of(x, weight, bias);
@@ -198,19 +210,11 @@ Tensor linear_int8(const Tensor& av, const Tensor& sa, int64_t cols, const Tenso
     return out;
 }
 
-template <typename... T>
-bool followed(const T&... tensors) {
-    return at::GradMode::is_enabled() && (tracked(tensors) || ...);
-}
-
 // Whether a leaf's gradients are added on the default stream, where a graph that was made there lives.
 bool adds_on_default_stream(const Tensor& leaf) {
     const auto node = torch::autograd::impl::try_get_grad_accumulator(leaf);
     const auto stream = node ? node->stream() : std::nullopt;
     return stream && stream->id() == c10::hip::getDefaultHIPStream(leaf.get_device()).id();
-}
-py::object node(const char* name) {  // of autograd; it calls back with gradients off
-    return py::module_::import("paper_2501_17788_amd.encoder").attr(name).attr("apply");
 }
 
 Tensor scratch_of(const Tensor& like, int64_t bytes) { return at::empty({bytes}, like.options().dtype(at::kByte)); }
@@ -491,6 +495,7 @@ PYBIND11_MODULE(_encoder, mod) {
     mod.def("quantize_rows", &quantize_rows);
     mod.def("layer_norm_int8", &layer_norm_int8);
     mod.def("linear_int8", &linear_int8);
+    mod.def("has_tangent", [](const Tensor& t) { return has_tangent(t); });
     mod.def("adds_on_default_stream", &adds_on_default_stream);
     mod.def("embedding", &embedding);
     mod.def("embedding_backward", &embedding_backward);

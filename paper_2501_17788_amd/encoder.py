@@ -6,7 +6,8 @@ csrc_encoder/encoder_binding.cpp) checks tensors, allocates outputs with torch a
 for tensors that do not fit, a WarpError for what the library refuses. A call works on the current stream of its
 tensors' device, or on `stream`; inputs of another stream are the caller's to wait for. Tensors have any row
 stride (a dimension's elements one after the other); leading dimensions are flattened to rows. autograd follows
-`embedding`, `layer_norm`, `linear` and `cross_entropy`; 8-bit rows and what is made of them carry no gradient.
+`embedding`, `layer_norm`, `linear` and `cross_entropy` backwards, and refuses forward-mode tangents there (a
+NotImplementedError); 8-bit rows and what is made of them carry no gradient.
 Calls can be captured into graphs; a backward pass only while no graph of the same leaves from outside the capture lives
 (a RuntimeError).
 """
@@ -69,6 +70,12 @@ def _refuse_capture(ctx):
         raise RuntimeError("a backward pass cannot be captured while a graph of the same leaves from outside the capture lives")
 
 
+def _refuse_tangent(dy):
+    """Refuses a gradient with a forward-mode tangent, which the gradients made of it would silently lose."""
+    if _native.has_tangent(dy):
+        raise NotImplementedError("forward-mode differentiation of a backward pass is not implemented")
+
+
 class _LayerNorm(torch.autograd.Function):
     """What `layer_norm` is to autograd. The statistics have no gradient, and y no second derivative."""
 
@@ -84,6 +91,7 @@ class _LayerNorm(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy, *_):
         _refuse_capture(ctx)
+        _refuse_tangent(dy)
         x, weight, mean, rstd = ctx.saved_tensors
         dx, dw, db = _native.layer_norm_backward(dy, x, weight, mean, rstd)
         return dx, None if weight is None else dw, None if ctx.bias_type is None else db.to(ctx.bias_type), None
@@ -143,6 +151,7 @@ class _Embedding(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         _refuse_capture(ctx)
+        _refuse_tangent(dy)
         return None, _native.embedding_backward(dy, *ctx.saved_tensors, ctx.vocabulary, ctx.scale), None
 
 
@@ -178,6 +187,7 @@ class _CrossEntropy(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dloss, _):
         _refuse_capture(ctx)
+        _refuse_tangent(dloss)
         want = ctx.needs_input_grad
         return *_native.cross_entropy_backward(dloss, *ctx.saved_tensors, ctx.scale, want[0], want[1]), None, None
 
@@ -222,6 +232,7 @@ class _Linear(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         _refuse_capture(ctx)
+        _refuse_tangent(dy)
         return *_native.linear_backward(dy, *ctx.saved_tensors, *ctx.needs_input_grad[:3], ctx.bias_type), None
 
 

@@ -928,3 +928,36 @@ def test_scratch_is_written_before_it_is_read(dtype):
             P(dy), vocabulary, tokens, vocabulary, code, P(q.values), q.values.stride(0), P(q.scale), cols, P(table), cols, P(a), cols,
             P(b), cols, P(c), code, P(room), 1 << 26, stream), ((tokens, cols), dtype), ((vocabulary, cols), dtype), ((vocabulary,), dtype))
         assert tokens or not (dw.any() or db.any())
+
+
+def differentiable(g):
+    """Calls that autograd follows, and their differentiable inputs."""
+    ids = torch.randint(-1, 30, (8,), generator=g, device="cuda")
+    x, table, weight = (randn(g, n, 16) for n in (8, 30, 24))
+    return {"embedding": (lambda t: w.embedding(ids, t, 2.0), [table]),
+            "layer_norm": (lambda a, b, c: w.layer_norm(a, b, c)[0], [x, randn(g, 16), randn(g, 16)]),
+            "linear": (lambda a, b, c: w.linear(a, b, c), [x, weight, randn(g, 24)]),
+            "cross_entropy": (lambda a, b: w.cross_entropy(a, b, ids, 0.1)[0], [x, table])}
+
+
+@pytest.mark.parametrize("name", ["embedding", "layer_norm", "linear", "cross_entropy"])
+def test_forward_mode_is_refused(name):
+    """A tangent is refused and not dropped, whichever input has it, with gradients off too; without one nothing is."""
+    from torch.autograd import forward_ad
+
+    call, inputs = differentiable(gen(70))[name]
+    want = call(*inputs)
+    with forward_ad.dual_level():
+        assert torch.equal(call(*inputs), want)
+        for i, t in enumerate(inputs):
+            args = list(inputs)
+            args[i] = forward_ad.make_dual(t, torch.ones_like(t))
+            with pytest.raises(NotImplementedError):
+                call(*args)
+            with torch.no_grad(), pytest.raises(NotImplementedError):
+                call(*args)
+    leaves = [t.clone().requires_grad_() for t in inputs]
+    out = call(*leaves)
+    with forward_ad.dual_level(), pytest.raises(NotImplementedError):
+        torch.autograd.grad(out, leaves, forward_ad.make_dual(torch.ones_like(out), torch.ones_like(out)), retain_graph=True)
+    assert all(t is not None for t in torch.autograd.grad(out, leaves, torch.ones_like(out)))
