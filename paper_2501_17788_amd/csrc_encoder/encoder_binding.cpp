@@ -1,6 +1,7 @@
 // The Python binding of the token encoder's operators: checks torch tensors, allocates outputs and calls the C
 // functions of warp.h on the current stream of the tensors' device. Native because a small call's time is the host's:
 // layer norm of 32 rows takes 10.2 us through ctypes and 6 us through this, 3.5 us of either being the launch.
+#include <ATen/TracerMode.h>
 #include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
@@ -90,21 +91,22 @@ bool tracked(const MaybeTensor& t) { return t && t->requires_grad(); }
 bool has_tangent(const MaybeTensor& t) {
     return t && c10::AutogradState::get_tls_state().get_fw_grad_mode() && t->_fw_grad(0).defined();
 }
-// Calls that autograd follows go through its node, which refuses tangents; it calls back with both modes off.
+// Whether torch.jit.trace records, which knows torch's own operations only: of a call it would keep the empty results.
+bool traced() { return at::tracer::impl::is_dispatch_enabled(); }
+void not_traced(const char* name) {  // a RuntimeError
+    if (traced()) throw std::runtime_error(std::string(name) + " cannot be traced: its results would not be recorded");
+}
+// Calls that autograd follows go through its node, which refuses tangents and is recorded as a whole; it calls the function of
+// the same name with _forward, which looks at none of these.
 template <typename... T>
 bool followed(const T&... tensors) {
-    return (at::GradMode::is_enabled() && (tracked(tensors) || ...)) || (has_tangent(tensors) || ...);
+    return traced() || (at::GradMode::is_enabled() && (tracked(tensors) || ...)) || (has_tangent(tensors) || ...);
 }
 py::object node(const char* name) {
     return py::module_::import("paper_2501_17788_amd.encoder").attr(name).attr("apply");
 }
 
-py::tuple layer_norm(const Tensor& x, const MaybeTensor& weight, const MaybeTensor& bias, double eps) {
-    on_device(x);
-    on_device(x, weight);
-    on_device(x, bias);
-    if (followed(x, weight, bias))
-        return node("_LayerNorm")(x, weight, bias, eps);
+py::tuple layer_norm_forward(const Tensor& x, const MaybeTensor& weight, const MaybeTensor& bias, double eps) {
     const c10::DeviceGuard guard(x.device());
     const Rows r = rows_of(x, "x");
     const Params p = params_of(x, weight, bias);
@@ -118,8 +120,18 @@ py::tuple layer_norm(const Tensor& x, const MaybeTensor& weight, const MaybeTens
     return py::make_tuple(y, mean, rstd);
 }
 
+py::tuple layer_norm(const Tensor& x, const MaybeTensor& weight, const MaybeTensor& bias, double eps) {
+    on_device(x);
+    on_device(x, weight);
+    on_device(x, bias);
+    if (followed(x, weight, bias))
+        return node("_LayerNorm")(x, weight, bias, eps);
+    return layer_norm_forward(x, weight, bias, eps);
+}
+
 py::tuple layer_norm_backward(const Tensor& dy, const Tensor& x, const MaybeTensor& weight, const Tensor& mean,
                               const Tensor& rstd) {
+    not_traced("layer_norm_backward");
     if (dy.sizes() != x.sizes() || dy.scalar_type() != x.scalar_type())
         refuse("dy must be like x (", x.sizes(), ", ", x.scalar_type(), "), got ", dy.sizes(), ", ", dy.scalar_type());
     if (x.dim() == 0) refuse("x must have at least one dimension");
@@ -151,8 +163,7 @@ std::pair<Tensor, Tensor> int8_rows(const Rows& r) {
             at::empty({r.rows}, r.t.options().dtype(at::kFloat))};
 }
 
-py::tuple quantize_rows(const Tensor& x) {
-    on_device(x);
+py::tuple quantize_rows_forward(const Tensor& x) {
     const c10::DeviceGuard guard(x.device());
     const Rows r = rows_of(x, "x");
     auto [q, scale] = int8_rows(r);
@@ -161,7 +172,14 @@ py::tuple quantize_rows(const Tensor& x) {
     return py::make_tuple(q, scale, r.cols);
 }
 
+py::tuple quantize_rows(const Tensor& x) {
+    not_traced("quantize_rows");
+    on_device(x);
+    return quantize_rows_forward(x);
+}
+
 py::tuple layer_norm_int8(const Tensor& x, const MaybeTensor& weight, const MaybeTensor& bias, double eps) {
+    not_traced("layer_norm_int8");
     on_device(x);
     on_device(x, weight);
     on_device(x, bias);
@@ -188,6 +206,7 @@ void check_int8(const char* name, const Tensor& v, const Tensor& s, int64_t padd
 
 Tensor linear_int8(const Tensor& av, const Tensor& sa, int64_t cols, const Tensor& wv, const Tensor& sw,
                    int64_t w_cols, const MaybeTensor& bias, at::ScalarType dtype) {
+    not_traced("linear_int8");
     if (!known(dtype)) refuse("dtype must be float32, float16 or bfloat16, got ", dtype);
     if (cols != w_cols) refuse("tokens of ", cols, " columns against a weight of ", w_cols);
     if (cols < 1 || cols > INT32_MAX - kPad) refuse("rows of ", cols, " columns");
@@ -244,11 +263,7 @@ std::vector<int64_t> with_last(at::IntArrayRef lead, int64_t last) {
     return s;
 }
 
-Tensor embedding(const Tensor& ids, const Tensor& table, double scale) {
-    on_device(table);
-    on_device(table, ids);
-    if (followed(table))
-        return node("_Embedding")(ids, table, scale).cast<Tensor>();
+Tensor embedding_forward(const Tensor& ids, const Tensor& table, double scale) {
     const c10::DeviceGuard guard(table.device());
     const Rows t = matrix_of(table, "table", -1);
     const Tensor i = whole_numbers(ids, "ids");
@@ -258,7 +273,16 @@ Tensor embedding(const Tensor& ids, const Tensor& table, double scale) {
     return out;
 }
 
+Tensor embedding(const Tensor& ids, const Tensor& table, double scale) {
+    on_device(table);
+    on_device(table, ids);
+    if (followed(table))
+        return node("_Embedding")(ids, table, scale).cast<Tensor>();
+    return embedding_forward(ids, table, scale);
+}
+
 Tensor embedding_backward(const Tensor& dy, const Tensor& ids, int64_t vocabulary, double scale) {
+    not_traced("embedding_backward");
     on_device(dy);
     on_device(dy, ids);
     if (dy.dim() < 1 || dy.sizes().slice(0, dy.dim() - 1) != ids.sizes())
@@ -287,12 +311,7 @@ struct Scores {
     }
 };
 
-py::tuple cross_entropy(const Tensor& hidden, const Tensor& table, const Tensor& targets, double scale) {
-    on_device(hidden);
-    on_device(hidden, table);
-    on_device(hidden, targets);
-    if (followed(hidden, table))
-        return node("_CrossEntropy")(hidden, table, targets, scale);
+py::tuple cross_entropy_forward(const Tensor& hidden, const Tensor& table, const Tensor& targets, double scale) {
     const c10::DeviceGuard guard(hidden.device());
     const Scores s(hidden, table, targets);
     const int32_t type = code(hidden.scalar_type());
@@ -306,8 +325,18 @@ py::tuple cross_entropy(const Tensor& hidden, const Tensor& table, const Tensor&
     return py::make_tuple(loss, lse);
 }
 
+py::tuple cross_entropy(const Tensor& hidden, const Tensor& table, const Tensor& targets, double scale) {
+    on_device(hidden);
+    on_device(hidden, table);
+    on_device(hidden, targets);
+    if (followed(hidden, table))
+        return node("_CrossEntropy")(hidden, table, targets, scale);
+    return cross_entropy_forward(hidden, table, targets, scale);
+}
+
 py::tuple cross_entropy_backward(const Tensor& dloss, const Tensor& hidden, const Tensor& table, const Tensor& targets,
                                  const Tensor& loss, const Tensor& lse, double scale, bool want_hidden, bool want_table) {
+    not_traced("cross_entropy_backward");
     on_device(hidden);
     for (const Tensor* t : {&dloss, &table, &targets, &loss, &lse}) on_device(hidden, *t);
     const c10::DeviceGuard guard(hidden.device());
@@ -332,12 +361,7 @@ py::tuple cross_entropy_backward(const Tensor& dloss, const Tensor& hidden, cons
     return py::make_tuple(dh, dt);
 }
 
-Tensor linear(const Tensor& x, const Tensor& weight, const MaybeTensor& bias, const py::object& rows) {
-    on_device(x);
-    on_device(x, weight);
-    on_device(x, bias);
-    if (followed(x, weight, bias))
-        return node("_Linear")(x, weight, bias, rows).cast<Tensor>();
+Tensor linear_forward(const Tensor& x, const Tensor& weight, const MaybeTensor& bias) {
     const c10::DeviceGuard guard(x.device());
     const Rows r = rows_of(x, "x"), w = matrix_of(weight, "weight", r.cols);
     same_type(weight, x, "weight", "x");
@@ -358,9 +382,20 @@ Tensor linear(const Tensor& x, const Tensor& weight, const MaybeTensor& bias, co
     return y;
 }
 
+Tensor linear(const Tensor& x, const Tensor& weight, const MaybeTensor& bias, const py::object& rows) {
+    if (!rows.is_none()) not_traced("linear of given rows");
+    on_device(x);
+    on_device(x, weight);
+    on_device(x, bias);
+    if (followed(x, weight, bias))
+        return node("_Linear")(x, weight, bias, rows).cast<Tensor>();
+    return linear_forward(x, weight, bias);
+}
+
 // dy [..., n] for the rows `values * scale` and the weight [n, cols]
 py::tuple linear_backward(const Tensor& dy, const MaybeTensor& values, const MaybeTensor& scale, const Tensor& weight,
                           bool want_x, bool want_weight, bool want_bias, at::ScalarType bias_type) {
+    not_traced("linear_backward");
     on_device(dy);
     on_device(dy, weight);
     on_device(dy, values);
@@ -413,6 +448,7 @@ void adamw_step(const py::list& params, const py::sequence& grads, const py::obj
                 int32_t bits, const Tensor& m, const MaybeTensor& m_scale, const Tensor& v, const MaybeTensor& v_scale,
                 double lr, double beta1, double beta2, double eps, double weight_decay, int64_t step,
                 const MaybeTensor& grad_scale) {
+    not_traced("AdamW.step");
     const size_t n = params.size();
     const Records held(table);
     const size_t bytes = (size_t)held.view.len;
@@ -471,6 +507,7 @@ void adamw_step(const py::list& params, const py::sequence& grads, const py::obj
 }
 
 py::tuple adamw_moments(const Tensor& m, const Tensor& m_scale, const Tensor& v, const Tensor& v_scale) {
+    not_traced("AdamW.moments");
     on_device(m);
     for (const Tensor* t : {&m_scale, &v, &v_scale}) on_device(m, *t);
     if (m.scalar_type() != at::kChar || v.scalar_type() != at::kByte || m_scale.scalar_type() != at::kFloat ||
@@ -491,17 +528,22 @@ py::tuple adamw_moments(const Tensor& m, const Tensor& m_scale, const Tensor& v,
 
 PYBIND11_MODULE(_encoder, mod) {
     mod.def("layer_norm", &layer_norm);
+    mod.def("layer_norm_forward", &layer_norm_forward);
     mod.def("layer_norm_backward", &layer_norm_backward);
     mod.def("quantize_rows", &quantize_rows);
+    mod.def("quantize_rows_forward", &quantize_rows_forward);
     mod.def("layer_norm_int8", &layer_norm_int8);
     mod.def("linear_int8", &linear_int8);
     mod.def("has_tangent", [](const Tensor& t) { return has_tangent(t); });
     mod.def("adds_on_default_stream", &adds_on_default_stream);
     mod.def("embedding", &embedding);
+    mod.def("embedding_forward", &embedding_forward);
     mod.def("embedding_backward", &embedding_backward);
     mod.def("cross_entropy", &cross_entropy);
+    mod.def("cross_entropy_forward", &cross_entropy_forward);
     mod.def("cross_entropy_backward", &cross_entropy_backward);
     mod.def("linear", &linear);
+    mod.def("linear_forward", &linear_forward);
     mod.def("linear_backward", &linear_backward);
     mod.def("adamw_step", &adamw_step);
     mod.def("adamw_moments", &adamw_moments);

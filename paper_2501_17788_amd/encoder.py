@@ -7,7 +7,8 @@ for tensors that do not fit, a WarpError for what the library refuses. A call wo
 tensors' device, or on `stream`; inputs of another stream are the caller's to wait for. Tensors have any row
 stride (a dimension's elements one after the other); leading dimensions are flattened to rows. autograd follows
 `embedding`, `layer_norm`, `linear` and `cross_entropy` backwards, and refuses forward-mode tangents there (a
-NotImplementedError); 8-bit rows and what is made of them carry no gradient.
+NotImplementedError); 8-bit rows and what is made of them carry no gradient. torch.jit.trace records these four (a
+`linear` without `rows`); every other call is refused under it (a RuntimeError).
 Calls can be captured into graphs; a backward pass only while no graph of the same leaves from outside the capture lives
 (a RuntimeError).
 """
@@ -81,7 +82,7 @@ class _LayerNorm(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, weight, bias, eps):
-        y, mean, rstd = _native.layer_norm(x, weight, bias, eps)
+        y, mean, rstd = _native.layer_norm_forward(x, weight, bias, eps)
         ctx.save_for_backward(x, weight, mean, rstd)
         ctx.mark_non_differentiable(mean, rstd)
         ctx.bias_type = None if bias is None else bias.dtype
@@ -145,7 +146,7 @@ class _Embedding(torch.autograd.Function):
     def forward(ctx, ids, table, scale):
         ctx.save_for_backward(ids)
         ctx.vocabulary, ctx.scale = table.shape[0], scale
-        return _native.embedding(ids, table, scale)
+        return _native.embedding_forward(ids, table, scale)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
@@ -176,7 +177,7 @@ class _CrossEntropy(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, hidden, table, targets, scale):
-        loss, lse = _native.cross_entropy(hidden, table, targets, scale)
+        loss, lse = _native.cross_entropy_forward(hidden, table, targets, scale)
         # a copy: the caller may change its losses in place
         ctx.save_for_backward(hidden, table, targets, loss.clone(), lse.clone())
         ctx.mark_non_differentiable(lse)
@@ -217,13 +218,14 @@ class _Linear(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, weight, bias, rows):
-        y = _native.linear(x, weight, bias, None)
+        y = _native.linear_forward(x, weight, bias)
         values = scale = None
         if ctx.needs_input_grad[1]:
-            values, scale, cols = _native.quantize_rows(x) if rows is None else rows
-            count = x.numel() // x.shape[-1]
-            if cols != x.shape[-1] or values.shape[0] != count or values.dtype != torch.int8 or scale.shape != (count,):
-                raise ValueError(f"rows in 8 bits of {tuple(values.shape)}, {cols} columns, for x {tuple(x.shape)}")
+            values, scale, cols = _native.quantize_rows_forward(x) if rows is None else rows
+            if rows is not None:
+                count = x.numel() // x.shape[-1]
+                if cols != x.shape[-1] or values.shape[0] != count or values.dtype != torch.int8 or scale.shape != (count,):
+                    raise ValueError(f"rows in 8 bits of {tuple(values.shape)}, {cols} columns, for x {tuple(x.shape)}")
         ctx.save_for_backward(values, scale, weight)
         ctx.bias_type = torch.float32 if bias is None else bias.dtype
         return y

@@ -961,3 +961,31 @@ def test_forward_mode_is_refused(name):
     with forward_ad.dual_level(), pytest.raises(NotImplementedError):
         torch.autograd.grad(out, leaves, forward_ad.make_dual(torch.ones_like(out), torch.ones_like(out)), retain_graph=True)
     assert all(t is not None for t in torch.autograd.grad(out, leaves, torch.ones_like(out)))
+
+
+@pytest.mark.parametrize("grads", [False, True])
+@pytest.mark.parametrize("name", ["embedding", "layer_norm", "linear", "cross_entropy"])
+def test_traced_calls_follow_their_inputs(name, grads):
+    """What torch.jit.trace recorded gives other inputs' results, and their gradients."""
+    call, inputs = differentiable(gen(71))[name]
+    traced = torch.jit.trace(lambda *a: call(*a) * 2.0, tuple(t.clone().requires_grad_(grads) for t in inputs))
+    others = [(t * 0.5 + 0.25).requires_grad_(grads) for t in inputs]
+    for _ in range(3):  # the executor rewrites a graph in its first runs
+        got, want = traced(*others), call(*others) * 2.0
+        assert torch.equal(got, want)
+        if grads:
+            for a, b in zip(torch.autograd.grad(got.sum(), others), torch.autograd.grad(want.sum(), others)):
+                assert torch.equal(a, b)
+
+
+def test_traced_tokens_and_targets_are_inputs():
+    g = gen(72)
+    table, ids = randn(g, 30, 16), torch.randint(-1, 30, (2, 8), generator=g, device="cuda")
+
+    def call(i, y):
+        return w.cross_entropy(w.embedding(i, table), table, y, 0.5)
+
+    traced = torch.jit.trace(call, (ids[0], ids[1]))
+    for i, y in ((ids[1], ids[0]), (ids[0, :5], ids[1, 3:])):
+        for a, b in zip(traced(i, y), call(i, y)):
+            assert torch.equal(a, b)

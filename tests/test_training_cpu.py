@@ -200,3 +200,18 @@ def test_product_sizes_reach_their_kernels():
     want = {(name, tile + 4 * split) for name in ("y", "dx", "dweight") for tile in range(3) for split in (0, 1)}
     want |= {("y", "few"), ("y", "whole"), ("dx", "few"), ("dx", "whole"), ("dweight", "outer"), ("dweight", "whole")} | {("dweight", 10 + tile + 4 * split) for tile in range(2) for split in (0, 1)}
     assert want <= seen, sorted(want - seen, key=str)
+
+
+@pytest.mark.parametrize("name", ["quantize_rows", "layer_norm_int8", "linear_int8", "layer_norm_backward", "embedding_backward",
+                                  "cross_entropy_backward", "linear_backward", "linear"])
+def test_calls_that_a_trace_cannot_hold_are_refused(name):
+    ids, stats = torch.zeros(3, dtype=torch.int64), torch.zeros(3)
+    rows = w.QuantizedRows(torch.zeros(3, 128, dtype=torch.int8), torch.zeros(3), 8)
+    call = {"quantize_rows": lambda x: w.quantize_rows(x).values, "layer_norm_int8": lambda x: w.layer_norm_int8(x).values,
+            "linear_int8": lambda x: w.linear_int8(rows, rows, x[0]), "linear": lambda x: w.linear(x, x, None, rows),
+            "layer_norm_backward": lambda x: w.layer_norm_backward(x, x, None, stats, stats)[0],
+            "embedding_backward": lambda x: w.embedding_backward(x, ids, 3),
+            "cross_entropy_backward": lambda x: w.cross_entropy_backward(stats, x, x, ids, stats, stats)[0],
+            "linear_backward": lambda x: w.linear_backward(x[:, :3], rows, x)[0]}[name]
+    with pytest.raises(RuntimeError, match=name + ".* cannot be traced"):
+        torch.jit.trace(call, torch.zeros(3, 8))
