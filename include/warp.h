@@ -423,8 +423,9 @@ int warp_embedding_backward_scratch(int64_t tokens, int64_t vocabulary, int32_t 
  *   targets      [tokens] whole numbers of target_bytes (4 or 8)
  *   loss, lse    [tokens] fp32
  *   scratch      warp_cross_entropy_scratch's `bytes`, 16-byte aligned
- * float32 products of many rows are made of 16-bit ones that keep all digits, of operands down to 2^-110 (of smaller ones what lies
- * below 2^-133 counts as zero); what an infinity enters may be NaN.
+ * float32 products of many rows are made of 16-bit ones: operands keep all digits down to 2^-110 (of smaller ones what is finer than
+ * 2^-133 is rounded away), and of a product a b at most 2^-23 |a b| is left out, as the sums' own roundings are; what an infinity
+ * enters may be NaN.
  * At most 2^22 tokens, a vocabulary of 2^25 and 2^14 columns (above: WARP_ENOTSUP).
  */
 int warp_cross_entropy(const void* hidden, int64_t hidden_stride, int64_t tokens, int32_t cols, int32_t dtype,

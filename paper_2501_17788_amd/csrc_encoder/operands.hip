@@ -171,6 +171,14 @@ void column_parts(const void* x, int64_t stride, int64_t rows, int64_t cols, flo
 
 }  // namespace
 
+void split_planes(const float* x, int64_t n, uint16_t* planes) {
+    for (int64_t i = 0; i < n; ++i) {
+        uint16_t p[3];
+        split_f32(x[i], p);
+        for (int t = 0; t < 3; ++t) planes[t * n + i] = p[t];
+    }
+}
+
 hipError_t pack_rows(const PackRows& a, const PackRows& b, int32_t dtype, hipStream_t s) {
     PackJobs jobs{{a.rows ? a : b, b}};
     const int count = !!a.rows + !!b.rows;

@@ -5,7 +5,8 @@
 // to the next multiple of 8 are zeros; across K a row is readable up to the next multiple of 8.
 //
 // float32 operands come as three planes of bfloat16, high + middle + low = x to the last bit (split_f32), and a
-// product as the six of nine products of planes that count: those left out are below 2^-23 of |a b| together.
+// product as the six of nine products of planes that count: those left out are at most 2^-24 (1 + 2^-10) of |a b| together (2^-23
+// beside the largest numbers), of either sign.
 // (A matrix instruction for fp32 operands has a 16th of the rate; six products are 2.7 times as fast.) Where there are few
 // rows, for which packing a whole weight would take longer than the product, they are multiplied as they are.
 #pragma once
@@ -142,8 +143,10 @@ inline ProductPlan plan_product(int64_t m, int64_t n, int64_t steps, bool may_sp
 // is split; with `bytes` that of 8-bit rows as they are, -1 where they are unpacked.
 int product_choice(int64_t m, int64_t n, int64_t k, int dtype, bool bytes);
 
-// x = high + middle + low, each a bfloat16 cut off towards zero: 8 + 8 + 8 bits. An infinity or a NaN stays in the
-// first. Below 2^-110 the last bits of x are below bfloat16's smallest number, 2^-133, and lost.
+// x = high + middle + low, each the bfloat16 that is nearest to what is left (ties away from zero): |middle| <= 2^-8 and |low| <= 2^-17 of
+// x's power of two, on either side of zero. Cut off towards zero they would be twice and four times as large and all of x's sign, and what
+// products leave out would be up to 2^-21 of them, always towards zero. Near the largest number the first is cut off: rounded up it is
+// infinite. An infinity or a NaN stays in the first. Below 2^-110 what is finer than bfloat16's smallest number, 2^-133, is rounded away.
 __host__ __device__ inline void split_f32(float x, uint16_t (&out)[3]) {
     uint32_t u;
     __builtin_memcpy(&u, &x, 4);
@@ -152,7 +155,8 @@ __host__ __device__ inline void split_f32(float x, uint16_t (&out)[3]) {
     for (int i = 0; i < 3; ++i) {
         uint32_t v;
         __builtin_memcpy(&v, &rest, 4);
-        v &= 0xffff0000u;
+        const bool top = i == 0 && (v & 0x7fffffffu) >= 0x7f7f8000u;
+        v = (top ? v : v + 0x8000u) & 0xffff0000u;
         if (special) v = i ? 0 : u & 0x7fffff ? 0x7fc00000u : u;
         out[i] = (uint16_t)(v >> 16);
         float part;
@@ -160,6 +164,8 @@ __host__ __device__ inline void split_f32(float x, uint16_t (&out)[3]) {
         rest -= part;
     }
 }
+// The same for the tests: [3][n].
+void split_planes(const float* x, int64_t n, uint16_t* planes);
 
 // Launches: element is WARP_F16 or WARP_BF16 (also for planes), or WARP_F32 up to kT128.
 hipError_t product_along(const ProductArgs& g, int element, Tile tile, Finish finish, hipStream_t s);   // A, B along K

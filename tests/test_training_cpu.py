@@ -1,6 +1,7 @@
 """Refusals and sizes of the operators that train a token encoder, before a device is touched."""
 import ctypes
 
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -215,3 +216,62 @@ def test_calls_that_a_trace_cannot_hold_are_refused(name):
             "linear_backward": lambda x: w.linear_backward(x[:, :3], rows, x)[0]}[name]
     with pytest.raises(RuntimeError, match=name + ".* cannot be traced"):
         torch.jit.trace(call, torch.zeros(3, 8))
+
+
+def planes_of(x):
+    """The three bfloat16 planes that float32 products are made of, as 64-bit numbers [3, n]."""
+    split = lib["_ZN4warp12split_planesEPKflPt"]  # void warp::split_planes(const float* x, int64_t n, uint16_t* planes)
+    split.argtypes, split.restype = [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p], None
+    x = np.ascontiguousarray(x, np.float32)
+    out = np.empty((3, len(x)), np.uint16)
+    split(x.ctypes.data, len(x), out.ctypes.data)
+    return (out.astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+
+
+def hard_operands(rng):
+    """Mantissas at which a plane is as large as it gets, and others; near one, by signs."""
+    some = [0x800000, 0x800001, 0x807fff, 0x808000, 0x808001, 0x80ffff, 0x810000, 0x8080ff, 0x80807f, 0x808080, 0x80ff80, 0xff7fff,
+            0xff8000, 0xff8080, 0xffffff, 0xffff00, 0xfffe80, 0x817f7f, 0x80fffe]
+    x = np.concatenate([np.array(some), rng.integers(1 << 23, 1 << 24, 3000)]).astype(np.float64) * 2.0 ** -23
+    return (x * rng.choice([-1.0, 1.0], len(x))).astype(np.float32)
+
+
+def test_planes_of_a_float32():
+    """Their sum is the number, to the last bit down to 2^-110 and within half of 2^-133 below; up to the largest one."""
+    rng = np.random.default_rng(1)
+    x = hard_operands(rng)
+    for by in (0, 40, -60, -110, 126):
+        a = x * np.float32(2.0 ** by)
+        assert np.isfinite(a).all() and (planes_of(a).sum(0) == a).all(), by
+    top = np.finfo(np.float32).max
+    near = np.array([top, -top, np.nextafter(np.float32(top), np.float32(0)), 0.998 * top, 0.0, -0.0], np.float32)
+    p = planes_of(near)
+    assert np.isfinite(p).all() and (p.sum(0) == near).all()
+    small = np.concatenate([(rng.standard_normal(3000) * 10.0 ** rng.uniform(-45, -33, 3000)), [1e-45, 2.0 ** -133]]).astype(np.float32)
+    p = planes_of(small)
+    assert (abs(p.sum(0) - small) <= 2.0 ** -134).all()
+    p = planes_of(np.array([np.inf, -np.inf, np.nan], np.float32))
+    assert p[0, 0] == np.inf and p[0, 1] == -np.inf and np.isnan(p[0, 2]) and not p[1:].any()
+
+
+def test_what_products_of_planes_leave_out():
+    """A product is six of nine products of planes: high, middle and low by each other but for middle by low and low by low. With
+    |middle| <= 2^-8 and |low| <= 2^-17 of an operand's power of two these are at most 2 x 2^-25 + 2^-34 of the operands', on either
+    side of zero: the mean of a million of them lies within 6 standard deviations, of at most 2^-24 / 1000 each."""
+    rng = np.random.default_rng(2)
+
+    def left_out(a, b):  # exact: each product has 16 bits
+        p, q = planes_of(a), planes_of(b)
+        return p[1] * q[2] + p[2] * q[1] + p[2] * q[2]
+
+    x = hard_operands(rng)
+    a, b = (t.reshape(-1) for t in np.meshgrid(x[:500], x[:500]))
+    for other in (b, b * np.float32(2.0 ** -100), rng.permutation(b)):
+        both = abs(a.astype(np.float64) * other)
+        assert (abs(left_out(a, other)) <= (2.0 ** -24 + 2.0 ** -34) * both).all()
+    # an operand near the largest number, whose first plane is cut off and not rounded up to infinity
+    top = x[:19] * np.float32(2.0 ** 127)
+    a, b = (t.reshape(-1) for t in np.meshgrid(np.concatenate([top, np.float32([3.4028235e38, 3.4e38])]), x[:200] * np.float32(0.25)))
+    assert (abs(left_out(a, b)) <= 2.0 ** -23 * abs(a.astype(np.float64) * b)).all()
+    a, b = (rng.standard_normal(1_000_000).astype(np.float32) for _ in range(2))
+    assert abs((left_out(a, b) / (a.astype(np.float64) * b)).mean()) <= 6 * 2.0 ** -24 / 1000
