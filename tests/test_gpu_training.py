@@ -989,3 +989,39 @@ def test_traced_tokens_and_targets_are_inputs():
     for i, y in ((ids[1], ids[0]), (ids[0, :5], ids[1, 3:])):
         for a, b in zip(traced(i, y), call(i, y)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("rows", [130, 500])
+def test_float32_products_of_full_mantissas(rows):
+    """Elements with 24 bits set, of either sign, in results of one to eight products, on both sides of the number of rows from which on
+    operands go in planes: each of the six products of planes is above the bound where it is left out, (1, 1), (0, 2) and (2, 0), the
+    smallest, for half of all pairs."""
+    g = gen(80 + rows)
+
+    def full(*shape):
+        m = (torch.randint(2 ** 23, 2 ** 24, shape, generator=g, device="cuda") | 1).float() * 2.0 ** -23
+        return torch.where(torch.rand(shape, generator=g, device="cuda") < 0.5, -m, m)
+
+    def bound(a, b, k):  # of sums whose other products are zeros, which round nothing
+        sizes = a.double().abs() @ b.double().abs()
+        return (12 * k + 2) * U * sizes + rounding(a.double() @ b.double(), torch.float32)
+
+    for k in (1, 2, 3, 8):
+        say("full mantissas", rows, k)
+        x, weight = full(rows, k), full(70, k)
+        for by in (1.0, 2.0 ** 110, 2.0 ** -100):
+            close(w.linear(x * by, weight), (x * by).double() @ weight.double().t(), bound(x * by, weight.t(), k), ("y", k, by))
+        dy, weight = full(rows, k), full(k, 72)
+        dx, _, _ = w.linear_backward(dy, w.quantize_rows(full(rows, 72)), weight)
+        close(dx, dy.double() @ weight.double(), bound(dy, weight, k), ("dx", k))
+        dy, kept = full(rows, 70), w.quantize_rows(full(rows, 72))
+        dy[torch.randperm(rows, generator=g, device="cuda")[k:]] = 0.0
+        _, dw, _ = w.linear_backward(dy, kept, full(70, 72))
+        back = kept.values[:, :72].double() * kept.scale.double()[:, None]  # rounded to float32 once
+        close(dw, dy.double().t() @ back, bound(dy.t(), back, k) + U * (dy.double().abs().t() @ back.abs()), ("dweight", k))
+        # a vocabulary of one: lse is the logit; its factor, the product with it, and back from units of log 2
+        table = full(1, k)
+        loss, lse = w.cross_entropy(x, table, torch.zeros(rows, dtype=torch.int64, device="cuda"), 0.5)
+        want = 0.5 * (x.double() @ table.double().t())
+        close(lse[:, None], want, 0.5 * bound(x, table.t(), k) + 8 * U * want.abs(), ("lse", k))
+        assert not loss.any()
