@@ -9,8 +9,8 @@ stride (a dimension's elements one after the other); leading dimensions are flat
 `embedding`, `layer_norm`, `linear` and `cross_entropy` backwards, and refuses forward-mode tangents there (a
 NotImplementedError); 8-bit rows and what is made of them carry no gradient. torch.jit.trace records these four (a
 `linear` without `rows`); every other call is refused under it (a RuntimeError).
-Calls can be captured into graphs; a backward pass only while no graph of the same leaves from outside the capture lives
-(a RuntimeError).
+Calls can be captured into graphs; a backward pass only while no graph of the leaves that it leads to from outside the
+capture lives (a RuntimeError).
 """
 from __future__ import annotations
 
@@ -63,11 +63,24 @@ def _on(stream, tensors, call, *args):
         return call(*args)
 
 
+def _leaves(node):
+    """The leaves to which gradients go from a node of autograd's graph, through whatever nodes lie between."""
+    seen, todo = set(), [f for f, _ in node.next_functions]
+    while todo:
+        f = todo.pop()
+        if f is None or f in seen:
+            continue
+        seen.add(f)
+        if isinstance(f, torch._C._functions.AccumulateGrad):
+            yield f.variable
+        else:
+            todo += [g for g, _ in f.next_functions]
+
+
 def _refuse_capture(ctx):
     """Refuses a backward pass under capture whose leaves' gradients would be added on the default stream, since a graph
     made there lives: a stream under capture cannot be joined with it, and trying ends the process."""
-    if torch.cuda.is_current_stream_capturing() and any(
-            hasattr(f, "variable") and _native.adds_on_default_stream(f.variable) for f, _ in ctx.next_functions):
+    if torch.cuda.is_current_stream_capturing() and any(map(_native.adds_on_default_stream, _leaves(ctx))):
         raise RuntimeError("a backward pass cannot be captured while a graph of the same leaves from outside the capture lives")
 
 

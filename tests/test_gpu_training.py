@@ -1025,3 +1025,43 @@ def test_float32_products_of_full_mantissas(rows):
         want = 0.5 * (x.double() @ table.double().t())
         close(lse[:, None], want, 0.5 * bound(x, table.t(), k) + 8 * U * want.abs(), ("lse", k))
         assert not loss.any()
+
+
+@pytest.mark.parametrize("name", ["embedding", "linear", "cross_entropy", "layer_norm"])
+def test_captured_backward_of_cast_leaves_in_use(name):
+    """The same where a leaf of 32 bits is cast for the call, as master weights are: refused while an eager graph of it lives, then
+    captured, and replays give what eager passes give."""
+    g = gen(61)
+    leaf = randn(g, 97, 64).requires_grad_() if name != "layer_norm" else (1 + 0.1 * randn(g, 64)).requires_grad_()
+    x, ids = randn(g, 70, 64).bfloat16(), torch.randint(-1, 97, (70,), generator=g, device="cuda")
+    call = {"embedding": lambda t: w.embedding(ids, t), "linear": lambda t: w.linear(x, t),
+            "cross_entropy": lambda t: w.cross_entropy(x, t, ids)[0], "layer_norm": lambda t: w.layer_norm(x, t)[0]}[name]
+    out = lambda: call(leaf.to(torch.bfloat16)).float()  # noqa: E731
+    dy = torch.randn(out().shape, generator=g, device="cuda")
+    lives = out()
+    torch.cuda.synchronize()
+    say("refused capture of a cast leaf:", name)
+    with pytest.raises(RuntimeError, match="cannot be captured"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            out().backward(dy)
+    assert leaf.grad is None
+    lives.backward(dy)
+    assert leaf.grad is not None
+    leaf.grad = None
+    del lives
+    gc.collect()
+    torch.cuda.synchronize()
+    say("capture of a cast leaf:", name)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out().backward(dy)
+    got = leaf.grad
+    for k in range(3):
+        x.copy_(randn(g, 70, 64))
+        dy.copy_(torch.randn(dy.shape, generator=g, device="cuda"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        with torch.no_grad():
+            kept = got.clone()
+        assert torch.equal(kept, torch.autograd.grad(out(), leaf, dy)[0]), k

@@ -275,3 +275,35 @@ def test_what_products_of_planes_leave_out():
     assert (abs(left_out(a, b)) <= 2.0 ** -23 * abs(a.astype(np.float64) * b)).all()
     a, b = (rng.standard_normal(1_000_000).astype(np.float32) for _ in range(2))
     assert abs((left_out(a, b) / (a.astype(np.float64) * b)).mean()) <= 6 * 2.0 ** -24 / 1000
+
+
+def test_leaves_behind_other_operations_are_seen(monkeypatch):
+    """A captured backward pass is refused by the leaves that it leads to, whatever lies between; on the host, since trying such a capture
+    ends the process."""
+    from paper_2501_17788_amd import encoder
+
+    leaf, other = torch.ones(4, 4, requires_grad=True), torch.ones(4, 4, requires_grad=True)
+
+    class Named(torch.autograd.Function):  # whose context holds something under an accumulator's name
+        @staticmethod
+        def forward(ctx, x):
+            ctx.variable = other
+            return x * 2
+
+        @staticmethod
+        def backward(ctx, dy):
+            return dy * 2
+
+    cast = leaf.to(torch.bfloat16)
+    behind = [cast.t() * 2, cast.view(2, 8)[:1], (cast.float() @ other).sum(), Named.apply(leaf.t()), torch.cat([other, leaf.t()]) + 1,
+              sum(leaf * i for i in range(3000))]
+    monkeypatch.setattr(encoder._native, "adds_on_default_stream", lambda t: t is leaf)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    for out in behind:
+        encoder._refuse_capture(out.grad_fn)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    for out in behind:
+        with pytest.raises(RuntimeError, match="cannot be captured"):
+            encoder._refuse_capture(out.grad_fn)
+    for out in (other * 2, Named.apply(other), (leaf.detach() * other).sum()):
+        encoder._refuse_capture(out.grad_fn)
