@@ -521,7 +521,7 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
     };
     V ones;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ones[e] = (E)1.f;
+    for (int e = 0; e < (int)(sizeof(V) / sizeof(E)); ++e) ones[e] = (E)1.f;
     float4v totals[kBM] = {};
     int turn = (int)(first % tiles_n);
     // The operands of each half step are read while the matrix cores work on the half step before it, across the
