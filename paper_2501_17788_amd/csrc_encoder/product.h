@@ -626,6 +626,7 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 128 ? 4 : 2) void k_product(Pro
         }
     } else if constexpr (F == kStats) {
         // 16,384 tokens by 32,128 rows of 1024: 1011 us, a little less than with the logits written (1028)
+        product_landed();
         __syncthreads();  // the staged operands have been read by all
         float2* shared = (float2*)a0;  // [WN][TM]
         const bool whole = c0 + TN <= g.n;  // of all lanes
