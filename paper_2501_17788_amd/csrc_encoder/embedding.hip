@@ -346,8 +346,10 @@ __device__ __forceinline__ void store_sums(const float (&sum)[V], const SumArgs&
 }
 
 // One wave a chunk and column block (those of a chunk are neighbours), half of its rows under way while the other half is
-// added; and the chunk's part of the rows' spans. Bound by memory where rows come in the tokens' order, which sorting
-// scatters: 91,750 rows of 2 KB take 73 us (2.6 TB/s), as long as an indexed copy of them in this order.
+// added; and the chunk's part of the rows' spans. 91,721 rows of 2 KB, 190 MB read and 46 written: 39 us (6.0 TB/s) where the last-level
+// cache holds dy, 73 in a training step and 85 (2.8 TB/s) where all of it comes from memory. That its rows lie scattered by
+// sorting is not why: of ids in order, whose rows come as they lie, 83. A wave waits for its keys, then for each half of its rows, and
+// ends with its chunk.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void k_sum_chunks(SumArgs g) {
     const int lane = threadIdx.x & 63;

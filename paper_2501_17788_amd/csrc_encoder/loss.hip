@@ -11,9 +11,10 @@
 //
 // Precision. The target's exponential is left out of the sums, S the rest relative to it: loss = log(1 + S) keeps its
 // digits where a token is sure, and so does the target's G, which is expm1(-loss). G is rounded to the inputs' type, as
-// matrix instructions need it (float32: three bfloat16 planes, which hold all of it). Before that it is divided by the
-// largest |dloss|, so that rows that count alike round 1 - p and not a multiple of it, and scaled to use float16's range;
-// both come back as a factor of the sums.
+// matrix instructions need it (float32: three bfloat16 planes, which hold all of it); with what that loses as a second operand
+// dE and dh would take twice as long. Before that it is divided by the largest |dloss|, so that rows that count alike round 1 - p and
+// not a multiple of it, and scaled to use float16's range; both come back as a factor of the sums. Against 64 bits the gradients of
+// 16,384 tokens in bf16 are off by 0.19% (15% of them: 0.18), of which their own rounding is 0.17.
 #include "operands.h"
 
 namespace warp {

@@ -78,7 +78,7 @@ struct PackRows {
     bool whole = false;  // float32 as it is
 };
 hipError_t pack_rows(const PackRows& a, const PackRows& b, int32_t dtype, hipStream_t s);
-// The same of 8-bit rows: q * scale, for products in `dtype`.
+// The same of 8-bit rows: q * scale, rounded to `dtype` for its products (as ByteStage does).
 hipError_t unpack_int8(const int8_t* q, int64_t q_stride, const float* scale, int64_t rows, int64_t cols, int32_t dtype,
                        uint16_t* out, hipStream_t s, bool whole = false);
 

@@ -253,8 +253,9 @@ class _Linear(torch.autograd.Function):
 
 def linear(x, weight, bias=None, rows: QuantizedRows | None = None, stream=None):
     """x [..., cols] by a weight [n, cols] of its type, plus bias [n] (float32 or of x's type): [..., n]. For autograd it
-    keeps x in 8 bits (`quantize_rows`), from which the weight's gradient is made; x's own gradient does not need x. `rows`:
-    x's 8-bit rows, where the caller has them already, as for several layers of one input."""
+    keeps x in 8 bits (`quantize_rows`) in every type, from which the weight's gradient is made: of steps of 1/127 of a row's largest
+    element, which are coarse for the others where one is far larger. x's own gradient does not need x. `rows`: x's 8-bit rows, where
+    the caller has them already, as for several layers of one input; above 16,384 columns they are needed for the weight's gradient."""
     if stream is None:
         return _native.linear(x, weight, bias, rows)
     kept = () if rows is None else (rows.values, rows.scale)
